@@ -54,7 +54,7 @@ typedef enum gws_status {
   GWS_ERR_SHAPE = 2,  /* negative size, ld < cols, ld % 8 != 0, size >= 2^31,
                          row0/col0 not a multiple of 32, n < 0                   */
   GWS_ERR_ALIGN = 3,  /* BF16 pointer not 16-byte aligned, fp32 pointer not 4-byte */
-  GWS_ERR_FORMAT = 4, /* unknown gws_format                                      */
+  GWS_ERR_FORMAT = 4, /* unknown gws_format, activation or form of kept values   */
   GWS_ERR_LAUNCH = 5, /* the HIP runtime refused a kernel launch                 */
   GWS_ERR_ALIAS = 6,  /* an output overlaps an input it must not overlap         */
   GWS_ERR_TOO_LARGE = 7 /* the operand exceeds a fixed capacity of the library (gws_linear_fwd_static) */
@@ -295,6 +295,71 @@ int gws_gemm_bf16_sample_next_n(const void* x, int64_t M, int64_t K, int64_t ldx
                                 const void* w, int64_t N, int64_t ldw, int w_is_nk,
                                 void* y, int64_t ldy,
                                 const gws_tensor* next, int n_next, int fmt, uint64_t step, void* stream);
+
+/* ---- The gated feed-forward block beside the sampled-weight linears ----
+ *   G = X * Wg,  U = X * Wu,  H = a(G) .* U,  Y = H * Wd
+ * for M tokens, with X [M x K], Wg and Wu (typically sampled beforehand, gws_sample_fwd) stored [K x F] or, when w_is_nk, [F x K].
+ * a is SiLU, a(z) = z / (1 + exp(-z)), or GELU in its tanh form, a(z) = z (1 + tanh(sqrt(2/pi) (z + 0.044715 z^3))) / 2.
+ * The sums of the products and the arithmetic of the gate are fp32; each output is rounded once.
+ * K and F (and D) must be multiples of 32, leading dimensions multiples of 8, BF16 buffers 16-byte aligned.  M is any number of
+ * tokens; M == 0 writes nothing.  Rows of X and of the gradients do not meet: a row of NaN leaves the others as they are.          */
+#define GWS_ACT_SILU 0
+#define GWS_ACT_GELU_TANH 1
+
+/* Activations in 8 bits: 32 neighbouring values of a row (the last 32 of a row may be fewer) share one E8M0 byte, the biased exponent of
+ *   X = 2^(xscale - 127) = the smallest power of two from 2^-117 to 2^119 for which their largest magnitude rounds to at most 448 X,
+ * and a value v is kept as the E4M3 code (OCP "fn", as gws_sample_fwd_mx) nearest to v / X, ties to even, gradual underflow, saturating
+ * (beyond 464 2^119).  Every decoded value is a finite BF16 value.  32 zeros get xscale = 127.  32 values with a NaN or an infinity among them get xscale = 255 and codes 0x7F, and decode to NaN.
+ * Bytes past a row's data are never written.                                                                                */
+typedef struct gws_act8 {
+  void* codes;      /* device, one byte a value, 8-byte aligned; row i at codes + i * ldc                  */
+  uint8_t* xscale;  /* device, one byte a block; row i at xscale + i * lds                                 */
+  int64_t ldc;      /* >= columns and a multiple of 8                                                      */
+  int64_t lds;      /* >= ceil(columns / 32)                                                               */
+} gws_act8;
+
+/* BF16 x [M x C] (any C >= 0; ldx >= C a multiple of 8) to and from that form.  x must not overlap codes or xscale.              */
+int gws_act8_encode(const void* x, int64_t M, int64_t C, int64_t ldx, const gws_act8* o, void* stream);
+int gws_act8_decode(const gws_act8* a, int64_t M, int64_t C, void* x, int64_t ldx, void* stream);
+
+/* G and U [M x F] as they are kept for the backward pass: as BF16 (g and u set, the codes NULL) or in 8 bits (g and u NULL, g8 and u8 set;
+ * the codes are those of the fp32 sums, not of their BF16 rounding).                                                           */
+typedef struct gws_gated_saved {
+  void *g, *u;           /* device, BF16                                                                 */
+  int64_t ldg, ldu;
+  gws_act8 g8, u8;
+} gws_gated_saved;
+
+/* Forward: H, and with `saved` (NULL: inference, nothing is kept) G and U.  H is formed from the fp32 G and U.  No output may overlap an
+ * input or another output; columns of one wider buffer are apart.  The order of the fp32 sums goes by the sizes, as in gws_linear_fwd. */
+int gws_gated_fwd(const void* x, int64_t M, int64_t K, int64_t ldx, const void* wg, const void* wu, int64_t F, int64_t ldw,
+                  int w_is_nk, int act, void* h, int64_t ldh, const gws_gated_saved* saved, void* stream);
+
+/* Backward through the product that follows and the gate, in one kernel: with dY [M x D] the gradient of Y = H * Wd (Wd stored
+ * [F x D] or, when w_is_nk, [D x F], as that product's forward call takes it), dH = dY * Wd^T kept in fp32,
+ *   dG = dH .* U .* a'(G),   dU = dH .* a(G),   and, where h is not NULL, H = a(G) .* U again (the input of Wd's weight gradient)
+ * from the kept G and U.  dG and dU share the leading dimension ldd.  An output may lie on the BF16 G or U it is formed from (same
+ * address and leading dimension), else on no input and no other output.                                                          */
+int gws_gated_bwd(const void* dy, int64_t M, int64_t D, int64_t lddy, const void* wd, int64_t F, int64_t ldw, int w_is_nk, int act,
+                  const gws_gated_saved* saved, void* dg, void* du, int64_t ldd, void* h, int64_t ldh, void* stream);
+
+/* The same from a given dH (BF16 [M x F]): a pass over memory.  An output may also lie on dH.                                     */
+int gws_gated_bwd_h(const void* dh, int64_t M, int64_t F, int64_t lddh, int act, const gws_gated_saved* saved, void* dg, void* du,
+                    int64_t ldd, void* h, int64_t ldh, void* stream);
+
+/* Input gradient dX = dG * Wg^T + dU * Wu^T [M x K] in one sum.  w_is_nk: how Wg and Wu are stored, as in gws_gated_fwd.
+ * (Their weight gradients are gws_linear_bwd_w with dY = dG and dU, or gws_linear_bwd_w_act8.)                                     */
+int gws_gated_bwd_x(const void* dg, const void* du, int64_t M, int64_t F, int64_t ldd, const void* wg, const void* wu, int64_t K,
+                    int64_t ldw, int w_is_nk, void* dx, int64_t ldx, void* stream);
+
+/* gws_linear_bwd_w_ws where the linear's input X [M x K] was kept in 8 bits: dW = X^T * dY with the decoded X, and dL/db_t.  X is decoded into
+ * `workspace` (256-byte aligned, owned by the caller, contents undefined afterwards, apart from every other buffer of the call), what is left
+ * of it serves as gws_linear_bwd_w_ws's.  Everything else is as there.
+ *   gws_linear_bwd_w_act8_workspace_bytes: the bytes it can use; the first 2 M K of them, rounded up to 256, it needs (else GWS_ERR_SHAPE).
+ *   0 for sizes that the call refuses.  Host function, no GPU work.                                                               */
+size_t gws_linear_bwd_w_act8_workspace_bytes(const gws_tensor* w, int w_is_nk, int64_t M);
+int gws_linear_bwd_w_act8(const gws_act8* x, const void* dy, int64_t M, int64_t ldy, const gws_tensor* w, int w_is_nk, uint64_t step,
+                          void* workspace, size_t workspace_bytes, void* stream);
 
 /* The comparison systems of the paper's Sec. 4 behind the same interface: the same forward and
  * backward passes with R drawn from another noise basis.  The paper compares GaussWS with the same

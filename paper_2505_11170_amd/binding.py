@@ -18,11 +18,14 @@ _LIB_PATH = os.environ.get("GWS_LIBRARY") or os.path.join(_HERE, "libgws.so")
 FMT_BF16, FMT_FP8_E4M3, FMT_FP6_E3M2 = 0, 1, 2
 LINEAR_AUTO, LINEAR_IN_OPERAND, LINEAR_TWO_KERNELS = 0, 2, 3
 BASIS_BITS, BASIS_UNIFORM_BF16, BASIS_BOX_MULLER = 0, 1, 2
+ACT_SILU, ACT_GELU_TANH = 0, 1
 
 # include/gws.h (the method) and include/gws_bench.h (measurement aids)
 EXPORTS = ("gws_sample_fwd", "gws_sample_bwd", "gws_sample_fwd_bi", "gws_sample_bwd_bi", "gws_sample_fwd_mx", "gws_linear_fwd", "gws_linear_fwd_mode",
            "gws_linear_fwd_ws", "gws_linear_fwd_workspace_bytes", "gws_linear_fwd_static", "gws_linear_bwd_w", "gws_linear_bwd_w_ws", "gws_linear_bwd_w_workspace_bytes", "gws_gemm_bf16", "gws_gemm_bf16_sample_next", "gws_gemm_bf16_sample_next_n", "gws_noise_packed",
            "gws_sample_fwd_basis", "gws_sample_bwd_basis", "gws_noise_basis",
+           "gws_act8_encode", "gws_act8_decode", "gws_gated_fwd", "gws_gated_bwd", "gws_gated_bwd_h", "gws_gated_bwd_x",
+           "gws_linear_bwd_w_act8", "gws_linear_bwd_w_act8_workspace_bytes",
            "gws_derive_seed", "gws_status_string", "gws_version")
 BENCH_EXPORTS = ("gws_copy_tiles", "gws_block_absmax", "gws_sample_bwd_tuned", "gws_sample_fwd_tuned", "gws_gemm_bf16_ride_probe", "gws_ride_plan",
                  "gws_ride_plan_layout", "gws_gemm_form", "gws_gemm_tile", "gws_gemm_stream_tile", "gws_linear_bwd_w_form", "gws_linear_bwd_w_form_rows", "gws_box_muller_check")
@@ -53,6 +56,34 @@ class _CBitwidth(ctypes.Structure):
 
 class _CMxOut(ctypes.Structure):
     _fields_ = [("codes", ctypes.c_void_p), ("xscale", ctypes.c_void_p), ("ldc", ctypes.c_int64)]
+
+
+class _CAct8(ctypes.Structure):
+    _fields_ = [("codes", ctypes.c_void_p), ("xscale", ctypes.c_void_p), ("ldc", ctypes.c_int64), ("lds", ctypes.c_int64)]
+
+
+class _CGatedSaved(ctypes.Structure):
+    _fields_ = [("g", ctypes.c_void_p), ("u", ctypes.c_void_p), ("ldg", ctypes.c_int64), ("ldu", ctypes.c_int64),
+                ("g8", _CAct8), ("u8", _CAct8)]
+
+
+@dataclass
+class Act8:
+    """Python-side mirror of ``gws_act8``: one-byte device tensors for the E4M3 codes [rows, columns] and the E8M0 block
+    scales [rows, ceil(columns / 32)]."""
+    codes: object
+    xscale: object
+    ldc: Optional[int] = None
+    lds: Optional[int] = None
+
+
+@dataclass
+class GatedSaved:
+    """Python-side mirror of ``gws_gated_saved``: G and U kept as BF16 (``g``, ``u``) or in 8 bits (``g8``, ``u8``)."""
+    g: Optional[object] = None
+    u: Optional[object] = None
+    g8: Optional[Act8] = None
+    u8: Optional[Act8] = None
 
 
 @dataclass
@@ -176,6 +207,23 @@ def load_library() -> ctypes.CDLL:
     L.gws_noise_basis.restype = ci
     L.gws_noise_packed.argtypes = [vp, i64, i64, i64, i64, u64, u64, vp]
     L.gws_noise_packed.restype = ci
+    ap, sp, sz = ctypes.POINTER(_CAct8), ctypes.POINTER(_CGatedSaved), ctypes.c_size_t
+    L.gws_act8_encode.argtypes = [vp, i64, i64, i64, ap, vp]
+    L.gws_act8_encode.restype = ci
+    L.gws_act8_decode.argtypes = [ap, i64, i64, vp, i64, vp]
+    L.gws_act8_decode.restype = ci
+    L.gws_gated_fwd.argtypes = [vp, i64, i64, i64, vp, vp, i64, i64, ci, ci, vp, i64, sp, vp]
+    L.gws_gated_fwd.restype = ci
+    L.gws_gated_bwd.argtypes = [vp, i64, i64, i64, vp, i64, i64, ci, ci, sp, vp, vp, i64, vp, i64, vp]
+    L.gws_gated_bwd.restype = ci
+    L.gws_gated_bwd_h.argtypes = [vp, i64, i64, i64, ci, sp, vp, vp, i64, vp, i64, vp]
+    L.gws_gated_bwd_h.restype = ci
+    L.gws_gated_bwd_x.argtypes = [vp, vp, i64, i64, i64, vp, vp, i64, i64, ci, vp, i64, vp]
+    L.gws_gated_bwd_x.restype = ci
+    L.gws_linear_bwd_w_act8_workspace_bytes.argtypes = [tp, ci, i64]
+    L.gws_linear_bwd_w_act8_workspace_bytes.restype = sz
+    L.gws_linear_bwd_w_act8.argtypes = [ap, vp, i64, i64, tp, ci, u64, vp, sz, vp]
+    L.gws_linear_bwd_w_act8.restype = ci
     L.gws_derive_seed.argtypes = [u64, u64]
     L.gws_derive_seed.restype = u64
     L.gws_status_string.argtypes = [ci]
@@ -518,6 +566,130 @@ def gws_block_absmax(t: Sequence[TensorDesc], stream=None) -> None:
     L = load_library()
     arr, n = _as_c(t)
     _check(L.gws_block_absmax(arr, n, _stream(stream)), "gws_block_absmax")
+
+
+_pack_act8 = struct.Struct("=2Q2q").pack
+_pack_saved = struct.Struct("=2Q2q2Q2q2Q2q").pack
+assert struct.calcsize("=2Q2q2Q2q2Q2q") == ctypes.sizeof(_CGatedSaved)
+_NO_ACT8 = (0, 0, 0, 0)
+
+
+def _act8_fields(a: Optional[Act8]):
+    if a is None:
+        return _NO_ACT8
+    c, s = a.codes, a.xscale
+    return (_p(c) or 0, _p(s) or 0, (c.stride(0) if c is not None else 0) if a.ldc is None else a.ldc,
+            (s.stride(0) if s is not None else 0) if a.lds is None else a.lds)
+
+
+def _marshal_act8(a: Optional[Act8]):
+    return None if a is None else _CAct8.from_buffer_copy(_pack_act8(*_act8_fields(a)))
+
+
+def _marshal_saved(s: Optional[GatedSaved]):
+    if s is None:
+        return None
+    g, u = s.g, s.u
+    return _CGatedSaved.from_buffer_copy(_pack_saved(_p(g) or 0, _p(u) or 0, g.stride(0) if g is not None else 0, u.stride(0) if u is not None else 0,
+                                                     *_act8_fields(s.g8), *_act8_fields(s.u8)))
+
+
+def _same(what: str, *sizes) -> None:
+    if len(set(sizes)) != 1:
+        raise ValueError(f"{what} differ: {sizes}")
+
+
+def _check_act8(a: Act8, rows: int, cols: int) -> None:
+    if tuple(a.codes.shape) != (rows, cols) or tuple(a.xscale.shape) != (rows, -(-cols // 32)):
+        raise ValueError(f"[{rows}, {cols}] in 8 bits has codes of that shape and scales [{rows}, {-(-cols // 32)}], not "
+                         f"{list(a.codes.shape)} and {list(a.xscale.shape)}")
+
+
+def _check_saved(s: Optional[GatedSaved], rows: int, cols: int) -> None:
+    if s is None:
+        return
+    for t in (s.g, s.u):
+        if t is not None and tuple(t.shape) != (rows, cols):
+            raise ValueError(f"a kept G or U has shape {list(t.shape)}, not [{rows}, {cols}]")
+    for a in (s.g8, s.u8):
+        if a is not None:
+            _check_act8(a, rows, cols)
+
+
+def gws_act8_encode(x, o: Act8, stream=None) -> None:
+    """BF16 ``x`` [rows, columns] to E4M3 codes and a scale for every 32 of a row."""
+    M, C = x.shape
+    _check_act8(o, M, C)
+    _check(load_library().gws_act8_encode(_p(x), M, C, x.stride(0), _marshal_act8(o), _stream(stream)), "gws_act8_encode")
+
+
+def gws_act8_decode(a: Act8, x, stream=None) -> None:
+    """The values of such codes into BF16 ``x``; exact."""
+    M, C = x.shape
+    _check_act8(a, M, C)
+    _check(load_library().gws_act8_decode(_marshal_act8(a), M, C, _p(x), x.stride(0), _stream(stream)), "gws_act8_decode")
+
+
+def gws_gated_fwd(x, wg, wu, h, act: int = ACT_SILU, saved: Optional[GatedSaved] = None, w_is_nk: bool = False, stream=None) -> None:
+    """H = a(X Wg) * (X Wu) by elements in one kernel; ``saved`` receives G and U for the backward pass."""
+    (M, K), F = x.shape, wg.shape[0 if w_is_nk else 1]
+    if tuple(wg.shape) != ((F, K) if w_is_nk else (K, F)) or wg.shape != wu.shape or tuple(h.shape) != (M, F):
+        raise ValueError(f"X {list(x.shape)}, Wg {list(wg.shape)}, Wu {list(wu.shape)} and H {list(h.shape)} do not fit together")
+    _same("leading dimensions of Wg and Wu", wg.stride(0), wu.stride(0))
+    _check_saved(saved, M, F)
+    _check(load_library().gws_gated_fwd(_p(x), M, K, x.stride(0), _p(wg), _p(wu), F, wg.stride(0), 1 if w_is_nk else 0, act, _p(h), h.stride(0),
+                                        _marshal_saved(saved), _stream(stream)), "gws_gated_fwd")
+
+
+def _check_gradients(dg, du, h, M, F):
+    if any(t is not None and tuple(t.shape) != (M, F) for t in (dg, du, h)):
+        raise ValueError(f"dG, dU and H have shape [{M}, {F}]")
+    _same("leading dimensions of dG and dU", dg.stride(0), du.stride(0))
+
+
+def gws_gated_bwd(dy, wd, saved: GatedSaved, dg, du, act: int = ACT_SILU, h=None, w_is_nk: bool = False, stream=None) -> None:
+    """dG and dU (and H again) from the gradient of Y = H Wd and the kept G and U; dH = dY Wd^T stays in the kernel."""
+    (M, D), F = dy.shape, wd.shape[1 if w_is_nk else 0]
+    if tuple(wd.shape) != ((D, F) if w_is_nk else (F, D)):
+        raise ValueError(f"dY {list(dy.shape)} and Wd {list(wd.shape)} do not fit together")
+    _check_gradients(dg, du, h, M, F)
+    _check_saved(saved, M, F)
+    _check(load_library().gws_gated_bwd(_p(dy), M, D, dy.stride(0), _p(wd), F, wd.stride(0), 1 if w_is_nk else 0, act, _marshal_saved(saved),
+                                        _p(dg), _p(du), dg.stride(0), _p(h), h.stride(0) if h is not None else 0, _stream(stream)), "gws_gated_bwd")
+
+
+def gws_gated_bwd_h(dh, saved: GatedSaved, dg, du, act: int = ACT_SILU, h=None, stream=None) -> None:
+    """``gws_gated_bwd`` from a given dH."""
+    M, F = dh.shape
+    _check_gradients(dg, du, h, M, F)
+    _check_saved(saved, M, F)
+    _check(load_library().gws_gated_bwd_h(_p(dh), M, F, dh.stride(0), act, _marshal_saved(saved), _p(dg), _p(du), dg.stride(0), _p(h),
+                                          h.stride(0) if h is not None else 0, _stream(stream)), "gws_gated_bwd_h")
+
+
+def gws_gated_bwd_x(dg, du, wg, wu, dx, w_is_nk: bool = False, stream=None) -> None:
+    """dX = dG Wg^T + dU Wu^T in one sum; ``w_is_nk`` as in ``gws_gated_fwd``."""
+    (M, F), K = dg.shape, wg.shape[1 if w_is_nk else 0]
+    if tuple(wg.shape) != ((F, K) if w_is_nk else (K, F)) or wg.shape != wu.shape or dg.shape != du.shape or tuple(dx.shape) != (M, K):
+        raise ValueError(f"dG {list(dg.shape)}, dU {list(du.shape)}, Wg {list(wg.shape)}, Wu {list(wu.shape)} and dX {list(dx.shape)} do not fit together")
+    _same("leading dimensions of dG and dU", dg.stride(0), du.stride(0))
+    _same("leading dimensions of Wg and Wu", wg.stride(0), wu.stride(0))
+    _check(load_library().gws_gated_bwd_x(_p(dg), _p(du), M, F, dg.stride(0), _p(wg), _p(wu), K, wg.stride(0), 1 if w_is_nk else 0, _p(dx), dx.stride(0),
+                                          _stream(stream)), "gws_gated_bwd_x")
+
+
+def gws_linear_bwd_w_act8_workspace_bytes(w: TensorDesc, M: int, w_is_nk: bool = False) -> int:
+    """Bytes of workspace that ``gws_linear_bwd_w_act8`` can use for this weight over ``M`` tokens."""
+    return int(load_library().gws_linear_bwd_w_act8_workspace_bytes(_marshal([w]), int(bool(w_is_nk)), int(M)))
+
+
+def gws_linear_bwd_w_act8(x: Act8, dy, w: TensorDesc, step: int, workspace, w_is_nk: bool = False, stream=None) -> None:
+    """``gws_linear_bwd_w_ws`` with the linear's input kept in 8 bits."""
+    M = dy.shape[0]
+    _check_act8(x, M, w.cols if w_is_nk else w.rows)
+    nbytes = 0 if workspace is None else int(workspace.numel() * workspace.element_size())
+    _check(load_library().gws_linear_bwd_w_act8(_marshal_act8(x), _p(dy), M, dy.stride(0), _marshal([w]), 1 if w_is_nk else 0, int(step), _p(workspace),
+                                                nbytes, _stream(stream)), "gws_linear_bwd_w_act8")
 
 
 def gws_sample_fwd_basis(t: Sequence[TensorDesc], basis: int, fmt: int, step: int, stream=None) -> None:

@@ -6,6 +6,8 @@
 #include <atomic>
 
 #include "gws_bench.h"
+#include "gws_check.h"
+#include "gws_gated.h"
 #include "gws_launch.h"
 
 // Staging buffer of gws_linear_fwd_static: device memory that belongs to the loaded code object, one copy
@@ -33,8 +35,6 @@ int scratch_of_current_device(void** out) {
   return GWS_OK;
 }
 
-inline bool aligned(const void* p, uintptr_t a) { return ((uintptr_t)p & (a - 1)) == 0; }
-
 // Shape rules common to forward and backward.
 int check_shape(const gws_tensor& t) {
   if (t.rows < 0 || t.cols < 0 || t.ld < 0) return GWS_ERR_SHAPE;
@@ -58,11 +58,6 @@ int check_fwd(const gws_tensor& t) {
   if (!aligned(t.w, 16) || !aligned(t.w_hat, 16) || !aligned(t.bt, 4) || !aligned(t.scale, 4)) return GWS_ERR_ALIGN;
   if (overlap(t.w, t.w_hat, (size_t)t.rows * t.ld * 2)) return GWS_ERR_ALIAS;
   return GWS_OK;
-}
-
-inline bool overlap2(const void* a, size_t abytes, const void* b, size_t bbytes) {
-  const uintptr_t x = (uintptr_t)a, y = (uintptr_t)b;
-  return x < y + bbytes && y < x + abytes;
 }
 
 int check_fwd_mx(const gws_tensor& t, const gws_mx_out& o, int fmt) {
@@ -683,6 +678,36 @@ int gws_linear_bwd_w_ws(const void* x, const void* dy, int64_t M, int64_t ldx, i
   return launch_bwd_w(g, w->dbt != nullptr, parts, workspace, (hipStream_t)stream);
 }
 
+// X decoded into the workspace, then the weight gradient as above with what is left of it.
+static size_t decoded_bytes(int64_t M, int64_t K) { return ((size_t)M * (size_t)K * 2 + 255) & ~(size_t)255; }
+
+size_t gws_linear_bwd_w_act8_workspace_bytes(const gws_tensor* w, int w_is_nk, int64_t M) {
+  if (!w || w->rows <= 0 || w->cols <= 0 || (w->rows & 255) != 0 || (w->cols & 255) != 0 || M <= 0 || (M & 63) != 0) return 0;
+  return decoded_bytes(M, w_is_nk ? w->cols : w->rows) + gws_linear_bwd_w_workspace_bytes(w, M);
+}
+
+int gws_linear_bwd_w_act8(const gws_act8* x, const void* dy, int64_t M, int64_t ldy, const gws_tensor* w, int w_is_nk, uint64_t step,
+                          void* workspace, size_t workspace_bytes, void* stream) {
+  if (!x || !w || !x->codes || !x->xscale || !workspace) return GWS_ERR_NULL;
+  const int64_t K = w_is_nk ? w->cols : w->rows;
+  GemmArgs g;
+  int rc = bwd_w_args(workspace, dy, M, K, ldy, w, w_is_nk, step, g);   // also: the gradient apart from the workspace's X and from dY
+  if (rc != GWS_OK) return rc;
+  if (!aligned(workspace, 256)) return GWS_ERR_ALIGN;
+  const size_t decoded = decoded_bytes(M, K);
+  if (workspace_bytes < decoded) return GWS_ERR_SHAPE;
+  const uint32_t parts = parts_within(g, workspace_bytes - decoded, compute_units());
+  const size_t used = decoded + (parts < 2 ? 0 : gemm256_tn_split_bytes(g, parts));
+  const Span2 ws = {workspace, 1, used, used}, dw = {w->dw, (size_t)w->rows, (size_t)w->cols * 2, (size_t)w->ld * 2};
+  const Span2 codes = {x->codes, (size_t)M, (size_t)K, (size_t)x->ldc}, scales = {x->xscale, (size_t)M, (size_t)K / 32, (size_t)x->lds};
+  const Span2 blocks = {w->dbt, 1, w->dbt ? (size_t)(w->rows / 32) * (w->cols / 32) * 4 : 0, 0}, in_scale = {w->scale, 1, blocks.bytes(), 0};
+  if (!apart(ws, Span2{dy, (size_t)M, (size_t)(w_is_nk ? w->rows : w->cols) * 2, (size_t)ldy * 2}) || !apart(ws, dw) || !apart(ws, codes) ||
+      !apart(ws, scales) || !apart(ws, blocks) || !apart(ws, in_scale) || !apart(dw, codes) || !apart(dw, scales)) return GWS_ERR_ALIAS;
+  rc = gws_act8_decode(x, M, K, workspace, K, stream);
+  if (rc != GWS_OK) return rc;
+  return launch_bwd_w(g, w->dbt != nullptr, parts < 2 ? 1 : parts, parts < 2 ? nullptr : (char*)workspace + decoded, (hipStream_t)stream);
+}
+
 int gws_linear_bwd_w_form_rows(const gws_tensor* w, int64_t M, size_t workspace_bytes, int on_lines) {
   if (!w || w->rows <= 0 || w->cols <= 0 || (w->rows & 255) != 0 || (w->cols & 255) != 0 || M <= 0 || (M & 63) != 0 ||
       w->rows >= (int64_t)1 << 31 || w->cols >= (int64_t)1 << 31 || M >= (int64_t)1 << 31) return 0;
@@ -926,7 +951,7 @@ const char* gws_status_string(int status) {
     case GWS_ERR_NULL: return "required pointer is NULL";
     case GWS_ERR_SHAPE: return "invalid shape, leading dimension or shard origin";
     case GWS_ERR_ALIGN: return "misaligned pointer";
-    case GWS_ERR_FORMAT: return "unknown target format";
+    case GWS_ERR_FORMAT: return "unknown format, activation or form";
     case GWS_ERR_LAUNCH: return "kernel launch failed";
     case GWS_ERR_ALIAS: return "output overlaps input";
     case GWS_ERR_TOO_LARGE: return "operand exceeds a fixed capacity of the library";
@@ -934,6 +959,6 @@ const char* gws_status_string(int status) {
   }
 }
 
-int gws_version(void) { return 7; }
+int gws_version(void) { return 8; }
 
 }  // extern "C"

@@ -1,0 +1,102 @@
+// The gate of the feed-forward block and the 8-bit form of activations: device arithmetic and launch arguments shared by
+// their kernels (internal to csrc/).
+//
+//   gate: with q = 1 / (1 + exp(-w(g))), a(g) = g q and a'(g) = q + g q (1 - q) w'(g); w(g) = c1 g + c3 g^3 is g itself for
+//   SiLU (a = g times the logistic function of g) and 2 sqrt(2/pi) (g + 0.044715 g^3) for the tanh form of GELU, since
+//   (1 + tanh z) / 2 is the logistic function of 2 z.
+//   8 bits: 32 neighbouring values of a row share X = 2^(byte - 127), the smallest for which the largest of them rounds to at
+//   most 448, the largest E4M3 value (1.8125 2^8 = 464 is the tie with what would be the next one and goes to 448), from 2^-117 to
+//   2^119 (values saturate at 448 2^119): every decoded value is then zero or a finite normal BF16 value, so decoding is exact.
+#pragma once
+
+#include "gws_device.h"
+#include "gws_launch.h"
+
+namespace gws {
+
+constexpr uint32_t kAct8Min = 10, kAct8Max = 246, kAct8Zero = 127, kAct8NaN = 255;
+
+// The scale's byte from the fp32 bits of a block's largest magnitude.  A NaN or infinity in the block makes its scale NaN.
+__device__ __forceinline__ uint32_t act8_byte(uint32_t amax) {
+  const int b = (int)(amax >> 23) - 8 + ((amax & 0x7FFFFFu) > 0x680000u ? 1 : 0);
+  const uint32_t byte = (uint32_t)(b < (int)kAct8Min ? (int)kAct8Min : b > (int)kAct8Max ? (int)kAct8Max : b);
+  return amax == 0 ? kAct8Zero : amax >= 0x7F800000u ? kAct8NaN : byte;
+}
+// X for the converters (a NaN scale's blocks are written and read apart from them).
+__device__ __forceinline__ float act8_scale(uint32_t byte) { return __uint_as_float(byte << 23); }
+
+// Four fp32 values to codes; NaN codes under a NaN scale.
+__device__ __forceinline__ uint32_t act8_codes(float (&v)[4], uint32_t byte) {
+  if (byte >= kAct8Max) {   // hardly ever: the converter does not saturate
+#pragma unroll
+    for (int e = 0; e < 4; ++e) v[e] = fminf(fmaxf(v[e], -0x1.cp127f), 0x1.cp127f);
+  }
+  i16x2 c = {0, 0};
+  c = __builtin_amdgcn_cvt_scalef32_pk_fp8_f32(c, v[0], v[1], act8_scale(byte), false);
+  c = __builtin_amdgcn_cvt_scalef32_pk_fp8_f32(c, v[2], v[3], act8_scale(byte), true);
+  uint32_t u;
+  __builtin_memcpy(&u, &c, 4);
+  return byte == kAct8NaN ? 0x7F7F7F7Fu : u;
+}
+// Two of four codes (HI: the upper two) to a packed BF16 pair.
+template <bool HI>
+__device__ __forceinline__ uint32_t act8_pair(uint32_t codes, uint32_t byte) {
+  const bf16x2 r = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(codes, act8_scale(byte), HI);
+  uint32_t u;
+  __builtin_memcpy(&u, &r, 4);
+  return byte == kAct8NaN ? 0x7FC07FC0u : u;
+}
+
+// w(g) = c1 g + c3 g^3 of an activation.
+struct Gate {
+  float c1, c3;
+};
+inline bool gate_of(int act, Gate& g) {
+  constexpr double c = 0.79788456080286535588;   // sqrt(2 / pi)
+  if (act == GWS_ACT_SILU) g = Gate{1.0f, 0.0f};
+  else if (act == GWS_ACT_GELU_TANH) g = Gate{(float)(2.0 * c), (float)(2.0 * c * 0.044715)};
+  else return false;
+  return true;
+}
+// g^2 stays finite: beyond it q is 0 or 1 and what it is multiplied by is 0.
+__device__ __forceinline__ float gate_square(float g) { return fminf(g * g, 3.0e38f); }
+__device__ __forceinline__ float gate_q(const Gate& c, float g, float g2) {
+  const float w = g * __fmaf_rn(c.c3, g2, c.c1);
+  return __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(w * -1.44269504088896340736f));
+}
+__device__ __forceinline__ float gate_a(const Gate& c, float g) { return g * gate_q(c, g, gate_square(g)); }
+// a(g) and a'(g)
+__device__ __forceinline__ void gate_both(const Gate& c, float g, float& a, float& slope) {
+  const float g2 = gate_square(g), q = gate_q(c, g, g2);
+  a = g * q;
+  slope = __fmaf_rn(a * (1.0f - q), __fmaf_rn(3.0f * c.c3, g2, c.c1), q);
+}
+__device__ __forceinline__ float bf16_lo(uint32_t pair) { return __uint_as_float(pair << 16); }
+__device__ __forceinline__ float bf16_hi(uint32_t pair) { return __uint_as_float(pair & 0xFFFF0000u); }
+
+// G and U as they are kept between the passes.
+enum class Kept { kNone = 0, kBf16 = 1, kE4m3 = 2 };
+struct KeptArgs {
+  uint8_t *g, *u;            // BF16 or codes
+  uint8_t *gs, *us;          // block scales of codes
+  uint32_t ldg, ldu;         // of g and u, in elements
+  uint32_t lsg, lsu;         // of gs and us, in bytes
+};
+
+// One product of the block: C[M x N] = A * B over K (and A2 * B2 over as many more, or A * B2 beside it).
+struct GatedArgs {
+  const uint16_t *a, *a2, *b, *b2;   // A [M x K]; B [K x N] (B_OC) or [N x K]
+  uint32_t M, N, K, lda, lda2, ldb;
+  uint32_t inv_band, inv_last;       // of the kernel's tile grid (TileGrid)
+  Gate gate;
+  KeptArgs kept;
+  uint16_t *h, *dg, *du;             // results: H; dL/dG and dL/dU; (input gradient: h)
+  uint32_t ldh, ldd;
+};
+enum class GatedOp { kFwd = 0, kBwd = 1, kDx = 2 };
+
+int launch_gated_any(const GatedArgs& g, GatedOp op, bool b_oc, Kept kept, hipStream_t stream);
+int launch_gated_bwd_h(const GatedArgs& g, Kept kept, hipStream_t stream);   // a = dL/dH, lda
+int launch_act8(bool encode, const void* x, uint64_t M, uint64_t C, uint64_t ldx, const gws_act8& o, hipStream_t stream);
+
+}  // namespace gws
