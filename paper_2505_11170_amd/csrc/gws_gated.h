@@ -86,7 +86,7 @@ struct KeptArgs {
 // One product of the block: C[M x N] = A * B over K (and A2 * B2 over as many more, or A * B2 beside it).
 struct GatedArgs {
   const uint16_t *a, *a2, *b, *b2;   // A [M x K]; B [K x N] (B_OC) or [N x K]
-  uint32_t M, N, K, lda, lda2, ldb;
+  uint32_t M, N, K, lda, ldb;
   uint32_t inv_band, inv_last;       // of the kernel's tile grid (TileGrid)
   Gate gate;
   KeptArgs kept;
@@ -95,6 +95,9 @@ struct GatedArgs {
 };
 enum class GatedOp { kFwd = 0, kBwd = 1, kDx = 2 };
 
+// 256 x 256 tiles (a pair of weights: 256 x 128 of each)
+bool gated256_applicable(const GatedArgs& g);
+int launch_gated256(const GatedArgs& g, GatedOp op, bool b_oc, Kept kept, hipStream_t stream);
 int launch_gated_any(const GatedArgs& g, GatedOp op, bool b_oc, Kept kept, hipStream_t stream);
 int launch_gated_bwd_h(const GatedArgs& g, Kept kept, hipStream_t stream);   // a = dL/dH, lda
 int launch_act8(bool encode, const void* x, uint64_t M, uint64_t C, uint64_t ldx, const gws_act8& o, hipStream_t stream);

@@ -56,9 +56,8 @@ __global__ __launch_bounds__(256) void gated_any_kernel(const GatedArgs g) {
     for (int j = 0; j < 4; ++j) acc[p][j] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
   for (int part = 0; part < (OP == GatedOp::kDx ? 2 : 1); ++part) {
     const uint16_t* a = part == 0 ? g.a : g.a2;
-    const uint32_t lda = part == 0 ? g.lda : g.lda2;
     for (uint32_t k = 8 * grp; k < g.K; k += 32) {
-      const Frag8 fa = along(a, row, lda, k);
+      const Frag8 fa = along(a, row, g.lda, k);
 #pragma unroll
       for (int p = 0; p < P; ++p) {
         const uint16_t* b = p + part == 0 ? g.b : g.b2;

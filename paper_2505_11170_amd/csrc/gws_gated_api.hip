@@ -72,6 +72,12 @@ void kept_buffers(const KeptArgs& k, Kept form, int64_t M, int64_t F, bool writt
   }
 }
 
+// The kernel by the sizes.
+int launch_gated(const GatedArgs& g, GatedOp op, bool b_oc, Kept kept, hipStream_t stream) {
+  if (gated256_applicable(g)) return launch_gated256(g, op, b_oc, kept, stream);
+  return launch_gated_any(g, op, b_oc, kept, stream);
+}
+
 }  // namespace
 }  // namespace gws
 
@@ -136,7 +142,7 @@ int gws_gated_fwd(const void* x, int64_t M, int64_t K, int64_t ldx, const void* 
   g.M = (uint32_t)M; g.N = (uint32_t)F; g.K = (uint32_t)K;
   g.lda = (uint32_t)ldx; g.ldb = (uint32_t)ldw;
   g.h = (uint16_t*)h; g.ldh = (uint32_t)ldh;
-  return launch_gated_any(g, GatedOp::kFwd, !w_is_nk, form, (hipStream_t)stream);
+  return launch_gated(g, GatedOp::kFwd, !w_is_nk, form, (hipStream_t)stream);
 }
 
 // What the two forms of the gate's backward pass share: outputs and kept values.
@@ -180,7 +186,7 @@ int gws_gated_bwd(const void* dy, int64_t M, int64_t D, int64_t lddy, const void
   g.a = (const uint16_t*)dy; g.b = (const uint16_t*)wd;
   g.K = (uint32_t)D;
   g.lda = (uint32_t)lddy; g.ldb = (uint32_t)ldw;
-  return launch_gated_any(g, GatedOp::kBwd, w_is_nk != 0, form, (hipStream_t)stream);   // contraction over D: [D x F] lies across it
+  return launch_gated(g, GatedOp::kBwd, w_is_nk != 0, form, (hipStream_t)stream);   // contraction over D: [D x F] lies across it
 }
 
 int gws_gated_bwd_h(const void* dh, int64_t M, int64_t F, int64_t lddh, int act, const gws_gated_saved* saved, void* dg, void* du,
@@ -225,9 +231,9 @@ int gws_gated_bwd_x(const void* dg, const void* du, int64_t M, int64_t F, int64_
   memset(&g, 0, sizeof g);
   g.a = (const uint16_t*)dg; g.a2 = (const uint16_t*)du; g.b = (const uint16_t*)wg; g.b2 = (const uint16_t*)wu;
   g.M = (uint32_t)M; g.N = (uint32_t)K; g.K = (uint32_t)F;
-  g.lda = g.lda2 = (uint32_t)ldd; g.ldb = (uint32_t)ldw;
+  g.lda = (uint32_t)ldd; g.ldb = (uint32_t)ldw;
   g.h = (uint16_t*)dx; g.ldh = (uint32_t)ldx;
-  return launch_gated_any(g, GatedOp::kDx, w_is_nk != 0, Kept::kNone, (hipStream_t)stream);   // contraction over F: [F x K] lies across it
+  return launch_gated(g, GatedOp::kDx, w_is_nk != 0, Kept::kNone, (hipStream_t)stream);   // contraction over F: [F x K] lies across it
 }
 
 }  // extern "C"

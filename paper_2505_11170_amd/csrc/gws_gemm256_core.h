@@ -65,6 +65,9 @@ constexpr int PC = 128 + 8;       // epilogue pitch of a wavefront's staging row
 constexpr uint32_t kMaxLd = 1u << 28;   // leading dimensions (elements) the 32-bit lane offsets of the loads reach: 7 rows x 2 bytes
 constexpr uint32_t kMaxLdEdge = 1u << 23;   // the same with edges: 255 rows x 2 bytes
 static_assert(64 * PC <= STAGE, "half a wavefront tile is staged in one stage array");
+// Where the operands come from: one of each; two B side by side, a tile then being the same 128 columns of both; or two of each, one
+// product after the other in the same sums.
+enum Source { kOne = 0, kPair = 1, kTwo = 2 };
 }  // namespace g256
 
 union Frag8 {
@@ -120,11 +123,17 @@ __device__ __forceinline__ void epilogue_bf16_half(const f32x4 (&a4)[4][8], int 
 // in the place of the others), and K (>= 64, a multiple of 32) need not be a multiple of 64; nk counts the half step.
 // NJ: column tiles of 16 of a wavefront: 8, or 6 for a tile of 256 x 192 (b and acc are that much narrower; its output-
 // contiguous B stage is 64 k-rows of 128 columns, as 256 of them are swizzled, and 64 k-rows of 64 behind it).
-template <bool A_OC, bool B_OC, bool EDGE = false, int NJ = 8, class Finish>
+// SRC = kPair: b and b2, of which n0 and b_out count the columns: acc[i][j] with j < 4 is column 64 (wave % 2) + 16 j of b's product, with
+// j >= 4 column 64 (wave % 2) + 16 (j - 4) of b2's.  Contraction-contiguous: stage rows 64 w .. 64 w + 63, one wavefront's loads, are columns
+// 64 (w / 2) .. of b (w even) or b2; output-contiguous: 64 k-rows of 128 columns of b and then of b2, two wavefronts each.
+// SRC = kTwo: nk K-steps, the first half over a, b and the others over a2, b2 (both K deep; the half step comes at the end of each).
+template <bool A_OC, bool B_OC, bool EDGE = false, int NJ = 8, int SRC = g256::kOne, class Finish>
 __device__ __forceinline__ void gemm256_accumulate(const uint16_t* __restrict__ a, uint32_t lda,
                                                    const uint16_t* __restrict__ b, uint32_t ldb, uint32_t nk, uint32_t m0,
                                                    uint32_t n0, Finish&& finish, uint32_t a_out = 0, uint32_t b_out = 0,
-                                                   uint32_t K = 0) {
+                                                   uint32_t K = 0, const uint16_t* __restrict__ a2 = nullptr,
+                                                   const uint16_t* __restrict__ b2 = nullptr) {
+  static_assert(SRC == g256::kOne || (!A_OC && NJ == 8), "");
   using namespace g256;
   __shared__ __attribute__((aligned(16))) uint16_t A0[STAGE];
   __shared__ __attribute__((aligned(16))) uint16_t A1[STAGE];
@@ -145,10 +154,27 @@ __device__ __forceinline__ void gemm256_accumulate(const uint16_t* __restrict__ 
     uint32_t voff[EDGE ? 8 : 4];   // per-lane byte offset; which one an instruction q uses: see load1
     uint32_t ld;
   };
-  auto make_src = [&](bool oc, bool narrow, const uint16_t* p, uint32_t ld, uint32_t o0, uint32_t out) {
+  auto make_src = [&](bool oc, bool narrow, const uint16_t* p, uint32_t ld, uint32_t o0, uint32_t out, bool pair = false) {
     Src s;
     s.ld = ld;
-    if (narrow && oc) {
+    if (pair && oc) {
+      // k-rows 32 (wave % 2) + 4 q + lane / 16 of 16 chunks, chunk ^ 4 (k % 4) ^ 2 (k / 8 % 2)
+      s.base = (const GWS_GLOBAL char*)((wave & 2 ? b2 : p) + (size_t)(32 * (wave & 1)) * ld + o0);
+#pragma unroll
+      for (int v = 0; v < 2; ++v) {
+        uint32_t c = (lane & 15) ^ ((lane >> 4) << 2) ^ (v << 1);
+        if (EDGE && c * 8 >= out) c = 0;
+        s.voff[v] = ((lane >> 4) * ld + c * 8) * 2;
+      }
+    } else if (pair) {   // as the forms below, of the wavefront's own weight and column half
+      const uint16_t* q0 = (wave & 1 ? b2 : p) + (size_t)(o0 + (EDGE ? 0 : 64 * (wave >> 1))) * ld;
+      s.base = (const GWS_GLOBAL char*)q0;
+#pragma unroll
+      for (int q = 0; q < (EDGE ? 8 : 4); ++q) {
+        const uint32_t row = 64 * (wave >> 1) + 8 * q + (lane >> 3);
+        s.voff[q] = ((EDGE ? (row < out ? row : out - 1) : lane >> 3) * ld + (((lane & 7) ^ (4 * (q & 1) + (lane >> 4))) * 8)) * 2;
+      }
+    } else if (narrow && oc) {
       // columns 0 .. 127: k-rows 16 wave + 4 q + lane / 16, q = 0 .. 3, chunk ^ 4 (k % 4) ^ 2 (k / 8 % 2);
       // columns 128 .. 191: k-rows 16 wave + 8 (q - 4) + lane / 8, chunk ^ 4 (k / 2 % 2) ^ 2 (k / 8 % 2)
       s.base = (const GWS_GLOBAL char*)(p + (size_t)(16 * wave) * ld + o0);
@@ -185,11 +211,18 @@ __device__ __forceinline__ void gemm256_accumulate(const uint16_t* __restrict__ 
     return s;
   };
   constexpr bool NARROW = NJ != 8;
-  const Src sa = make_src(A_OC, false, a, lda, m0, a_out), sb = make_src(B_OC, NARROW, b, ldb, n0, b_out);
-  auto load1 = [&](bool oc, bool narrow, const Src& s, uint16_t* stage, uint32_t kt, int q) {
+  constexpr bool PAIR = SRC == kPair, TWO = SRC == kTwo;
+  const Src sa = make_src(A_OC, false, a, lda, m0, a_out), sb = make_src(B_OC, NARROW, b, ldb, n0, b_out, PAIR);
+  const uint32_t nk1 = TWO ? nk >> 1 : nk;
+  const ptrdiff_t a_next = TWO ? (const char*)a2 - (const char*)a : 0, b_next = TWO ? (const char*)b2 - (const char*)b : 0;
+  auto load1 = [&](bool oc, bool narrow, const Src& s, uint16_t* stage, uint32_t kt, int q, bool pair = false, ptrdiff_t next = 0) {
+    const bool second = TWO && kt >= nk1;   // uniform
+    if (TWO) kt = __builtin_amdgcn_readfirstlane(second ? kt - nk1 : kt);
+    const GWS_GLOBAL char* base = second ? s.base + next : s.base;
     // EDGE: the half step at the end of K is fetched as the second half of a whole one
     const uint32_t k0 = EDGE ? __builtin_amdgcn_readfirstlane(kt * TK + TK > K ? K - TK : kt * TK) : kt * TK;
-    const size_t uni = narrow && oc ? (size_t)(k0 + (q < 4 ? 4 * q : 8 * (q - 4))) * s.ld
+    const size_t uni = pair && oc     ? (size_t)(k0 + 4 * q) * s.ld
+                       : narrow && oc ? (size_t)(k0 + (q < 4 ? 4 * q : 8 * (q - 4))) * s.ld
                        : oc         ? (size_t)(k0 + 2 * q) * s.ld
                        : EDGE       ? (size_t)k0
                                     : (size_t)(8 * q) * s.ld + k0;   // elements
@@ -202,13 +235,13 @@ __device__ __forceinline__ void gemm256_accumulate(const uint16_t* __restrict__ 
     // overwritten; it has to be told)
 #pragma clang diagnostic push
 #pragma clang diagnostic ignored "-Winline-asm"
-    const int v = narrow && oc ? (q < 4 ? q >> 1 : 2 + (q & 1)) : oc ? (q & 1) + 2 * ((q >> 2) & 1) : EDGE ? q : (q & 1);
+    const int v = pair && oc ? (q >> 1) & 1 : narrow && oc ? (q < 4 ? q >> 1 : 2 + (q & 1)) : oc ? (q & 1) + 2 * ((q >> 2) & 1) : EDGE ? q : (q & 1);
     asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %1"
-                 :: "v"(s.voff[v]), "s"(s.base + uni * 2), "s"(lds_addr) : "m0", "memory");
+                 :: "v"(s.voff[v]), "s"(base + uni * 2), "s"(lds_addr) : "m0", "memory");
 #pragma clang diagnostic pop
   };
-  auto load_a = [&](uint16_t* st, uint32_t kt, int q) { load1(A_OC, false, sa, st, kt, q); };
-  auto load_b = [&](uint16_t* st, uint32_t kt, int q) { load1(B_OC, NARROW, sb, st, kt, q); };
+  auto load_a = [&](uint16_t* st, uint32_t kt, int q) { load1(A_OC, false, sa, st, kt, q, false, a_next); };
+  auto load_b = [&](uint16_t* st, uint32_t kt, int q) { load1(B_OC, NARROW, sb, st, kt, q, PAIR, b_next); };
 
   // ---- fragment reads: per-lane element offsets into a stage ----
   // A fragment of the 16x16x32 MFMA is 16 outputs x 32 k: lane l holds output l % 16, k = 8 (l / 16) .. + 7.
@@ -222,7 +255,13 @@ __device__ __forceinline__ void gemm256_accumulate(const uint16_t* __restrict__ 
     }
   };
   make_off(A_OC, wm, a_off);
-  if (NARROW && B_OC) {
+  if (PAIR && B_OC) {
+#pragma unroll
+    for (int f = 0; f < 4; ++f) {   // 16-column tile 4 wn + f of either weight's half
+      const uint32_t k = 8 * grp + (li >> 2), c = 2 * (4 * wn + f) + ((li >> 1) & 1);
+      b_off[f] = k * 128 + (c ^ ((k & 3) << 2) ^ (((k >> 3) & 1) << 1)) * 8 + (li & 1) * 4;
+    }
+  } else if (NARROW && B_OC) {
 #pragma unroll
     for (int f = 0; f < NJ; ++f) {   // 16-column tile t of the stage; k = 8 grp + li / 4 (+ 4 half + 32 ks)
       const uint32_t t = NJ * wn + f, k = 8 * grp + (li >> 2), c = 2 * t + ((li >> 1) & 1);
@@ -236,8 +275,11 @@ __device__ __forceinline__ void gemm256_accumulate(const uint16_t* __restrict__ 
     make_off(B_OC, wn, b_off);
   }
   // read `half` of fragment f (0..7) of slice ks (0, 1) from a stage
-  auto read_frag = [&](bool oc, bool narrow, const uint32_t* off, Frag8& fr, const uint16_t* stage, int ks, int f, int half) {
-    if (narrow && oc) {
+  auto read_frag = [&](bool oc, bool narrow, const uint32_t* off, Frag8& fr, const uint16_t* stage, int ks, int f, int half, bool pair = false) {
+    if (pair && oc) {
+      const uint16_t* p = stage + off[f & 3] + (f >> 2) * 8192 + (ks * 32 + half * 4) * 128;
+      fr.h[half] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((GWS_LDS i16x4*)p);
+    } else if (narrow && oc) {
       // rows of 256 or 128 bytes (which part a fragment lies in depends on the wavefront); the 4 rows of `half` change
       // neither k % 4, k / 8 % 2 nor, by 4, k / 2 % 2
       const uint32_t w = NJ * wn + f < 8 ? 128 : 64;
@@ -267,7 +309,7 @@ __device__ __forceinline__ void gemm256_accumulate(const uint16_t* __restrict__ 
       read_frag(A_OC, false, a_off, fa[buf][0], As, ks, 0, n);
     } else if (n < RA + NJ * RB) {
       const int m = n - RA;
-      read_frag(B_OC, NARROW, b_off, fb[buf][m / RB], Bs, ks, m / RB, m % RB);
+      read_frag(B_OC, NARROW, b_off, fb[buf][m / RB], Bs, ks, m / RB, m % RB, PAIR);
     } else {
       const int m = n - RA - NJ * RB;
       read_frag(A_OC, false, a_off, fa[buf][1 + m / RA], As, ks, 1 + m / RA, m % RA);
@@ -352,7 +394,7 @@ __device__ __forceinline__ void gemm256_accumulate(const uint16_t* __restrict__ 
   __builtin_amdgcn_sched_barrier(0);
   // EDGE: in front of a half step, whose stage's first half belongs to the step before, that half's fragments become zeros
   auto half_step = [&](uint32_t k) {
-    if (EDGE && k * TK + TK > K) {
+    if (EDGE && (TWO ? (k >= nk1 ? k - nk1 : k) : k) * TK + TK > K) {
 #pragma unroll
       for (int f = 0; f < 8; ++f) fa[0][f].u = u32x4{0, 0, 0, 0};
 #pragma unroll
@@ -363,12 +405,20 @@ __device__ __forceinline__ void gemm256_accumulate(const uint16_t* __restrict__ 
     }
   };
   uint32_t kt = 0;
+  // with two products the first one's half step comes in it (a comparison before every step)
+  auto inner_half = [&](uint32_t k) { if (TWO) half_step(k); };
   for (; kt + 6 <= nk - (EDGE ? 1 : 0); kt += 6) {   // EDGE: the last step is never in the unrolled loop
+    inner_half(kt);
     kstep(A0, B0, A1, B1, cl(kt + 2), cl(kt + 3));
+    inner_half(kt + 1);
     kstep(A1, B1, A0, B2, cl(kt + 3), cl(kt + 4));
+    inner_half(kt + 2);
     kstep(A0, B2, A1, B0, cl(kt + 4), cl(kt + 5));
+    inner_half(kt + 3);
     kstep(A1, B0, A0, B1, cl(kt + 5), cl(kt + 6));
+    inner_half(kt + 4);
     kstep(A0, B1, A1, B2, cl(kt + 6), cl(kt + 7));
+    inner_half(kt + 5);
     kstep(A1, B2, A0, B0, cl(kt + 7), cl(kt + 8));
   }
   const uint32_t rem = nk - kt;

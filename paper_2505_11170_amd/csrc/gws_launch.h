@@ -136,7 +136,8 @@ struct TileGrid {
   __host__ __device__ __forceinline__ uint32_t log_band() const { return 3 - (inv_band & 1); }
   __host__ __device__ __forceinline__ bool joined() const { return (inv_last & 1) != 0; }
 };
-inline void set_tile_grid(GemmArgs& g, uint32_t mt, uint32_t nt, uint32_t band = 8, bool joined = false) {
+template <class Args>   // GemmArgs, GatedArgs
+inline void set_tile_grid(Args& g, uint32_t mt, uint32_t nt, uint32_t band = 8, bool joined = false) {
   const uint32_t over = mt % band, last = over == 0 ? band : over <= 2 && joined && mt > band ? band + over : over;
   g.inv_band = (reciprocal(band * nt) & ~1u) | (band == 4 ? 1 : 0);
   g.inv_last = (reciprocal(last) & ~1u) | (joined ? 1 : 0);
@@ -252,6 +253,7 @@ struct RideList {
 int launch_gemm256_ride(const GemmArgs& g, int w_is_nk, const RideList& r, int fmt, uint64_t step, uint32_t extra,
                         int rider, hipStream_t stream);
 int compute_units();   // of the current device; 0 if the query fails
+uint32_t tile_band(uint32_t mt, uint32_t nt);   // of mt x nt tiles of 256 x 256
 // Bands of four that leave one or two tile rows to a band of their own, which is the part of one or two XCDs and reads all of the other
 // operand there.
 inline bool leaves_few(uint32_t mt) { return mt % 4 == 1 || mt % 4 == 2; }
