@@ -83,6 +83,21 @@ struct KeptArgs {
   uint32_t lsg, lsu;         // of gs and us, in bytes
 };
 
+// Kept values of four columns as fp32.
+template <Kept KEPT>
+__device__ __forceinline__ void kept_four(const uint8_t* p, const uint8_t* s, uint32_t ld, uint32_t ls, uint32_t row, uint32_t col, float (&v)[4]) {
+  typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+  u32x2 w;
+  if (KEPT == Kept::kBf16) {
+    w = *(const u32x2*)(p + ((size_t)row * ld + col) * 2);
+  } else {
+    const uint32_t c = *(const uint32_t*)(p + (size_t)row * ld + col), b = s[(size_t)row * ls + (col >> 5)];
+    w = u32x2{act8_pair<false>(c, b), act8_pair<true>(c, b)};
+  }
+#pragma unroll
+  for (int e = 0; e < 4; ++e) v[e] = e & 1 ? bf16_hi(w[e >> 1]) : bf16_lo(w[e >> 1]);
+}
+
 // One product of the block: C[M x N] = A * B over K (and A2 * B2 over as many more, or A * B2 beside it).
 struct GatedArgs {
   const uint16_t *a, *a2, *b, *b2;   // A [M x K]; B [K x N] (B_OC) or [N x K]
@@ -98,6 +113,17 @@ enum class GatedOp { kFwd = 0, kBwd = 1, kDx = 2 };
 // 256 x 256 tiles (a pair of weights: 256 x 128 of each)
 bool gated256_applicable(const GatedArgs& g);
 int launch_gated256(const GatedArgs& g, GatedOp op, bool b_oc, Kept kept, hipStream_t stream);
+// 128 x 128 tiles (a pair of weights: 128 x 64 of each)
+bool gated128_applicable(const GatedArgs& g);
+int launch_gated128(const GatedArgs& g, GatedOp op, bool b_oc, Kept kept, hipStream_t stream);
+// few tokens or few tiles: the wavefronts of a workgroup split the contraction; the tile in units of 16 rows and 16 columns (of a pair of
+// weights: half of them of each), the parts, and the estimated time; p == 0: not a shape for it
+struct GatedStreamPlan {
+  int mt, nt, p;
+  double us;
+};
+GatedStreamPlan gated_stream_plan(const GatedArgs& g, GatedOp op, bool b_oc, Kept kept);
+int launch_gated_stream(const GatedArgs& g, GatedOp op, bool b_oc, Kept kept, const GatedStreamPlan& p, hipStream_t stream);
 int launch_gated_any(const GatedArgs& g, GatedOp op, bool b_oc, Kept kept, hipStream_t stream);
 int launch_gated_bwd_h(const GatedArgs& g, Kept kept, hipStream_t stream);   // a = dL/dH, lda
 int launch_act8(bool encode, const void* x, uint64_t M, uint64_t C, uint64_t ldx, const gws_act8& o, hipStream_t stream);

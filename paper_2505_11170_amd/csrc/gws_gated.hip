@@ -23,20 +23,6 @@ __device__ __forceinline__ Frag8 across(const uint16_t* p, uint32_t col, uint32_
     f.u[e] = (uint32_t)p[(size_t)(k + 2 * e) * ld + col] | (uint32_t)p[(size_t)(k + 2 * e + 1) * ld + col] << 16;
   return f;
 }
-
-// Kept values of four columns as fp32.
-template <Kept KEPT>
-__device__ __forceinline__ void kept_four(const uint8_t* p, const uint8_t* s, uint32_t ld, uint32_t ls, uint32_t row, uint32_t col, float (&v)[4]) {
-  u32x2 w;
-  if (KEPT == Kept::kBf16) {
-    w = *(const u32x2*)(p + ((size_t)row * ld + col) * 2);
-  } else {
-    const uint32_t c = *(const uint32_t*)(p + (size_t)row * ld + col), b = s[(size_t)row * ls + (col >> 5)];
-    w = u32x2{act8_pair<false>(c, b), act8_pair<true>(c, b)};
-  }
-#pragma unroll
-  for (int e = 0; e < 4; ++e) v[e] = e & 1 ? bf16_hi(w[e >> 1]) : bf16_lo(w[e >> 1]);
-}
 }  // namespace
 
 // A lane's sums: row lane % 16 of its wavefront's 16, columns 16 j + 4 (lane / 16) .. + 3.

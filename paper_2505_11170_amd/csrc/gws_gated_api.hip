@@ -74,6 +74,8 @@ void kept_buffers(const KeptArgs& k, Kept form, int64_t M, int64_t F, bool writt
 
 // The kernel by the sizes.
 int launch_gated(const GatedArgs& g, GatedOp op, bool b_oc, Kept kept, hipStream_t stream) {
+  const GatedStreamPlan stream_plan = gated_stream_plan(g, op, b_oc, kept);
+  if (stream_plan.p > 0 && stream_plan.us < 25.0) return launch_gated_stream(g, op, b_oc, kept, stream_plan, stream);
   if (gated256_applicable(g)) return launch_gated256(g, op, b_oc, kept, stream);
   return launch_gated_any(g, op, b_oc, kept, stream);
 }
