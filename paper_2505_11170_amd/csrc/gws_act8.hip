@@ -44,6 +44,10 @@ __global__ __launch_bounds__(256) void act8_encode_kernel(const Act8Args a) {
 #pragma unroll
   for (int t = 0; t < 2; ++t) {
     float v[4] = {bf16_lo(x[2 * t]), bf16_hi(x[2 * t]), bf16_lo(x[2 * t + 1]), bf16_hi(x[2 * t + 1])};
+    if (byte == kAct8Max) {
+#pragma unroll
+      for (int e = 0; e < 4; ++e) v[e] = act8_clamp(v[e]);
+    }
     code[t] = act8_codes(v, byte);
   }
   uint8_t* to = a.codes + (size_t)row * a.ldc + c;
@@ -61,7 +65,7 @@ __global__ __launch_bounds__(256) void act8_decode_kernel(const Act8Args a) {
   uint32_t row, c;
   if (!act8_place(a, row, c) || c >= a.C) return;
   const uint64_t code = *(const uint64_t*)(a.codes + (size_t)row * a.ldc + c);   // ldc is a multiple of 8
-  const uint32_t byte = a.scales[(size_t)row * a.lds + (c >> 5)], lo = (uint32_t)code, hi = (uint32_t)(code >> 32);
+  const uint32_t byte = a.scales[(size_t)row * a.lds + (c >> 5)], lo = act8_read((uint32_t)code, byte), hi = act8_read((uint32_t)(code >> 32), byte);
   const u32x4 v = {act8_pair<false>(lo, byte), act8_pair<true>(lo, byte), act8_pair<false>(hi, byte), act8_pair<true>(hi, byte)};
   uint16_t* to = a.x + (size_t)row * a.ldx + c;
   if (c + 8 <= a.C) {

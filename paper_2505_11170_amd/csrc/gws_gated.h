@@ -1,7 +1,7 @@
 // The gate of the feed-forward block and the 8-bit form of activations: device arithmetic and launch arguments shared by
 // their kernels (internal to csrc/).
 //
-//   gate: with q = 1 / (1 + exp(-w(g))), a(g) = g q and a'(g) = q + g q (1 - q) w'(g); w(g) = c1 g + c3 g^3 is g itself for
+//   gate: with q = 1 / (1 + exp(-w(g))), a(g) = g q and a'(g) = q + g q (1 - q) w'(g); w(g) is g itself for
 //   SiLU (a = g times the logistic function of g) and 2 sqrt(2/pi) (g + 0.044715 g^3) for the tanh form of GELU, since
 //   (1 + tanh z) / 2 is the logistic function of 2 z.
 //   8 bits: 32 neighbouring values of a row share X = 2^(byte - 127), the smallest for which the largest of them rounds to at
@@ -25,12 +25,14 @@ __device__ __forceinline__ uint32_t act8_byte(uint32_t amax) {
 // X for the converters (a NaN scale's blocks are written and read apart from them).
 __device__ __forceinline__ float act8_scale(uint32_t byte) { return __uint_as_float(byte << 23); }
 
+// The larger magnitude of m and two values; a NaN stays one.
+__device__ __forceinline__ float act8_larger(float m, float a, float b) {
+  return __builtin_elementwise_maximum(__builtin_elementwise_maximum(m, __builtin_fabsf(a)), __builtin_fabsf(b));
+}
+// The converter does not saturate: where a scale is the largest one (hardly ever), its values first.
+__device__ __forceinline__ float act8_clamp(float v) { return fminf(fmaxf(v, -0x1.cp127f), 0x1.cp127f); }
 // Four fp32 values to codes; NaN codes under a NaN scale.
-__device__ __forceinline__ uint32_t act8_codes(float (&v)[4], uint32_t byte) {
-  if (byte >= kAct8Max) {   // hardly ever: the converter does not saturate
-#pragma unroll
-    for (int e = 0; e < 4; ++e) v[e] = fminf(fmaxf(v[e], -0x1.cp127f), 0x1.cp127f);
-  }
+__device__ __forceinline__ uint32_t act8_codes(const float (&v)[4], uint32_t byte) {
   i16x2 c = {0, 0};
   c = __builtin_amdgcn_cvt_scalef32_pk_fp8_f32(c, v[0], v[1], act8_scale(byte), false);
   c = __builtin_amdgcn_cvt_scalef32_pk_fp8_f32(c, v[2], v[3], act8_scale(byte), true);
@@ -38,39 +40,52 @@ __device__ __forceinline__ uint32_t act8_codes(float (&v)[4], uint32_t byte) {
   __builtin_memcpy(&u, &c, 4);
   return byte == kAct8NaN ? 0x7F7F7F7Fu : u;
 }
-// Two of four codes (HI: the upper two) to a packed BF16 pair.
+// Codes as the converters take them: under a NaN scale NaN codes, whatever they are.
+__device__ __forceinline__ uint32_t act8_read(uint32_t codes, uint32_t byte) { return byte == kAct8NaN ? 0x7F7F7F7Fu : codes; }
+// Two of four codes (HI: the upper two) to fp32.
+typedef float f32x2 __attribute__((ext_vector_type(2)));
+template <bool HI>
+__device__ __forceinline__ f32x2 act8_values(uint32_t codes, uint32_t byte) {
+  return __builtin_amdgcn_cvt_scalef32_pk_f32_fp8(codes, act8_scale(byte), HI);
+}
+// The same to a packed BF16 pair.
 template <bool HI>
 __device__ __forceinline__ uint32_t act8_pair(uint32_t codes, uint32_t byte) {
   const bf16x2 r = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(codes, act8_scale(byte), HI);
   uint32_t u;
   __builtin_memcpy(&u, &r, 4);
-  return byte == kAct8NaN ? 0x7FC07FC0u : u;
+  return u;
 }
 
-// w(g) = c1 g + c3 g^3 of an activation.
+// q, a(g) and a'(g) of an activation.  g^2 stays finite: beyond it q is 0 or 1 and what it is multiplied by is 0.
+constexpr float kLog2e = 1.44269504088896340736f, kGelu1 = 1.5957691216057307118f, kGelu3 = 0.0713548162726009f;   // 2 sqrt(2/pi), that times 0.044715
+template <int ACT>
 struct Gate {
-  float c1, c3;
+  __device__ static __forceinline__ float logistic(float minus_w_log2e) { return __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(minus_w_log2e)); }
+  __device__ static __forceinline__ float square(float g) { return fminf(g * g, 3.0e38f); }
+  __device__ static __forceinline__ float a(float g) {
+    if (ACT == GWS_ACT_SILU) return g * logistic(g * -kLog2e);
+    return g * logistic(g * __fmaf_rn(-kLog2e * kGelu3, square(g), -kLog2e * kGelu1));
+  }
+  __device__ static __forceinline__ void both(float g, float& a, float& slope) {
+    if (ACT == GWS_ACT_SILU) {
+      const float q = logistic(g * -kLog2e);
+      a = g * q;
+      slope = q + __fmaf_rn(-a, q, a);
+    } else {
+      const float g2 = square(g), q = logistic(g * __fmaf_rn(-kLog2e * kGelu3, g2, -kLog2e * kGelu1));
+      a = g * q;
+      slope = __fmaf_rn(__fmaf_rn(-a, q, a), __fmaf_rn(3.0f * kGelu3, g2, kGelu1), q);
+    }
+  }
 };
-inline bool gate_of(int act, Gate& g) {
-  constexpr double c = 0.79788456080286535588;   // sqrt(2 / pi)
-  if (act == GWS_ACT_SILU) g = Gate{1.0f, 0.0f};
-  else if (act == GWS_ACT_GELU_TANH) g = Gate{(float)(2.0 * c), (float)(2.0 * c * 0.044715)};
-  else return false;
-  return true;
+// f(Gate<act>()) for the activation of a call: a uniform branch, not a kernel for each.
+template <class F>
+__device__ __forceinline__ void with_gate(int act, F&& f) {
+  if (act == GWS_ACT_SILU) f(Gate<GWS_ACT_SILU>());
+  else f(Gate<GWS_ACT_GELU_TANH>());
 }
-// g^2 stays finite: beyond it q is 0 or 1 and what it is multiplied by is 0.
-__device__ __forceinline__ float gate_square(float g) { return fminf(g * g, 3.0e38f); }
-__device__ __forceinline__ float gate_q(const Gate& c, float g, float g2) {
-  const float w = g * __fmaf_rn(c.c3, g2, c.c1);
-  return __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(w * -1.44269504088896340736f));
-}
-__device__ __forceinline__ float gate_a(const Gate& c, float g) { return g * gate_q(c, g, gate_square(g)); }
-// a(g) and a'(g)
-__device__ __forceinline__ void gate_both(const Gate& c, float g, float& a, float& slope) {
-  const float g2 = gate_square(g), q = gate_q(c, g, g2);
-  a = g * q;
-  slope = __fmaf_rn(a * (1.0f - q), __fmaf_rn(3.0f * c.c3, g2, c.c1), q);
-}
+inline bool known_act(int act) { return act == GWS_ACT_SILU || act == GWS_ACT_GELU_TANH; }
 __device__ __forceinline__ float bf16_lo(uint32_t pair) { return __uint_as_float(pair << 16); }
 __device__ __forceinline__ float bf16_hi(uint32_t pair) { return __uint_as_float(pair & 0xFFFF0000u); }
 
@@ -87,15 +102,15 @@ struct KeptArgs {
 template <Kept KEPT>
 __device__ __forceinline__ void kept_four(const uint8_t* p, const uint8_t* s, uint32_t ld, uint32_t ls, uint32_t row, uint32_t col, float (&v)[4]) {
   typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
-  u32x2 w;
   if (KEPT == Kept::kBf16) {
-    w = *(const u32x2*)(p + ((size_t)row * ld + col) * 2);
-  } else {
-    const uint32_t c = *(const uint32_t*)(p + (size_t)row * ld + col), b = s[(size_t)row * ls + (col >> 5)];
-    w = u32x2{act8_pair<false>(c, b), act8_pair<true>(c, b)};
-  }
+    const u32x2 w = *(const u32x2*)(p + ((size_t)row * ld + col) * 2);
 #pragma unroll
-  for (int e = 0; e < 4; ++e) v[e] = e & 1 ? bf16_hi(w[e >> 1]) : bf16_lo(w[e >> 1]);
+    for (int e = 0; e < 4; ++e) v[e] = e & 1 ? bf16_hi(w[e >> 1]) : bf16_lo(w[e >> 1]);
+  } else {
+    const uint32_t b = s[(size_t)row * ls + (col >> 5)], c = act8_read(*(const uint32_t*)(p + (size_t)row * ld + col), b);
+    const f32x2 lo = act8_values<false>(c, b), hi = act8_values<true>(c, b);
+    v[0] = lo[0]; v[1] = lo[1]; v[2] = hi[0]; v[3] = hi[1];
+  }
 }
 
 // One product of the block: C[M x N] = A * B over K (and A2 * B2 over as many more, or A * B2 beside it).
@@ -103,7 +118,7 @@ struct GatedArgs {
   const uint16_t *a, *a2, *b, *b2;   // A [M x K]; B [K x N] (B_OC) or [N x K]
   uint32_t M, N, K, lda, ldb;
   uint32_t inv_band, inv_last;       // of the kernel's tile grid (TileGrid)
-  Gate gate;
+  int act;
   KeptArgs kept;
   uint16_t *h, *dg, *du;             // results: H; dL/dG and dL/dU; (input gradient: h)
   uint32_t ldh, ldd;

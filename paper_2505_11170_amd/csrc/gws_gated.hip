@@ -68,8 +68,12 @@ __global__ __launch_bounds__(256) void gated_any_kernel(const GatedArgs g) {
       for (int e = 0; e < 4; ++e) {
         v[0][e] = acc[0][j][e];
         v[1][e] = acc[P - 1][j][e];
-        h[e] = gate_a(g.gate, v[0][e]) * v[1][e];
+        h[e] = v[1][e];
       }
+      with_gate(g.act, [&](auto gate) {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) h[e] *= gate.a(v[0][e]);
+      });
       if (here) *(u32x2*)(g.h + (size_t)row * g.ldh + c) = u32x2{pack_bf16_rne(h[0], h[1]), pack_bf16_rne(h[2], h[3])};
 #pragma unroll
       for (int p = 0; p < 2; ++p) {
@@ -78,14 +82,20 @@ __global__ __launch_bounds__(256) void gated_any_kernel(const GatedArgs g) {
         if (KEPT == Kept::kBf16 && here) *(u32x2*)(to + ((size_t)row * ld + c) * 2) = u32x2{pack_bf16_rne(v[p][0], v[p][1]), pack_bf16_rne(v[p][2], v[p][3])};
         if (KEPT == Kept::kE4m3) {
           // a block of 32 columns: MFMA tiles 2 (j / 2) and the next, the four lanes lane % 16 + 16 x
-          uint32_t m = 0;
+          float top = 0.0f;
 #pragma unroll
-          for (int t = 0; t < 2; ++t)
-#pragma unroll
-            for (int e = 0; e < 4; ++e) m = max(m, __float_as_uint(acc[p == 0 ? 0 : P - 1][(j & 2) + t][e]) & 0x7FFFFFFFu);
+          for (int t = 0; t < 4; ++t) {
+            const f32x4& s = acc[p == 0 ? 0 : P - 1][(j & 2) + (t >> 1)];
+            top = act8_larger(top, s[2 * (t & 1)], s[2 * (t & 1) + 1]);
+          }
+          uint32_t m = __float_as_uint(top) & 0x7FFFFFFFu;
           m = max(m, (uint32_t)__shfl_xor((int)m, 16));
           m = max(m, (uint32_t)__shfl_xor((int)m, 32));
           const uint32_t byte = act8_byte(m);
+          if (byte == kAct8Max) {
+#pragma unroll
+            for (int e = 0; e < 4; ++e) v[p][e] = act8_clamp(v[p][e]);
+          }
           if (here) *(uint32_t*)(to + (size_t)row * ld + c) = act8_codes(v[p], byte);
           if (here && grp == 0 && (j & 1) == 0) (p == 0 ? g.kept.gs : g.kept.us)[(size_t)row * (p == 0 ? g.kept.lsg : g.kept.lsu) + (c >> 5)] = (uint8_t)byte;
         }
@@ -94,14 +104,16 @@ __global__ __launch_bounds__(256) void gated_any_kernel(const GatedArgs g) {
       float vg[4], vu[4], h[4], dg[4], du[4];
       kept_four<KEPT>(g.kept.g, g.kept.gs, g.kept.ldg, g.kept.lsg, row, c, vg);
       kept_four<KEPT>(g.kept.u, g.kept.us, g.kept.ldu, g.kept.lsu, row, c, vu);
+      with_gate(g.act, [&](auto gate) {
 #pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        float a, slope;
-        gate_both(g.gate, vg[e], a, slope);
-        h[e] = a * vu[e];
-        du[e] = acc[0][j][e] * a;
-        dg[e] = acc[0][j][e] * vu[e] * slope;
-      }
+        for (int e = 0; e < 4; ++e) {
+          float a, slope;
+          gate.both(vg[e], a, slope);
+          h[e] = a * vu[e];
+          du[e] = acc[0][j][e] * a;
+          dg[e] = acc[0][j][e] * vu[e] * slope;
+        }
+      });
       *(u32x2*)(g.dg + (size_t)row * g.ldd + c) = u32x2{pack_bf16_rne(dg[0], dg[1]), pack_bf16_rne(dg[2], dg[3])};
       *(u32x2*)(g.du + (size_t)row * g.ldd + c) = u32x2{pack_bf16_rne(du[0], du[1]), pack_bf16_rne(du[2], du[3])};
       if (g.h != nullptr) *(u32x2*)(g.h + (size_t)row * g.ldh + c) = u32x2{pack_bf16_rne(h[0], h[1]), pack_bf16_rne(h[2], h[3])};
@@ -149,18 +161,20 @@ __global__ __launch_bounds__(256) void gated_bwd_h_kernel(const GatedArgs g, con
     kept_four<KEPT>(g.kept.u, g.kept.us, g.kept.ldu, g.kept.lsu, row, c + 4 * t, vu[t]);
   }
   u32x4 odg, odu, oh;
+  with_gate(g.act, [&](auto gate) {
 #pragma unroll
-  for (int p = 0; p < 4; ++p) {
-    float a[2], slope[2], u[2], dh[2] = {bf16_lo(d[p]), bf16_hi(d[p])};
+    for (int p = 0; p < 4; ++p) {
+      float a[2], slope[2], u[2], dh[2] = {bf16_lo(d[p]), bf16_hi(d[p])};
 #pragma unroll
-    for (int e = 0; e < 2; ++e) {
-      gate_both(g.gate, vg[p >> 1][2 * (p & 1) + e], a[e], slope[e]);
-      u[e] = vu[p >> 1][2 * (p & 1) + e];
+      for (int e = 0; e < 2; ++e) {
+        gate.both(vg[p >> 1][2 * (p & 1) + e], a[e], slope[e]);
+        u[e] = vu[p >> 1][2 * (p & 1) + e];
+      }
+      odg[p] = pack_bf16_rne(dh[0] * u[0] * slope[0], dh[1] * u[1] * slope[1]);
+      odu[p] = pack_bf16_rne(dh[0] * a[0], dh[1] * a[1]);
+      oh[p] = pack_bf16_rne(a[0] * u[0], a[1] * u[1]);
     }
-    odg[p] = pack_bf16_rne(dh[0] * u[0] * slope[0], dh[1] * u[1] * slope[1]);
-    odu[p] = pack_bf16_rne(dh[0] * a[0], dh[1] * a[1]);
-    oh[p] = pack_bf16_rne(a[0] * u[0], a[1] * u[1]);
-  }
+  });
   *(u32x4*)(g.dg + (size_t)row * g.ldd + c) = odg;
   *(u32x4*)(g.du + (size_t)row * g.ldd + c) = odu;
   if (g.h != nullptr) *(u32x4*)(g.h + (size_t)row * g.ldh + c) = oh;

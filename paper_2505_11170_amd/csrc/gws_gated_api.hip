@@ -124,7 +124,8 @@ int gws_gated_fwd(const void* x, int64_t M, int64_t K, int64_t ldx, const void* 
   if (!size_ok(M) || !size_ok(K) || !size_ok(F)) return GWS_ERR_SHAPE;
   GatedArgs g;
   memset(&g, 0, sizeof g);
-  if (!gate_of(act, g.gate)) return GWS_ERR_FORMAT;
+  if (!known_act(act)) return GWS_ERR_FORMAT;
+  g.act = act;
   if (M == 0 || F == 0) return GWS_OK;
   if (K == 0 || ((K | F) & 31) != 0) return GWS_ERR_SHAPE;
   if (!ld_ok(ldx, K) || !ld_ok(ldw, w_is_nk ? K : F) || !ld_ok(ldh, F)) return GWS_ERR_SHAPE;
@@ -169,7 +170,8 @@ int gws_gated_bwd(const void* dy, int64_t M, int64_t D, int64_t lddy, const void
   if (!size_ok(M) || !size_ok(D) || !size_ok(F)) return GWS_ERR_SHAPE;
   GatedArgs g;
   memset(&g, 0, sizeof g);
-  if (!gate_of(act, g.gate)) return GWS_ERR_FORMAT;
+  if (!known_act(act)) return GWS_ERR_FORMAT;
+  g.act = act;
   if (M == 0 || F == 0) return GWS_OK;
   if (D == 0 || ((D | F) & 31) != 0) return GWS_ERR_SHAPE;
   if (!ld_ok(lddy, D) || !ld_ok(ldw, w_is_nk ? F : D)) return GWS_ERR_SHAPE;
@@ -196,7 +198,8 @@ int gws_gated_bwd_h(const void* dh, int64_t M, int64_t F, int64_t lddh, int act,
   if (!size_ok(M) || !size_ok(F)) return GWS_ERR_SHAPE;
   GatedArgs g;
   memset(&g, 0, sizeof g);
-  if (!gate_of(act, g.gate)) return GWS_ERR_FORMAT;
+  if (!known_act(act)) return GWS_ERR_FORMAT;
+  g.act = act;
   if (M == 0 || F == 0) return GWS_OK;
   if ((F & 31) != 0 || !ld_ok(lddh, F)) return GWS_ERR_SHAPE;
   if (!dh) return GWS_ERR_NULL;

@@ -14,6 +14,15 @@ __device__ __forceinline__ void own_lds_wait() {
   __builtin_amdgcn_wave_barrier();
 }
 
+// The largest m of the four lanes lane % 16 + 16 x: v_permlane16_swap and v_permlane32_swap of m with itself leave a lane's own value in one
+// result and its partner's in the other.
+__device__ __forceinline__ uint32_t max_over_rows(uint32_t m) {
+  const auto a = __builtin_amdgcn_permlane16_swap(m, m, false, false);
+  m = max((uint32_t)a[0], (uint32_t)a[1]);
+  const auto b = __builtin_amdgcn_permlane32_swap(m, m, false, false);
+  return max((uint32_t)b[0], (uint32_t)b[1]);
+}
+
 // Pitch in bytes of a staged row of 16 NG values, BF16 or codes.
 template <int NG, int BYTES>
 constexpr int kPitch = 16 * NG * BYTES + 16;
@@ -35,8 +44,8 @@ __device__ __forceinline__ void rows_out(const uint8_t* cs, uint8_t* to, size_t 
 // H, and G and U as they are kept, of a wavefront's 16 NI rows x 16 NG columns from (p0, q0): a lane has both halves of an element
 // (acc[i][j] with j < NG is G, acc[i][j + NG] U), and the four lanes of a block of 32 that is kept in 8 bits meet in two cross-lane
 // steps.  Everything leaves through LDS by rows, 64 rows at a time.
-template <Kept KEPT, bool EDGE, int NI, int NG>
-__device__ __forceinline__ void fwd_out(const GatedArgs& g, const f32x4 (&acc)[NI][2 * NG], uint8_t* cs, uint32_t p0, uint32_t q0, uint32_t lane) {
+template <Kept KEPT, bool EDGE, int NI, int NG, class G>
+__device__ __forceinline__ void fwd_out_by(G gate, const GatedArgs& g, const f32x4 (&acc)[NI][2 * NG], uint8_t* cs, uint32_t p0, uint32_t q0, uint32_t lane) {
   const uint32_t li = lane & 15, grp = lane >> 4;
   uint8_t* const hs = cs;                                    // 64 rows of H, then of G and of U
   constexpr int PH = kPitch<NG, 2>, PB = kPitch<NG, 1>;
@@ -56,43 +65,49 @@ __device__ __forceinline__ void fwd_out(const GatedArgs& g, const f32x4 (&acc)[N
 #pragma unroll
     for (int i2 = 0; i2 < 4; ++i2) {
       const int i = 4 * h + i2;
-      uint32_t byte[2][NB] = {};   // [G, U][block]
+      const uint32_t row = 16 * i2 + li;
+#pragma unroll
+      for (int j = 0; j < NG; ++j) {
+        const f32x4 vg = acc[i][j], vu = acc[i][j + NG];
+        float o[4];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) o[e] = gate.a(vg[e]) * vu[e];
+        *(u32x2*)(hs + row * PH + (16 * j + 4 * grp) * 2) = u32x2{pack_bf16_rne(o[0], o[1]), pack_bf16_rne(o[2], o[3])};
+        if (KEPT == Kept::kBf16) {
+          *(u32x2*)(ks[0] + row * PH + (16 * j + 4 * grp) * 2) = u32x2{pack_bf16_rne(vg[0], vg[1]), pack_bf16_rne(vg[2], vg[3])};
+          *(u32x2*)(ks[1] + row * PH + (16 * j + 4 * grp) * 2) = u32x2{pack_bf16_rne(vu[0], vu[1]), pack_bf16_rne(vu[2], vu[3])};
+        }
+      }
       if (KEPT == Kept::kE4m3) {
+        uint32_t byte[2][NB];   // [G, U][block]
+        bool largest = false;
 #pragma unroll
         for (int p = 0; p < 2; ++p)
 #pragma unroll
           for (int b = 0; b < (int)NB; ++b) {
-            uint32_t m = 0;
+            float top = 0.0f;
 #pragma unroll
-            for (int t = 0; t < 2; ++t)
-#pragma unroll
-              for (int e = 0; e < 4; ++e) m = max(m, __float_as_uint(acc[i][NG * p + 2 * b + t][e]) & 0x7FFFFFFFu);
-            m = max(m, (uint32_t)__shfl_xor((int)m, 16));
-            m = max(m, (uint32_t)__shfl_xor((int)m, 32));
-            byte[p][b] = act8_byte(m);
+            for (int t = 0; t < 4; ++t) {
+              const f32x4& v = acc[i][NG * p + 2 * b + (t >> 1)];
+              top = act8_larger(top, v[2 * (t & 1)], v[2 * (t & 1) + 1]);
+            }
+            byte[p][b] = act8_byte(max_over_rows(__float_as_uint(top) & 0x7FFFFFFFu));
+            largest |= byte[p][b] == kAct8Max;
           }
         uint32_t mine = byte[0][0];
 #pragma unroll
         for (uint32_t n = 1; n < 2 * NB; ++n) mine = grp == n ? byte[n / NB][n % NB] : mine;
         if (grp < 2 * NB && (!EDGE || (16 * i + (int)li < rows && 32 * (int)(grp % NB) < cols))) sp[(size_t)(16 * i) * ls] = (uint8_t)mine;
-      }
-      const uint32_t row = 16 * i2 + li;
+        auto codes = [&](auto&& value) {
 #pragma unroll
-      for (int j = 0; j < NG; ++j) {
-        float v[2][4], o[4];
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          v[0][e] = acc[i][j][e];
-          v[1][e] = acc[i][j + NG][e];
-          o[e] = gate_a(g.gate, v[0][e]) * v[1][e];
-        }
-        *(u32x2*)(hs + row * PH + (16 * j + 4 * grp) * 2) = u32x2{pack_bf16_rne(o[0], o[1]), pack_bf16_rne(o[2], o[3])};
-#pragma unroll
-        for (int p = 0; p < 2; ++p) {
-          if (KEPT == Kept::kBf16)
-            *(u32x2*)(ks[p] + row * PH + (16 * j + 4 * grp) * 2) = u32x2{pack_bf16_rne(v[p][0], v[p][1]), pack_bf16_rne(v[p][2], v[p][3])};
-          if (KEPT == Kept::kE4m3) *(uint32_t*)(ks[p] + row * PB + 16 * j + 4 * grp) = act8_codes(v[p], byte[p][j >> 1]);
-        }
+          for (int j = 0; j < 2 * NG; ++j) {
+            const float v[4] = {value(acc[i][j][0]), value(acc[i][j][1]), value(acc[i][j][2]), value(acc[i][j][3])};
+            *(uint32_t*)(ks[j / NG] + row * PB + 16 * (j % NG) + 4 * grp) = act8_codes(v, byte[j / NG][j % NG / 2]);
+          }
+        };
+        // uniform; a block under a smaller scale has nothing that large
+        if (__builtin_amdgcn_ballot_w64(largest) == 0) codes([](float v) { return v; });
+        else codes([](float v) { return act8_clamp(v); });
       }
     }
     own_lds_wait();
@@ -115,39 +130,54 @@ template <Kept KEPT>
 struct KeptEight {
   u32x4 w;          // BF16, or codes in the first two
   uint32_t byte;
-  __device__ __forceinline__ void load(const uint8_t* p, const uint8_t* s, uint32_t ld, uint32_t ls, uint32_t row, uint32_t col) {
+  // p, s: uniform; off, soff: the lane's bytes from there
+  __device__ __forceinline__ void load(const GWS_GLOBAL uint8_t* p, const GWS_GLOBAL uint8_t* s, uint32_t off, uint32_t soff) {
     if (KEPT == Kept::kBf16) {
-      w = *(const u32x4*)(p + ((size_t)row * ld + col) * 2);
+      w = *(const GWS_GLOBAL u32x4*)(p + off);
     } else {
-      const u32x2 c = *(const u32x2*)(p + (size_t)row * ld + col);
+      const u32x2 c = *(const GWS_GLOBAL u32x2*)(p + off);
       w = u32x4{c[0], c[1], 0, 0};
-      byte = s[(size_t)row * ls + (col >> 5)];
+      byte = s[soff];
     }
   }
-  __device__ __forceinline__ uint32_t pair(int d) const {
-    if (KEPT == Kept::kBf16) return w[d];
-    return d & 1 ? act8_pair<true>(w[d >> 1], byte) : act8_pair<false>(w[d >> 1], byte);
+  __device__ __forceinline__ void landed() {
+    if (KEPT == Kept::kE4m3) {
+      w[0] = act8_read(w[0], byte);
+      w[1] = act8_read(w[1], byte);
+    }
+  }
+  __device__ __forceinline__ f32x2 pair(int d) const {
+    if (KEPT == Kept::kBf16) return f32x2{bf16_lo(w[d]), bf16_hi(w[d])};
+    return d & 1 ? act8_values<true>(w[d >> 1], byte) : act8_values<false>(w[d >> 1], byte);
   }
 };
 
 // dL/dG, dL/dU and H of a wavefront's 16 NI x 16 NJ part from (p0, q0): dL/dH leaves the accumulators through LDS as fp32, 32 rows at
 // a time, and meets the kept G and U, which were requested before, 8 columns of a row a lane.
-template <Kept KEPT, bool EDGE, int NI, int NJ>
-__device__ __forceinline__ void bwd_out(const GatedArgs& g, const f32x4 (&acc)[NI][NJ], float* cs, uint32_t p0, uint32_t q0, uint32_t lane) {
+template <Kept KEPT, bool EDGE, int NI, int NJ, class G>
+__device__ __forceinline__ void bwd_out_by(G gate, const GatedArgs& g, const f32x4 (&acc)[NI][NJ], float* cs, uint32_t p0, uint32_t q0, uint32_t lane) {
   constexpr int PF = 16 * NJ + 4;   // pitch of a staged row of fp32 (32 of them)
   constexpr uint32_t LANES = 2 * NJ, ROWS = 64 / LANES, IT = 32 / ROWS;
   const uint32_t li = lane & 15, grp = lane >> 4;
   const uint32_t r = lane / LANES, c = lane % LANES * 8;   // on the way out: row % ROWS, column
   const int rows = (int)g.M - (int)p0, cols = (int)g.N - (int)q0;
   const bool col_in = !EDGE || (int)c < cols;
-  KeptEight<KEPT> vg[IT], vu[IT];
+  KeptEight<KEPT> kg[2][IT], ku[2][IT];
+  // scalar bases and 32-bit lane offsets: leading dimensions are below 2^24 here
+  constexpr uint32_t E = KEPT == Kept::kBf16 ? 2 : 1;
+  auto base = [&](const void* p, size_t row_bytes, size_t col_bytes) { return (GWS_GLOBAL uint8_t*)(uintptr_t)p + (size_t)p0 * row_bytes + col_bytes; };
+  const GWS_GLOBAL uint8_t *gp = base(g.kept.g, (size_t)g.kept.ldg * E, (size_t)q0 * E), *up = base(g.kept.u, (size_t)g.kept.ldu * E, (size_t)q0 * E);
+  const GWS_GLOBAL uint8_t *gsp = base(g.kept.gs, g.kept.lsg, q0 >> 5), *usp = base(g.kept.us, g.kept.lsu, q0 >> 5);
+  GWS_GLOBAL uint8_t *dgp = base(g.dg, (size_t)g.ldd * 2, (size_t)q0 * 2), *dup = base(g.du, (size_t)g.ldd * 2, (size_t)q0 * 2), *hp = base(g.h, (size_t)g.ldh * 2, (size_t)q0 * 2);
+  const uint32_t g_off = (r * g.kept.ldg + c) * E, u_off = (r * g.kept.ldu + c) * E, gs_off = r * g.kept.lsg + (c >> 5), us_off = r * g.kept.lsu + (c >> 5);
+  const uint32_t d_off = (r * g.ldd + c) * 2, h_off = (r * g.ldh + c) * 2;
   auto request = [&](int quarter) {
 #pragma unroll
     for (uint32_t it = 0; it < IT; ++it) {
-      const uint32_t row = 32 * quarter + ROWS * it + r;
-      if (!EDGE || ((int)row < rows && col_in)) {
-        vg[it].load(g.kept.g, g.kept.gs, g.kept.ldg, g.kept.lsg, p0 + row, q0 + c);
-        vu[it].load(g.kept.u, g.kept.us, g.kept.ldu, g.kept.lsu, p0 + row, q0 + c);
+      const uint32_t row0 = 32 * quarter + ROWS * it;
+      if (!EDGE || ((int)(row0 + r) < rows && col_in)) {
+        kg[quarter & 1][it].load(gp + (size_t)row0 * g.kept.ldg * E, gsp + (size_t)row0 * g.kept.lsg, g_off, gs_off);
+        ku[quarter & 1][it].load(up + (size_t)row0 * g.kept.ldu * E, usp + (size_t)row0 * g.kept.lsu, u_off, us_off);
       }
     }
   };
@@ -158,34 +188,48 @@ __device__ __forceinline__ void bwd_out(const GatedArgs& g, const f32x4 (&acc)[N
     for (int i2 = 0; i2 < 2; ++i2)
 #pragma unroll
       for (int j = 0; j < NJ; ++j) *(f32x4*)(cs + (16 * i2 + li) * PF + 16 * j + 4 * grp) = acc[2 * quarter + i2][j];
+    // before this quarter's stores: loads and stores complete in one order, and a wait for loads behind stores is one for those too
+    if (quarter + 1 < NI / 2) request(quarter + 1);
+    __builtin_amdgcn_sched_barrier(0);
     own_lds_wait();
+    KeptEight<KEPT> (&vg)[IT] = kg[quarter & 1], (&vu)[IT] = ku[quarter & 1];
 #pragma unroll
     for (uint32_t it = 0; it < IT; ++it) {
       const uint32_t row = ROWS * it + r;
       const f32x4 d0 = *(const f32x4*)(cs + row * PF + c), d1 = *(const f32x4*)(cs + row * PF + c + 4);
       if (!EDGE || (32 * quarter + (int)row < rows && col_in)) {
         u32x4 odg, odu, oh;
+        vg[it].landed();
+        vu[it].landed();
 #pragma unroll
         for (int p = 0; p < 4; ++p) {
-          const uint32_t pg = vg[it].pair(p), pu = vu[it].pair(p);
-          const float u0 = bf16_lo(pu), u1 = bf16_hi(pu);
+          const f32x2 pg = vg[it].pair(p), pu = vu[it].pair(p);
+          const float u0 = pu[0], u1 = pu[1];
           const float h0 = p < 2 ? d0[2 * p] : d1[2 * p - 4], h1 = p < 2 ? d0[2 * p + 1] : d1[2 * p - 3];
           float a0, a1, s0, s1;
-          gate_both(g.gate, bf16_lo(pg), a0, s0);
-          gate_both(g.gate, bf16_hi(pg), a1, s1);
+          gate.both(pg[0], a0, s0);
+          gate.both(pg[1], a1, s1);
           odg[p] = pack_bf16_rne(h0 * u0 * s0, h1 * u1 * s1);
           odu[p] = pack_bf16_rne(h0 * a0, h1 * a1);
           oh[p] = pack_bf16_rne(a0 * u0, a1 * u1);
         }
-        const size_t at = p0 + 32 * quarter + row;
-        *(u32x4*)(g.dg + at * g.ldd + q0 + c) = odg;
-        *(u32x4*)(g.du + at * g.ldd + q0 + c) = odu;
-        if (g.h != nullptr) *(u32x4*)(g.h + at * g.ldh + q0 + c) = oh;
+        const uint32_t row0 = 32 * quarter + ROWS * it;
+        *(GWS_GLOBAL u32x4*)(dgp + (size_t)row0 * g.ldd * 2 + d_off) = odg;
+        *(GWS_GLOBAL u32x4*)(dup + (size_t)row0 * g.ldd * 2 + d_off) = odu;
+        if (g.h != nullptr) *(GWS_GLOBAL u32x4*)(hp + (size_t)row0 * g.ldh * 2 + h_off) = oh;
       }
     }
-    if (quarter + 1 < NI / 2) request(quarter + 1);
     own_lds_wait();
   }
+}
+
+template <Kept KEPT, bool EDGE, int NI, int NG>
+__device__ __forceinline__ void fwd_out(const GatedArgs& g, const f32x4 (&acc)[NI][2 * NG], uint8_t* cs, uint32_t p0, uint32_t q0, uint32_t lane) {
+  with_gate(g.act, [&](auto gate) { fwd_out_by<KEPT, EDGE, NI, NG>(gate, g, acc, cs, p0, q0, lane); });
+}
+template <Kept KEPT, bool EDGE, int NI, int NJ>
+__device__ __forceinline__ void bwd_out(const GatedArgs& g, const f32x4 (&acc)[NI][NJ], float* cs, uint32_t p0, uint32_t q0, uint32_t lane) {
+  with_gate(g.act, [&](auto gate) { bwd_out_by<KEPT, EDGE, NI, NJ>(gate, g, acc, cs, p0, q0, lane); });
 }
 
 }  // namespace gws

@@ -29,8 +29,12 @@ __device__ __forceinline__ void four_out(const GatedArgs& g, uint32_t row, uint3
     for (int e = 0; e < 4; ++e) {
       v[0][e] = sums[0][e];
       v[1][e] = sums[1][e];
-      h[e] = gate_a(g.gate, v[0][e]) * v[1][e];
+      h[e] = v[1][e];
     }
+    with_gate(g.act, [&](auto gate) {
+#pragma unroll
+      for (int e = 0; e < 4; ++e) h[e] *= gate.a(v[0][e]);
+    });
     if (here) *(u32x2*)(g.h + (size_t)row * g.ldh + col) = pack4(h);
 #pragma unroll
     for (int p = 0; p < 2; ++p) {
@@ -38,13 +42,15 @@ __device__ __forceinline__ void four_out(const GatedArgs& g, uint32_t row, uint3
       const uint32_t ld = p == 0 ? g.kept.ldg : g.kept.ldu;
       if (KEPT == Kept::kBf16 && here) *(u32x2*)(to + ((size_t)row * ld + col) * 2) = pack4(v[p]);
       if (KEPT == Kept::kE4m3) {
-        uint32_t m = 0;
-#pragma unroll
-        for (int e = 0; e < 4; ++e) m = max(m, __float_as_uint(v[p][e]) & 0x7FFFFFFFu);
+        uint32_t m = __float_as_uint(act8_larger(act8_larger(0.0f, v[p][0], v[p][1]), v[p][2], v[p][3])) & 0x7FFFFFFFu;
         m = max(m, dpp_u32<0xB1>(m));    // lane ^ 1
         m = max(m, dpp_u32<0x4E>(m));    // lane ^ 2
         m = max(m, dpp_u32<0x141>(m));   // row_half_mirror: the other four of eight
         const uint32_t byte = act8_byte(m);
+        if (byte == kAct8Max) {
+#pragma unroll
+          for (int e = 0; e < 4; ++e) v[p][e] = act8_clamp(v[p][e]);
+        }
         if (here) *(uint32_t*)(to + (size_t)row * ld + col) = act8_codes(v[p], byte);
         if (here && (col & 31) == 0) (p == 0 ? g.kept.gs : g.kept.us)[(size_t)row * (p == 0 ? g.kept.lsg : g.kept.lsu) + (col >> 5)] = (uint8_t)byte;
       }
@@ -53,14 +59,16 @@ __device__ __forceinline__ void four_out(const GatedArgs& g, uint32_t row, uint3
     float vg[4], vu[4], h[4], dg[4], du[4];
     kept_four<KEPT>(g.kept.g, g.kept.gs, g.kept.ldg, g.kept.lsg, row, col, vg);
     kept_four<KEPT>(g.kept.u, g.kept.us, g.kept.ldu, g.kept.lsu, row, col, vu);
+    with_gate(g.act, [&](auto gate) {
 #pragma unroll
-    for (int e = 0; e < 4; ++e) {
-      float a, slope;
-      gate_both(g.gate, vg[e], a, slope);
-      h[e] = a * vu[e];
-      du[e] = sums[0][e] * a;
-      dg[e] = sums[0][e] * vu[e] * slope;
-    }
+      for (int e = 0; e < 4; ++e) {
+        float a, slope;
+        gate.both(vg[e], a, slope);
+        h[e] = a * vu[e];
+        du[e] = sums[0][e] * a;
+        dg[e] = sums[0][e] * vu[e] * slope;
+      }
+    });
     *(u32x2*)(g.dg + (size_t)row * g.ldd + col) = pack4(dg);
     *(u32x2*)(g.du + (size_t)row * g.ldd + col) = pack4(du);
     if (g.h != nullptr) *(u32x2*)(g.h + (size_t)row * g.ldh + col) = pack4(h);
