@@ -101,6 +101,18 @@ int gws_linear_bwd_w_form_rows(const gws_tensor* w, int64_t M, size_t workspace_
  *           2^-24 of the window's width: how much of the half window, 2^23, the hardware's errors need              */
 int gws_box_muller_check(uint64_t first, uint64_t n, void* out, void* stream);
 
+/* The kernel that gws_gated_fwd, gws_gated_bwd (K: its D) or gws_gated_bwd_x takes for these sizes, layout (w_is_nk as the call takes it) and
+ * kept form (0 none, 1 BF16, 2 in 8 bits; gws_gated_bwd_x: 0): GWS_GATED_*, of GWS_GATED_STREAM with the tile's rows / 16 in bits 16.. and
+ * its columns / 16, of both weights together, in bits 8 .. 15.  lda: of X, dY, dG.  0 for what the call refuses.  Host function.             */
+#define GWS_GATED_FWD 0
+#define GWS_GATED_BWD 1
+#define GWS_GATED_BWD_X 2
+#define GWS_GATED_ANY 1
+#define GWS_GATED_STREAM 2
+#define GWS_GATED_MIDDLE 3
+#define GWS_GATED_LARGE 4
+int gws_gated_form(int op, int64_t M, int64_t K, int64_t F, int64_t lda, int64_t ldw, int w_is_nk, int kept);
+
 #ifdef __cplusplus
 }
 #endif

@@ -19,6 +19,8 @@ FMT_BF16, FMT_FP8_E4M3, FMT_FP6_E3M2 = 0, 1, 2
 LINEAR_AUTO, LINEAR_IN_OPERAND, LINEAR_TWO_KERNELS = 0, 2, 3
 BASIS_BITS, BASIS_UNIFORM_BF16, BASIS_BOX_MULLER = 0, 1, 2
 ACT_SILU, ACT_GELU_TANH = 0, 1
+GATED_FWD, GATED_BWD, GATED_BWD_X = 0, 1, 2                                          # of gws_gated_form: the call,
+GATED_ANY, GATED_STREAM, GATED_MIDDLE, GATED_LARGE = 1, 2, 3, 4                      # and its kernel
 
 # include/gws.h (the method) and include/gws_bench.h (measurement aids)
 EXPORTS = ("gws_sample_fwd", "gws_sample_bwd", "gws_sample_fwd_bi", "gws_sample_bwd_bi", "gws_sample_fwd_mx", "gws_linear_fwd", "gws_linear_fwd_mode",
@@ -28,7 +30,7 @@ EXPORTS = ("gws_sample_fwd", "gws_sample_bwd", "gws_sample_fwd_bi", "gws_sample_
            "gws_linear_bwd_w_act8", "gws_linear_bwd_w_act8_workspace_bytes",
            "gws_derive_seed", "gws_status_string", "gws_version")
 BENCH_EXPORTS = ("gws_copy_tiles", "gws_block_absmax", "gws_sample_bwd_tuned", "gws_sample_fwd_tuned", "gws_gemm_bf16_ride_probe", "gws_ride_plan",
-                 "gws_ride_plan_layout", "gws_gemm_form", "gws_gemm_tile", "gws_gemm_stream_tile", "gws_linear_bwd_w_form", "gws_linear_bwd_w_form_rows", "gws_box_muller_check")
+                 "gws_ride_plan_layout", "gws_gemm_form", "gws_gemm_tile", "gws_gemm_stream_tile", "gws_linear_bwd_w_form", "gws_linear_bwd_w_form_rows", "gws_gated_form", "gws_box_muller_check")
 # kernels as gws_gemm_form and gws_linear_bwd_w_form name them
 GEMM_STREAM, GEMM_MIDDLE, GEMM_LARGE, GEMM_LARGE_EDGE, GEMM_NARROW, GEMM_ANY_SHAPE, GEMM_STREAM_SAMPLE, GEMM_ROWS_SAMPLE, GEMM_ANY_SHAPE_SAMPLE = range(1, 10)
 BWD_W_WIDE, BWD_W_NARROW, BWD_W_PIECES_64, BWD_W_PIECES_128, BWD_W_SPLIT = 1, 2, 3, 4, 16
@@ -207,7 +209,10 @@ def load_library() -> ctypes.CDLL:
     L.gws_noise_basis.restype = ci
     L.gws_noise_packed.argtypes = [vp, i64, i64, i64, i64, u64, u64, vp]
     L.gws_noise_packed.restype = ci
-    ap, sp, sz = ctypes.POINTER(_CAct8), ctypes.POINTER(_CGatedSaved), ctypes.c_size_t
+    L.gws_gated_form.argtypes = [ci, i64, i64, i64, i64, i64, ci, ci]
+    L.gws_gated_form.restype = ci
+    ap = sp = vp   # gws_act8 and gws_gated_saved, as bytes or by reference
+    sz = ctypes.c_size_t
     L.gws_act8_encode.argtypes = [vp, i64, i64, i64, ap, vp]
     L.gws_act8_encode.restype = ci
     L.gws_act8_decode.argtypes = [ap, i64, i64, vp, i64, vp]
@@ -569,113 +574,103 @@ def gws_block_absmax(t: Sequence[TensorDesc], stream=None) -> None:
 
 
 _pack_act8 = struct.Struct("=2Q2q").pack
-_pack_saved = struct.Struct("=2Q2q2Q2q2Q2q").pack
-assert struct.calcsize("=2Q2q2Q2q2Q2q") == ctypes.sizeof(_CGatedSaved)
-_NO_ACT8 = (0, 0, 0, 0)
+_pack_saved = struct.Struct("=2Q2q2Q2q2Q2q").pack   # the fields in one go, passed as bytes (building the structures takes as long as the call)
+assert struct.calcsize("=2Q2q") == ctypes.sizeof(_CAct8) and struct.calcsize("=2Q2q2Q2q2Q2q") == ctypes.sizeof(_CGatedSaved)
 
 
-def _act8_fields(a: Optional[Act8]):
-    if a is None:
-        return _NO_ACT8
-    c, s = a.codes, a.xscale
-    return (_p(c) or 0, _p(s) or 0, (c.stride(0) if c is not None else 0) if a.ldc is None else a.ldc,
-            (s.stride(0) if s is not None else 0) if a.lds is None else a.lds)
+def _act8_fields(a: Act8, rows: int, cols: int):
+    c, s, ldc, lds = a.codes, a.xscale, a.ldc, a.lds
+    if c.shape != (rows, cols) or s.shape != (rows, -(-cols // 32)):
+        raise ValueError(f"[{rows}, {cols}] in 8 bits has codes of that shape and scales [{rows}, {-(-cols // 32)}], not {list(c.shape)} and {list(s.shape)}")
+    return c.data_ptr(), s.data_ptr(), c.stride(0) if ldc is None else ldc, s.stride(0) if lds is None else lds
 
 
-def _marshal_act8(a: Optional[Act8]):
-    return None if a is None else _CAct8.from_buffer_copy(_pack_act8(*_act8_fields(a)))
-
-
-def _marshal_saved(s: Optional[GatedSaved]):
+def _marshal_saved(s: Optional[GatedSaved], rows: int, cols: int):
     if s is None:
         return None
-    g, u = s.g, s.u
-    return _CGatedSaved.from_buffer_copy(_pack_saved(_p(g) or 0, _p(u) or 0, g.stride(0) if g is not None else 0, u.stride(0) if u is not None else 0,
-                                                     *_act8_fields(s.g8), *_act8_fields(s.u8)))
-
-
-def _same(what: str, *sizes) -> None:
-    if len(set(sizes)) != 1:
-        raise ValueError(f"{what} differ: {sizes}")
-
-
-def _check_act8(a: Act8, rows: int, cols: int) -> None:
-    if tuple(a.codes.shape) != (rows, cols) or tuple(a.xscale.shape) != (rows, -(-cols // 32)):
-        raise ValueError(f"[{rows}, {cols}] in 8 bits has codes of that shape and scales [{rows}, {-(-cols // 32)}], not "
-                         f"{list(a.codes.shape)} and {list(a.xscale.shape)}")
-
-
-def _check_saved(s: Optional[GatedSaved], rows: int, cols: int) -> None:
-    if s is None:
-        return
-    for t in (s.g, s.u):
-        if t is not None and tuple(t.shape) != (rows, cols):
-            raise ValueError(f"a kept G or U has shape {list(t.shape)}, not [{rows}, {cols}]")
-    for a in (s.g8, s.u8):
-        if a is not None:
-            _check_act8(a, rows, cols)
+    g, u, g8, u8 = s.g, s.u, s.g8, s.u8
+    if g8 is None and u8 is None and g is not None and u is not None:
+        if g.shape != (rows, cols) or u.shape != (rows, cols):
+            raise ValueError(f"a kept G or U has shape {list(g.shape)} or {list(u.shape)}, not [{rows}, {cols}]")
+        return _pack_saved(g.data_ptr(), u.data_ptr(), g.stride(0), u.stride(0), 0, 0, 0, 0, 0, 0, 0, 0)
+    if g is None and u is None and g8 is not None and u8 is not None:
+        return _pack_saved(0, 0, 0, 0, *_act8_fields(g8, rows, cols), *_act8_fields(u8, rows, cols))
+    raise ValueError("G and U are kept both as BF16 (g, u) or both in 8 bits (g8, u8)")
 
 
 def gws_act8_encode(x, o: Act8, stream=None) -> None:
     """BF16 ``x`` [rows, columns] to E4M3 codes and a scale for every 32 of a row."""
     M, C = x.shape
-    _check_act8(o, M, C)
-    _check(load_library().gws_act8_encode(_p(x), M, C, x.stride(0), _marshal_act8(o), _stream(stream)), "gws_act8_encode")
+    _check((_lib or load_library()).gws_act8_encode(x.data_ptr(), M, C, x.stride(0), _pack_act8(*_act8_fields(o, M, C)), _stream(stream)), "gws_act8_encode")
 
 
 def gws_act8_decode(a: Act8, x, stream=None) -> None:
     """The values of such codes into BF16 ``x``; exact."""
     M, C = x.shape
-    _check_act8(a, M, C)
-    _check(load_library().gws_act8_decode(_marshal_act8(a), M, C, _p(x), x.stride(0), _stream(stream)), "gws_act8_decode")
+    _check((_lib or load_library()).gws_act8_decode(_pack_act8(*_act8_fields(a, M, C)), M, C, x.data_ptr(), x.stride(0), _stream(stream)), "gws_act8_decode")
 
 
 def gws_gated_fwd(x, wg, wu, h, act: int = ACT_SILU, saved: Optional[GatedSaved] = None, w_is_nk: bool = False, stream=None) -> None:
     """H = a(X Wg) * (X Wu) by elements in one kernel; ``saved`` receives G and U for the backward pass."""
-    (M, K), F = x.shape, wg.shape[0 if w_is_nk else 1]
-    if tuple(wg.shape) != ((F, K) if w_is_nk else (K, F)) or wg.shape != wu.shape or tuple(h.shape) != (M, F):
-        raise ValueError(f"X {list(x.shape)}, Wg {list(wg.shape)}, Wu {list(wu.shape)} and H {list(h.shape)} do not fit together")
-    _same("leading dimensions of Wg and Wu", wg.stride(0), wu.stride(0))
-    _check_saved(saved, M, F)
-    _check(load_library().gws_gated_fwd(_p(x), M, K, x.stride(0), _p(wg), _p(wu), F, wg.stride(0), 1 if w_is_nk else 0, act, _p(h), h.stride(0),
-                                        _marshal_saved(saved), _stream(stream)), "gws_gated_fwd")
+    M, K = x.shape
+    size, ldw, ldh = wg.shape, wg.stride(0), h.stride(0)
+    F, Kw = size if w_is_nk else (size[1], size[0])
+    if Kw != K or wu.shape != size or h.shape != (M, F):
+        raise ValueError(f"X {list(x.shape)}, Wg {list(size)}, Wu {list(wu.shape)} and H {list(h.shape)} do not fit together")
+    if wu.stride(0) != ldw:
+        raise ValueError(f"leading dimensions of Wg and Wu differ: {ldw} and {wu.stride(0)}")
+    _check((_lib or load_library()).gws_gated_fwd(x.data_ptr(), M, K, x.stride(0), wg.data_ptr(), wu.data_ptr(), F, ldw, 1 if w_is_nk else 0, act,
+                                                  h.data_ptr(), ldh, _marshal_saved(saved, M, F), _stream(stream)), "gws_gated_fwd")
 
 
-def _check_gradients(dg, du, h, M, F):
-    if any(t is not None and tuple(t.shape) != (M, F) for t in (dg, du, h)):
+def _gradient_fields(dg, du, h, M, F):
+    """dG, dU, their leading dimension, H and its."""
+    size, ldd = (M, F), dg.stride(0)
+    if dg.shape != size or du.shape != size or (h is not None and h.shape != size):
         raise ValueError(f"dG, dU and H have shape [{M}, {F}]")
-    _same("leading dimensions of dG and dU", dg.stride(0), du.stride(0))
+    if du.stride(0) != ldd:
+        raise ValueError(f"leading dimensions of dG and dU differ: {ldd} and {du.stride(0)}")
+    return (dg.data_ptr(), du.data_ptr(), ldd, None, 0) if h is None else (dg.data_ptr(), du.data_ptr(), ldd, h.data_ptr(), h.stride(0))
 
 
 def gws_gated_bwd(dy, wd, saved: GatedSaved, dg, du, act: int = ACT_SILU, h=None, w_is_nk: bool = False, stream=None) -> None:
     """dG and dU (and H again) from the gradient of Y = H Wd and the kept G and U; dH = dY Wd^T stays in the kernel."""
-    (M, D), F = dy.shape, wd.shape[1 if w_is_nk else 0]
-    if tuple(wd.shape) != ((D, F) if w_is_nk else (F, D)):
-        raise ValueError(f"dY {list(dy.shape)} and Wd {list(wd.shape)} do not fit together")
-    _check_gradients(dg, du, h, M, F)
-    _check_saved(saved, M, F)
-    _check(load_library().gws_gated_bwd(_p(dy), M, D, dy.stride(0), _p(wd), F, wd.stride(0), 1 if w_is_nk else 0, act, _marshal_saved(saved),
-                                        _p(dg), _p(du), dg.stride(0), _p(h), h.stride(0) if h is not None else 0, _stream(stream)), "gws_gated_bwd")
+    M, D = dy.shape
+    size = wd.shape
+    F, Dw = (size[1], size[0]) if w_is_nk else size
+    if Dw != D:
+        raise ValueError(f"dY {list(dy.shape)} and Wd {list(size)} do not fit together")
+    _check((_lib or load_library()).gws_gated_bwd(dy.data_ptr(), M, D, dy.stride(0), wd.data_ptr(), F, wd.stride(0), 1 if w_is_nk else 0, act,
+                                                  _marshal_saved(saved, M, F), *_gradient_fields(dg, du, h, M, F), _stream(stream)), "gws_gated_bwd")
 
 
 def gws_gated_bwd_h(dh, saved: GatedSaved, dg, du, act: int = ACT_SILU, h=None, stream=None) -> None:
     """``gws_gated_bwd`` from a given dH."""
     M, F = dh.shape
-    _check_gradients(dg, du, h, M, F)
-    _check_saved(saved, M, F)
-    _check(load_library().gws_gated_bwd_h(_p(dh), M, F, dh.stride(0), act, _marshal_saved(saved), _p(dg), _p(du), dg.stride(0), _p(h),
-                                          h.stride(0) if h is not None else 0, _stream(stream)), "gws_gated_bwd_h")
+    _check((_lib or load_library()).gws_gated_bwd_h(dh.data_ptr(), M, F, dh.stride(0), act, _marshal_saved(saved, M, F),
+                                                    *_gradient_fields(dg, du, h, M, F), _stream(stream)), "gws_gated_bwd_h")
 
 
 def gws_gated_bwd_x(dg, du, wg, wu, dx, w_is_nk: bool = False, stream=None) -> None:
     """dX = dG Wg^T + dU Wu^T in one sum; ``w_is_nk`` as in ``gws_gated_fwd``."""
-    (M, F), K = dg.shape, wg.shape[1 if w_is_nk else 0]
-    if tuple(wg.shape) != ((F, K) if w_is_nk else (K, F)) or wg.shape != wu.shape or dg.shape != du.shape or tuple(dx.shape) != (M, K):
-        raise ValueError(f"dG {list(dg.shape)}, dU {list(du.shape)}, Wg {list(wg.shape)}, Wu {list(wu.shape)} and dX {list(dx.shape)} do not fit together")
-    _same("leading dimensions of dG and dU", dg.stride(0), du.stride(0))
-    _same("leading dimensions of Wg and Wu", wg.stride(0), wu.stride(0))
-    _check(load_library().gws_gated_bwd_x(_p(dg), _p(du), M, F, dg.stride(0), _p(wg), _p(wu), K, wg.stride(0), 1 if w_is_nk else 0, _p(dx), dx.stride(0),
-                                          _stream(stream)), "gws_gated_bwd_x")
+    M, F = dg.shape
+    size, ldw, ldd = wg.shape, wg.stride(0), dg.stride(0)
+    K, Fw = (size[1], size[0]) if w_is_nk else size
+    if Fw != F or wu.shape != size or du.shape != (M, F) or dx.shape != (M, K):
+        raise ValueError(f"dG {list(dg.shape)}, dU {list(du.shape)}, Wg {list(size)}, Wu {list(wu.shape)} and dX {list(dx.shape)} do not fit together")
+    if wu.stride(0) != ldw or du.stride(0) != ldd:
+        raise ValueError(f"leading dimensions differ: dG and dU {ldd} and {du.stride(0)}, Wg and Wu {ldw} and {wu.stride(0)}")
+    _check((_lib or load_library()).gws_gated_bwd_x(dg.data_ptr(), du.data_ptr(), M, F, ldd, wg.data_ptr(), wu.data_ptr(), K, ldw, 1 if w_is_nk else 0,
+                                                    dx.data_ptr(), dx.stride(0), _stream(stream)), "gws_gated_bwd_x")
+
+
+def gws_gated_form(op: int, M: int, K: int, F: int, w_is_nk: bool = False, kept: int = 0, lda: Optional[int] = None, ldw: Optional[int] = None) -> tuple:
+    """The kernel (``GATED_*``) of a call (``GATED_FWD``, ``GATED_BWD`` with K columns of dY, ``GATED_BWD_X``) and, of ``GATED_STREAM``, its tile in
+    units of 16 rows and columns; ``kept``: 0 nothing, 1 BF16, 2 in 8 bits.  0 for sizes that the call refuses."""
+    wide = op == GATED_BWD
+    f = int(load_library().gws_gated_form(op, M, K, F, (F if op == GATED_BWD_X else K) if lda is None else lda,
+                                          (F if w_is_nk == wide else K) if ldw is None else ldw, int(bool(w_is_nk)), kept))
+    return f & 0xFF, f >> 16, f >> 8 & 0xFF
 
 
 def gws_linear_bwd_w_act8_workspace_bytes(w: TensorDesc, M: int, w_is_nk: bool = False) -> int:
@@ -686,9 +681,8 @@ def gws_linear_bwd_w_act8_workspace_bytes(w: TensorDesc, M: int, w_is_nk: bool =
 def gws_linear_bwd_w_act8(x: Act8, dy, w: TensorDesc, step: int, workspace, w_is_nk: bool = False, stream=None) -> None:
     """``gws_linear_bwd_w_ws`` with the linear's input kept in 8 bits."""
     M = dy.shape[0]
-    _check_act8(x, M, w.cols if w_is_nk else w.rows)
     nbytes = 0 if workspace is None else int(workspace.numel() * workspace.element_size())
-    _check(load_library().gws_linear_bwd_w_act8(_marshal_act8(x), _p(dy), M, dy.stride(0), _marshal([w]), 1 if w_is_nk else 0, int(step), _p(workspace),
+    _check(load_library().gws_linear_bwd_w_act8(_pack_act8(*_act8_fields(x, M, w.cols if w_is_nk else w.rows)), _p(dy), M, dy.stride(0), _marshal([w]), 1 if w_is_nk else 0, int(step), _p(workspace),
                                                 nbytes, _stream(stream)), "gws_linear_bwd_w_act8")
 
 

@@ -1,7 +1,9 @@
 // C ABI of the gated feed-forward block and of activations kept in 8 bits: argument checks and the choice of kernel.
 // Declarations and the meaning of every argument are in include/gws.h.
+#include <math.h>
 #include <string.h>
 
+#include "gws_bench.h"
 #include "gws_check.h"
 #include "gws_gated.h"
 
@@ -72,12 +74,44 @@ void kept_buffers(const KeptArgs& k, Kept form, int64_t M, int64_t F, bool writt
   }
 }
 
-// The kernel by the sizes.
+// The kernel by the sizes: the fastest by estimates in us, each a launch and, per round of workgroups (one per compute unit), what a tile takes
+// beside its K-steps, the gate and the kept values among it, and the K-steps of 64, which take longer the more compute units are at work (busy).
+// Measured and estimated, in 256 x 256 tiles and in 128 x 128:
+//   forward, nothing kept: 1021 x 768 -> 2048 20.7, 20.3 and 9.9, 10.2; 256 x 2048 -> 5632 39.4, 37.7 and 17.3, 17.7; 2048 x 2048 -> 5632 87, 90
+//   and 97, 97; 8192 x 2048 -> 5632 291, 267 and 420, 348
+//   backward, BF16 kept: 1021 x 768 -> 2048 39, 41 and 14.5, 16.9; 3000 x 1024 -> 4096 62, 54 and 54, 54; 8192 x 2048 -> 5632 213, 223 and 306, 262
+//   input gradient: 5000 x 2 x 1280 -> 640 51, 50 and 21.7, 23.7; 2048 x 2 x 5632 -> 2048 192, 207 and 100, 99; 8192 x 2 x 5632 -> 2048 263, 262
+enum class GatedForm { kAny = GWS_GATED_ANY, kStream = GWS_GATED_STREAM, kMiddle = GWS_GATED_MIDDLE, kLarge = GWS_GATED_LARGE };
+GatedForm gated_form(const GatedArgs& g, GatedOp op, bool b_oc, Kept kept, GatedStreamPlan& plan) {
+  plan = gated_stream_plan(g, op, b_oc, kept);
+  const double cus = compute_units() > 0 ? compute_units() : 256, nk = ceil(g.K / 64.0) * (op == GatedOp::kDx ? 2 : 1);
+  const bool keeps = op == GatedOp::kFwd && kept != Kept::kNone;
+  double large = 1e30, middle = 1e30;
+  if (gated256_applicable(g)) {
+    const double n = ceil(g.M / 256.0) * ceil(g.N / (op == GatedOp::kFwd ? 128.0 : 256.0)), busy = n / (ceil(n / cus) * cus);
+    const double beside = op == GatedOp::kBwd ? 27.0 + 9.0 * busy : keeps ? 12.0 : 6.5;
+    const double step = op == GatedOp::kDx ? 1.03 + 0.42 * busy : 0.875 + 0.3 * busy;
+    large = 2.5 + ceil(n / cus) * (beside + nk * step);
+  }
+  if (gated128_applicable(g)) {
+    const double n = ceil(g.M / 128.0) * ceil(g.N / (op == GatedOp::kFwd ? 64.0 : 128.0)), busy = n / (ceil(n / cus) * cus);
+    const double beside = op == GatedOp::kBwd ? 8.0 + 2.5 * busy : keeps ? 5.6 : 2.6;
+    const double step = op == GatedOp::kDx ? 0.35 + 0.18 * busy * busy : 0.34 + 0.07 * busy;
+    middle = 2.7 + ceil(n / cus) * (beside + nk * step);
+  }
+  if (plan.p > 0 && plan.us < fmin(large, middle)) return GatedForm::kStream;
+  if (fmin(large, middle) > 1e29) return GatedForm::kAny;
+  return middle < large ? GatedForm::kMiddle : GatedForm::kLarge;
+}
+
 int launch_gated(const GatedArgs& g, GatedOp op, bool b_oc, Kept kept, hipStream_t stream) {
-  const GatedStreamPlan stream_plan = gated_stream_plan(g, op, b_oc, kept);
-  if (stream_plan.p > 0 && stream_plan.us < 25.0) return launch_gated_stream(g, op, b_oc, kept, stream_plan, stream);
-  if (gated256_applicable(g)) return launch_gated256(g, op, b_oc, kept, stream);
-  return launch_gated_any(g, op, b_oc, kept, stream);
+  GatedStreamPlan plan;
+  switch (gated_form(g, op, b_oc, kept, plan)) {
+    case GatedForm::kStream: return launch_gated_stream(g, op, b_oc, kept, plan, stream);
+    case GatedForm::kMiddle: return launch_gated128(g, op, b_oc, kept, stream);
+    case GatedForm::kLarge: return launch_gated256(g, op, b_oc, kept, stream);
+    default: return launch_gated_any(g, op, b_oc, kept, stream);
+  }
 }
 
 }  // namespace
@@ -239,6 +273,23 @@ int gws_gated_bwd_x(const void* dg, const void* du, int64_t M, int64_t F, int64_
   g.lda = (uint32_t)ldd; g.ldb = (uint32_t)ldw;
   g.h = (uint16_t*)dx; g.ldh = (uint32_t)ldx;
   return launch_gated(g, GatedOp::kDx, w_is_nk != 0, Kept::kNone, (hipStream_t)stream);   // contraction over F: [F x K] lies across it
+}
+
+int gws_gated_form(int op, int64_t M, int64_t K, int64_t F, int64_t lda, int64_t ldw, int w_is_nk, int kept) {
+  if (op < 0 || op > 2 || kept < 0 || kept > 2 || (op == GWS_GATED_BWD && kept == 0) || M <= 0 || K <= 0 || F <= 0 || ((K | F) & 31) != 0 ||
+      !size_ok(M) || !size_ok(K) || !size_ok(F) || !ld_ok(lda, op == GWS_GATED_BWD_X ? F : K) ||
+      !ld_ok(ldw, op == GWS_GATED_BWD ? (w_is_nk ? F : K) : (w_is_nk ? K : F))) return 0;
+  GatedArgs g;
+  memset(&g, 0, sizeof g);
+  g.M = (uint32_t)M;
+  g.N = (uint32_t)(op == GWS_GATED_BWD_X ? K : F);
+  g.K = (uint32_t)(op == GWS_GATED_BWD_X ? F : K);
+  g.lda = (uint32_t)lda;
+  g.ldb = (uint32_t)ldw;
+  GatedStreamPlan plan;
+  const GatedOp o = op == GWS_GATED_FWD ? GatedOp::kFwd : op == GWS_GATED_BWD ? GatedOp::kBwd : GatedOp::kDx;
+  const GatedForm form = gated_form(g, o, op == GWS_GATED_FWD ? !w_is_nk : w_is_nk != 0, o == GatedOp::kDx ? Kept::kNone : (Kept)kept, plan);
+  return (int)form | (form == GatedForm::kStream ? plan.mt << 16 | plan.nt << 8 : 0);
 }
 
 }  // extern "C"

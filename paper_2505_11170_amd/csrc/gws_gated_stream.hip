@@ -212,19 +212,31 @@ __global__ __launch_bounds__(64 * P) void gated_stream_kernel(const GatedArgs g)
   }
 }
 
+// The tile by an estimate in us: a launch and, per round of workgroups (one per compute unit: the rings fill its LDS), a fixed part, the gate
+// and the bytes of the tile's operands at the rate (bytes per ns) that a compute unit takes them.  Narrow tiles only where few columns would leave
+// compute units idle (the input gradient's K columns).  Measured and estimated:
+//   forward, G and U not kept, [F x K]: 1 x 2048 -> 5632 9.1 us; 27 9.9, 9.9; 64 11.4, 9.7; 128 15.4, 15.4; [K x F], whose 64-byte pieces of rows
+//   are half lines: 11.5; 12.3, 9.7; 14.5, 11.4; 19.3, 19.0
+//   input gradient, [K x F]: 64 x 2 x 5632 -> 2048 25.5, 26.1; 1021 x 2 x 2048 -> 768 14.6, 15.0
 GatedStreamPlan gated_stream_plan(const GatedArgs& g, GatedOp op, bool b_oc, Kept kept) {
   GatedStreamPlan best = {0, 0, 0, 1e30};
   if (g.K < 64 || g.lda >= stream::kMaxLd || g.ldb >= stream::kMaxLd) return best;
   const uint64_t cus = compute_units() > 0 ? compute_units() : 256;
-  const bool pair = op == GatedOp::kFwd;
-  const double K = op == GatedOp::kDx ? 2.0 * g.K : (double)g.K;
-  static const struct { int mt, nt, p; double rate; } tiles[] = {{1, 2, 8, 130.0}, {1, 4, 8, 130.0}, {2, 4, 4, 100.0}, {4, 4, 4, 100.0}, {8, 4, 4, 72.0}};
+  const bool pair = op == GatedOp::kFwd, two = op == GatedOp::kDx;
+  const double K = two ? 2.0 * g.K : (double)g.K;
+  static const struct { int mt, nt, p; double rate; } tiles[] = {{1, 1, 8, 130.0}, {1, 2, 8, 130.0}, {2, 2, 8, 130.0}, {1, 4, 8, 130.0},
+                                                                 {2, 4, 4, 100.0}, {4, 4, 4, 100.0}, {8, 4, 4, 72.0}};
   for (const auto& t : tiles) {
     if (t.mt == 1 && g.M > 16) continue;
+    if ((t.nt == 1 || (t.mt == 2 && t.nt == 2)) && !two) continue;
+    if (t.nt == 1 && b_oc) continue;
     if (t.nt == 2 && pair && (b_oc || kept == Kept::kE4m3)) continue;   // 16 columns of each weight: half a block, a quarter of a line
     const uint64_t bn = 16 * t.nt / (pair ? 2 : 1), wgs = ((uint64_t)g.M + 16 * t.mt - 1) / (16 * t.mt) * ((g.N + bn - 1) / bn);
+    // a weight across the contraction comes in pieces of lines; the kept values and the gate's results of a tile go through few wavefronts
+    const double weight = t.nt * (b_oc && pair ? 1.8 : b_oc && two ? 1.35 : 1.0);
+    const double beside = t.mt * t.nt * (op == GatedOp::kBwd ? 0.14 : pair && kept != Kept::kNone ? 0.06 : 0.0);
     const double rounds = (double)((wgs + cus - 1) / cus);
-    const double us = 1.8 + 2.7 * rounds + rounds * K * 2 * 16 * (t.mt + t.nt) / t.rate * 1e-3;
+    const double us = 1.8 + rounds * (2.7 + beside + K * 2 * 16 * (t.mt + weight) / t.rate * 1e-3);
     if (wgs < 0x7FFFFFFFull && us < best.us) best = {t.mt, t.nt, t.p, us};
   }
   return best;
@@ -249,6 +261,10 @@ static int launch_tile(GatedArgs g, bool b_oc, hipStream_t s) {
 
 template <GatedOp OP, Kept KEPT>
 static int launch_plan(const GatedArgs& g, bool b_oc, const GatedStreamPlan& p, hipStream_t s) {
+  if constexpr (OP == GatedOp::kDx) {
+    if (p.nt == 1) return g.M <= 8 ? launch_tile<OP, 1, 1, 8, 2, KEPT, 8>(g, b_oc, s) : launch_tile<OP, 1, 1, 8, 2, KEPT>(g, b_oc, s);
+    if (p.mt == 2 && p.nt == 2) return launch_tile<OP, 2, 2, 8, 2, KEPT>(g, b_oc, s);
+  }
   if constexpr (OP != GatedOp::kFwd || KEPT != Kept::kE4m3) {
     if (p.nt == 2) return g.M <= 8 ? launch_tile<OP, 1, 2, 8, 2, KEPT, 8>(g, b_oc, s) : launch_tile<OP, 1, 2, 8, 2, KEPT>(g, b_oc, s);
   }

@@ -177,3 +177,24 @@ def test_definition_of_the_8_bit_form():
     z = torch.tensor([[0.0, -0.0] * 16 + [math.nan] + [1.0] * 31])
     codes, xs = ref.encode(z.double())
     assert xs.tolist() == [[127, 255]] and codes[0, :2].tolist() == [0, 128] and (codes[0, 32:] == 127).all()
+
+
+def test_gated_kernels_use_no_scratch():
+    # a kernel with scratch starts later, and the tiles leave no registers over
+    from test_kernel_resources import kernels
+    mine = [k for k in kernels().values() if any(p in k[".name"] for p in ("gated", "act8"))]
+    assert len(mine) > 80 and not [k[".name"] for k in mine if k[".private_segment_fixed_size"] != 0]
+
+
+def test_query_of_the_chosen_kernel():
+    # a host function; without a device for 256 compute units
+    ensure_built()
+    form = binding.gws_gated_form
+    assert form(binding.GATED_FWD, 8192, 2048, 5632, True, 2)[0] == binding.GATED_LARGE
+    assert form(binding.GATED_FWD, 1021, 768, 2048, False, 1)[0] == binding.GATED_MIDDLE
+    assert form(binding.GATED_FWD, 1, 2048, 5632, True) == (binding.GATED_STREAM, 1, 2) or form(binding.GATED_FWD, 1, 2048, 5632, True) == (binding.GATED_STREAM, 1, 4)
+    assert form(binding.GATED_FWD, 8192, 32, 5632)[0] == binding.GATED_ANY and form(binding.GATED_FWD, 4, 2048, 64, True, lda=1 << 24)[0] == binding.GATED_ANY
+    assert form(binding.GATED_BWD_X, 8192, 2048, 5632, True)[0] == binding.GATED_LARGE
+    for bad in ((3, 4, 64, 64), (0, 0, 64, 64), (0, 4, 48, 64), (1, 4, 64, 64, False, 0), (0, 4, 64, 64, False, 3)):
+        assert form(*bad)[0] == 0
+    assert form(binding.GATED_FWD, 4, 64, 64, lda=56)[0] == 0

@@ -1,0 +1,87 @@
+"""Every kernel and tile behind the gated block's entry points, at sizes that take it: whole tiles, edges of rows and columns, half a K-step
+of 64 at the end of the contraction (of either product of the input gradient), one K-step, and activations whose scale saturates."""
+import pytest
+import torch
+
+import gated_ref as ref
+import paper_2505_11170_amd as gws
+from gpu_util import DEV, ensure_built
+from test_gpu_gated import check_bwd, check_dx, check_fwd, kept_buffers
+
+pytestmark = pytest.mark.gpu
+ANY, STREAM, MIDDLE, LARGE = (1, 0, 0), 2, (3, 0, 0), (4, 0, 0)
+KEPT = {"none": 0, "bf16": 1, "e4m3": 2}
+
+
+@pytest.fixture(scope="module", autouse=True)
+def _lib():
+    ensure_built()
+
+
+def taken(form, *args, **kw):
+    assert gws.gws_gated_form(*args, **kw) == form, (gws.gws_gated_form(*args, **kw), args, kw)
+
+
+# M, K, F, kernel; of the tiles of few tokens 16-column tiles of both weights together, narrow ones where the layout and what is kept allow them
+FORWARD = [(5, 32, 160, ANY), (7, 96, 96, (STREAM, 1, 2)), (9, 64, 64, (STREAM, 1, 2)), (3, 96, 4640, (STREAM, 1, 4)), (14, 160, 4704, (STREAM, 1, 4)),
+           (19, 96, 96, (STREAM, 2, 4)), (32, 1024, 128, (STREAM, 2, 4)), (239, 480, 1088, (STREAM, 4, 4)), (64, 512, 5632, (STREAM, 4, 4)),
+           (84, 96, 4960, (STREAM, 8, 4)), (128, 256, 5632, (STREAM, 8, 4)), (700, 736, 2080, MIDDLE), (1024, 64, 2048, MIDDLE), (256, 2048, 5632, MIDDLE),
+           (1300, 96, 5024, LARGE), (1792, 384, 2816, LARGE), (2304, 2048, 3584, LARGE), (1460, 288, 4448, LARGE)]
+BACKWARD = [(5, 32, 160, ANY), (7, 96, 96, (STREAM, 1, 2)), (16, 64, 96, (STREAM, 1, 2)), (3, 96, 9248, (STREAM, 1, 4)), (13, 64, 12288, (STREAM, 1, 4)),
+            (19, 96, 96, (STREAM, 2, 4)), (32, 1024, 128, (STREAM, 2, 4)), (202, 96, 2400, (STREAM, 4, 4)), (118, 448, 4800, (STREAM, 4, 4)),
+            (1110, 96, 928, (STREAM, 8, 4)), (1021, 768, 2048, (STREAM, 8, 4)), (1211, 416, 2112, MIDDLE), (2048, 512, 2048, MIDDLE), (600, 1056, 5536, MIDDLE),
+            (2048, 2048, 5632, LARGE), (2300, 2080, 5152, LARGE)]
+GRADIENT = [(5, 160, 32, ANY), (7, 96, 96, (STREAM, 1, 2)), (16, 4160, 64, (STREAM, 1, 2)), (11, 12288, 96, (STREAM, 1, 4)), (21, 96, 96, (STREAM, 2, 2)),
+            (32, 1024, 1024, (STREAM, 2, 2)), (184, 1376, 96, (STREAM, 2, 4)), (700, 768, 2016, (STREAM, 4, 4)), (2061, 480, 96, (STREAM, 8, 4)),
+            (1169, 1696, 96, MIDDLE), (2048, 2048, 544, MIDDLE), (4096, 768, 1056, MIDDLE), (6000, 2016, 480, LARGE), (8192, 2048, 256, LARGE)]
+
+
+@pytest.mark.parametrize("kept", ["none", "bf16", "e4m3"])
+@pytest.mark.parametrize("nk", [False, True])
+@pytest.mark.parametrize("M,K,F,form", FORWARD)
+def test_forward(M, K, F, form, nk, kept):
+    f = gws.gws_gated_form(gws.GATED_FWD, M, K, F, nk, KEPT[kept])
+    if form == (STREAM, 1, 2) and (not nk or kept == "e4m3"):
+        form = (STREAM, 1, 4)                        # 32 columns of each weight at least
+    if form == (STREAM, 1, 4) and nk and kept != "e4m3":
+        assert f in ((STREAM, 1, 2), (STREAM, 1, 4))
+    else:
+        taken(form, gws.GATED_FWD, M, K, F, nk, KEPT[kept])
+    check_fwd(M, K, F, nk, M % 2, kept, pad=8 * (M % 3))
+
+
+@pytest.mark.parametrize("kept", ["bf16", "e4m3"])
+@pytest.mark.parametrize("nk", [False, True])
+@pytest.mark.parametrize("M,D,F,form", BACKWARD)
+def test_backward(M, D, F, form, nk, kept):
+    taken(form, gws.GATED_BWD, M, D, F, nk, KEPT[kept])
+    check_bwd(M, D, F, nk, M % 2, kept, pad=8 * (M % 3), h=M % 5 != 0)
+
+
+@pytest.mark.parametrize("nk", [False, True])
+@pytest.mark.parametrize("M,K,F,form", GRADIENT)
+def test_input_gradient(M, K, F, form, nk):
+    if form == (STREAM, 1, 2) and not nk and K < 4160:
+        form = (STREAM, 1, 1)                        # 16 columns of a weight along the contraction
+    taken(form, gws.GATED_BWD_X, M, K, F, nk)
+    check_dx(M, K, F, nk, pad=8 * (M % 3))
+
+
+@pytest.mark.parametrize("M,F,form", [(9, 160, (STREAM, 1, 4)), (700, 2080, MIDDLE), (1300, 5024, LARGE), (5, 160, ANY)])
+def test_values_beyond_the_largest_scale(M, F, form):
+    # one product per sum: G of up to 3.2e38, which its BF16 rounding and 464 2^119 = 3.08e38 lie below
+    K = 32 if form == ANY else 96
+    taken(form, gws.GATED_FWD, M, K, F, True, 2)
+    x = torch.zeros(M, K, dtype=torch.bfloat16, device=DEV)
+    x[:, 0] = torch.tensor([2.0 ** 64, -(2.0 ** 64), 2.0 ** 60, 1.0], dtype=torch.bfloat16).repeat(-(-M // 4))[:M].to(DEV)
+    w = torch.zeros(F, K, dtype=torch.bfloat16, device=DEV)
+    w[:, 0] = (2.0 ** 63 * (1.0 + torch.arange(F, device=DEV) % 32 * (0.875 / 31))).bfloat16()
+    u = torch.zeros_like(w)
+    h = torch.zeros(M, F, dtype=torch.bfloat16, device=DEV)
+    saved, _ = kept_buffers("e4m3", M, F)
+    gws.gws_gated_fwd(x, w, u, h, saved=saved, w_is_nk=True)
+    torch.cuda.synchronize()
+    codes, scales = ref.encode(x.double() @ w.double().t())
+    assert int(scales.max()) == 246
+    assert torch.equal(saved.g8.codes, codes) and torch.equal(saved.g8.xscale, scales)
+    assert (saved.u8.codes & 127 == 0).all() and (saved.u8.xscale == 127).all()
