@@ -111,6 +111,7 @@ int gws_box_muller_check(uint64_t first, uint64_t n, void* out, void* stream);
 #define GWS_GATED_STREAM 2
 #define GWS_GATED_MIDDLE 3
 #define GWS_GATED_LARGE 4
+#define GWS_GATED_SHARED 5 /* the middle tile, two workgroups a compute unit */
 int gws_gated_form(int op, int64_t M, int64_t K, int64_t F, int64_t lda, int64_t ldw, int w_is_nk, int kept);
 
 #ifdef __cplusplus

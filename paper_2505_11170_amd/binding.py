@@ -20,7 +20,7 @@ LINEAR_AUTO, LINEAR_IN_OPERAND, LINEAR_TWO_KERNELS = 0, 2, 3
 BASIS_BITS, BASIS_UNIFORM_BF16, BASIS_BOX_MULLER = 0, 1, 2
 ACT_SILU, ACT_GELU_TANH = 0, 1
 GATED_FWD, GATED_BWD, GATED_BWD_X = 0, 1, 2                                          # of gws_gated_form: the call,
-GATED_ANY, GATED_STREAM, GATED_MIDDLE, GATED_LARGE = 1, 2, 3, 4                      # and its kernel
+GATED_ANY, GATED_STREAM, GATED_MIDDLE, GATED_LARGE, GATED_SHARED = 1, 2, 3, 4, 5     # and its kernel
 
 # include/gws.h (the method) and include/gws_bench.h (measurement aids)
 EXPORTS = ("gws_sample_fwd", "gws_sample_bwd", "gws_sample_fwd_bi", "gws_sample_bwd_bi", "gws_sample_fwd_mx", "gws_linear_fwd", "gws_linear_fwd_mode",

@@ -98,20 +98,38 @@ struct KeptArgs {
   uint32_t lsg, lsu;         // of gs and us, in bytes
 };
 
-// Kept values of four columns as fp32.
+// Kept values of four columns, on their way and as fp32.
 template <Kept KEPT>
-__device__ __forceinline__ void kept_four(const uint8_t* p, const uint8_t* s, uint32_t ld, uint32_t ls, uint32_t row, uint32_t col, float (&v)[4]) {
-  typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
-  if (KEPT == Kept::kBf16) {
-    const u32x2 w = *(const u32x2*)(p + ((size_t)row * ld + col) * 2);
-#pragma unroll
-    for (int e = 0; e < 4; ++e) v[e] = e & 1 ? bf16_hi(w[e >> 1]) : bf16_lo(w[e >> 1]);
-  } else {
-    const uint32_t b = s[(size_t)row * ls + (col >> 5)], c = act8_read(*(const uint32_t*)(p + (size_t)row * ld + col), b);
-    const f32x2 lo = act8_values<false>(c, b), hi = act8_values<true>(c, b);
-    v[0] = lo[0]; v[1] = lo[1]; v[2] = hi[0]; v[3] = hi[1];
+struct KeptFour {
+  uint32_t lo, hi, byte;   // BF16 pairs, or codes and their scale
+  __device__ __forceinline__ void load(const uint8_t* p, const uint8_t* s, uint32_t ld, uint32_t ls, uint32_t row, uint32_t col) {
+    if (KEPT == Kept::kBf16) {
+      const uint64_t w = *(const uint64_t*)(p + ((size_t)row * ld + col) * 2);
+      lo = (uint32_t)w;
+      hi = (uint32_t)(w >> 32);
+    } else {
+      lo = *(const uint32_t*)(p + (size_t)row * ld + col);
+      byte = s[(size_t)row * ls + (col >> 5)];
+    }
   }
-}
+  __device__ __forceinline__ void values(float (&v)[4]) const {
+    if (KEPT == Kept::kBf16) {
+      v[0] = bf16_lo(lo); v[1] = bf16_hi(lo); v[2] = bf16_lo(hi); v[3] = bf16_hi(hi);
+    } else {
+      const uint32_t c = act8_read(lo, byte);
+      const f32x2 a = act8_values<false>(c, byte), b = act8_values<true>(c, byte);
+      v[0] = a[0]; v[1] = a[1]; v[2] = b[0]; v[3] = b[1];
+    }
+  }
+};
+template <Kept KEPT>
+struct KeptFours {
+  KeptFour<KEPT> g, u;
+  __device__ __forceinline__ void load(const KeptArgs& k, uint32_t row, uint32_t col) {
+    g.load(k.g, k.gs, k.ldg, k.lsg, row, col);
+    u.load(k.u, k.us, k.ldu, k.lsu, row, col);
+  }
+};
 
 // One product of the block: C[M x N] = A * B over K (and A2 * B2 over as many more, or A * B2 beside it).
 struct GatedArgs {
@@ -130,7 +148,8 @@ bool gated256_applicable(const GatedArgs& g);
 int launch_gated256(const GatedArgs& g, GatedOp op, bool b_oc, Kept kept, hipStream_t stream);
 // 128 x 128 tiles (a pair of weights: 128 x 64 of each)
 bool gated128_applicable(const GatedArgs& g);
-int launch_gated128(const GatedArgs& g, GatedOp op, bool b_oc, Kept kept, hipStream_t stream);
+// two: two workgroups a compute unit (not the input gradient)
+int launch_gated128(const GatedArgs& g, GatedOp op, bool b_oc, Kept kept, bool two, hipStream_t stream);
 // few tokens or few tiles: the wavefronts of a workgroup split the contraction; the tile in units of 16 rows and 16 columns (of a pair of
 // weights: half of them of each), the parts, and the estimated time; p == 0: not a shape for it
 struct GatedStreamPlan {

@@ -102,8 +102,10 @@ __global__ __launch_bounds__(256) void gated_any_kernel(const GatedArgs g) {
       }
     } else if (here) {
       float vg[4], vu[4], h[4], dg[4], du[4];
-      kept_four<KEPT>(g.kept.g, g.kept.gs, g.kept.ldg, g.kept.lsg, row, c, vg);
-      kept_four<KEPT>(g.kept.u, g.kept.us, g.kept.ldu, g.kept.lsu, row, c, vu);
+      KeptFours<KEPT> kept;
+      kept.load(g.kept, row, c);
+      kept.g.values(vg);
+      kept.u.values(vu);
       with_gate(g.act, [&](auto gate) {
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
@@ -155,10 +157,13 @@ __global__ __launch_bounds__(256) void gated_bwd_h_kernel(const GatedArgs g, con
   }
   const u32x4 d = *(const u32x4*)(g.a + (size_t)row * g.lda + c);
   float vg[2][4], vu[2][4];
+  KeptFours<KEPT> kept[2];
+  kept[0].load(g.kept, row, c);
+  kept[1].load(g.kept, row, c + 4);
 #pragma unroll
   for (int t = 0; t < 2; ++t) {
-    kept_four<KEPT>(g.kept.g, g.kept.gs, g.kept.ldg, g.kept.lsg, row, c + 4 * t, vg[t]);
-    kept_four<KEPT>(g.kept.u, g.kept.us, g.kept.ldu, g.kept.lsu, row, c + 4 * t, vu[t]);
+    kept[t].g.values(vg[t]);
+    kept[t].u.values(vu[t]);
   }
   u32x4 odg, odu, oh;
   with_gate(g.act, [&](auto gate) {

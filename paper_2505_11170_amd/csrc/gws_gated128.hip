@@ -1,6 +1,9 @@
 // The products of the gated block in 128 x 128 tiles (gfx950), for sizes with too few 256 x 256 tiles: the loop of gws_gemm128.hip (2 x 2
 // wavefronts, K-steps of 64, operand tiles straight into a ring of four LDS stages, one barrier a K-step between its two halves), with
 // 64 columns of two weights side by side (forward) or two products in one sum (input gradient).
+// D: stages.  With four a workgroup has a compute unit for itself; with two a second one shares it, whose K-steps run under the other's way
+// out: more tiles than compute units, 4096 x 768 -> 2048 backward from 8 bits 29 -> 22.5 us, forward 32 -> 26; 2048 x 2048 -> 5632 forward 99
+// -> 82.  One workgroup alone waits longer for its loads: 256 x 2048 -> 5632 forward 17.4 and 23.0.
 //   forward: stage rows 32 w .. 32 w + 31 of [F x K] weights, one wavefront's loads, are columns 32 (w / 2) .. of Wg (w even) or Wu; of [K x F]
 //   weights 64 k-rows of 64 columns of Wg and then of Wu, two wavefronts each.  Either way a wavefront multiplies 32 columns of both.
 #include "gws_gated_out.h"
@@ -9,13 +12,13 @@
 namespace gws {
 
 namespace {
-constexpr int T = 128, TK = 64, D = 4, NJ = 4;   // rows and stage columns of a tile, depth of a K-step, stages, column tiles of a wavefront
+constexpr int T = 128, TK = 64, NJ = 4;              // rows and stage columns of a tile, depth of a K-step, column tiles of a wavefront
 constexpr int OPERAND = T * TK, STG = 2 * OPERAND;   // elements of one operand's tile, of a stage
 constexpr uint32_t kMaxLd128 = 1u << 24;             // 32-bit lane offsets: 127 rows x 2 bytes
 }  // namespace
 
-template <GatedOp OP, bool W_NK, Kept KEPT>
-__global__ __launch_bounds__(256) void gated128_kernel(const GatedArgs g) {
+template <GatedOp OP, bool W_NK, Kept KEPT, int D>
+__global__ __launch_bounds__(256, D == 2 ? 2 : 1) void gated128_kernel(const GatedArgs g) {
   using stream::umin;
   constexpr bool PAIR = OP == GatedOp::kFwd, TWO = OP == GatedOp::kDx;
   constexpr uint32_t TC = PAIR ? T / 2 : T;          // columns of a tile
@@ -116,6 +119,9 @@ __global__ __launch_bounds__(256) void gated128_kernel(const GatedArgs g) {
     const int i = n / NJ, j = n % NJ;
     acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(fw[h][j].v, fx[h][i].v, acc[i][j], 0, 0, 0);
   };
+  const uint32_t p0 = m0 + 64 * wm, q0 = n0 + TC / 2 * wn;   // of the wavefront's part of the result
+  [[maybe_unused]] KeptTile<KEPT == Kept::kNone ? Kept::kBf16 : KEPT, true, 4, 4> kept;
+  if constexpr (OP == GatedOp::kBwd) kept.request(g, p0, q0, lane, 0);   // its first rows land under the loop
   constexpr int LOADS = 8;   // load instructions of a wavefront and K-step
 #pragma unroll
   for (int s = 0; s < D; ++s)
@@ -184,12 +190,11 @@ __global__ __launch_bounds__(256) void gated128_kernel(const GatedArgs g) {
   }
   asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");   // the ring is read
 
-  uint16_t* cs = lds + wave * STG;
-  const uint32_t p0 = m0 + 64 * wm, q0 = n0 + TC / 2 * wn;
+  uint16_t* cs = lds + wave * (D * STG / 4);
   if constexpr (OP == GatedOp::kFwd) {
     fwd_out<KEPT, true, 4, 2>(g, acc, (uint8_t*)cs, p0, q0, lane);
   } else if constexpr (OP == GatedOp::kBwd) {
-    bwd_out<KEPT, true, 4, 4>(g, acc, (float*)cs, p0, q0, lane);
+    bwd_out<KEPT, true, 4, 4>(g, acc, kept, (float*)cs, p0, q0, lane);
   } else {
 #pragma unroll
     for (int i = 0; i < 4; ++i)
@@ -201,25 +206,27 @@ __global__ __launch_bounds__(256) void gated128_kernel(const GatedArgs g) {
   }
 }
 
-bool gated128_applicable(const GatedArgs& g) { return g.K >= 64 && g.lda < kMaxLd128 && g.ldb < kMaxLd128; }
+bool gated128_applicable(const GatedArgs& g) { return g.K >= 64 && out_lds_ok(g) && g.lda < kMaxLd128 && g.ldb < kMaxLd128; }
 
-template <GatedOp OP, Kept KEPT>
+template <GatedOp OP, Kept KEPT, int D>
 static int launch_tiles(GatedArgs g, bool b_oc, hipStream_t stream) {
   constexpr uint32_t TC = OP == GatedOp::kFwd ? T / 2 : T;
   const uint32_t mt = (uint32_t)(((uint64_t)g.M + T - 1) / T), nt = (uint32_t)(((uint64_t)g.N + TC - 1) / TC);
   if ((uint64_t)mt * nt >= 0x7FFFFFFFull) return GWS_ERR_SHAPE;
   set_tile_grid(g, mt, nt);
-  if (b_oc) hipLaunchKernelGGL((gated128_kernel<OP, false, KEPT>), dim3(mt * nt), dim3(256), 0, stream, g);
-  else hipLaunchKernelGGL((gated128_kernel<OP, true, KEPT>), dim3(mt * nt), dim3(256), 0, stream, g);
+  if (b_oc) hipLaunchKernelGGL((gated128_kernel<OP, false, KEPT, D>), dim3(mt * nt), dim3(256), 0, stream, g);
+  else hipLaunchKernelGGL((gated128_kernel<OP, true, KEPT, D>), dim3(mt * nt), dim3(256), 0, stream, g);
   return hipGetLastError() == hipSuccess ? GWS_OK : GWS_ERR_LAUNCH;
 }
 
-int launch_gated128(const GatedArgs& g, GatedOp op, bool b_oc, Kept kept, hipStream_t stream) {
-  if (op == GatedOp::kDx) return launch_tiles<GatedOp::kDx, Kept::kNone>(g, b_oc, stream);
-  if (op == GatedOp::kBwd)
-    return kept == Kept::kE4m3 ? launch_tiles<GatedOp::kBwd, Kept::kE4m3>(g, b_oc, stream) : launch_tiles<GatedOp::kBwd, Kept::kBf16>(g, b_oc, stream);
-  return kept == Kept::kE4m3 ? launch_tiles<GatedOp::kFwd, Kept::kE4m3>(g, b_oc, stream)
-         : kept == Kept::kBf16 ? launch_tiles<GatedOp::kFwd, Kept::kBf16>(g, b_oc, stream) : launch_tiles<GatedOp::kFwd, Kept::kNone>(g, b_oc, stream);
+int launch_gated128(const GatedArgs& g, GatedOp op, bool b_oc, Kept kept, bool two, hipStream_t stream) {
+  constexpr GatedOp F = GatedOp::kFwd, B = GatedOp::kBwd;
+  if (op == GatedOp::kDx) return launch_tiles<GatedOp::kDx, Kept::kNone, 4>(g, b_oc, stream);
+  if (op == B && kept == Kept::kE4m3) return two ? launch_tiles<B, Kept::kE4m3, 2>(g, b_oc, stream) : launch_tiles<B, Kept::kE4m3, 4>(g, b_oc, stream);
+  if (op == B) return two ? launch_tiles<B, Kept::kBf16, 2>(g, b_oc, stream) : launch_tiles<B, Kept::kBf16, 4>(g, b_oc, stream);
+  if (kept == Kept::kE4m3) return two ? launch_tiles<F, Kept::kE4m3, 2>(g, b_oc, stream) : launch_tiles<F, Kept::kE4m3, 4>(g, b_oc, stream);
+  if (kept == Kept::kBf16) return two ? launch_tiles<F, Kept::kBf16, 2>(g, b_oc, stream) : launch_tiles<F, Kept::kBf16, 4>(g, b_oc, stream);
+  return two ? launch_tiles<F, Kept::kNone, 2>(g, b_oc, stream) : launch_tiles<F, Kept::kNone, 4>(g, b_oc, stream);
 }
 
 }  // namespace gws

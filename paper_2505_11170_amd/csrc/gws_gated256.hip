@@ -18,8 +18,11 @@ __global__ __launch_bounds__(256, 1) void gated256_kernel(const GatedArgs g) {
       fwd_out<KEPT, EDGE, 8, 4>(g, acc, (uint8_t*)cs, m0 + 128 * (wave >> 1), n0 + 64 * (wave & 1), lane);
     }, rows, cols, g.K, nullptr, g.b2);
   } else if constexpr (OP == GatedOp::kBwd) {
+    const uint32_t wave0 = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    KeptTile<KEPT, EDGE, 8, 8> kept;   // its first rows land under the loop, in the registers that the loop leaves
+    kept.request(g, m0 + 128 * (wave0 >> 1), n0 + 128 * (wave0 & 1), threadIdx.x & 63, 0);
     gemm256_accumulate<false, B_OC, EDGE>(g.a, g.lda, g.b, g.ldb, nk, m0, n0, [&](f32x4 (&acc)[8][8], uint16_t* cs, uint32_t wave, uint32_t lane) {
-      bwd_out<KEPT, EDGE, 8, 8>(g, acc, (float*)cs, m0 + 128 * (wave >> 1), n0 + 128 * (wave & 1), lane);
+      bwd_out<KEPT, EDGE, 8, 8>(g, acc, kept, (float*)cs, m0 + 128 * (wave >> 1), n0 + 128 * (wave & 1), lane);
     }, rows, cols, g.K);
   } else {
     gemm256_accumulate<false, B_OC, EDGE, 8, kTwo>(g.a, g.lda, g.b, g.ldb, 2 * nk, m0, n0, [&](f32x4 (&acc)[8][8], uint16_t* cs, uint32_t wave, uint32_t lane) {
@@ -31,7 +34,7 @@ __global__ __launch_bounds__(256, 1) void gated256_kernel(const GatedArgs g) {
   }
 }
 
-bool gated256_applicable(const GatedArgs& g) { return g.K >= 64 && g.lda < g256::kMaxLdEdge && g.ldb < g256::kMaxLdEdge; }
+bool gated256_applicable(const GatedArgs& g) { return g.K >= 64 && out_lds_ok(g) && g.lda < g256::kMaxLdEdge && g.ldb < g256::kMaxLdEdge; }
 
 template <GatedOp OP, Kept KEPT, bool EDGE>
 static int launch_tiles(GatedArgs g, bool b_oc, hipStream_t stream) {

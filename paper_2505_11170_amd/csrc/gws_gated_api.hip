@@ -81,15 +81,15 @@ void kept_buffers(const KeptArgs& k, Kept form, int64_t M, int64_t F, bool writt
 //   and 97, 97; 8192 x 2048 -> 5632 291, 267 and 420, 348
 //   backward, BF16 kept: 1021 x 768 -> 2048 39, 41 and 14.5, 16.9; 3000 x 1024 -> 4096 62, 54 and 54, 54; 8192 x 2048 -> 5632 213, 223 and 306, 262
 //   input gradient: 5000 x 2 x 1280 -> 640 51, 50 and 21.7, 23.7; 2048 x 2 x 5632 -> 2048 192, 207 and 100, 99; 8192 x 2 x 5632 -> 2048 263, 262
-enum class GatedForm { kAny = GWS_GATED_ANY, kStream = GWS_GATED_STREAM, kMiddle = GWS_GATED_MIDDLE, kLarge = GWS_GATED_LARGE };
+enum class GatedForm { kAny = GWS_GATED_ANY, kStream = GWS_GATED_STREAM, kMiddle = GWS_GATED_MIDDLE, kLarge = GWS_GATED_LARGE, kShared = GWS_GATED_SHARED };
 GatedForm gated_form(const GatedArgs& g, GatedOp op, bool b_oc, Kept kept, GatedStreamPlan& plan) {
   plan = gated_stream_plan(g, op, b_oc, kept);
   const double cus = compute_units() > 0 ? compute_units() : 256, nk = ceil(g.K / 64.0) * (op == GatedOp::kDx ? 2 : 1);
   const bool keeps = op == GatedOp::kFwd && kept != Kept::kNone;
-  double large = 1e30, middle = 1e30;
+  double large = 1e30, middle = 1e30, shared = 1e30;
   if (gated256_applicable(g)) {
     const double n = ceil(g.M / 256.0) * ceil(g.N / (op == GatedOp::kFwd ? 128.0 : 256.0)), busy = n / (ceil(n / cus) * cus);
-    const double beside = op == GatedOp::kBwd ? 27.0 + 9.0 * busy : keeps ? 12.0 : 6.5;
+    const double beside = op == GatedOp::kBwd ? 20.0 + 9.0 * busy : keeps ? 12.0 : 6.5;
     const double step = op == GatedOp::kDx ? 1.03 + 0.42 * busy : 0.875 + 0.3 * busy;
     large = 2.5 + ceil(n / cus) * (beside + nk * step);
   }
@@ -98,17 +98,23 @@ GatedForm gated_form(const GatedArgs& g, GatedOp op, bool b_oc, Kept kept, Gated
     const double beside = op == GatedOp::kBwd ? 8.0 + 2.5 * busy : keeps ? 5.6 : 2.6;
     const double step = op == GatedOp::kDx ? 0.35 + 0.18 * busy * busy : 0.34 + 0.07 * busy;
     middle = 2.7 + ceil(n / cus) * (beside + nk * step);
+    if (n > cus && op != GatedOp::kDx) {   // two workgroups a compute unit
+      const double both = n / (ceil(n / (2 * cus)) * 2 * cus), way_out = op == GatedOp::kBwd ? 3.0 + 13.0 * both : keeps ? 6.5 : 3.0;
+      shared = 2.7 + ceil(n / (2 * cus)) * (way_out + nk * (0.5 + 0.3 * both));
+    }
   }
-  if (plan.p > 0 && plan.us < fmin(large, middle)) return GatedForm::kStream;
-  if (fmin(large, middle) > 1e29) return GatedForm::kAny;
-  return middle < large ? GatedForm::kMiddle : GatedForm::kLarge;
+  const double best = fmin(large, fmin(middle, shared));
+  if (plan.p > 0 && plan.us < best) return GatedForm::kStream;
+  if (best > 1e29) return GatedForm::kAny;
+  return best == large ? GatedForm::kLarge : best == shared ? GatedForm::kShared : GatedForm::kMiddle;
 }
 
 int launch_gated(const GatedArgs& g, GatedOp op, bool b_oc, Kept kept, hipStream_t stream) {
   GatedStreamPlan plan;
   switch (gated_form(g, op, b_oc, kept, plan)) {
     case GatedForm::kStream: return launch_gated_stream(g, op, b_oc, kept, plan, stream);
-    case GatedForm::kMiddle: return launch_gated128(g, op, b_oc, kept, stream);
+    case GatedForm::kMiddle: return launch_gated128(g, op, b_oc, kept, false, stream);
+    case GatedForm::kShared: return launch_gated128(g, op, b_oc, kept, true, stream);
     case GatedForm::kLarge: return launch_gated256(g, op, b_oc, kept, stream);
     default: return launch_gated_any(g, op, b_oc, kept, stream);
   }

@@ -29,7 +29,7 @@ constexpr int kPitch = 16 * NG * BYTES + 16;
 
 // 64 staged rows of 16 NG BF16 values (codes) to rows of `ld` bytes at `to`; of them `rows` and, of the columns, `cols` exist
 // (cols a multiple of 32).
-template <int NG, int BYTES, bool EDGE>
+template <int NG, int BYTES, bool EDGE, bool STREAM = false>
 __device__ __forceinline__ void rows_out(const uint8_t* cs, uint8_t* to, size_t ld, uint32_t lane, int rows, int cols) {
   constexpr int PITCH = kPitch<NG, BYTES>, LANES = NG * BYTES, ROWS = 64 / LANES;   // lanes of a row, rows of an instruction
   const uint32_t r = lane / LANES, c = (lane % LANES) * 16;
@@ -37,7 +37,11 @@ __device__ __forceinline__ void rows_out(const uint8_t* cs, uint8_t* to, size_t 
 #pragma unroll 4
   for (int it = 0; it < 64 / ROWS; ++it) {
     const uint32_t row = it * ROWS + r;
-    if (!EDGE || ((int)row < rows && col_in)) *(u32x4*)(to + row * ld + c) = *(const u32x4*)(cs + row * PITCH + c);
+    if (!EDGE || ((int)row < rows && col_in)) {
+      const u32x4 v = *(const u32x4*)(cs + row * PITCH + c);
+      if (STREAM) __builtin_nontemporal_store(v, (u32x4*)(to + row * ld + c));
+      else *(u32x4*)(to + row * ld + c) = v;
+    }
   }
 }
 
@@ -114,12 +118,12 @@ __device__ __forceinline__ void fwd_out_by(G gate, const GatedArgs& g, const f32
     const uint32_t r0 = p0 + 64 * h;
     rows_out<NG, 2, EDGE>(hs, (uint8_t*)(g.h + (size_t)r0 * g.ldh + q0), (size_t)g.ldh * 2, lane, rows - 64 * h, cols);
     if (KEPT == Kept::kBf16) {
-      rows_out<NG, 2, EDGE>(ks[0], g.kept.g + ((size_t)r0 * g.kept.ldg + q0) * 2, (size_t)g.kept.ldg * 2, lane, rows - 64 * h, cols);
-      rows_out<NG, 2, EDGE>(ks[1], g.kept.u + ((size_t)r0 * g.kept.ldu + q0) * 2, (size_t)g.kept.ldu * 2, lane, rows - 64 * h, cols);
+      rows_out<NG, 2, EDGE, true>(ks[0], g.kept.g + ((size_t)r0 * g.kept.ldg + q0) * 2, (size_t)g.kept.ldg * 2, lane, rows - 64 * h, cols);
+      rows_out<NG, 2, EDGE, true>(ks[1], g.kept.u + ((size_t)r0 * g.kept.ldu + q0) * 2, (size_t)g.kept.ldu * 2, lane, rows - 64 * h, cols);
     }
     if (KEPT == Kept::kE4m3) {
-      rows_out<NG, 1, EDGE>(ks[0], g.kept.g + (size_t)r0 * g.kept.ldg + q0, g.kept.ldg, lane, rows - 64 * h, cols);
-      rows_out<NG, 1, EDGE>(ks[1], g.kept.u + (size_t)r0 * g.kept.ldu + q0, g.kept.ldu, lane, rows - 64 * h, cols);
+      rows_out<NG, 1, EDGE, true>(ks[0], g.kept.g + (size_t)r0 * g.kept.ldg + q0, g.kept.ldg, lane, rows - 64 * h, cols);
+      rows_out<NG, 1, EDGE, true>(ks[1], g.kept.u + (size_t)r0 * g.kept.ldu + q0, g.kept.ldu, lane, rows - 64 * h, cols);
     }
     own_lds_wait();
   }
@@ -133,9 +137,9 @@ struct KeptEight {
   // p, s: uniform; off, soff: the lane's bytes from there
   __device__ __forceinline__ void load(const GWS_GLOBAL uint8_t* p, const GWS_GLOBAL uint8_t* s, uint32_t off, uint32_t soff) {
     if (KEPT == Kept::kBf16) {
-      w = *(const GWS_GLOBAL u32x4*)(p + off);
+      w = __builtin_nontemporal_load((const GWS_GLOBAL u32x4*)(p + off));
     } else {
-      const u32x2 c = *(const GWS_GLOBAL u32x2*)(p + off);
+      const u32x2 c = __builtin_nontemporal_load((const GWS_GLOBAL u32x2*)(p + off));
       w = u32x4{c[0], c[1], 0, 0};
       byte = s[soff];
     }
@@ -152,36 +156,47 @@ struct KeptEight {
   }
 };
 
+// A uniform pointer into row p0, byte `col` of a matrix; the rest of an address is uniform too but for a 32-bit lane offset of up to
+// seven rows.
+__device__ __forceinline__ GWS_GLOBAL uint8_t* at_row(const void* p, uint32_t row, size_t row_bytes, size_t col) {
+  return (GWS_GLOBAL uint8_t*)(uintptr_t)p + (size_t)row * row_bytes + col;
+}
+constexpr uint32_t kMaxLdOut = 1u << 28;   // leading dimensions (elements) that reaches
+
+// The kept G and U of a wavefront's 16 NI x 16 NJ part from (p0, q0), 32 rows at a time in two buffers; lane = (row % ROWS, 8 columns).
+template <Kept KEPT, bool EDGE, int NI, int NJ>
+struct KeptTile {
+  static constexpr uint32_t LANES = 2 * NJ, ROWS = 64 / LANES, IT = 32 / ROWS, E = KEPT == Kept::kBf16 ? 2 : 1;
+  KeptEight<KEPT> g[2][IT], u[2][IT];
+  __device__ __forceinline__ void request(const GatedArgs& a, uint32_t p0, uint32_t q0, uint32_t lane, int quarter) {
+    const uint32_t r = lane / LANES, c = lane % LANES * 8;
+    const int rows = (int)a.M - (int)p0, cols = (int)a.N - (int)q0;
+    const uint32_t g_off = (r * a.kept.ldg + c) * E, u_off = (r * a.kept.ldu + c) * E, gs_off = r * a.kept.lsg + (c >> 5), us_off = r * a.kept.lsu + (c >> 5);
+#pragma unroll
+    for (uint32_t it = 0; it < IT; ++it) {
+      const uint32_t row0 = 32 * quarter + ROWS * it;
+      if (!EDGE || ((int)(row0 + r) < rows && (int)c < cols)) {
+        g[quarter & 1][it].load(at_row(a.kept.g, p0 + row0, (size_t)a.kept.ldg * E, (size_t)q0 * E), at_row(a.kept.gs, p0 + row0, a.kept.lsg, q0 >> 5), g_off, gs_off);
+        u[quarter & 1][it].load(at_row(a.kept.u, p0 + row0, (size_t)a.kept.ldu * E, (size_t)q0 * E), at_row(a.kept.us, p0 + row0, a.kept.lsu, q0 >> 5), u_off, us_off);
+      }
+    }
+  }
+};
+
 // dL/dG, dL/dU and H of a wavefront's 16 NI x 16 NJ part from (p0, q0): dL/dH leaves the accumulators through LDS as fp32, 32 rows at
-// a time, and meets the kept G and U, which were requested before, 8 columns of a row a lane.
+// a time, and meets the kept G and U, which were requested before (the first 32 rows by the caller), 8 columns of a row a lane.
 template <Kept KEPT, bool EDGE, int NI, int NJ, class G>
-__device__ __forceinline__ void bwd_out_by(G gate, const GatedArgs& g, const f32x4 (&acc)[NI][NJ], float* cs, uint32_t p0, uint32_t q0, uint32_t lane) {
+__device__ __forceinline__ void bwd_out_by(G gate, const GatedArgs& g, const f32x4 (&acc)[NI][NJ], KeptTile<KEPT, EDGE, NI, NJ>& kept, float* cs, uint32_t p0,
+                                           uint32_t q0, uint32_t lane) {
   constexpr int PF = 16 * NJ + 4;   // pitch of a staged row of fp32 (32 of them)
   constexpr uint32_t LANES = 2 * NJ, ROWS = 64 / LANES, IT = 32 / ROWS;
   const uint32_t li = lane & 15, grp = lane >> 4;
   const uint32_t r = lane / LANES, c = lane % LANES * 8;   // on the way out: row % ROWS, column
   const int rows = (int)g.M - (int)p0, cols = (int)g.N - (int)q0;
   const bool col_in = !EDGE || (int)c < cols;
-  KeptEight<KEPT> kg[2][IT], ku[2][IT];
-  // scalar bases and 32-bit lane offsets: leading dimensions are below 2^24 here
-  constexpr uint32_t E = KEPT == Kept::kBf16 ? 2 : 1;
-  auto base = [&](const void* p, size_t row_bytes, size_t col_bytes) { return (GWS_GLOBAL uint8_t*)(uintptr_t)p + (size_t)p0 * row_bytes + col_bytes; };
-  const GWS_GLOBAL uint8_t *gp = base(g.kept.g, (size_t)g.kept.ldg * E, (size_t)q0 * E), *up = base(g.kept.u, (size_t)g.kept.ldu * E, (size_t)q0 * E);
-  const GWS_GLOBAL uint8_t *gsp = base(g.kept.gs, g.kept.lsg, q0 >> 5), *usp = base(g.kept.us, g.kept.lsu, q0 >> 5);
-  GWS_GLOBAL uint8_t *dgp = base(g.dg, (size_t)g.ldd * 2, (size_t)q0 * 2), *dup = base(g.du, (size_t)g.ldd * 2, (size_t)q0 * 2), *hp = base(g.h, (size_t)g.ldh * 2, (size_t)q0 * 2);
-  const uint32_t g_off = (r * g.kept.ldg + c) * E, u_off = (r * g.kept.ldu + c) * E, gs_off = r * g.kept.lsg + (c >> 5), us_off = r * g.kept.lsu + (c >> 5);
+  GWS_GLOBAL uint8_t *dgp = at_row(g.dg, p0, (size_t)g.ldd * 2, (size_t)q0 * 2), *dup = at_row(g.du, p0, (size_t)g.ldd * 2, (size_t)q0 * 2);
+  GWS_GLOBAL uint8_t* hp = at_row(g.h, p0, (size_t)g.ldh * 2, (size_t)q0 * 2);
   const uint32_t d_off = (r * g.ldd + c) * 2, h_off = (r * g.ldh + c) * 2;
-  auto request = [&](int quarter) {
-#pragma unroll
-    for (uint32_t it = 0; it < IT; ++it) {
-      const uint32_t row0 = 32 * quarter + ROWS * it;
-      if (!EDGE || ((int)(row0 + r) < rows && col_in)) {
-        kg[quarter & 1][it].load(gp + (size_t)row0 * g.kept.ldg * E, gsp + (size_t)row0 * g.kept.lsg, g_off, gs_off);
-        ku[quarter & 1][it].load(up + (size_t)row0 * g.kept.ldu * E, usp + (size_t)row0 * g.kept.lsu, u_off, us_off);
-      }
-    }
-  };
-  request(0);
 #pragma unroll
   for (int quarter = 0; quarter < NI / 2; ++quarter) {
 #pragma unroll
@@ -189,10 +204,10 @@ __device__ __forceinline__ void bwd_out_by(G gate, const GatedArgs& g, const f32
 #pragma unroll
       for (int j = 0; j < NJ; ++j) *(f32x4*)(cs + (16 * i2 + li) * PF + 16 * j + 4 * grp) = acc[2 * quarter + i2][j];
     // before this quarter's stores: loads and stores complete in one order, and a wait for loads behind stores is one for those too
-    if (quarter + 1 < NI / 2) request(quarter + 1);
+    if (quarter + 1 < NI / 2) kept.request(g, p0, q0, lane, quarter + 1);
     __builtin_amdgcn_sched_barrier(0);
     own_lds_wait();
-    KeptEight<KEPT> (&vg)[IT] = kg[quarter & 1], (&vu)[IT] = ku[quarter & 1];
+    KeptEight<KEPT> (&vg)[IT] = kept.g[quarter & 1], (&vu)[IT] = kept.u[quarter & 1];
 #pragma unroll
     for (uint32_t it = 0; it < IT; ++it) {
       const uint32_t row = ROWS * it + r;
@@ -214,9 +229,9 @@ __device__ __forceinline__ void bwd_out_by(G gate, const GatedArgs& g, const f32
           oh[p] = pack_bf16_rne(a0 * u0, a1 * u1);
         }
         const uint32_t row0 = 32 * quarter + ROWS * it;
-        *(GWS_GLOBAL u32x4*)(dgp + (size_t)row0 * g.ldd * 2 + d_off) = odg;
-        *(GWS_GLOBAL u32x4*)(dup + (size_t)row0 * g.ldd * 2 + d_off) = odu;
-        if (g.h != nullptr) *(GWS_GLOBAL u32x4*)(hp + (size_t)row0 * g.ldh * 2 + h_off) = oh;
+        __builtin_nontemporal_store(odg, (GWS_GLOBAL u32x4*)(dgp + (size_t)row0 * g.ldd * 2 + d_off));
+        __builtin_nontemporal_store(odu, (GWS_GLOBAL u32x4*)(dup + (size_t)row0 * g.ldd * 2 + d_off));
+        if (g.h != nullptr) __builtin_nontemporal_store(oh, (GWS_GLOBAL u32x4*)(hp + (size_t)row0 * g.ldh * 2 + h_off));
       }
     }
     own_lds_wait();
@@ -228,8 +243,13 @@ __device__ __forceinline__ void fwd_out(const GatedArgs& g, const f32x4 (&acc)[N
   with_gate(g.act, [&](auto gate) { fwd_out_by<KEPT, EDGE, NI, NG>(gate, g, acc, cs, p0, q0, lane); });
 }
 template <Kept KEPT, bool EDGE, int NI, int NJ>
-__device__ __forceinline__ void bwd_out(const GatedArgs& g, const f32x4 (&acc)[NI][NJ], float* cs, uint32_t p0, uint32_t q0, uint32_t lane) {
-  with_gate(g.act, [&](auto gate) { bwd_out_by<KEPT, EDGE, NI, NJ>(gate, g, acc, cs, p0, q0, lane); });
+__device__ __forceinline__ void bwd_out(const GatedArgs& g, const f32x4 (&acc)[NI][NJ], KeptTile<KEPT, EDGE, NI, NJ>& kept, float* cs, uint32_t p0, uint32_t q0,
+                                        uint32_t lane) {
+  with_gate(g.act, [&](auto gate) { bwd_out_by<KEPT, EDGE, NI, NJ>(gate, g, acc, kept, cs, p0, q0, lane); });
+}
+inline bool out_lds_ok(const GatedArgs& g) {
+  const KeptArgs& k = g.kept;
+  return g.ldd < kMaxLdOut && g.ldh < kMaxLdOut && k.ldg < kMaxLdOut && k.ldu < kMaxLdOut && k.lsg < kMaxLdOut && k.lsu < kMaxLdOut;
 }
 
 }  // namespace gws

@@ -19,7 +19,7 @@ __device__ __forceinline__ u32x2 pack4(const float (&v)[4]) { return u32x2{pack_
 // Four columns of one row on their way out: sums[0] of G and sums[1] of U, or sums[0] alone.  All lanes of a wavefront come here, eight
 // neighbouring ones with the 32 columns of a block; `here`: the row exists.
 template <GatedOp OP, Kept KEPT>
-__device__ __forceinline__ void four_out(const GatedArgs& g, uint32_t row, uint32_t col, bool here, const f32x4 (&sums)[2]) {
+__device__ __forceinline__ void four_out(const GatedArgs& g, uint32_t row, uint32_t col, bool here, const f32x4 (&sums)[2], const KeptFours<KEPT>& kept) {
   if (OP == GatedOp::kDx) {
     const float v[4] = {sums[0][0], sums[0][1], sums[0][2], sums[0][3]};
     if (here) *(u32x2*)(g.h + (size_t)row * g.ldh + col) = pack4(v);
@@ -57,8 +57,8 @@ __device__ __forceinline__ void four_out(const GatedArgs& g, uint32_t row, uint3
     }
   } else if (here) {
     float vg[4], vu[4], h[4], dg[4], du[4];
-    kept_four<KEPT>(g.kept.g, g.kept.gs, g.kept.ldg, g.kept.lsg, row, col, vg);
-    kept_four<KEPT>(g.kept.u, g.kept.us, g.kept.ldu, g.kept.lsu, row, col, vu);
+    kept.g.values(vg);
+    kept.u.values(vu);
     with_gate(g.act, [&](auto gate) {
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
@@ -142,6 +142,29 @@ __global__ __launch_bounds__(64 * P) void gated_stream_kernel(const GatedArgs g)
     for (int q = 0; q < QX; ++q) direct(xb + (size_t)k0 * 2, xo[q], st + q * 512);
   };
 
+  // Backward: what a thread needs of the kept G and U when the sums are there, four columns `fours` times a pass of the reduction, is
+  // requested before anything else
+  constexpr uint32_t PITCH = 4 * NT + 1, C4 = 4 * T;   // four-column groups of one weight
+  constexpr int FOURS = (MC * 16 * C4 + P * 64 - 1) / (P * 64), PASSES = MT / MC;
+  auto place = [&](int pass, int n, uint32_t& r, uint32_t& c, uint32_t& row, uint32_t& col) {
+    const uint32_t it = threadIdx.x + n * P * 64;
+    r = it / C4;
+    c = it % C4;
+    row = m0 + 16 * MC * pass + r;
+    col = n0 + 4 * c;
+    return row < g.M && col < g.N && r < 16 * MC && (BM == 16 * MT || r < BM);
+  };
+  KeptFours<KEPT> kept[PASSES][FOURS];
+  if (OP == GatedOp::kBwd) {
+#pragma unroll
+    for (int pass = 0; pass < PASSES; ++pass)
+#pragma unroll
+      for (int n = 0; n < FOURS; ++n) {
+        uint32_t r, c, row, col;
+        if (place(pass, n, r, c, row, col)) kept[pass][n].load(g.kept, row, col);
+      }
+  }
+
   f32x4 acc[MT][NT];
 #pragma unroll
   for (int i = 0; i < MT; ++i)
@@ -187,18 +210,20 @@ __global__ __launch_bounds__(64 * P) void gated_stream_kernel(const GatedArgs g)
   }
 
   // the partial sums, MC row tiles at a time, added in the order of the wavefronts
-  constexpr uint32_t PITCH = 4 * NT + 1, C4 = 4 * T;   // four-column groups of one weight
   f32x4* red = (f32x4*)lds;
 #pragma unroll
-  for (int i0 = 0; i0 < MT; i0 += MC) {
+  for (int pass = 0; pass < PASSES; ++pass) {
     __syncthreads();   // what was in this memory is read
 #pragma unroll
     for (int i = 0; i < MC; ++i)
 #pragma unroll
-      for (int j = 0; j < NT; ++j) red[((wave * MC + i) * 16 + li) * PITCH + 4 * j + grp] = acc[i0 + i][j];
+      for (int j = 0; j < NT; ++j) red[((wave * MC + i) * 16 + li) * PITCH + 4 * j + grp] = acc[MC * pass + i][j];
     __syncthreads();
-    for (uint32_t it = threadIdx.x; it < MC * 16 * C4; it += P * 64) {   // whole wavefronts
-      const uint32_t r = it / C4, c = it % C4;
+#pragma unroll
+    for (int n = 0; n < FOURS; ++n) {
+      if (threadIdx.x + n * P * 64 >= MC * 16 * C4) continue;   // whole wavefronts
+      uint32_t r, c, row, col;
+      const bool here = place(pass, n, r, c, row, col);
       f32x4 s[2];
 #pragma unroll
       for (int p = 0; p < (PAIR ? 2 : 1); ++p) {
@@ -206,8 +231,7 @@ __global__ __launch_bounds__(64 * P) void gated_stream_kernel(const GatedArgs g)
 #pragma unroll
         for (int w = 1; w < P; ++w) s[p] = add4(s[p], red[(w * MC * 16 + r) * PITCH + p * C4 + c]);
       }
-      const uint32_t row = m0 + 16 * i0 + r, col = n0 + 4 * c;
-      four_out<OP, KEPT>(g, row, col, row < g.M && col < g.N && (BM == 16 * MT || r < BM), s);
+      four_out<OP, KEPT>(g, row, col, here, s, kept[pass][n]);
     }
   }
 }
@@ -234,7 +258,7 @@ GatedStreamPlan gated_stream_plan(const GatedArgs& g, GatedOp op, bool b_oc, Kep
     const uint64_t bn = 16 * t.nt / (pair ? 2 : 1), wgs = ((uint64_t)g.M + 16 * t.mt - 1) / (16 * t.mt) * ((g.N + bn - 1) / bn);
     // a weight across the contraction comes in pieces of lines; the kept values and the gate's results of a tile go through few wavefronts
     const double weight = t.nt * (b_oc && pair ? 1.8 : b_oc && two ? 1.35 : 1.0);
-    const double beside = t.mt * t.nt * (op == GatedOp::kBwd ? 0.14 : pair && kept != Kept::kNone ? 0.06 : 0.0);
+    const double beside = t.mt * t.nt * (op == GatedOp::kBwd ? 0.09 : pair && kept != Kept::kNone ? 0.06 : 0.0);
     const double rounds = (double)((wgs + cus - 1) / cus);
     const double us = 1.8 + rounds * (2.7 + beside + K * 2 * 16 * (t.mt + weight) / t.rate * 1e-3);
     if (wgs < 0x7FFFFFFFull && us < best.us) best = {t.mt, t.nt, t.p, us};

@@ -9,7 +9,7 @@ from gpu_util import DEV, ensure_built
 from test_gpu_gated import check_bwd, check_dx, check_fwd, kept_buffers
 
 pytestmark = pytest.mark.gpu
-ANY, STREAM, MIDDLE, LARGE = (1, 0, 0), 2, (3, 0, 0), (4, 0, 0)
+ANY, STREAM, MIDDLE, LARGE, SHARED = (1, 0, 0), 2, (3, 0, 0), (4, 0, 0), (5, 0, 0)
 KEPT = {"none": 0, "bf16": 1, "e4m3": 2}
 
 
@@ -26,11 +26,12 @@ def taken(form, *args, **kw):
 FORWARD = [(5, 32, 160, ANY), (7, 96, 96, (STREAM, 1, 2)), (9, 64, 64, (STREAM, 1, 2)), (3, 96, 4640, (STREAM, 1, 4)), (14, 160, 4704, (STREAM, 1, 4)),
            (19, 96, 96, (STREAM, 2, 4)), (32, 1024, 128, (STREAM, 2, 4)), (239, 480, 1088, (STREAM, 4, 4)), (64, 512, 5632, (STREAM, 4, 4)),
            (84, 96, 4960, (STREAM, 8, 4)), (128, 256, 5632, (STREAM, 8, 4)), (700, 736, 2080, MIDDLE), (1024, 64, 2048, MIDDLE), (256, 2048, 5632, MIDDLE),
+           (408, 96, 4160, SHARED), (914, 352, 3520, SHARED),
            (1300, 96, 5024, LARGE), (1792, 384, 2816, LARGE), (2304, 2048, 3584, LARGE), (1460, 288, 4448, LARGE)]
 BACKWARD = [(5, 32, 160, ANY), (7, 96, 96, (STREAM, 1, 2)), (16, 64, 96, (STREAM, 1, 2)), (3, 96, 9248, (STREAM, 1, 4)), (13, 64, 12288, (STREAM, 1, 4)),
             (19, 96, 96, (STREAM, 2, 4)), (32, 1024, 128, (STREAM, 2, 4)), (202, 96, 2400, (STREAM, 4, 4)), (118, 448, 4800, (STREAM, 4, 4)),
             (1110, 96, 928, (STREAM, 8, 4)), (1021, 768, 2048, (STREAM, 8, 4)), (1211, 416, 2112, MIDDLE), (2048, 512, 2048, MIDDLE), (600, 1056, 5536, MIDDLE),
-            (2048, 2048, 5632, LARGE), (2300, 2080, 5152, LARGE)]
+            (900, 96, 4288, SHARED), (1849, 224, 4768, SHARED), (4096, 768, 2048, SHARED), (2048, 2048, 5632, LARGE), (2300, 2080, 5152, LARGE)]
 GRADIENT = [(5, 160, 32, ANY), (7, 96, 96, (STREAM, 1, 2)), (16, 4160, 64, (STREAM, 1, 2)), (11, 12288, 96, (STREAM, 1, 4)), (21, 96, 96, (STREAM, 2, 2)),
             (32, 1024, 1024, (STREAM, 2, 2)), (184, 1376, 96, (STREAM, 2, 4)), (700, 768, 2016, (STREAM, 4, 4)), (2061, 480, 96, (STREAM, 8, 4)),
             (1169, 1696, 96, MIDDLE), (2048, 2048, 544, MIDDLE), (4096, 768, 1056, MIDDLE), (6000, 2016, 480, LARGE), (8192, 2048, 256, LARGE)]
