@@ -202,7 +202,7 @@ __global__ __launch_bounds__(256, D == 2 ? 2 : 1) void gated128_kernel(const Gat
       for (int j = 0; j < NJ; ++j)
         *(u32x2*)((uint8_t*)cs + (16 * i + li) * kPitch<4, 2> + (16 * j + 4 * grp) * 2) = u32x2{pack_bf16_rne(acc[i][j][0], acc[i][j][1]), pack_bf16_rne(acc[i][j][2], acc[i][j][3])};
     own_lds_wait();
-    rows_out<4, 2, true>((const uint8_t*)cs, (uint8_t*)(g.h + (size_t)p0 * g.ldh + q0), (size_t)g.ldh * 2, lane, (int)g.M - (int)p0, (int)g.N - (int)q0);
+    rows_out<4, 2, true, false>((const uint8_t*)cs, (uint8_t*)(g.h + (size_t)p0 * g.ldh + q0), (size_t)g.ldh * 2, lane, (int)g.M - (int)p0, (int)g.N - (int)q0);
   }
 }
 

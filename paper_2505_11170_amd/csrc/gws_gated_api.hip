@@ -185,6 +185,7 @@ int gws_gated_fwd(const void* x, int64_t M, int64_t K, int64_t ldx, const void* 
   g.M = (uint32_t)M; g.N = (uint32_t)F; g.K = (uint32_t)K;
   g.lda = (uint32_t)ldx; g.ldb = (uint32_t)ldw;
   g.h = (uint16_t*)h; g.ldh = (uint32_t)ldh;
+  g.stream_h = (uint64_t)M * (uint64_t)F * 2 >= (uint64_t)64 << 20;
   return launch_gated(g, GatedOp::kFwd, !w_is_nk, form, (hipStream_t)stream);
 }
 

@@ -29,7 +29,7 @@ constexpr int kPitch = 16 * NG * BYTES + 16;
 
 // 64 staged rows of 16 NG BF16 values (codes) to rows of `ld` bytes at `to`; of them `rows` and, of the columns, `cols` exist
 // (cols a multiple of 32).
-template <int NG, int BYTES, bool EDGE, bool STREAM = false>
+template <int NG, int BYTES, bool EDGE, bool STREAM>
 __device__ __forceinline__ void rows_out(const uint8_t* cs, uint8_t* to, size_t ld, uint32_t lane, int rows, int cols) {
   constexpr int PITCH = kPitch<NG, BYTES>, LANES = NG * BYTES, ROWS = 64 / LANES;   // lanes of a row, rows of an instruction
   const uint32_t r = lane / LANES, c = (lane % LANES) * 16;
@@ -116,7 +116,13 @@ __device__ __forceinline__ void fwd_out_by(G gate, const GatedArgs& g, const f32
     }
     own_lds_wait();
     const uint32_t r0 = p0 + 64 * h;
-    rows_out<NG, 2, EDGE>(hs, (uint8_t*)(g.h + (size_t)r0 * g.ldh + q0), (size_t)g.ldh * 2, lane, rows - 64 * h, cols);
+    // What is kept is wanted again a pass later: past the caches.  H mostly at once: so too only where it is too large for the caches to
+    // keep until then (64 MB).  8192 tokens, 2048 -> 5632 (92 MB), all ordinary, G and U streaming, all streaming: 337, 335, 319 us, with
+    // the product that follows 474, 462, 468; 4096 tokens, with that product, 277, 269, 273; 1024 tokens 97.1, 94.3, 94.1.
+    // (Two loops: of one with both stores the compiler makes ordinary ones.)
+    uint8_t* const hp = (uint8_t*)(g.h + (size_t)r0 * g.ldh + q0);
+    if (g.stream_h) rows_out<NG, 2, EDGE, true>(hs, hp, (size_t)g.ldh * 2, lane, rows - 64 * h, cols);
+    else rows_out<NG, 2, EDGE, false>(hs, hp, (size_t)g.ldh * 2, lane, rows - 64 * h, cols);
     if (KEPT == Kept::kBf16) {
       rows_out<NG, 2, EDGE, true>(ks[0], g.kept.g + ((size_t)r0 * g.kept.ldg + q0) * 2, (size_t)g.kept.ldg * 2, lane, rows - 64 * h, cols);
       rows_out<NG, 2, EDGE, true>(ks[1], g.kept.u + ((size_t)r0 * g.kept.ldu + q0) * 2, (size_t)g.kept.ldu * 2, lane, rows - 64 * h, cols);
