@@ -25,19 +25,30 @@ __device__ __forceinline__ uint32_t act8_byte(uint32_t amax) {
 // X for the converters (a NaN scale's blocks are written and read apart from them).
 __device__ __forceinline__ float act8_scale(uint32_t byte) { return __uint_as_float(byte << 23); }
 
+// X for the converters from the same bits where no value is large: below 2^119, and what a block of zeros is divided by does not matter.
+constexpr uint32_t kAct8Large = 0x7F000000u;   // from 2^127: the largest scale may be needed, or there is a NaN or an infinity
+__device__ __forceinline__ float act8_small_scale(uint32_t amax) {
+  const uint32_t e = (amax + 0x17FFFFu) >> 23;   // one more beyond 1.8125 2^x
+  return __uint_as_float(((e < kAct8Min + 8 ? kAct8Min + 8 : e) << 23) - (8u << 23));
+}
 // The larger magnitude of m and two values; a NaN stays one.
 __device__ __forceinline__ float act8_larger(float m, float a, float b) {
   return __builtin_elementwise_maximum(__builtin_elementwise_maximum(m, __builtin_fabsf(a)), __builtin_fabsf(b));
 }
 // The converter does not saturate: where a scale is the largest one (hardly ever), its values first.
 __device__ __forceinline__ float act8_clamp(float v) { return fminf(fmaxf(v, -0x1.cp127f), 0x1.cp127f); }
-// Four fp32 values to codes; NaN codes under a NaN scale.
-__device__ __forceinline__ uint32_t act8_codes(const float (&v)[4], uint32_t byte) {
+// Four fp32 values to codes.
+__device__ __forceinline__ uint32_t act8_convert(const float (&v)[4], float scale) {
   i16x2 c = {0, 0};
-  c = __builtin_amdgcn_cvt_scalef32_pk_fp8_f32(c, v[0], v[1], act8_scale(byte), false);
-  c = __builtin_amdgcn_cvt_scalef32_pk_fp8_f32(c, v[2], v[3], act8_scale(byte), true);
+  c = __builtin_amdgcn_cvt_scalef32_pk_fp8_f32(c, v[0], v[1], scale, false);
+  c = __builtin_amdgcn_cvt_scalef32_pk_fp8_f32(c, v[2], v[3], scale, true);
   uint32_t u;
   __builtin_memcpy(&u, &c, 4);
+  return u;
+}
+// NaN codes under a NaN scale.
+__device__ __forceinline__ uint32_t act8_codes(const float (&v)[4], uint32_t byte) {
+  const uint32_t u = act8_convert(v, act8_scale(byte));
   return byte == kAct8NaN ? 0x7F7F7F7Fu : u;
 }
 // Codes as the converters take them: under a NaN scale NaN codes, whatever they are.

@@ -14,13 +14,20 @@ __device__ __forceinline__ void own_lds_wait() {
   __builtin_amdgcn_wave_barrier();
 }
 
-// The largest m of the four lanes lane % 16 + 16 x: v_permlane16_swap and v_permlane32_swap of m with itself leave a lane's own value in one
-// result and its partner's in the other.
-__device__ __forceinline__ uint32_t max_over_rows(uint32_t m) {
-  const auto a = __builtin_amdgcn_permlane16_swap(m, m, false, false);
-  m = max((uint32_t)a[0], (uint32_t)a[1]);
-  const auto b = __builtin_amdgcn_permlane32_swap(m, m, false, false);
-  return max((uint32_t)b[0], (uint32_t)b[1]);
+// Each m's largest of the four lanes lane % 16 + 16 x: v_permlane16_swap and v_permlane32_swap of m with itself leave a lane's own value in
+// one result and its partner's in the other.  Together, so that one's steps fill the waits between another's.
+template <int N>
+__device__ __forceinline__ void max_over_rows(uint32_t (&m)[N]) {
+#pragma unroll
+  for (int n = 0; n < N; ++n) {
+    const auto a = __builtin_amdgcn_permlane16_swap(m[n], m[n], false, false);
+    m[n] = max((uint32_t)a[0], (uint32_t)a[1]);
+  }
+#pragma unroll
+  for (int n = 0; n < N; ++n) {
+    const auto b = __builtin_amdgcn_permlane32_swap(m[n], m[n], false, false);
+    m[n] = max((uint32_t)b[0], (uint32_t)b[1]);
+  }
 }
 
 // Pitch in bytes of a staged row of 16 NG values, BF16 or codes.
@@ -83,35 +90,43 @@ __device__ __forceinline__ void fwd_out_by(G gate, const GatedArgs& g, const f32
         }
       }
       if (KEPT == Kept::kE4m3) {
-        uint32_t byte[2][NB];   // [G, U][block]
-        bool largest = false;
+        uint32_t m[2 * NB];   // largest magnitudes of G's blocks, then of U's
 #pragma unroll
-        for (int p = 0; p < 2; ++p)
+        for (uint32_t b = 0; b < 2 * NB; ++b) {
+          float top = 0.0f;
 #pragma unroll
-          for (int b = 0; b < (int)NB; ++b) {
-            float top = 0.0f;
-#pragma unroll
-            for (int t = 0; t < 4; ++t) {
-              const f32x4& v = acc[i][NG * p + 2 * b + (t >> 1)];
-              top = act8_larger(top, v[2 * (t & 1)], v[2 * (t & 1) + 1]);
-            }
-            byte[p][b] = act8_byte(max_over_rows(__float_as_uint(top) & 0x7FFFFFFFu));
-            largest |= byte[p][b] == kAct8Max;
+          for (int t = 0; t < 4; ++t) {
+            const f32x4& v = acc[i][2 * b + (t >> 1)];
+            top = act8_larger(top, v[2 * (t & 1)], v[2 * (t & 1) + 1]);
           }
-        uint32_t mine = byte[0][0];
+          m[b] = __float_as_uint(top) & 0x7FFFFFFFu;
+        }
+        max_over_rows(m);
+        uint32_t mine = m[0], most = m[0];
 #pragma unroll
-        for (uint32_t n = 1; n < 2 * NB; ++n) mine = grp == n ? byte[n / NB][n % NB] : mine;
-        if (grp < 2 * NB && (!EDGE || (16 * i + (int)li < rows && 32 * (int)(grp % NB) < cols))) sp[(size_t)(16 * i) * ls] = (uint8_t)mine;
-        auto codes = [&](auto&& value) {
+        for (uint32_t b = 1; b < 2 * NB; ++b) {
+          mine = grp == b ? m[b] : mine;
+          most = max(most, m[b]);
+        }
+        if (grp < 2 * NB && (!EDGE || (16 * i + (int)li < rows && 32 * (int)(grp % NB) < cols))) sp[(size_t)(16 * i) * ls] = (uint8_t)act8_byte(mine);
+        auto codes = [&](auto&& four) {
 #pragma unroll
           for (int j = 0; j < 2 * NG; ++j) {
-            const float v[4] = {value(acc[i][j][0]), value(acc[i][j][1]), value(acc[i][j][2]), value(acc[i][j][3])};
-            *(uint32_t*)(ks[j / NG] + row * PB + 16 * (j % NG) + 4 * grp) = act8_codes(v, byte[j / NG][j % NG / 2]);
+            const float v[4] = {acc[i][j][0], acc[i][j][1], acc[i][j][2], acc[i][j][3]};
+            *(uint32_t*)(ks[j / NG] + row * PB + 16 * (j % NG) + 4 * grp) = four(v, j / 2);
           }
         };
-        // uniform; a block under a smaller scale has nothing that large
-        if (__builtin_amdgcn_ballot_w64(largest) == 0) codes([](float v) { return v; });
-        else codes([](float v) { return act8_clamp(v); });
+        if (__builtin_amdgcn_ballot_w64(most >= kAct8Large) == 0) {   // uniform
+          float scale[2 * NB];
+#pragma unroll
+          for (uint32_t b = 0; b < 2 * NB; ++b) scale[b] = act8_small_scale(m[b]);
+          codes([&](const float (&v)[4], int b) { return act8_convert(v, scale[b]); });
+        } else {
+          codes([&](const float (&v)[4], int b) {
+            const float w[4] = {act8_clamp(v[0]), act8_clamp(v[1]), act8_clamp(v[2]), act8_clamp(v[3])};   // under a smaller scale nothing is that large
+            return act8_codes(w, act8_byte(m[b]));
+          });
+        }
       }
     }
     own_lds_wait();
