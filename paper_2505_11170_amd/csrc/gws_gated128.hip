@@ -192,7 +192,7 @@ __global__ __launch_bounds__(256, D == 2 ? 2 : 1) void gated128_kernel(const Gat
 
   uint16_t* cs = lds + wave * (D * STG / 4);
   if constexpr (OP == GatedOp::kFwd) {
-    fwd_out<KEPT, true, 4, 2>(g, acc, (uint8_t*)cs, p0, q0, lane);
+    fwd_out<KEPT, true, 4, 2>(g, acc, (uint8_t*)cs, (uint8_t*)(lds + 2 * wm * (D * STG / 4)), wn, p0, q0, lane);
   } else if constexpr (OP == GatedOp::kBwd) {
     bwd_out<KEPT, true, 4, 4>(g, acc, kept, (float*)cs, p0, q0, lane);
   } else {

@@ -14,8 +14,8 @@ __global__ __launch_bounds__(256, 1) void gated256_kernel(const GatedArgs g) {
   const uint32_t m0 = tile_m * TM, n0 = tile_n * TC, rows = g.M - m0 < TM ? g.M - m0 : TM, cols = g.N - n0 < TC ? g.N - n0 : TC;
   const uint32_t nk = (g.K + TK - 1) / TK;
   if constexpr (OP == GatedOp::kFwd) {
-    gemm256_accumulate<false, B_OC, EDGE, 8, kPair>(g.a, g.lda, g.b, g.ldb, nk, m0, n0, [&](f32x4 (&acc)[8][8], uint16_t* cs, uint32_t wave, uint32_t lane) {
-      fwd_out<KEPT, EDGE, 8, 4>(g, acc, (uint8_t*)cs, m0 + 128 * (wave >> 1), n0 + 64 * (wave & 1), lane);
+    gemm256_accumulate<false, B_OC, EDGE, 8, kPair>(g.a, g.lda, g.b, g.ldb, nk, m0, n0, [&](f32x4 (&acc)[8][8], uint16_t* cs, uint32_t wave, uint32_t lane, uint16_t* first) {
+      fwd_out<KEPT, EDGE, 8, 4>(g, acc, (uint8_t*)cs, (uint8_t*)first, wave & 1, m0 + 128 * (wave >> 1), n0 + 64 * (wave & 1), lane);
     }, rows, cols, g.K, nullptr, g.b2);
   } else if constexpr (OP == GatedOp::kBwd) {
     const uint32_t wave0 = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);

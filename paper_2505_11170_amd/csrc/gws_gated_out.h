@@ -14,6 +14,9 @@ __device__ __forceinline__ void own_lds_wait() {
   __builtin_amdgcn_wave_barrier();
 }
 
+// The same of every wavefront of the workgroup.
+__device__ __forceinline__ void both_lds_wait() { asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory"); }
+
 // Each m's largest of the four lanes lane % 16 + 16 x: v_permlane16_swap and v_permlane32_swap of m with itself leave a lane's own value in
 // one result and its partner's in the other.  Together, so that one's steps fill the waits between another's.
 template <int N>
@@ -54,13 +57,17 @@ __device__ __forceinline__ void rows_out(const uint8_t* cs, uint8_t* to, size_t 
 
 // H, and G and U as they are kept, of a wavefront's 16 NI rows x 16 NG columns from (p0, q0): a lane has both halves of an element
 // (acc[i][j] with j < NG is G, acc[i][j + NG] U), and the four lanes of a block of 32 that is kept in 8 bits meet in two cross-lane
-// steps.  Everything leaves through LDS by rows, 64 rows at a time.
+// steps.  Everything leaves through LDS by rows, 64 rows at a time; codes, of which a wavefront's columns are half a line or less, by the two
+// wavefronts that share the rows (`odd`: this is the one with the later columns; first: the other's cs) together, G's by the one and U's by the
+// other (8192 tokens, 2048 -> 5632: 323 -> 319 us; in 128 x 128 tiles 1021 x 768 -> 2048 12.8 -> 12.2).
 template <Kept KEPT, bool EDGE, int NI, int NG, class G>
-__device__ __forceinline__ void fwd_out_by(G gate, const GatedArgs& g, const f32x4 (&acc)[NI][2 * NG], uint8_t* cs, uint32_t p0, uint32_t q0, uint32_t lane) {
+__device__ __forceinline__ void fwd_out_by(G gate, const GatedArgs& g, const f32x4 (&acc)[NI][2 * NG], uint8_t* cs, uint8_t* first, bool odd, uint32_t p0,
+                                        uint32_t q0, uint32_t lane) {
   const uint32_t li = lane & 15, grp = lane >> 4;
   uint8_t* const hs = cs;                                    // 64 rows of H, then of G and of U
-  constexpr int PH = kPitch<NG, 2>, PB = kPitch<NG, 1>;
-  uint8_t* const ks[2] = {cs + 64 * PH, cs + 64 * PH + 64 * (KEPT == Kept::kE4m3 ? PB : PH)};
+  constexpr int PH = kPitch<NG, 2>, PB = kPitch<2 * NG, 1>;
+  constexpr int KS = 64 * (KEPT == Kept::kE4m3 ? PB : PH);   // bytes of staged G, of U
+  uint8_t* const ks = (KEPT == Kept::kE4m3 ? first + 16 * NG * odd : cs) + 64 * PH;
   const int rows = (int)g.M - (int)p0, cols = (int)g.N - (int)q0;   // EDGE: what exists, may be <= 0
   // 8 bits: the lane groups store the scales, of G's NG / 2 blocks and then of U's
   constexpr uint32_t NB = NG / 2;
@@ -85,8 +92,8 @@ __device__ __forceinline__ void fwd_out_by(G gate, const GatedArgs& g, const f32
         for (int e = 0; e < 4; ++e) o[e] = gate.a(vg[e]) * vu[e];
         *(u32x2*)(hs + row * PH + (16 * j + 4 * grp) * 2) = u32x2{pack_bf16_rne(o[0], o[1]), pack_bf16_rne(o[2], o[3])};
         if (KEPT == Kept::kBf16) {
-          *(u32x2*)(ks[0] + row * PH + (16 * j + 4 * grp) * 2) = u32x2{pack_bf16_rne(vg[0], vg[1]), pack_bf16_rne(vg[2], vg[3])};
-          *(u32x2*)(ks[1] + row * PH + (16 * j + 4 * grp) * 2) = u32x2{pack_bf16_rne(vu[0], vu[1]), pack_bf16_rne(vu[2], vu[3])};
+          *(u32x2*)(ks + row * PH + (16 * j + 4 * grp) * 2) = u32x2{pack_bf16_rne(vg[0], vg[1]), pack_bf16_rne(vg[2], vg[3])};
+          *(u32x2*)(ks + KS + row * PH + (16 * j + 4 * grp) * 2) = u32x2{pack_bf16_rne(vu[0], vu[1]), pack_bf16_rne(vu[2], vu[3])};
         }
       }
       if (KEPT == Kept::kE4m3) {
@@ -113,7 +120,7 @@ __device__ __forceinline__ void fwd_out_by(G gate, const GatedArgs& g, const f32
 #pragma unroll
           for (int j = 0; j < 2 * NG; ++j) {
             const float v[4] = {acc[i][j][0], acc[i][j][1], acc[i][j][2], acc[i][j][3]};
-            *(uint32_t*)(ks[j / NG] + row * PB + 16 * (j % NG) + 4 * grp) = four(v, j / 2);
+            *(uint32_t*)(ks + j / NG * KS + row * PB + 16 * (j % NG) + 4 * grp) = four(v, j / 2);
           }
         };
         if (__builtin_amdgcn_ballot_w64(most >= kAct8Large) == 0) {   // uniform
@@ -130,6 +137,7 @@ __device__ __forceinline__ void fwd_out_by(G gate, const GatedArgs& g, const f32
       }
     }
     own_lds_wait();
+    if (KEPT == Kept::kE4m3) both_lds_wait();
     const uint32_t r0 = p0 + 64 * h;
     // What is kept is wanted again a pass later: past the caches.  H mostly at once: so too only where it is too large for the caches to
     // keep until then (64 MB).  8192 tokens, 2048 -> 5632 (92 MB), all ordinary, G and U streaming, all streaming: 337, 335, 319 us, with
@@ -139,12 +147,14 @@ __device__ __forceinline__ void fwd_out_by(G gate, const GatedArgs& g, const f32
     if (g.stream_h) rows_out<NG, 2, EDGE, true>(hs, hp, (size_t)g.ldh * 2, lane, rows - 64 * h, cols);
     else rows_out<NG, 2, EDGE, false>(hs, hp, (size_t)g.ldh * 2, lane, rows - 64 * h, cols);
     if (KEPT == Kept::kBf16) {
-      rows_out<NG, 2, EDGE, true>(ks[0], g.kept.g + ((size_t)r0 * g.kept.ldg + q0) * 2, (size_t)g.kept.ldg * 2, lane, rows - 64 * h, cols);
-      rows_out<NG, 2, EDGE, true>(ks[1], g.kept.u + ((size_t)r0 * g.kept.ldu + q0) * 2, (size_t)g.kept.ldu * 2, lane, rows - 64 * h, cols);
+      rows_out<NG, 2, EDGE, true>(ks, g.kept.g + ((size_t)r0 * g.kept.ldg + q0) * 2, (size_t)g.kept.ldg * 2, lane, rows - 64 * h, cols);
+      rows_out<NG, 2, EDGE, true>(ks + KS, g.kept.u + ((size_t)r0 * g.kept.ldu + q0) * 2, (size_t)g.kept.ldu * 2, lane, rows - 64 * h, cols);
     }
     if (KEPT == Kept::kE4m3) {
-      rows_out<NG, 1, EDGE, true>(ks[0], g.kept.g + (size_t)r0 * g.kept.ldg + q0, g.kept.ldg, lane, rows - 64 * h, cols);
-      rows_out<NG, 1, EDGE, true>(ks[1], g.kept.u + (size_t)r0 * g.kept.ldu + q0, g.kept.ldu, lane, rows - 64 * h, cols);
+      const uint32_t c0 = q0 - 16 * NG * odd;
+      const uint32_t ld = odd ? g.kept.ldu : g.kept.ldg;
+      rows_out<2 * NG, 1, EDGE, true>(first + 64 * PH + KS * odd, (odd ? g.kept.u : g.kept.g) + (size_t)r0 * ld + c0, ld, lane, rows - 64 * h, (int)g.N - (int)c0);
+      if (h + 1 < NI / 4) both_lds_wait();
     }
     own_lds_wait();
   }
@@ -260,8 +270,9 @@ __device__ __forceinline__ void bwd_out_by(G gate, const GatedArgs& g, const f32
 }
 
 template <Kept KEPT, bool EDGE, int NI, int NG>
-__device__ __forceinline__ void fwd_out(const GatedArgs& g, const f32x4 (&acc)[NI][2 * NG], uint8_t* cs, uint32_t p0, uint32_t q0, uint32_t lane) {
-  with_gate(g.act, [&](auto gate) { fwd_out_by<KEPT, EDGE, NI, NG>(gate, g, acc, cs, p0, q0, lane); });
+__device__ __forceinline__ void fwd_out(const GatedArgs& g, const f32x4 (&acc)[NI][2 * NG], uint8_t* cs, uint8_t* first, bool odd, uint32_t p0,
+                                        uint32_t q0, uint32_t lane) {
+  with_gate(g.act, [&](auto gate) { fwd_out_by<KEPT, EDGE, NI, NG>(gate, g, acc, cs, first, odd, p0, q0, lane); });
 }
 template <Kept KEPT, bool EDGE, int NI, int NJ>
 __device__ __forceinline__ void bwd_out(const GatedArgs& g, const f32x4 (&acc)[NI][NJ], KeptTile<KEPT, EDGE, NI, NJ>& kept, float* cs, uint32_t p0, uint32_t q0,

@@ -125,7 +125,8 @@ __device__ __forceinline__ void epilogue_bf16_half(const f32x4 (&a4)[4][8], int 
 // contiguous B stage is 64 k-rows of 128 columns, as 256 of them are swizzled, and 64 k-rows of 64 behind it).
 // SRC = kPair: b and b2, of which n0 and b_out count the columns: acc[i][j] with j < 4 is column 64 (wave % 2) + 16 j of b's product, with
 // j >= 4 column 64 (wave % 2) + 16 (j - 4) of b2's.  Contraction-contiguous: stage rows 64 w .. 64 w + 63, one wavefront's loads, are columns
-// 64 (w / 2) .. of b (w even) or b2; output-contiguous: 64 k-rows of 128 columns of b and then of b2, two wavefronts each.
+// 64 (w / 2) .. of b (w even) or b2; output-contiguous: 64 k-rows of 128 columns of b and then of b2, two wavefronts each.  finish also gets
+// the cs of the even one of the two wavefronts that share the rows.
 // SRC = kTwo: nk K-steps, the first half over a, b and the others over a2, b2 (both K deep; the half step comes at the end of each).
 template <bool A_OC, bool B_OC, bool EDGE = false, int NJ = 8, int SRC = g256::kOne, class Finish>
 __device__ __forceinline__ void gemm256_accumulate(const uint16_t* __restrict__ a, uint32_t lda,
@@ -445,7 +446,8 @@ __device__ __forceinline__ void gemm256_accumulate(const uint16_t* __restrict__ 
   uint32_t all = 0xFFFFFFFFu;
   asm volatile("" : "+s"(all));
   const uint32_t lane_out = __builtin_amdgcn_mbcnt_hi(all, __builtin_amdgcn_mbcnt_lo(all, 0));
-  finish(acc, wave == 0 ? A0 : wave == 1 ? A1 : wave == 2 ? B0 : B1, wave, lane_out);
+  if constexpr (PAIR) finish(acc, wave == 0 ? A0 : wave == 1 ? A1 : wave == 2 ? B0 : B1, wave, lane_out, wave < 2 ? A0 : B0);
+  else finish(acc, wave == 0 ? A0 : wave == 1 ? A1 : wave == 2 ? B0 : B1, wave, lane_out);
 }
 
 // The way out of half h (64 rows) of a wavefront's 128 x 96 part of a narrow tile: as epilogue_bf16_half, but by 32 x 32
