@@ -1,5 +1,7 @@
 // Activations kept in 8 bits (gfx950): BF16 [M x C] to E4M3 codes with an E8M0 scale for every 32 of a row, and back.
-// One pass over memory: a lane takes eight values, the four lanes of a block meet in two cross-lane steps.
+// One pass over memory: a lane takes eight values, the four lanes of a block meet in two cross-lane steps, the scaled converters do the rest.
+// Bound by memory: 8192 x 5632 to codes 26.3 us, 5.3 TB/s of the 3 bytes a value (a large copy reaches 5.15); 8192 x 2048 back 10.4 us, 4.9 TB/s
+// where the codes come from memory.  301 x 1000 back is a launch, 2.1 us.
 #include "gws_gated.h"
 
 namespace gws {

