@@ -69,7 +69,7 @@ class _CGatedSaved(ctypes.Structure):
                 ("g8", _CAct8), ("u8", _CAct8)]
 
 
-@dataclass
+@dataclass(slots=True)
 class Act8:
     """Python-side mirror of ``gws_act8``: one-byte device tensors for the E4M3 codes [rows, columns] and the E8M0 block
     scales [rows, ceil(columns / 32)]."""
@@ -79,7 +79,7 @@ class Act8:
     lds: Optional[int] = None
 
 
-@dataclass
+@dataclass(slots=True)
 class GatedSaved:
     """Python-side mirror of ``gws_gated_saved``: G and U kept as BF16 (``g``, ``u``) or in 8 bits (``g8``, ``u8``)."""
     g: Optional[object] = None
@@ -573,6 +573,7 @@ def gws_block_absmax(t: Sequence[TensorDesc], stream=None) -> None:
     _check(L.gws_block_absmax(arr, n, _stream(stream)), "gws_block_absmax")
 
 
+# (stride()[0]: half the time of stride(0), which takes its argument apart)
 _pack_act8 = struct.Struct("=2Q2q").pack
 _pack_saved = struct.Struct("=2Q2q2Q2q2Q2q").pack   # the fields in one go, passed as bytes (building the structures takes as long as the call)
 assert struct.calcsize("=2Q2q") == ctypes.sizeof(_CAct8) and struct.calcsize("=2Q2q2Q2q2Q2q") == ctypes.sizeof(_CGatedSaved)
@@ -582,7 +583,7 @@ def _act8_fields(a: Act8, rows: int, cols: int):
     c, s, ldc, lds = a.codes, a.xscale, a.ldc, a.lds
     if c.shape != (rows, cols) or s.shape != (rows, -(-cols // 32)):
         raise ValueError(f"[{rows}, {cols}] in 8 bits has codes of that shape and scales [{rows}, {-(-cols // 32)}], not {list(c.shape)} and {list(s.shape)}")
-    return c.data_ptr(), s.data_ptr(), c.stride(0) if ldc is None else ldc, s.stride(0) if lds is None else lds
+    return c.data_ptr(), s.data_ptr(), c.stride()[0] if ldc is None else ldc, s.stride()[0] if lds is None else lds
 
 
 def _marshal_saved(s: Optional[GatedSaved], rows: int, cols: int):
@@ -592,7 +593,7 @@ def _marshal_saved(s: Optional[GatedSaved], rows: int, cols: int):
     if g8 is None and u8 is None and g is not None and u is not None:
         if g.shape != (rows, cols) or u.shape != (rows, cols):
             raise ValueError(f"a kept G or U has shape {list(g.shape)} or {list(u.shape)}, not [{rows}, {cols}]")
-        return _pack_saved(g.data_ptr(), u.data_ptr(), g.stride(0), u.stride(0), 0, 0, 0, 0, 0, 0, 0, 0)
+        return _pack_saved(g.data_ptr(), u.data_ptr(), g.stride()[0], u.stride()[0], 0, 0, 0, 0, 0, 0, 0, 0)
     if g is None and u is None and g8 is not None and u8 is not None:
         return _pack_saved(0, 0, 0, 0, *_act8_fields(g8, rows, cols), *_act8_fields(u8, rows, cols))
     raise ValueError("G and U are kept both as BF16 (g, u) or both in 8 bits (g8, u8)")
@@ -601,36 +602,36 @@ def _marshal_saved(s: Optional[GatedSaved], rows: int, cols: int):
 def gws_act8_encode(x, o: Act8, stream=None) -> None:
     """BF16 ``x`` [rows, columns] to E4M3 codes and a scale for every 32 of a row."""
     M, C = x.shape
-    _check((_lib or load_library()).gws_act8_encode(x.data_ptr(), M, C, x.stride(0), _pack_act8(*_act8_fields(o, M, C)), _stream(stream)), "gws_act8_encode")
+    _check((_lib or load_library()).gws_act8_encode(x.data_ptr(), M, C, x.stride()[0], _pack_act8(*_act8_fields(o, M, C)), _stream(stream)), "gws_act8_encode")
 
 
 def gws_act8_decode(a: Act8, x, stream=None) -> None:
     """The values of such codes into BF16 ``x``; exact."""
     M, C = x.shape
-    _check((_lib or load_library()).gws_act8_decode(_pack_act8(*_act8_fields(a, M, C)), M, C, x.data_ptr(), x.stride(0), _stream(stream)), "gws_act8_decode")
+    _check((_lib or load_library()).gws_act8_decode(_pack_act8(*_act8_fields(a, M, C)), M, C, x.data_ptr(), x.stride()[0], _stream(stream)), "gws_act8_decode")
 
 
 def gws_gated_fwd(x, wg, wu, h, act: int = ACT_SILU, saved: Optional[GatedSaved] = None, w_is_nk: bool = False, stream=None) -> None:
     """H = a(X Wg) * (X Wu) by elements in one kernel; ``saved`` receives G and U for the backward pass."""
     M, K = x.shape
-    size, ldw, ldh = wg.shape, wg.stride(0), h.stride(0)
+    size, ldw, ldh = wg.shape, wg.stride()[0], h.stride()[0]
     F, Kw = size if w_is_nk else (size[1], size[0])
     if Kw != K or wu.shape != size or h.shape != (M, F):
         raise ValueError(f"X {list(x.shape)}, Wg {list(size)}, Wu {list(wu.shape)} and H {list(h.shape)} do not fit together")
-    if wu.stride(0) != ldw:
-        raise ValueError(f"leading dimensions of Wg and Wu differ: {ldw} and {wu.stride(0)}")
-    _check((_lib or load_library()).gws_gated_fwd(x.data_ptr(), M, K, x.stride(0), wg.data_ptr(), wu.data_ptr(), F, ldw, 1 if w_is_nk else 0, act,
+    if wu.stride()[0] != ldw:
+        raise ValueError(f"leading dimensions of Wg and Wu differ: {ldw} and {wu.stride()[0]}")
+    _check((_lib or load_library()).gws_gated_fwd(x.data_ptr(), M, K, x.stride()[0], wg.data_ptr(), wu.data_ptr(), F, ldw, 1 if w_is_nk else 0, act,
                                                   h.data_ptr(), ldh, _marshal_saved(saved, M, F), _stream(stream)), "gws_gated_fwd")
 
 
 def _gradient_fields(dg, du, h, M, F):
     """dG, dU, their leading dimension, H and its."""
-    size, ldd = (M, F), dg.stride(0)
+    size, ldd = (M, F), dg.stride()[0]
     if dg.shape != size or du.shape != size or (h is not None and h.shape != size):
         raise ValueError(f"dG, dU and H have shape [{M}, {F}]")
-    if du.stride(0) != ldd:
-        raise ValueError(f"leading dimensions of dG and dU differ: {ldd} and {du.stride(0)}")
-    return (dg.data_ptr(), du.data_ptr(), ldd, None, 0) if h is None else (dg.data_ptr(), du.data_ptr(), ldd, h.data_ptr(), h.stride(0))
+    if du.stride()[0] != ldd:
+        raise ValueError(f"leading dimensions of dG and dU differ: {ldd} and {du.stride()[0]}")
+    return (dg.data_ptr(), du.data_ptr(), ldd, None, 0) if h is None else (dg.data_ptr(), du.data_ptr(), ldd, h.data_ptr(), h.stride()[0])
 
 
 def gws_gated_bwd(dy, wd, saved: GatedSaved, dg, du, act: int = ACT_SILU, h=None, w_is_nk: bool = False, stream=None) -> None:
@@ -640,28 +641,28 @@ def gws_gated_bwd(dy, wd, saved: GatedSaved, dg, du, act: int = ACT_SILU, h=None
     F, Dw = (size[1], size[0]) if w_is_nk else size
     if Dw != D:
         raise ValueError(f"dY {list(dy.shape)} and Wd {list(size)} do not fit together")
-    _check((_lib or load_library()).gws_gated_bwd(dy.data_ptr(), M, D, dy.stride(0), wd.data_ptr(), F, wd.stride(0), 1 if w_is_nk else 0, act,
+    _check((_lib or load_library()).gws_gated_bwd(dy.data_ptr(), M, D, dy.stride()[0], wd.data_ptr(), F, wd.stride()[0], 1 if w_is_nk else 0, act,
                                                   _marshal_saved(saved, M, F), *_gradient_fields(dg, du, h, M, F), _stream(stream)), "gws_gated_bwd")
 
 
 def gws_gated_bwd_h(dh, saved: GatedSaved, dg, du, act: int = ACT_SILU, h=None, stream=None) -> None:
     """``gws_gated_bwd`` from a given dH."""
     M, F = dh.shape
-    _check((_lib or load_library()).gws_gated_bwd_h(dh.data_ptr(), M, F, dh.stride(0), act, _marshal_saved(saved, M, F),
+    _check((_lib or load_library()).gws_gated_bwd_h(dh.data_ptr(), M, F, dh.stride()[0], act, _marshal_saved(saved, M, F),
                                                     *_gradient_fields(dg, du, h, M, F), _stream(stream)), "gws_gated_bwd_h")
 
 
 def gws_gated_bwd_x(dg, du, wg, wu, dx, w_is_nk: bool = False, stream=None) -> None:
     """dX = dG Wg^T + dU Wu^T in one sum; ``w_is_nk`` as in ``gws_gated_fwd``."""
     M, F = dg.shape
-    size, ldw, ldd = wg.shape, wg.stride(0), dg.stride(0)
+    size, ldw, ldd = wg.shape, wg.stride()[0], dg.stride()[0]
     K, Fw = (size[1], size[0]) if w_is_nk else size
     if Fw != F or wu.shape != size or du.shape != (M, F) or dx.shape != (M, K):
         raise ValueError(f"dG {list(dg.shape)}, dU {list(du.shape)}, Wg {list(size)}, Wu {list(wu.shape)} and dX {list(dx.shape)} do not fit together")
-    if wu.stride(0) != ldw or du.stride(0) != ldd:
-        raise ValueError(f"leading dimensions differ: dG and dU {ldd} and {du.stride(0)}, Wg and Wu {ldw} and {wu.stride(0)}")
+    if wu.stride()[0] != ldw or du.stride()[0] != ldd:
+        raise ValueError(f"leading dimensions differ: dG and dU {ldd} and {du.stride()[0]}, Wg and Wu {ldw} and {wu.stride()[0]}")
     _check((_lib or load_library()).gws_gated_bwd_x(dg.data_ptr(), du.data_ptr(), M, F, ldd, wg.data_ptr(), wu.data_ptr(), K, ldw, 1 if w_is_nk else 0,
-                                                    dx.data_ptr(), dx.stride(0), _stream(stream)), "gws_gated_bwd_x")
+                                                    dx.data_ptr(), dx.stride()[0], _stream(stream)), "gws_gated_bwd_x")
 
 
 def gws_gated_form(op: int, M: int, K: int, F: int, w_is_nk: bool = False, kept: int = 0, lda: Optional[int] = None, ldw: Optional[int] = None) -> tuple:
@@ -682,7 +683,7 @@ def gws_linear_bwd_w_act8(x: Act8, dy, w: TensorDesc, step: int, workspace, w_is
     """``gws_linear_bwd_w_ws`` with the linear's input kept in 8 bits."""
     M = dy.shape[0]
     nbytes = 0 if workspace is None else int(workspace.numel() * workspace.element_size())
-    _check(load_library().gws_linear_bwd_w_act8(_pack_act8(*_act8_fields(x, M, w.cols if w_is_nk else w.rows)), _p(dy), M, dy.stride(0), _marshal([w]), 1 if w_is_nk else 0, int(step), _p(workspace),
+    _check(load_library().gws_linear_bwd_w_act8(_pack_act8(*_act8_fields(x, M, w.cols if w_is_nk else w.rows)), _p(dy), M, dy.stride()[0], _marshal([w]), 1 if w_is_nk else 0, int(step), _p(workspace),
                                                 nbytes, _stream(stream)), "gws_linear_bwd_w_act8")
 
 
