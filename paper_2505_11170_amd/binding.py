@@ -667,11 +667,17 @@ def gws_gated_bwd_x(dg, du, wg, wu, dx, w_is_nk: bool = False, stream=None) -> N
 
 def gws_gated_form(op: int, M: int, K: int, F: int, w_is_nk: bool = False, kept: int = 0, lda: Optional[int] = None, ldw: Optional[int] = None) -> tuple:
     """The kernel (``GATED_*``) of a call (``GATED_FWD``, ``GATED_BWD`` with K columns of dY, ``GATED_BWD_X``) and, of ``GATED_STREAM``, its tile in
-    units of 16 rows and columns; ``kept``: 0 nothing, 1 BF16, 2 in 8 bits.  0 for sizes that the call refuses."""
+    units of 16 rows and columns; ``kept``: 0 nothing, 1 BF16, 2 in 8 bits.  0 for sizes that the call refuses.  A call of two launches: of the first
+    (``gws_gated_forms`` has both)."""
+    return gws_gated_forms(op, M, K, F, w_is_nk, kept, lda, ldw)[0]
+
+
+def gws_gated_forms(op: int, M: int, K: int, F: int, w_is_nk: bool = False, kept: int = 0, lda: Optional[int] = None, ldw: Optional[int] = None) -> tuple:
+    """``gws_gated_form`` of the first launch, the kernel of the second (0: there is none), and whether the launches share the rows rather than the columns."""
     wide = op == GATED_BWD
     f = int(load_library().gws_gated_form(op, M, K, F, (F if op == GATED_BWD_X else K) if lda is None else lda,
                                           (F if w_is_nk == wide else K) if ldw is None else ldw, int(bool(w_is_nk)), kept))
-    return f & 0xFF, f >> 16, f >> 8 & 0xFF
+    return (f & 0xFF, f >> 16 & 0xFF, f >> 8 & 0xFF), f >> 24 & 0xF, bool(f >> 28)
 
 
 def gws_linear_bwd_w_act8_workspace_bytes(w: TensorDesc, M: int, w_is_nk: bool = False) -> int:

@@ -74,50 +74,133 @@ void kept_buffers(const KeptArgs& k, Kept form, int64_t M, int64_t F, bool writt
   }
 }
 
-// The kernel by the sizes: the fastest by estimates in us, each a launch and, per round of workgroups (one per compute unit), what a tile takes
-// beside its K-steps, the gate and the kept values among it, and the K-steps of 64, which take longer the more compute units are at work (busy).
-// Measured and estimated, in 256 x 256 tiles and in 128 x 128:
-//   forward, nothing kept: 1021 x 768 -> 2048 20.7, 20.3 and 9.9, 10.2; 256 x 2048 -> 5632 39.4, 37.7 and 17.3, 17.7; 2048 x 2048 -> 5632 87, 90
-//   and 97, 97; 8192 x 2048 -> 5632 291, 267 and 420, 348
-//   backward, BF16 kept: 1021 x 768 -> 2048 39, 41 and 14.5, 16.9; 3000 x 1024 -> 4096 62, 54 and 54, 54; 8192 x 2048 -> 5632 213, 223 and 306, 262
-//   input gradient: 5000 x 2 x 1280 -> 640 51, 50 and 21.7, 23.7; 2048 x 2 x 5632 -> 2048 192, 207 and 100, 99; 8192 x 2 x 5632 -> 2048 263, 262
+// The kernel by the sizes: the fastest by estimates in us, each a launch and, per round of workgroups, what a tile takes beside its K-steps,
+// the gate and the kept values among it, and the K-steps of 64, which take longer the more compute units are at work (busy).  Over 160 drawn
+// sizes the choice takes 1.02 of the fastest form's time in the mean.  Measured with the sums in 256 x 256 tiles, in
+// 128 x 128, and in those two workgroups a compute unit:
+//   forward, nothing kept: 1021 x 768 -> 2048 20.8, 10.2, 11.9; 2048 x 2048 -> 5632 85, 94, 79; 8192 x 2048 -> 5632 271, 396, 345
+//   forward, 8 bits kept: 8192 x 2048 -> 5632 297, 443, 384; BF16 kept: 4096 x 768 -> 2048 28.7, 33.5, 28.9
+//   backward, BF16 kept: 1021 x 768 -> 2048 34.6, 14.9, 16.7 (8 x 4 of the streaming kernel: 12.5); 3000 x 1024 -> 4096 47, 52, 51
+//   backward, 8 bits kept: 8192 x 2048 -> 5632 196, 257, 223
+//   input gradient (no third form): 5000 x 2 x 1280 -> 640 51, 21.9; 2048 x 2 x 5632 -> 2048 213, 102; 8192 x 2 x 5632 -> 2048 262, 386
 enum class GatedForm { kAny = GWS_GATED_ANY, kStream = GWS_GATED_STREAM, kMiddle = GWS_GATED_MIDDLE, kLarge = GWS_GATED_LARGE, kShared = GWS_GATED_SHARED };
-GatedForm gated_form(const GatedArgs& g, GatedOp op, bool b_oc, Kept kept, GatedStreamPlan& plan) {
-  plan = gated_stream_plan(g, op, b_oc, kept);
-  const double cus = compute_units() > 0 ? compute_units() : 256, nk = ceil(g.K / 64.0) * (op == GatedOp::kDx ? 2 : 1);
-  const bool keeps = op == GatedOp::kFwd && kept != Kept::kNone;
-  double large = 1e30, middle = 1e30, shared = 1e30;
-  if (gated256_applicable(g)) {
-    const double n = ceil(g.M / 256.0) * ceil(g.N / (op == GatedOp::kFwd ? 128.0 : 256.0)), busy = n / (ceil(n / cus) * cus);
-    const double beside = op == GatedOp::kBwd ? 20.0 + 9.0 * busy : keeps ? 12.0 : 6.5;
-    const double step = op == GatedOp::kDx ? 1.03 + 0.42 * busy : 0.875 + 0.3 * busy;
-    large = 2.5 + ceil(n / cus) * (beside + nk * step);
+struct GatedPlan {
+  GatedForm form;
+  GatedStreamPlan stream;
+  double us;
+};
+// The tiles of a form: rows and columns of one, and how many are at work together.
+struct Tiles {
+  uint32_t rows, cols;
+  double together;
+};
+double units() { return compute_units() > 0 ? compute_units() : 256; }
+Tiles tiles_of(GatedForm form, GatedOp op) {
+  const uint32_t half = op == GatedOp::kFwd ? 2 : 1;   // of a pair of weights the tile has half of its columns of each
+  return form == GatedForm::kLarge ? Tiles{256, 256 / half, units()} : Tiles{128, 128 / half, units() * (form == GatedForm::kShared ? 2.0 : 1.0)};
+}
+double form_us(const GatedArgs& g, GatedOp op, Kept kept, GatedForm form) {
+  if (form == GatedForm::kLarge ? !gated256_applicable(g) : !gated128_applicable(g)) return 1e30;
+  const Tiles t = tiles_of(form, op);
+  // n tiles in rounds, of which the last may leave compute units idle
+  const double n = ceil(g.M / (double)t.rows) * ceil(g.N / (double)t.cols), rounds = ceil(n / t.together), busy = n / (rounds * t.together);
+  const double nk = ceil(g.K / 64.0) * (op == GatedOp::kDx ? 2 : 1);
+  const bool keeps = op == GatedOp::kFwd && kept != Kept::kNone, back = op == GatedOp::kBwd, two = op == GatedOp::kDx;
+  if (form == GatedForm::kLarge) return 2.5 + rounds * ((back ? 22.0 + 13.0 * busy : keeps ? 12.0 : 6.5) + nk * (two ? 1.03 + 0.42 * busy : 0.875 + 0.3 * busy));
+  if (form == GatedForm::kMiddle) {
+    const double last = n / t.together - (rounds - 1), off_lines = (g.lda & 63) != 0 ? 1.1 : 1.0;   // rows of 128-byte pieces on two lines each
+    auto round_us = [&](double f) { return (back ? 8.0 + 2.5 * f : keeps ? 5.6 : 2.6) + nk * (two ? (0.35 + 0.18 * f * f) * off_lines : 0.34 + 0.07 * f); };
+    return 2.7 + (rounds - 1) * round_us(1.0) + round_us(last);
   }
-  if (gated128_applicable(g)) {
-    const double n = ceil(g.M / 128.0) * ceil(g.N / (op == GatedOp::kFwd ? 64.0 : 128.0)), busy = n / (ceil(n / cus) * cus);
-    const double beside = op == GatedOp::kBwd ? 8.0 + 2.5 * busy : keeps ? 5.6 : 2.6;
-    const double step = op == GatedOp::kDx ? 0.35 + 0.18 * busy * busy : 0.34 + 0.07 * busy;
-    middle = 2.7 + ceil(n / cus) * (beside + nk * step);
-    if (n > cus && op != GatedOp::kDx) {   // two workgroups a compute unit
-      const double both = n / (ceil(n / (2 * cus)) * 2 * cus), way_out = op == GatedOp::kBwd ? 3.0 + 13.0 * both : keeps ? 6.5 : 3.0;
-      shared = 2.7 + ceil(n / (2 * cus)) * (way_out + nk * (0.5 + 0.3 * both));
-    }
+  if (two || n <= units()) return 1e30;   // a compute unit has one workgroup, or the form is not built
+  // no rounds: a compute unit takes the next tile while the other one goes on, and the last tiles, alone, are faster
+  return 2.7 + (n / t.together + 0.25) * (back ? 11.5 + nk * 0.88 : (keeps ? 3.5 : 0.3) + nk * 0.95);
+}
+GatedPlan plan_whole(const GatedArgs& g, GatedOp op, bool b_oc, Kept kept) {
+  GatedPlan best = {GatedForm::kAny, gated_stream_plan(g, op, b_oc, kept), 1e30};
+  if (best.stream.p > 0) best = {GatedForm::kStream, best.stream, best.stream.us};
+  for (GatedForm form : {GatedForm::kLarge, GatedForm::kMiddle, GatedForm::kShared}) {
+    const double us = form_us(g, op, kept, form);
+    if (us < best.us) best = {form, best.stream, us};
   }
-  const double best = fmin(large, fmin(middle, shared));
-  if (plan.p > 0 && plan.us < best) return GatedForm::kStream;
-  if (best > 1e29) return GatedForm::kAny;
-  return best == large ? GatedForm::kLarge : best == shared ? GatedForm::kShared : GatedForm::kMiddle;
+  return best;
 }
 
-int launch_gated(const GatedArgs& g, GatedOp op, bool b_oc, Kept kept, hipStream_t stream) {
-  GatedStreamPlan plan;
-  switch (gated_form(g, op, b_oc, kept, plan)) {
-    case GatedForm::kStream: return launch_gated_stream(g, op, b_oc, kept, plan, stream);
+// Rows [m0, m0 + M) and columns [n0, n0 + N) of a call's result; n0 a multiple of 32.
+GatedArgs part_of(GatedArgs g, GatedOp op, bool b_oc, Kept kept, uint32_t m0, uint32_t M, uint32_t n0, uint32_t N) {
+  const size_t m = m0, n = n0, e = kept == Kept::kBf16 ? 2 : 1;
+  g.M = M;
+  g.N = N;
+  g.a += m * g.lda;
+  if (g.a2) g.a2 += m * g.lda;
+  g.b += b_oc ? n : n * g.ldb;
+  if (g.b2) g.b2 += b_oc ? n : n * g.ldb;
+  if (g.h) g.h += m * g.ldh + n;
+  if (op == GatedOp::kBwd) {
+    g.dg += m * g.ldd + n;
+    g.du += m * g.ldd + n;
+  }
+  if (kept != Kept::kNone) {
+    g.kept.g += (m * g.kept.ldg + n) * e;
+    g.kept.u += (m * g.kept.ldu + n) * e;
+  }
+  if (kept == Kept::kE4m3) {
+    g.kept.gs += m * g.kept.lsg + n / 32;
+    g.kept.us += m * g.kept.lsu + n / 32;
+  }
+  return g;
+}
+
+// One launch, or two: where a form's tiles leave a round of compute units partly empty, its whole rounds' columns or rows by that form and the
+// rest by whatever is the fastest for it, where the estimates say that this is worth a second launch.  Of 120 drawn sizes that take two, they
+// are 0.88 of the fastest single launch in the mean, at worst 1.03.  The best single launch and the two, us: forward 2217 x 1152 -> 3808 45.5, 38.7, with
+// BF16 kept 1796 x 1184 -> 4416 58.3, 44.3; backward 4621 x 1664 -> 3520 91, 74, with 8 bits kept 5271 x 1664 -> 3104 95, 87; input gradient
+// 2866 x 2 x 2176 -> 1728 65, 52, 8088 x 2 x 2368 -> 544 71, 61.
+struct GatedSplit {
+  GatedPlan first, rest;
+  uint32_t rows, cols;   // of the first part; 0, 0: one launch
+  double us;
+};
+GatedSplit plan_gated(const GatedArgs& g, GatedOp op, bool b_oc, Kept kept) {
+  const GatedPlan whole = plan_whole(g, op, b_oc, kept);
+  GatedSplit best = {whole, whole, 0, 0, 0.98 * whole.us};
+  if (whole.form == GatedForm::kAny || whole.form == GatedForm::kStream) return best;
+  for (GatedForm form : {GatedForm::kLarge, GatedForm::kMiddle, GatedForm::kShared}) {
+    const Tiles t = tiles_of(form, op);
+    const uint64_t mt = ((uint64_t)g.M + t.rows - 1) / t.rows, nt = ((uint64_t)g.N + t.cols - 1) / t.cols;
+    const uint64_t fit = (uint64_t)(floor((double)(mt * nt) / t.together) * t.together);   // tiles of whole rounds
+    const uint64_t cols = fit / mt * t.cols, rows = fit / nt * t.rows;
+    for (int by_rows = 0; by_rows < 2; ++by_rows) {
+      if (by_rows ? rows == 0 || rows >= g.M : cols == 0 || cols >= g.N) continue;
+      const uint32_t m = by_rows ? (uint32_t)rows : g.M, n = by_rows ? g.N : (uint32_t)cols;
+      const GatedArgs first = part_of(g, op, b_oc, kept, 0, m, 0, n);
+      const GatedArgs rest = part_of(g, op, b_oc, kept, by_rows ? m : 0, by_rows ? g.M - m : g.M, by_rows ? 0 : n, by_rows ? g.N : g.N - n);
+      const double us = form_us(first, op, kept, form);
+      const GatedPlan after = plan_whole(rest, op, b_oc, kept);
+      const double both = us + after.us + 4.0;   // the second launch's start and a second end of work
+      if (both < best.us) best = {{form, whole.stream, us}, after, by_rows ? m : 0, by_rows ? 0 : n, both};
+    }
+  }
+  return best;
+}
+
+int launch_form(const GatedArgs& g, GatedOp op, bool b_oc, Kept kept, const GatedPlan& plan, hipStream_t stream) {
+  switch (plan.form) {
+    case GatedForm::kStream: return launch_gated_stream(g, op, b_oc, kept, plan.stream, stream);
     case GatedForm::kMiddle: return launch_gated128(g, op, b_oc, kept, false, stream);
     case GatedForm::kShared: return launch_gated128(g, op, b_oc, kept, true, stream);
     case GatedForm::kLarge: return launch_gated256(g, op, b_oc, kept, stream);
     default: return launch_gated_any(g, op, b_oc, kept, stream);
   }
+}
+
+int launch_gated(const GatedArgs& g, GatedOp op, bool b_oc, Kept kept, hipStream_t stream) {
+  const GatedSplit p = plan_gated(g, op, b_oc, kept);
+  if (p.rows + p.cols == 0) return launch_form(g, op, b_oc, kept, p.first, stream);
+  const uint32_t m = p.rows ? p.rows : g.M, n = p.cols ? p.cols : g.N;
+  const int rc = launch_form(part_of(g, op, b_oc, kept, 0, m, 0, n), op, b_oc, kept, p.first, stream);
+  if (rc != GWS_OK) return rc;
+  return launch_form(part_of(g, op, b_oc, kept, p.rows, g.M - p.rows, p.cols, g.N - p.cols), op, b_oc, kept, p.rest, stream);
 }
 
 }  // namespace
@@ -293,10 +376,10 @@ int gws_gated_form(int op, int64_t M, int64_t K, int64_t F, int64_t lda, int64_t
   g.K = (uint32_t)(op == GWS_GATED_BWD_X ? F : K);
   g.lda = (uint32_t)lda;
   g.ldb = (uint32_t)ldw;
-  GatedStreamPlan plan;
   const GatedOp o = op == GWS_GATED_FWD ? GatedOp::kFwd : op == GWS_GATED_BWD ? GatedOp::kBwd : GatedOp::kDx;
-  const GatedForm form = gated_form(g, o, op == GWS_GATED_FWD ? !w_is_nk : w_is_nk != 0, o == GatedOp::kDx ? Kept::kNone : (Kept)kept, plan);
-  return (int)form | (form == GatedForm::kStream ? plan.mt << 16 | plan.nt << 8 : 0);
+  const GatedSplit p = plan_gated(g, o, op == GWS_GATED_FWD ? !w_is_nk : w_is_nk != 0, o == GatedOp::kDx ? Kept::kNone : (Kept)kept);
+  return (int)p.first.form | (p.first.form == GatedForm::kStream ? p.first.stream.mt << 16 | p.first.stream.nt << 8 : 0) |
+         (p.rows + p.cols ? (int)p.rest.form << 24 | (p.rows ? 1 << 28 : 0) : 0);
 }
 
 }  // extern "C"

@@ -263,7 +263,10 @@ GatedStreamPlan gated_stream_plan(const GatedArgs& g, GatedOp op, bool b_oc, Kep
     const double weight = t.nt * (b_oc && pair ? 1.8 : b_oc && two ? 1.35 : 1.0);
     const double beside = t.mt * t.nt * (op == GatedOp::kBwd ? 0.09 : pair && kept != Kept::kNone ? 0.06 : 0.0);
     const double rounds = (double)((wgs + cus - 1) / cus);
-    const double us = 1.8 + rounds * (2.7 + beside + K * 2 * 16 * (t.mt + weight) / t.rate * 1e-3);
+    // two wide operands of more than the L2s hold come from memory more slowly than the tiles ask for them: 5211 x 2 x 2944 -> 320 (61 MB) 51 us, 36
+    // without this (128 x 128 tiles: 42); 6384 x 2 x 3968 -> 256 (101 MB) 78, 44
+    const double rows_mb = (double)g.M * K * 2e-6, cold = two && rows_mb > 48.0 ? (rows_mb - 48.0) / 1.5 : 0.0;
+    const double us = 1.8 + cold + rounds * (2.7 + beside + K * 2 * 16 * (t.mt + weight) / t.rate * 1e-3);
     if (wgs < 0x7FFFFFFFull && us < best.us) best = {t.mt, t.nt, t.p, us};
   }
   return best;

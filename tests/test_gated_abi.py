@@ -195,6 +195,9 @@ def test_query_of_the_chosen_kernel():
     assert form(binding.GATED_FWD, 1, 2048, 5632, True) == (binding.GATED_STREAM, 1, 2) or form(binding.GATED_FWD, 1, 2048, 5632, True) == (binding.GATED_STREAM, 1, 4)
     assert form(binding.GATED_FWD, 8192, 32, 5632)[0] == binding.GATED_ANY and form(binding.GATED_FWD, 4, 2048, 64, True, lda=1 << 24)[0] == binding.GATED_ANY
     assert form(binding.GATED_BWD_X, 8192, 2048, 5632, True)[0] == binding.GATED_LARGE
+    assert binding.gws_gated_forms(binding.GATED_FWD, 1021, 768, 2048, False, 1) == ((binding.GATED_MIDDLE, 0, 0), 0, False)
+    assert binding.gws_gated_forms(binding.GATED_FWD, 2217, 1152, 3808, True) == ((binding.GATED_LARGE, 0, 0), binding.GATED_STREAM, False)
+    assert binding.gws_gated_forms(binding.GATED_FWD, 2914, 1376, 3424, True) == ((binding.GATED_LARGE, 0, 0), binding.GATED_SHARED, True)
     for bad in ((3, 4, 64, 64), (0, 0, 64, 64), (0, 4, 48, 64), (1, 4, 64, 64, False, 0), (0, 4, 64, 64, False, 3)):
         assert form(*bad)[0] == 0
     assert form(binding.GATED_FWD, 4, 64, 64, lda=56)[0] == 0

@@ -27,14 +27,60 @@ FORWARD = [(5, 32, 160, ANY), (7, 96, 96, (STREAM, 1, 2)), (9, 64, 64, (STREAM, 
            (19, 96, 96, (STREAM, 2, 4)), (32, 1024, 128, (STREAM, 2, 4)), (239, 480, 1088, (STREAM, 4, 4)), (64, 512, 5632, (STREAM, 4, 4)),
            (84, 96, 4960, (STREAM, 8, 4)), (128, 256, 5632, (STREAM, 8, 4)), (700, 736, 2080, MIDDLE), (1024, 64, 2048, MIDDLE), (256, 2048, 5632, MIDDLE),
            (408, 96, 4160, SHARED), (914, 352, 3520, SHARED),
-           (1300, 96, 5024, LARGE), (1792, 384, 2816, LARGE), (2304, 2048, 3584, LARGE), (1460, 288, 4448, LARGE)]
+           (1300, 96, 5024, SHARED), (1792, 384, 2816, SHARED), (1460, 288, 4448, SHARED),
+           (1024, 896, 5632, LARGE), (1948, 416, 3712, LARGE), (2112, 416, 3552, LARGE), (2304, 2048, 3584, LARGE)]
 BACKWARD = [(5, 32, 160, ANY), (7, 96, 96, (STREAM, 1, 2)), (16, 64, 96, (STREAM, 1, 2)), (3, 96, 9248, (STREAM, 1, 4)), (13, 64, 12288, (STREAM, 1, 4)),
             (19, 96, 96, (STREAM, 2, 4)), (32, 1024, 128, (STREAM, 2, 4)), (202, 96, 2400, (STREAM, 4, 4)), (118, 448, 4800, (STREAM, 4, 4)),
             (1110, 96, 928, (STREAM, 8, 4)), (1021, 768, 2048, (STREAM, 8, 4)), (1211, 416, 2112, MIDDLE), (2048, 512, 2048, MIDDLE), (600, 1056, 5536, MIDDLE),
-            (900, 96, 4288, SHARED), (1849, 224, 4768, SHARED), (4096, 768, 2048, SHARED), (2048, 2048, 5632, LARGE), (2300, 2080, 5152, LARGE)]
+            (900, 96, 4288, SHARED), (1849, 224, 4768, SHARED), (4096, 768, 2048, SHARED), (2048, 2048, 5632, SHARED),
+            (2560, 1152, 5632, LARGE), (2977, 864, 5248, LARGE), (2300, 2080, 5152, LARGE)]
 GRADIENT = [(5, 160, 32, ANY), (7, 96, 96, (STREAM, 1, 2)), (16, 4160, 64, (STREAM, 1, 2)), (11, 12288, 96, (STREAM, 1, 4)), (21, 96, 96, (STREAM, 2, 2)),
             (32, 1024, 1024, (STREAM, 2, 2)), (184, 1376, 96, (STREAM, 2, 4)), (700, 768, 2016, (STREAM, 4, 4)), (2061, 480, 96, (STREAM, 8, 4)),
             (1169, 1696, 96, MIDDLE), (2048, 2048, 544, MIDDLE), (4096, 768, 1056, MIDDLE), (6000, 2016, 480, LARGE), (8192, 2048, 256, LARGE)]
+# M, K, F, (kernel of the first launch, of the second, whether they share the rows rather than the columns)
+FORWARD_SPLIT = [(2217, 1152, 3808, (LARGE, 2, False)), (1796, 1184, 4416, (LARGE, 2, True)), (1951, 1152, 4864, (LARGE, 3, False)),
+                 (2147, 1088, 4608, (LARGE, 3, True)), (1927, 1280, 5152, (LARGE, 5, False)), (2914, 1376, 3424, (LARGE, 5, True))]
+BACKWARD_SPLIT = [(5271, 1664, 3104, (LARGE, 2, False)), (3848, 1504, 4352, (LARGE, 2, True)), (3999, 1792, 5056, (LARGE, 3, False)),
+                  (3814, 1824, 5280, (LARGE, 3, True))]
+GRADIENT_SPLIT = [(2208, 1888, 672, (MIDDLE, 2, False)), (3289, 1280, 800, (MIDDLE, 2, True))]
+
+
+@pytest.mark.parametrize("kept", ["none", "bf16", "e4m3"])
+@pytest.mark.parametrize("nk", [False, True])
+@pytest.mark.parametrize("M,K,F,forms", FORWARD_SPLIT)
+def test_forward_of_two_launches(M, K, F, forms, nk, kept):
+    assert gws.gws_gated_forms(gws.GATED_FWD, M, K, F, nk, KEPT[kept]) == forms
+    check_fwd(M, K, F, nk, M % 2, kept, pad=8 * (M % 3))
+
+
+@pytest.mark.parametrize("kept", ["bf16", "e4m3"])
+@pytest.mark.parametrize("nk", [False, True])
+@pytest.mark.parametrize("M,D,F,forms", BACKWARD_SPLIT)
+def test_backward_of_two_launches(M, D, F, forms, nk, kept):
+    assert gws.gws_gated_forms(gws.GATED_BWD, M, D, F, nk, KEPT[kept]) == forms
+    check_bwd(M, D, F, nk, M % 2, kept, pad=8 * (M % 3))
+
+
+@pytest.mark.parametrize("nk", [False, True])
+@pytest.mark.parametrize("M,K,F,forms", GRADIENT_SPLIT)
+def test_input_gradient_of_two_launches(M, K, F, forms, nk):
+    assert gws.gws_gated_forms(gws.GATED_BWD_X, M, K, F, nk) == forms
+    check_dx(M, K, F, nk, pad=8 * (M % 3))
+
+
+def test_two_launches_in_place():
+    # dG and dU in the places of the kept BF16 values: each launch reads and writes its own columns, or rows, alone
+    for M, D, F, forms in BACKWARD_SPLIT[:2]:
+        assert gws.gws_gated_forms(gws.GATED_BWD, M, D, F, True, KEPT["bf16"]) == forms
+        gen = torch.Generator(device=DEV).manual_seed(M)
+        def some(r, c, std):
+            return (torch.randn(r, c, device=DEV, generator=gen) * std).bfloat16()
+        dy, w, g, u = some(M, D, 1e-3), some(D, F, 0.02), some(M, F, 1.0), some(M, F, 1.0)
+        dg, du = torch.empty_like(g), torch.empty_like(u)
+        gws.gws_gated_bwd(dy, w, gws.GatedSaved(g=g, u=u), dg, du, w_is_nk=True)
+        gws.gws_gated_bwd(dy, w, gws.GatedSaved(g=g, u=u), g, u, w_is_nk=True)
+        torch.cuda.synchronize()
+        assert torch.equal(g, dg) and torch.equal(u, du)
 
 
 @pytest.mark.parametrize("kept", ["none", "bf16", "e4m3"])
@@ -68,10 +114,10 @@ def test_input_gradient(M, K, F, form, nk):
     check_dx(M, K, F, nk, pad=8 * (M % 3))
 
 
-@pytest.mark.parametrize("M,F,form", [(9, 160, (STREAM, 1, 4)), (700, 2080, MIDDLE), (1300, 5024, LARGE), (5, 160, ANY)])
+@pytest.mark.parametrize("M,F,form", [(9, 160, (STREAM, 1, 4)), (700, 2080, MIDDLE), (1300, 5024, SHARED), (1948, 3712, LARGE), (5, 160, ANY)])
 def test_values_beyond_the_largest_scale(M, F, form):
     # one product per sum: G of up to 3.2e38, which its BF16 rounding and 464 2^119 = 3.08e38 lie below
-    K = 32 if form == ANY else 96
+    K = {ANY: 32, LARGE: 416}.get(form, 96)
     taken(form, gws.GATED_FWD, M, K, F, True, 2)
     x = torch.zeros(M, K, dtype=torch.bfloat16, device=DEV)
     x[:, 0] = torch.tensor([2.0 ** 64, -(2.0 ** 64), 2.0 ** 60, 1.0], dtype=torch.bfloat16).repeat(-(-M // 4))[:M].to(DEV)
