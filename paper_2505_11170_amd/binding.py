@@ -573,7 +573,30 @@ def gws_block_absmax(t: Sequence[TensorDesc], stream=None) -> None:
     _check(L.gws_block_absmax(arr, n, _stream(stream)), "gws_block_absmax")
 
 
-# (stride()[0]: half the time of stride(0), which takes its argument apart)
+# A kernel reads BF16 rows, or bytes, in memory order: other types and spread columns are told here, where the tensors still say so.  The calls
+# compare in line (a function for every tensor takes as long as the call) and come here only for the message, and once for torch's types.
+_bf16, _one_byte = None, frozenset()
+
+
+def _check_plain(*matrices) -> None:
+    global _bf16
+    if _bf16 is None:
+        import torch
+        _bf16 = torch.bfloat16
+    for t in matrices:
+        if t.dtype is not _bf16 or (t.stride()[1] != 1 and t.shape[1] > 1):
+            raise ValueError(f"a matrix is BF16 with its columns next to each other, not {t.dtype} of shape {list(t.shape)} and strides {list(t.stride())}")
+
+
+def _check_bytes(*matrices) -> None:
+    global _one_byte
+    for t in matrices:
+        if t.element_size() != 1 or (t.stride()[1] != 1 and t.shape[1] > 1):
+            raise ValueError(f"codes and scales are of one byte and next to each other, not {t.dtype} of shape {list(t.shape)} and strides {list(t.stride())}")
+        _one_byte |= {t.dtype}
+
+
+# (stride() whole: half the time of stride(0), which takes its argument apart)
 _pack_act8 = struct.Struct("=2Q2q").pack
 _pack_saved = struct.Struct("=2Q2q2Q2q2Q2q").pack   # the fields in one go, passed as bytes (building the structures takes as long as the call)
 assert struct.calcsize("=2Q2q") == ctypes.sizeof(_CAct8) and struct.calcsize("=2Q2q2Q2q2Q2q") == ctypes.sizeof(_CGatedSaved)
@@ -583,7 +606,10 @@ def _act8_fields(a: Act8, rows: int, cols: int):
     c, s, ldc, lds = a.codes, a.xscale, a.ldc, a.lds
     if c.shape != (rows, cols) or s.shape != (rows, -(-cols // 32)):
         raise ValueError(f"[{rows}, {cols}] in 8 bits has codes of that shape and scales [{rows}, {-(-cols // 32)}], not {list(c.shape)} and {list(s.shape)}")
-    return c.data_ptr(), s.data_ptr(), c.stride()[0] if ldc is None else ldc, s.stride()[0] if lds is None else lds
+    (cs, c1), (ss, s1) = c.stride(), s.stride()
+    if c1 != 1 or s1 != 1 or c.dtype not in _one_byte or s.dtype not in _one_byte:
+        _check_bytes(c, s)
+    return c.data_ptr(), s.data_ptr(), cs if ldc is None else ldc, ss if lds is None else lds
 
 
 def _marshal_saved(s: Optional[GatedSaved], rows: int, cols: int):
@@ -593,7 +619,10 @@ def _marshal_saved(s: Optional[GatedSaved], rows: int, cols: int):
     if g8 is None and u8 is None and g is not None and u is not None:
         if g.shape != (rows, cols) or u.shape != (rows, cols):
             raise ValueError(f"a kept G or U has shape {list(g.shape)} or {list(u.shape)}, not [{rows}, {cols}]")
-        return _pack_saved(g.data_ptr(), u.data_ptr(), g.stride()[0], u.stride()[0], 0, 0, 0, 0, 0, 0, 0, 0)
+        (ldg, g1), (ldu, u1) = g.stride(), u.stride()
+        if not (g1 == u1 == 1 and g.dtype is u.dtype is _bf16):
+            _check_plain(g, u)
+        return _pack_saved(g.data_ptr(), u.data_ptr(), ldg, ldu, 0, 0, 0, 0, 0, 0, 0, 0)
     if g is None and u is None and g8 is not None and u8 is not None:
         return _pack_saved(0, 0, 0, 0, *_act8_fields(g8, rows, cols), *_act8_fields(u8, rows, cols))
     raise ValueError("G and U are kept both as BF16 (g, u) or both in 8 bits (g8, u8)")
@@ -601,68 +630,83 @@ def _marshal_saved(s: Optional[GatedSaved], rows: int, cols: int):
 
 def gws_act8_encode(x, o: Act8, stream=None) -> None:
     """BF16 ``x`` [rows, columns] to E4M3 codes and a scale for every 32 of a row."""
-    M, C = x.shape
-    _check((_lib or load_library()).gws_act8_encode(x.data_ptr(), M, C, x.stride()[0], _pack_act8(*_act8_fields(o, M, C)), _stream(stream)), "gws_act8_encode")
+    (M, C), (ldx, x1) = x.shape, x.stride()
+    if x1 != 1 or x.dtype is not _bf16:
+        _check_plain(x)
+    _check((_lib or load_library()).gws_act8_encode(x.data_ptr(), M, C, ldx, _pack_act8(*_act8_fields(o, M, C)), _stream(stream)), "gws_act8_encode")
 
 
 def gws_act8_decode(a: Act8, x, stream=None) -> None:
     """The values of such codes into BF16 ``x``; exact."""
-    M, C = x.shape
-    _check((_lib or load_library()).gws_act8_decode(_pack_act8(*_act8_fields(a, M, C)), M, C, x.data_ptr(), x.stride()[0], _stream(stream)), "gws_act8_decode")
+    (M, C), (ldx, x1) = x.shape, x.stride()
+    if x1 != 1 or x.dtype is not _bf16:
+        _check_plain(x)
+    _check((_lib or load_library()).gws_act8_decode(_pack_act8(*_act8_fields(a, M, C)), M, C, x.data_ptr(), ldx, _stream(stream)), "gws_act8_decode")
 
 
 def gws_gated_fwd(x, wg, wu, h, act: int = ACT_SILU, saved: Optional[GatedSaved] = None, w_is_nk: bool = False, stream=None) -> None:
     """H = a(X Wg) * (X Wu) by elements in one kernel; ``saved`` receives G and U for the backward pass."""
-    M, K = x.shape
-    size, ldw, ldh = wg.shape, wg.stride()[0], h.stride()[0]
+    (M, K), size = x.shape, wg.shape
+    (ldx, x1), (ldw, g1), (ldwu, u1), (ldh, h1) = x.stride(), wg.stride(), wu.stride(), h.stride()
     F, Kw = size if w_is_nk else (size[1], size[0])
     if Kw != K or wu.shape != size or h.shape != (M, F):
         raise ValueError(f"X {list(x.shape)}, Wg {list(size)}, Wu {list(wu.shape)} and H {list(h.shape)} do not fit together")
-    if wu.stride()[0] != ldw:
-        raise ValueError(f"leading dimensions of Wg and Wu differ: {ldw} and {wu.stride()[0]}")
-    _check((_lib or load_library()).gws_gated_fwd(x.data_ptr(), M, K, x.stride()[0], wg.data_ptr(), wu.data_ptr(), F, ldw, 1 if w_is_nk else 0, act,
+    if not (x1 == g1 == u1 == h1 == 1 and x.dtype is wg.dtype is wu.dtype is h.dtype is _bf16):
+        _check_plain(x, wg, wu, h)
+    if ldwu != ldw:
+        raise ValueError(f"leading dimensions of Wg and Wu differ: {ldw} and {ldwu}")
+    _check((_lib or load_library()).gws_gated_fwd(x.data_ptr(), M, K, ldx, wg.data_ptr(), wu.data_ptr(), F, ldw, 1 if w_is_nk else 0, act,
                                                   h.data_ptr(), ldh, _marshal_saved(saved, M, F), _stream(stream)), "gws_gated_fwd")
 
 
 def _gradient_fields(dg, du, h, M, F):
     """dG, dU, their leading dimension, H and its."""
-    size, ldd = (M, F), dg.stride()[0]
+    size, (ldd, g1), (lddu, u1) = (M, F), dg.stride(), du.stride()
+    ldh, h1 = (0, 1) if h is None else h.stride()
     if dg.shape != size or du.shape != size or (h is not None and h.shape != size):
         raise ValueError(f"dG, dU and H have shape [{M}, {F}]")
-    if du.stride()[0] != ldd:
-        raise ValueError(f"leading dimensions of dG and dU differ: {ldd} and {du.stride()[0]}")
-    return (dg.data_ptr(), du.data_ptr(), ldd, None, 0) if h is None else (dg.data_ptr(), du.data_ptr(), ldd, h.data_ptr(), h.stride()[0])
+    if not (g1 == u1 == h1 == 1 and dg.dtype is du.dtype is _bf16 and (h is None or h.dtype is _bf16)):
+        _check_plain(*((dg, du) if h is None else (dg, du, h)))
+    if lddu != ldd:
+        raise ValueError(f"leading dimensions of dG and dU differ: {ldd} and {lddu}")
+    return dg.data_ptr(), du.data_ptr(), ldd, None if h is None else h.data_ptr(), ldh
 
 
 def gws_gated_bwd(dy, wd, saved: GatedSaved, dg, du, act: int = ACT_SILU, h=None, w_is_nk: bool = False, stream=None) -> None:
     """dG and dU (and H again) from the gradient of Y = H Wd and the kept G and U; dH = dY Wd^T stays in the kernel."""
-    M, D = dy.shape
-    size = wd.shape
+    (M, D), size = dy.shape, wd.shape
+    (ldy, y1), (ldw, w1) = dy.stride(), wd.stride()
     F, Dw = (size[1], size[0]) if w_is_nk else size
     if Dw != D:
         raise ValueError(f"dY {list(dy.shape)} and Wd {list(size)} do not fit together")
-    _check((_lib or load_library()).gws_gated_bwd(dy.data_ptr(), M, D, dy.stride()[0], wd.data_ptr(), F, wd.stride()[0], 1 if w_is_nk else 0, act,
+    if not (y1 == w1 == 1 and dy.dtype is wd.dtype is _bf16):
+        _check_plain(dy, wd)
+    _check((_lib or load_library()).gws_gated_bwd(dy.data_ptr(), M, D, ldy, wd.data_ptr(), F, ldw, 1 if w_is_nk else 0, act,
                                                   _marshal_saved(saved, M, F), *_gradient_fields(dg, du, h, M, F), _stream(stream)), "gws_gated_bwd")
 
 
 def gws_gated_bwd_h(dh, saved: GatedSaved, dg, du, act: int = ACT_SILU, h=None, stream=None) -> None:
     """``gws_gated_bwd`` from a given dH."""
-    M, F = dh.shape
-    _check((_lib or load_library()).gws_gated_bwd_h(dh.data_ptr(), M, F, dh.stride()[0], act, _marshal_saved(saved, M, F),
+    (M, F), (ldh, h1) = dh.shape, dh.stride()
+    if h1 != 1 or dh.dtype is not _bf16:
+        _check_plain(dh)
+    _check((_lib or load_library()).gws_gated_bwd_h(dh.data_ptr(), M, F, ldh, act, _marshal_saved(saved, M, F),
                                                     *_gradient_fields(dg, du, h, M, F), _stream(stream)), "gws_gated_bwd_h")
 
 
 def gws_gated_bwd_x(dg, du, wg, wu, dx, w_is_nk: bool = False, stream=None) -> None:
     """dX = dG Wg^T + dU Wu^T in one sum; ``w_is_nk`` as in ``gws_gated_fwd``."""
-    M, F = dg.shape
-    size, ldw, ldd = wg.shape, wg.stride()[0], dg.stride()[0]
+    (M, F), size = dg.shape, wg.shape
+    (ldd, d1), (lddu, e1), (ldw, g1), (ldwu, u1), (ldx, x1) = dg.stride(), du.stride(), wg.stride(), wu.stride(), dx.stride()
     K, Fw = (size[1], size[0]) if w_is_nk else size
     if Fw != F or wu.shape != size or du.shape != (M, F) or dx.shape != (M, K):
         raise ValueError(f"dG {list(dg.shape)}, dU {list(du.shape)}, Wg {list(size)}, Wu {list(wu.shape)} and dX {list(dx.shape)} do not fit together")
-    if wu.stride()[0] != ldw or du.stride()[0] != ldd:
-        raise ValueError(f"leading dimensions differ: dG and dU {ldd} and {du.stride()[0]}, Wg and Wu {ldw} and {wu.stride()[0]}")
+    if not (d1 == e1 == g1 == u1 == x1 == 1 and dg.dtype is du.dtype is wg.dtype is wu.dtype is dx.dtype is _bf16):
+        _check_plain(dg, du, wg, wu, dx)
+    if ldwu != ldw or lddu != ldd:
+        raise ValueError(f"leading dimensions differ: dG and dU {ldd} and {lddu}, Wg and Wu {ldw} and {ldwu}")
     _check((_lib or load_library()).gws_gated_bwd_x(dg.data_ptr(), du.data_ptr(), M, F, ldd, wg.data_ptr(), wu.data_ptr(), K, ldw, 1 if w_is_nk else 0,
-                                                    dx.data_ptr(), dx.stride()[0], _stream(stream)), "gws_gated_bwd_x")
+                                                    dx.data_ptr(), ldx, _stream(stream)), "gws_gated_bwd_x")
 
 
 def gws_gated_form(op: int, M: int, K: int, F: int, w_is_nk: bool = False, kept: int = 0, lda: Optional[int] = None, ldw: Optional[int] = None) -> tuple:
@@ -687,9 +731,11 @@ def gws_linear_bwd_w_act8_workspace_bytes(w: TensorDesc, M: int, w_is_nk: bool =
 
 def gws_linear_bwd_w_act8(x: Act8, dy, w: TensorDesc, step: int, workspace, w_is_nk: bool = False, stream=None) -> None:
     """``gws_linear_bwd_w_ws`` with the linear's input kept in 8 bits."""
-    M = dy.shape[0]
+    M, (ldy, y1) = dy.shape[0], dy.stride()
+    if y1 != 1 or dy.dtype is not _bf16:
+        _check_plain(dy)
     nbytes = 0 if workspace is None else int(workspace.numel() * workspace.element_size())
-    _check(load_library().gws_linear_bwd_w_act8(_pack_act8(*_act8_fields(x, M, w.cols if w_is_nk else w.rows)), _p(dy), M, dy.stride()[0], _marshal([w]), 1 if w_is_nk else 0, int(step), _p(workspace),
+    _check(load_library().gws_linear_bwd_w_act8(_pack_act8(*_act8_fields(x, M, w.cols if w_is_nk else w.rows)), _p(dy), M, ldy, _marshal([w]), 1 if w_is_nk else 0, int(step), _p(workspace),
                                                 nbytes, _stream(stream)), "gws_linear_bwd_w_act8")
 
 

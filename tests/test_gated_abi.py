@@ -157,6 +157,38 @@ def test_python_shapes():
         binding.gws_linear_bwd_w_act8(a, z(4, 256), binding.TensorDesc(rows=256, cols=256, seed=0), 0, None)
 
 
+def test_python_types_and_strides():
+    # what the kernels would read as something else: other types, columns apart, each argument of each call in turn
+    def call(name, **bad):
+        z = lambda *s: torch.zeros(*s, dtype=torch.bfloat16)  # noqa: E731
+        b = lambda *s: torch.zeros(*s, dtype=torch.uint8)  # noqa: E731
+        t = dict(x=z(4, 64), wg=z(64, 64), wu=z(64, 64), h=z(4, 64), g=z(4, 64), u=z(4, 64), dg=z(4, 64), du=z(4, 64), codes=b(4, 64), xscale=b(4, 2))
+        t.update({k: v(t[k]) for k, v in bad.items()})
+        a = lambda: Act8(t["codes"], t["xscale"])  # noqa: E731
+        {"encode": lambda: binding.gws_act8_encode(t["x"], a()), "decode": lambda: binding.gws_act8_decode(a(), t["x"]),
+         "fwd": lambda: binding.gws_gated_fwd(t["x"], t["wg"], t["wu"], t["h"], 9, saved=GatedSaved(g=t["g"], u=t["u"])),
+         "bwd": lambda: binding.gws_gated_bwd(t["x"], t["wg"], GatedSaved(g=t["g"], u=t["u"]), t["dg"], t["du"], 9, h=t["h"]),
+         "bwd8": lambda: binding.gws_gated_bwd(t["x"], t["wg"], GatedSaved(g8=a(), u8=a()), t["dg"], t["du"], 9),
+         "bwd_h": lambda: binding.gws_gated_bwd_h(t["x"], GatedSaved(g=t["g"], u=t["u"]), t["dg"], t["du"], 9, h=t["h"]),
+         "bwd_x": lambda: binding.gws_gated_bwd_x(t["dg"], t["du"], t["wg"], t["wu"], t["x"]),
+         "bwd_w": lambda: binding.gws_linear_bwd_w_act8(a(), t["x"], binding.TensorDesc(rows=64, cols=64, seed=0), 0, None)}[name]()
+
+    def apart(v):
+        return torch.zeros(v.shape[0], 2 * v.shape[1], dtype=v.dtype)[:, ::2]
+
+    takes = {"encode": ("x", "codes", "xscale"), "decode": ("x", "codes", "xscale"), "fwd": ("x", "wg", "wu", "h", "g", "u"),
+             "bwd": ("x", "wg", "g", "u", "dg", "du", "h"), "bwd8": ("codes", "xscale"), "bwd_h": ("x", "g", "u", "dg", "du", "h"),
+             "bwd_x": ("dg", "du", "wg", "wu", "x"), "bwd_w": ("x", "codes", "xscale")}
+    for name, args in takes.items():
+        for arg in args:
+            for wrong in (apart, lambda v: v.float(), lambda v: v.half()):
+                with pytest.raises(ValueError, match="next to each other"):
+                    call(name, **{arg: wrong})
+    for one_byte in (torch.float8_e4m3fn, torch.int8):
+        binding._check_bytes(torch.zeros(4, 64, dtype=torch.uint8).view(one_byte))
+    binding._check_plain(torch.zeros(4, 8, dtype=torch.bfloat16)[:, ::8])                           # one column has no next
+
+
 def test_definition_of_the_8_bit_form():
     # the reference that the GPU tests compare with, against torch's own casts where it has them
     gen = torch.Generator().manual_seed(1)
