@@ -5,7 +5,7 @@
 //   input gradient: the units of 64 of both products, one after the other, are what the wavefronts split.
 // What bounds it for a few tokens: the weights' bytes.  2048 x 5632 [F x K], 46 MB, out of the last-level cache: one token 8.5 us (5.4 TB/s; a large
 // copy reaches 5.15), 27 tokens 9.4.  With more rows the operands that a compute unit takes out of its L2: input gradient of 1021 tokens, 768 x 2048,
-// 13.9 us (192 workgroups, 1 MiB each).
+// 13.9 us in 64 x 64 (192 workgroups, 1 MiB each), 12.4 in 64 x 48 (256, 0.875 MiB).
 // Backward, the kept values requested first of all instead of when the sums are there: 1021 x 768 -> 2048 14.4 -> 12.5 us.
 #include "gws_gated.h"
 #include "gws_gemm_stream_core.h"
@@ -241,31 +241,34 @@ __global__ __launch_bounds__(64 * P) void gated_stream_kernel(const GatedArgs g)
 
 // The tile by an estimate in us: a launch and, per round of workgroups (one per compute unit: the rings fill its LDS), a fixed part, the gate
 // and the bytes of the tile's operands at the rate (bytes per ns) that a compute unit takes them.  Narrow tiles only where few columns would leave
-// compute units idle (the input gradient's K columns).  Measured and estimated:
+// compute units idle (the input gradient's K columns).  Over 120 drawn sizes of input gradients the choice takes 1.004 of the fastest tile's time.
+// Measured and estimated:
 //   forward, G and U not kept, [F x K]: 1 x 2048 -> 5632 9.1 us; 27 9.9, 9.9; 64 11.4, 9.7; 128 15.4, 15.4; [K x F], whose 64-byte pieces of rows
 //   are half lines: 11.5; 12.3, 9.7; 14.5, 11.4; 19.3, 19.0
-//   input gradient, [K x F]: 64 x 2 x 5632 -> 2048 25.5, 26.1; 1021 x 2 x 2048 -> 768 14.6, 15.0
+//   input gradient, [K x F]: 64 x 2 x 5632 -> 2048 25.5, 26.1; 1021 x 2 x 2048 -> 768 in 64 x 64 14.5, 15.0 (192 workgroups), in
+//   64 x 48 13.2, 13.7 (256), in 128 x 64 21.5, 24.1 (96); 1978 x 2 x 1728 -> 928 24.7, 24.9, 31.1, 33.1 and 20.0, 21.5
 GatedStreamPlan gated_stream_plan(const GatedArgs& g, GatedOp op, bool b_oc, Kept kept) {
   GatedStreamPlan best = {0, 0, 0, 1e30};
   if (g.K < 64 || g.lda >= stream::kMaxLd || g.ldb >= stream::kMaxLd) return best;
   const uint64_t cus = compute_units() > 0 ? compute_units() : 256;
   const bool pair = op == GatedOp::kFwd, two = op == GatedOp::kDx;
   const double K = two ? 2.0 * g.K : (double)g.K;
-  static const struct { int mt, nt, p; double rate; } tiles[] = {{1, 1, 8, 130.0}, {1, 2, 8, 130.0}, {2, 2, 8, 130.0}, {1, 4, 8, 130.0},
-                                                                 {2, 4, 4, 100.0}, {4, 4, 4, 100.0}, {8, 4, 4, 72.0}};
+  const struct { int mt, nt, p; double rate; } tiles[] = {{1, 1, 8, 130.0}, {1, 2, 8, 130.0}, {2, 2, 8, 130.0}, {1, 4, 8, 130.0},
+                                                                 {2, 4, 4, 100.0}, {4, 3, 4, 100.0}, {4, 4, 4, 100.0}, {8, 4, 4, two ? 95.0 : 72.0}};
   for (const auto& t : tiles) {
     if (t.mt == 1 && g.M > 16) continue;
     if ((t.nt == 1 || (t.mt == 2 && t.nt == 2)) && !two) continue;
     if (t.nt == 1 && b_oc) continue;
+    if (t.nt == 3 && (b_oc || !two)) continue;                          // 48 columns: not of a weight across the contraction, whose lines it would cut
     if (t.nt == 2 && pair && (b_oc || kept == Kept::kE4m3)) continue;   // 16 columns of each weight: half a block, a quarter of a line
     const uint64_t bn = 16 * t.nt / (pair ? 2 : 1), wgs = ((uint64_t)g.M + 16 * t.mt - 1) / (16 * t.mt) * ((g.N + bn - 1) / bn);
     // a weight across the contraction comes in pieces of lines; the kept values and the gate's results of a tile go through few wavefronts
     const double weight = t.nt * (b_oc && pair ? 1.8 : b_oc && two ? 1.35 : 1.0);
-    const double beside = t.mt * t.nt * (op == GatedOp::kBwd ? 0.09 : pair && kept != Kept::kNone ? 0.06 : 0.0);
+    const double beside = two && t.mt == 8 ? 3.0 : t.mt * t.nt * (op == GatedOp::kBwd ? 0.09 : pair && kept != Kept::kNone ? 0.06 : 0.0);
     const double rounds = (double)((wgs + cus - 1) / cus);
     // two wide operands of more than the L2s hold come from memory more slowly than the tiles ask for them: 5211 x 2 x 2944 -> 320 (61 MB) 51 us, 36
     // without this (128 x 128 tiles: 42); 6384 x 2 x 3968 -> 256 (101 MB) 78, 44
-    const double rows_mb = (double)g.M * K * 2e-6, cold = two && rows_mb > 48.0 ? (rows_mb - 48.0) / 1.5 : 0.0;
+    const double rows_mb = (double)g.M * K * 2e-6, cold = two && rows_mb > 45.0 ? (rows_mb - 45.0) / 1.5 : 0.0;
     const double us = 1.8 + cold + rounds * (2.7 + beside + K * 2 * 16 * (t.mt + weight) / t.rate * 1e-3);
     if (wgs < 0x7FFFFFFFull && us < best.us) best = {t.mt, t.nt, t.p, us};
   }
@@ -281,7 +284,7 @@ static int launch_tile(GatedArgs g, bool b_oc, hipStream_t s) {
   const dim3 grid((uint32_t)(rows * columns));
   if (!b_oc) {
     hipLaunchKernelGGL((gated_stream_kernel<OP, MT, NT, P, D, true, KEPT, BM>), grid, dim3(64 * P), 0, s, g);
-  } else if constexpr (BN >= 32) {
+  } else if constexpr (BN >= 32 && BN != 48) {
     hipLaunchKernelGGL((gated_stream_kernel<OP, MT, NT, P, D, false, KEPT, BM>), grid, dim3(64 * P), 0, s, g);
   } else {
     return GWS_ERR_SHAPE;
@@ -294,6 +297,7 @@ static int launch_plan(const GatedArgs& g, bool b_oc, const GatedStreamPlan& p, 
   if constexpr (OP == GatedOp::kDx) {
     if (p.nt == 1) return g.M <= 8 ? launch_tile<OP, 1, 1, 8, 2, KEPT, 8>(g, b_oc, s) : launch_tile<OP, 1, 1, 8, 2, KEPT>(g, b_oc, s);
     if (p.mt == 2 && p.nt == 2) return launch_tile<OP, 2, 2, 8, 2, KEPT>(g, b_oc, s);
+    if (p.nt == 3) return launch_tile<OP, 4, 3, 4, 2, KEPT>(g, b_oc, s);
   }
   if constexpr (OP != GatedOp::kFwd || KEPT != Kept::kE4m3) {
     if (p.nt == 2) return g.M <= 8 ? launch_tile<OP, 1, 2, 8, 2, KEPT, 8>(g, b_oc, s) : launch_tile<OP, 1, 2, 8, 2, KEPT>(g, b_oc, s);
