@@ -75,9 +75,9 @@ void kept_buffers(const KeptArgs& k, Kept form, int64_t M, int64_t F, bool writt
 }
 
 // The kernel by the sizes: the fastest by estimates in us, each a launch and, per round of workgroups, what a tile takes beside its K-steps,
-// the gate and the kept values among it, and the K-steps of 64, which take longer the more compute units are at work (busy).  Over 160 drawn
-// sizes the choice takes 1.02 of the fastest form's time in the mean.  Measured with the sums in 256 x 256 tiles, in
-// 128 x 128, and in those two workgroups a compute unit:
+// the gate and the kept values among it, and the K-steps of 64, which take longer the more compute units are at work (busy).  Of 100 drawn
+// sizes of more than 256 tiles of 128 x 128 the choice takes at worst 1.09 of the fastest single launch's time, in the mean, two launches
+// included, 0.99.  Measured with the sums in 256 x 256 tiles, in 128 x 128, and in those two workgroups a compute unit:
 //   forward, nothing kept: 1021 x 768 -> 2048 20.8, 10.2, 11.9; 2048 x 2048 -> 5632 85, 94, 79; 8192 x 2048 -> 5632 271, 396, 345
 //   forward, 8 bits kept: 8192 x 2048 -> 5632 297, 443, 384; BF16 kept: 4096 x 768 -> 2048 28.7, 33.5, 28.9
 //   backward, BF16 kept: 1021 x 768 -> 2048 34.6, 14.9, 16.7 (8 x 4 of the streaming kernel: 12.5); 3000 x 1024 -> 4096 47, 52, 51
@@ -107,14 +107,18 @@ double form_us(const GatedArgs& g, GatedOp op, Kept kept, GatedForm form) {
   const double nk = ceil(g.K / 64.0) * (op == GatedOp::kDx ? 2 : 1);
   const bool keeps = op == GatedOp::kFwd && kept != Kept::kNone, back = op == GatedOp::kBwd, two = op == GatedOp::kDx;
   if (form == GatedForm::kLarge) return 2.5 + rounds * ((back ? 22.0 + 13.0 * busy : keeps ? 12.0 : 6.5) + nk * (two ? 1.03 + 0.42 * busy : 0.875 + 0.3 * busy));
-  if (form == GatedForm::kMiddle) {
-    const double last = n / t.together - (rounds - 1), off_lines = (g.lda & 63) != 0 ? 1.1 : 1.0;   // rows of 128-byte pieces on two lines each
-    auto round_us = [&](double f) { return (back ? 8.0 + 2.5 * f : keeps ? 5.6 : 2.6) + nk * (two ? (0.35 + 0.18 * f * f) * off_lines : 0.34 + 0.07 * f); };
-    return 2.7 + (rounds - 1) * round_us(1.0) + round_us(last);
-  }
+  const double off_lines = (g.lda & 63) != 0 ? 1.1 : 1.0;   // rows of 128-byte pieces on two lines each
+  auto round_us = [&](double f) {   // of 128 x 128 tiles, f of the compute units with one each
+    return (back ? 8.0 + 2.5 * f : keeps ? 5.6 : 2.6) + nk * (two ? (0.35 + 0.18 * f * f) * off_lines : 0.34 + 0.07 * f);
+  };
+  const double last = n / t.together - (rounds - 1);
+  if (form == GatedForm::kMiddle) return 2.7 + (rounds - 1) * round_us(1.0) + round_us(last);
   if (two || n <= units()) return 1e30;   // a compute unit has one workgroup, or the form is not built
-  // no rounds: a compute unit takes the next tile while the other one goes on, and the last tiles, alone, are faster
-  return 2.7 + (n / t.together + 0.25) * (back ? 11.5 + nk * 0.88 : (keeps ? 3.5 : 0.3) + nk * 0.95);
+  // Many tiles go out of step: a compute unit takes the next one while its other goes on.  A few go in rounds, of which a last one of up to half
+  // is one tile a compute unit, faster alone.
+  if (rounds > (back ? 1 : 3)) return 2.7 + (n / t.together + 0.25) * (back ? 11.5 + nk * 0.88 : (keeps ? 3.5 : 0.3) + nk * 0.95);
+  const double full = back ? 16.0 + nk * 0.94 : keeps ? 2.9 + nk * 0.98 : 1.5 + nk * 0.95, both = fmax(0.0, 2 * last - 1);
+  return 2.7 + (rounds - 1 + both) * full + (1 - both) * round_us(fmin(1.0, 2 * last));
 }
 GatedPlan plan_whole(const GatedArgs& g, GatedOp op, bool b_oc, Kept kept) {
   GatedPlan best = {GatedForm::kAny, gated_stream_plan(g, op, b_oc, kept), 1e30};
@@ -152,8 +156,8 @@ GatedArgs part_of(GatedArgs g, GatedOp op, bool b_oc, Kept kept, uint32_t m0, ui
 }
 
 // One launch, or two: where a form's tiles leave a round of compute units partly empty, its whole rounds' columns or rows by that form and the
-// rest by whatever is the fastest for it, where the estimates say that this is worth a second launch.  Of 120 drawn sizes that take two, they
-// are 0.88 of the fastest single launch in the mean, at worst 1.03.  The best single launch and the two, us: forward 2217 x 1152 -> 3808 45.5, 38.7, with
+// rest by whatever is the fastest for it, where the estimates say that this is worth a second launch.  Of 180 drawn sizes that take two, they
+// are 0.89 of the fastest single launch in the mean, at worst 1.03.  The best single launch and the two, us: forward 2217 x 1152 -> 3808 45.5, 38.7, with
 // BF16 kept 1796 x 1184 -> 4416 58.3, 44.3; backward 4621 x 1664 -> 3520 91, 74, with 8 bits kept 5271 x 1664 -> 3104 95, 87; input gradient
 // 2866 x 2 x 2176 -> 1728 65, 52, 8088 x 2 x 2368 -> 544 71, 61.
 struct GatedSplit {
