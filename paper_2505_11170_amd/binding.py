@@ -731,11 +731,15 @@ def gws_linear_bwd_w_act8_workspace_bytes(w: TensorDesc, M: int, w_is_nk: bool =
 
 def gws_linear_bwd_w_act8(x: Act8, dy, w: TensorDesc, step: int, workspace, w_is_nk: bool = False, stream=None) -> None:
     """``gws_linear_bwd_w_ws`` with the linear's input kept in 8 bits."""
-    M, (ldy, y1) = dy.shape[0], dy.stride()
+    (M, Ny), (ldy, y1) = dy.shape, dy.stride()
+    K, N = (w.cols, w.rows) if w_is_nk else (w.rows, w.cols)
     if y1 != 1 or dy.dtype is not _bf16:
         _check_plain(dy)
+    # the call itself sees leading dimensions alone, which columns of a wider buffer have too
+    if Ny != N or (w.dw is not None and w.dw.shape != (w.rows, w.cols)):
+        raise ValueError(f"dY {list(dy.shape)} and dW {None if w.dw is None else list(w.dw.shape)} do not fit a weight of {w.rows} x {w.cols} with N = {N}")
     nbytes = 0 if workspace is None else int(workspace.numel() * workspace.element_size())
-    _check(load_library().gws_linear_bwd_w_act8(_pack_act8(*_act8_fields(x, M, w.cols if w_is_nk else w.rows)), _p(dy), M, ldy, _marshal([w]), 1 if w_is_nk else 0, int(step), _p(workspace),
+    _check(load_library().gws_linear_bwd_w_act8(_pack_act8(*_act8_fields(x, M, K)), _p(dy), M, ldy, _marshal([w]), 1 if w_is_nk else 0, int(step), _p(workspace),
                                                 nbytes, _stream(stream)), "gws_linear_bwd_w_act8")
 
 

@@ -157,6 +157,27 @@ def test_python_shapes():
         binding.gws_linear_bwd_w_act8(a, z(4, 256), binding.TensorDesc(rows=256, cols=256, seed=0), 0, None)
 
 
+def test_python_shapes_of_the_weight_gradient():
+    # columns of a wider buffer have a leading dimension that fits any weight: the shapes have to
+    z = lambda *s, d=torch.bfloat16: torch.zeros(*s, dtype=d)  # noqa: E731
+    for nk in (False, True):
+        rows, cols, K, N = (512, 256, 256, 512) if nk else (256, 512, 256, 512)
+        x = Act8(z(128, K, d=torch.uint8), z(128, K // 32, d=torch.uint8))
+
+        def call(dy, dw=None, x=x):
+            w = binding.TensorDesc(rows=rows, cols=cols, seed=0, dw=z(rows, cols) if dw is None else dw)
+            binding.gws_linear_bwd_w_act8(x, dy, w, 0, z(1 << 20, d=torch.uint8), w_is_nk=nk)
+
+        for dy in (z(128, 1024)[:, :256], z(128, 1024)[:, :N + 8], z(128, N - 256), z(128, K)):
+            with pytest.raises(ValueError, match="do not fit"):
+                call(dy)
+        for dw in (z(cols, rows), z(rows, 2 * cols)[:, : cols - 32], z(rows - 32, cols)):
+            with pytest.raises(ValueError, match="do not fit"):
+                call(z(128, N), dw)
+        with pytest.raises(ValueError):
+            call(z(192, N))                                                                           # other tokens than X's
+
+
 def test_python_types_and_strides():
     # what the kernels would read as something else: other types, columns apart, each argument of each call in turn
     def call(name, **bad):
