@@ -444,9 +444,17 @@ def gws_linear_fwd_static(x, w: TensorDesc, y, fmt: int, step: int, w_is_nk: boo
                                    _p(y), int(y.stride(0)), _stream(stream)), "gws_linear_fwd_static")
 
 
+def _check_tokens(x, dy, w: TensorDesc, w_is_nk: bool, what: str) -> None:
+    """X and dY hold what the weight's sizes make the kernel read: the call sees leading dimensions alone, which columns of a wider buffer have too."""
+    K, N = (w.cols, w.rows) if w_is_nk else (w.rows, w.cols)
+    if x.shape[-1] < K or dy.shape[-1] < N or dy.shape[0] < x.shape[0]:
+        raise GwsError(2, what)
+
+
 def gws_linear_bwd_w(x, dy, w: TensorDesc, step: int, w_is_nk: bool = False, stream=None) -> None:
     """dW = X^T dY into ``w.dw`` and, when ``w.dbt`` is given, dL/db_t (paper Eq. 4) from the GEMM's epilogue."""
     L = load_library()
+    _check_tokens(x, dy, w, w_is_nk, "gws_linear_bwd_w")
     _check(L.gws_linear_bwd_w(_p(x), _p(dy), int(x.shape[0]), int(x.stride(0)), int(dy.stride(0)), _marshal([w]),
                               int(bool(w_is_nk)), int(step), _stream(stream)), "gws_linear_bwd_w")
 
@@ -460,6 +468,7 @@ def gws_linear_bwd_w_workspace_bytes(w: TensorDesc, M: int) -> int:
 def gws_linear_bwd_w_ws(x, dy, w: TensorDesc, step: int, workspace, w_is_nk: bool = False, stream=None) -> None:
     """``gws_linear_bwd_w`` with the tokens split into parts through ``workspace`` (a device tensor, or None)."""
     L = load_library()
+    _check_tokens(x, dy, w, w_is_nk, "gws_linear_bwd_w_ws")
     nbytes = 0 if workspace is None else int(workspace.numel() * workspace.element_size())
     _check(L.gws_linear_bwd_w_ws(_p(x), _p(dy), int(x.shape[0]), int(x.stride(0)), int(dy.stride(0)), _marshal([w]),
                                  int(bool(w_is_nk)), int(step), _p(workspace), nbytes, _stream(stream)), "gws_linear_bwd_w_ws")

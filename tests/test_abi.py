@@ -252,3 +252,18 @@ def test_missing_library_fails_loudly(monkeypatch, tmp_path):
     monkeypatch.setattr(binding, "_LIB_PATH", str(tmp_path / "libgws.so"))
     with pytest.raises(RuntimeError, match="no CPU or PyTorch fallback"):
         binding.load_library()
+
+
+def test_weight_gradients_refuse_tokens_narrower_than_the_weight():
+    # columns of a wider buffer have a leading dimension that fits any weight; the kernel would read past them
+    import torch
+    z = lambda *s: torch.zeros(*s, dtype=torch.bfloat16)  # noqa: E731
+    for nk in (False, True):
+        w = binding.TensorDesc(rows=512 if nk else 256, cols=256 if nk else 512, seed=0, dw=z(512, 256) if nk else z(256, 512))
+        for x, dy in ((z(128, 256), z(128, 1024)[:, :256]), (z(128, 1024)[:, :128], z(128, 512)), (z(128, 256), z(64, 512))):
+            with pytest.raises(binding.GwsError) as e:
+                binding.gws_linear_bwd_w(x, dy, w, 0, w_is_nk=nk)
+            assert e.value.status == 2
+            with pytest.raises(binding.GwsError) as e:
+                binding.gws_linear_bwd_w_ws(x, dy, w, 0, None, w_is_nk=nk)
+            assert e.value.status == 2
