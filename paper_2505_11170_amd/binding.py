@@ -727,10 +727,19 @@ def gws_gated_form(op: int, M: int, K: int, F: int, w_is_nk: bool = False, kept:
 
 def gws_gated_forms(op: int, M: int, K: int, F: int, w_is_nk: bool = False, kept: int = 0, lda: Optional[int] = None, ldw: Optional[int] = None) -> tuple:
     """``gws_gated_form`` of the first launch, the kernel of the second (0: there is none), and whether the launches share the rows rather than the columns."""
+    f = _gated_form(op, M, K, F, w_is_nk, kept, lda, ldw)
+    return (f & 0xFF, f >> 16 & 0xFF, f >> 8 & 0xFF), f >> 24 & 0xF, bool(f >> 28 & 1)
+
+
+def gws_gated_past_caches(op: int, M: int, K: int, F: int, w_is_nk: bool = False, kept: int = 0, lda: Optional[int] = None, ldw: Optional[int] = None) -> bool:
+    """Whether such a call stores its H past the caches."""
+    return bool(_gated_form(op, M, K, F, w_is_nk, kept, lda, ldw) >> 29 & 1)
+
+
+def _gated_form(op, M, K, F, w_is_nk, kept, lda, ldw) -> int:
     wide = op == GATED_BWD
-    f = int(load_library().gws_gated_form(op, M, K, F, (F if op == GATED_BWD_X else K) if lda is None else lda,
-                                          (F if w_is_nk == wide else K) if ldw is None else ldw, int(bool(w_is_nk)), kept))
-    return (f & 0xFF, f >> 16 & 0xFF, f >> 8 & 0xFF), f >> 24 & 0xF, bool(f >> 28)
+    return int(load_library().gws_gated_form(op, M, K, F, (F if op == GATED_BWD_X else K) if lda is None else lda,
+                                             (F if w_is_nk == wide else K) if ldw is None else ldw, int(bool(w_is_nk)), kept))
 
 
 def gws_linear_bwd_w_act8_workspace_bytes(w: TensorDesc, M: int, w_is_nk: bool = False) -> int:

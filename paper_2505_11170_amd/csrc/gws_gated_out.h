@@ -139,12 +139,11 @@ __device__ __forceinline__ void fwd_out_by(G gate, const GatedArgs& g, const f32
     own_lds_wait();
     if (KEPT == Kept::kE4m3) both_lds_wait();
     const uint32_t r0 = p0 + 64 * h;
-    // What is kept is wanted again a pass later: past the caches.  H mostly at once: so too only where it is too large for the caches to
-    // keep until then (64 MB).  8192 tokens, 2048 -> 5632 (92 MB), all ordinary, G and U streaming, all streaming: 337, 335, 319 us, with
-    // the product that follows 474, 462, 468; 4096 tokens, with that product, 277, 269, 273; 1024 tokens 97.1, 94.3, 94.1.
+    // What is kept is wanted again a pass later: past the caches.  H is read at once, by the product that follows: so too only where it is
+    // too large for the caches to keep until then (past_caches in gws_gated_api.hip).
     // (Two loops: of one with both stores the compiler makes ordinary ones.)
     uint8_t* const hp = (uint8_t*)(g.h + (size_t)r0 * g.ldh + q0);
-    if (g.stream_h) rows_out<NG, 2, EDGE, true>(hs, hp, (size_t)g.ldh * 2, lane, rows - 64 * h, cols);
+    if (g.past_caches) rows_out<NG, 2, EDGE, true>(hs, hp, (size_t)g.ldh * 2, lane, rows - 64 * h, cols);
     else rows_out<NG, 2, EDGE, false>(hs, hp, (size_t)g.ldh * 2, lane, rows - 64 * h, cols);
     if (KEPT == Kept::kBf16) {
       rows_out<NG, 2, EDGE, true>(ks, g.kept.g + ((size_t)r0 * g.kept.ldg + q0) * 2, (size_t)g.kept.ldg * 2, lane, rows - 64 * h, cols);

@@ -239,6 +239,19 @@ def test_gated_kernels_use_no_scratch():
     assert len(mine) > 80 and not [k[".name"] for k in mine if k[".private_segment_fixed_size"] != 0]
 
 
+def test_h_is_kept_in_the_caches_for_the_product_that_reads_it():
+    # by the time of the call and that product together: past the caches only where H outgrows them
+    ensure_built()
+    past = binding.gws_gated_past_caches
+    for kept in (0, 1, 2):
+        for M in (1, 1024, 4096, 8192, 12288, 15360):
+            assert not past(binding.GATED_FWD, M, 2048, 5632, True, kept)
+        for M in (16384, 32768):
+            assert past(binding.GATED_FWD, M, 2048, 5632, True, kept)
+    assert not past(binding.GATED_FWD, 16384, 768, 2048) and not past(binding.GATED_BWD_X, 32768, 2048, 5632)
+    assert not past(binding.GATED_FWD, 32768, 2048, 5600 + 16)                                      # refused
+
+
 def test_query_of_the_chosen_kernel():
     # a host function; without a device for 256 compute units
     ensure_built()

@@ -68,6 +68,15 @@ def test_input_gradient_of_two_launches(M, K, F, forms, nk):
     check_dx(M, K, F, nk, pad=8 * (M % 3))
 
 
+@pytest.mark.parametrize("kept", ["none", "bf16", "e4m3"])
+@pytest.mark.parametrize("M,K,F,form", [(16384, 64, 5632, SHARED), (46007, 64, 2016, SHARED), (16384, 512, 5632, LARGE), (12211, 1024, 7520, LARGE)])
+def test_forward_past_the_caches(M, K, F, form, kept):
+    nk = M % 2 == 0
+    assert gws.gws_gated_past_caches(gws.GATED_FWD, M, K, F, nk, KEPT[kept])
+    taken(form, gws.GATED_FWD, M, K, F, nk, KEPT[kept])
+    check_fwd(M, K, F, nk, M % 2, kept, pad=8 * (M % 3))
+
+
 def test_two_launches_in_place():
     # dG and dU in the places of the kept BF16 values: each launch reads and writes its own columns, or rows, alone
     for M, D, F, forms in BACKWARD_SPLIT[:2]:
