@@ -732,7 +732,7 @@ def gws_gated_forms(op: int, M: int, K: int, F: int, w_is_nk: bool = False, kept
 
 
 def gws_gated_past_caches(op: int, M: int, K: int, F: int, w_is_nk: bool = False, kept: int = 0, lda: Optional[int] = None, ldw: Optional[int] = None) -> bool:
-    """Whether such a call stores its H past the caches."""
+    """Whether the 128 x 128 and 256 x 256 tiles of such a call store H, or dG, dU and H, past the caches."""
     return bool(_gated_form(op, M, K, F, w_is_nk, kept, lda, ldw) >> 29 & 1)
 
 

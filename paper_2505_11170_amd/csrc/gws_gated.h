@@ -148,7 +148,7 @@ struct GatedArgs {
   uint32_t M, N, K, lda, ldb;
   uint32_t inv_band, inv_last;       // of the kernel's tile grid (TileGrid)
   int act;
-  bool past_caches;                  // forward: how H is stored
+  bool past_caches;                  // forward: H, backward: dL/dG, dL/dU and H; 128 and 256 tiles
   KeptArgs kept;
   uint16_t *h, *dg, *du;             // results: H; dL/dG and dL/dU; (input gradient: h)
   uint32_t ldh, ldd;

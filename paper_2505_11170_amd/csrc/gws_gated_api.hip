@@ -131,11 +131,17 @@ GatedPlan plan_whole(const GatedArgs& g, GatedOp op, bool b_oc, Kept kept) {
 }
 
 // Whether the results of a call are stored past the caches: by its time together with what reads them next, not by its own, which ordinary stores
-// always lengthen.
+// mostly lengthen.
 // Forward: H of 172 MB and more.  2048 -> 5632, G and U kept in 8 bits, ordinary and past the caches, us: 8192 tokens (H of 88 MB) alone 324, 307, with
 // the product that follows 457, 462; 12288 (132 MB) 474, 467 and 708, 719; 15360 (165 MB) 593, 578 and 856, 865; 16384 (176 MB) 617, 600 and 898, 886;
 // 32768 (352 MB) 1221, 1207 and 1777, 1759.  Nothing kept: 8192 298, 282 and 429, 433; 15360 537, 532 and 805, 808; 32768 1110, 1104 and 1665, 1661.
-bool stored_past_caches(GatedOp op, int64_t M, int64_t N) { return op == GatedOp::kFwd && (uint64_t)M * (uint64_t)N * 2 >= (uint64_t)172 << 20; }
+// Backward: dG, dU and H where the products that read them are bound by the matrix cores, D of 1024 and more.  The whole pass (this call, Wd's weight
+// gradient, dX, the two other weight gradients; kept in 8 bits), ordinary and past the caches, us: 2048 tokens, D 768, F 2048 82.8, 90.8; 4096 125, 137;
+// 8192 254, 262; 4096, 768, 2304 154, 157; 2048, 1024, 4096 152, 150; 8192, 1024, 4096 465, 458; 1024, 2048, 5632 205, 199; 2048, 2048, 5632 320, 314;
+// 8192, 2048, 5632 958, 960.  (D = 768 alone: 2048 tokens 19.5, 18.3, 4096 28.6, 27.8.)
+bool stored_past_caches(GatedOp op, int64_t M, int64_t N, int64_t K) {
+  return op == GatedOp::kFwd ? (uint64_t)M * (uint64_t)N * 2 >= (uint64_t)172 << 20 : op == GatedOp::kBwd && K >= 1024;
+}
 
 // Rows [m0, m0 + M) and columns [n0, n0 + N) of a call's result; n0 a multiple of 32.
 GatedArgs part_of(GatedArgs g, GatedOp op, bool b_oc, Kept kept, uint32_t m0, uint32_t M, uint32_t n0, uint32_t N) {
@@ -279,7 +285,7 @@ int gws_gated_fwd(const void* x, int64_t M, int64_t K, int64_t ldx, const void* 
   g.M = (uint32_t)M; g.N = (uint32_t)F; g.K = (uint32_t)K;
   g.lda = (uint32_t)ldx; g.ldb = (uint32_t)ldw;
   g.h = (uint16_t*)h; g.ldh = (uint32_t)ldh;
-  g.past_caches = stored_past_caches(GatedOp::kFwd, M, F);
+  g.past_caches = stored_past_caches(GatedOp::kFwd, M, F, K);
   return launch_gated(g, GatedOp::kFwd, !w_is_nk, form, (hipStream_t)stream);
 }
 
@@ -325,6 +331,7 @@ int gws_gated_bwd(const void* dy, int64_t M, int64_t D, int64_t lddy, const void
   g.a = (const uint16_t*)dy; g.b = (const uint16_t*)wd;
   g.K = (uint32_t)D;
   g.lda = (uint32_t)lddy; g.ldb = (uint32_t)ldw;
+  g.past_caches = stored_past_caches(GatedOp::kBwd, M, F, D);
   return launch_gated(g, GatedOp::kBwd, w_is_nk != 0, form, (hipStream_t)stream);   // contraction over D: [D x F] lies across it
 }
 
@@ -390,7 +397,7 @@ int gws_gated_form(int op, int64_t M, int64_t K, int64_t F, int64_t lda, int64_t
   const GatedOp o = op == GWS_GATED_FWD ? GatedOp::kFwd : op == GWS_GATED_BWD ? GatedOp::kBwd : GatedOp::kDx;
   const GatedSplit p = plan_gated(g, o, op == GWS_GATED_FWD ? !w_is_nk : w_is_nk != 0, o == GatedOp::kDx ? Kept::kNone : (Kept)kept);
   return (int)p.first.form | (p.first.form == GatedForm::kStream ? p.first.stream.mt << 16 | p.first.stream.nt << 8 : 0) |
-         (p.rows + p.cols ? (int)p.rest.form << 24 | (p.rows ? 1 << 28 : 0) : 0) | (stored_past_caches(o, g.M, g.N) ? 1 << 29 : 0);
+         (p.rows + p.cols ? (int)p.rest.form << 24 | (p.rows ? 1 << 28 : 0) : 0) | (stored_past_caches(o, g.M, g.N, g.K) ? 1 << 29 : 0);
 }
 
 }  // extern "C"

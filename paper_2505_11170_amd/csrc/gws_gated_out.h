@@ -215,7 +215,12 @@ struct KeptTile {
 
 // dL/dG, dL/dU and H of a wavefront's 16 NI x 16 NJ part from (p0, q0): dL/dH leaves the accumulators through LDS as fp32, 32 rows at
 // a time, and meets the kept G and U, which were requested before (the first 32 rows by the caller), 8 columns of a row a lane.
-template <Kept KEPT, bool EDGE, int NI, int NJ, class G>
+template <bool STREAM>
+__device__ __forceinline__ void store_out(const u32x4& v, GWS_GLOBAL uint8_t* to) {
+  if (STREAM) __builtin_nontemporal_store(v, (GWS_GLOBAL u32x4*)to);
+  else *(GWS_GLOBAL u32x4*)to = v;
+}
+template <bool STREAM, Kept KEPT, bool EDGE, int NI, int NJ, class G>
 __device__ __forceinline__ void bwd_out_by(G gate, const GatedArgs& g, const f32x4 (&acc)[NI][NJ], KeptTile<KEPT, EDGE, NI, NJ>& kept, float* cs, uint32_t p0,
                                            uint32_t q0, uint32_t lane) {
   constexpr int PF = 16 * NJ + 4;   // pitch of a staged row of fp32 (32 of them)
@@ -259,9 +264,9 @@ __device__ __forceinline__ void bwd_out_by(G gate, const GatedArgs& g, const f32
           oh[p] = pack_bf16_rne(a0 * u0, a1 * u1);
         }
         const uint32_t row0 = 32 * quarter + ROWS * it;
-        __builtin_nontemporal_store(odg, (GWS_GLOBAL u32x4*)(dgp + (size_t)row0 * g.ldd * 2 + d_off));
-        __builtin_nontemporal_store(odu, (GWS_GLOBAL u32x4*)(dup + (size_t)row0 * g.ldd * 2 + d_off));
-        if (g.h != nullptr) __builtin_nontemporal_store(oh, (GWS_GLOBAL u32x4*)(hp + (size_t)row0 * g.ldh * 2 + h_off));
+        store_out<STREAM>(odg, dgp + (size_t)row0 * g.ldd * 2 + d_off);
+        store_out<STREAM>(odu, dup + (size_t)row0 * g.ldd * 2 + d_off);
+        if (g.h != nullptr) store_out<STREAM>(oh, hp + (size_t)row0 * g.ldh * 2 + h_off);
       }
     }
     own_lds_wait();
@@ -276,7 +281,10 @@ __device__ __forceinline__ void fwd_out(const GatedArgs& g, const f32x4 (&acc)[N
 template <Kept KEPT, bool EDGE, int NI, int NJ>
 __device__ __forceinline__ void bwd_out(const GatedArgs& g, const f32x4 (&acc)[NI][NJ], KeptTile<KEPT, EDGE, NI, NJ>& kept, float* cs, uint32_t p0, uint32_t q0,
                                         uint32_t lane) {
-  with_gate(g.act, [&](auto gate) { bwd_out_by<KEPT, EDGE, NI, NJ>(gate, g, acc, kept, cs, p0, q0, lane); });
+  with_gate(g.act, [&](auto gate) {
+    if (g.past_caches) bwd_out_by<true, KEPT, EDGE, NI, NJ>(gate, g, acc, kept, cs, p0, q0, lane);   // uniform
+    else bwd_out_by<false, KEPT, EDGE, NI, NJ>(gate, g, acc, kept, cs, p0, q0, lane);
+  });
 }
 inline bool out_lds_ok(const GatedArgs& g) {
   const KeptArgs& k = g.kept;

@@ -252,6 +252,17 @@ def test_h_is_kept_in_the_caches_for_the_product_that_reads_it():
     assert not past(binding.GATED_FWD, 32768, 2048, 5600 + 16)                                      # refused
 
 
+def test_gradients_are_kept_in_the_caches_where_what_reads_them_waits_for_memory():
+    # by the time of the whole backward pass: past the caches where the products are bound by the matrix cores
+    ensure_built()
+    past = binding.gws_gated_past_caches
+    for kept in (1, 2):
+        for M, D, F in ((2048, 768, 2048), (4096, 768, 2048), (8192, 768, 2048), (16384, 768, 2048), (4096, 768, 2304)):
+            assert not past(binding.GATED_BWD, M, D, F, True, kept)
+        for M, D, F in ((2048, 1024, 4096), (8192, 1024, 4096), (1024, 2048, 5632), (4096, 2048, 5632), (8192, 2048, 5632)):
+            assert past(binding.GATED_BWD, M, D, F, True, kept)
+
+
 def test_query_of_the_chosen_kernel():
     # a host function; without a device for 256 compute units
     ensure_built()
