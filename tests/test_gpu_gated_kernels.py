@@ -68,6 +68,21 @@ def test_input_gradient_of_two_launches(M, K, F, forms, nk):
     check_dx(M, K, F, nk, pad=8 * (M % 3))
 
 
+# What check_dx runs: dG and dU are the halves of one buffer, and rows that start off the lines of 128 bytes count in the choice.
+# M, K, F, w_is_nk or None for either, (kernel of the first launch, of the second, whether they share the rows)
+GRADIENT_AS_RUN = [(849, 1184, 544, None, (MIDDLE, 0, False)), (584, 1696, 544, None, ((STREAM, 8, 4), 0, False)), (2061, 480, 96, None, (MIDDLE, 0, False)),
+                   (3848, 1056, 608, None, (MIDDLE, 2, False)), (3943, 1056, 608, None, (MIDDLE, 2, False)), (4604, 928, 608, None, (MIDDLE, 2, False)),
+                   (2478, 1632, 672, True, (MIDDLE, 2, False)), (2208, 1888, 672, False, (MIDDLE, 2, False)), (2208, 1888, 672, True, (MIDDLE, 0, False)),
+                   (2692, 1536, 608, None, (MIDDLE, 2, True)), (3343, 1248, 608, None, (MIDDLE, 2, True)), (2051, 2016, 672, None, (MIDDLE, 2, True))]
+
+
+@pytest.mark.parametrize("M,K,F,nk,forms", [(M, K, F, nk, forms) for M, K, F, one, forms in GRADIENT_AS_RUN for nk in ([False, True] if one is None else [one])])
+def test_input_gradient_as_it_is_run(M, K, F, nk, forms):
+    pad = 8 * (M % 3)
+    assert gws.gws_gated_forms(gws.GATED_BWD_X, M, K, F, nk, lda=2 * F + pad, ldw=(K if nk else F) + pad) == forms
+    check_dx(M, K, F, nk, pad=pad)
+
+
 @pytest.mark.parametrize("kept", ["none", "bf16", "e4m3"])
 @pytest.mark.parametrize("M,K,F,form", [(16384, 64, 5632, SHARED), (46007, 64, 2016, SHARED), (16384, 512, 5632, LARGE), (12211, 1024, 7520, LARGE)])
 def test_forward_past_the_caches(M, K, F, form, kept):
