@@ -83,6 +83,37 @@ def test_input_gradient_as_it_is_run(M, K, F, nk, forms):
     check_dx(M, K, F, nk, pad=pad)
 
 
+@pytest.mark.parametrize("nk", [False, True])
+@pytest.mark.parametrize("M,K,F", [(8192, 2048, 64), (8192, 2048, 96), (6007, 2016, 160), (8190, 2048, 224), (8192, 2048, 288), (8191, 2048, 352), (8192, 2016, 416)])
+def test_input_gradient_of_few_steps_in_large_tiles(M, K, F, nk):
+    # the first product's half step of 64 in each place of the ring of K-steps, inside the unrolled six and behind them
+    pad = 8 * (M % 3)
+    assert gws.gws_gated_forms(gws.GATED_BWD_X, M, K, F, nk, lda=2 * F + pad, ldw=(K if nk else F) + pad) == (LARGE, 0, False)
+    check_dx(M, K, F, nk, pad=pad)
+
+
+@pytest.mark.parametrize("kept", ["bf16", "e4m3"])
+@pytest.mark.parametrize("M,K,F,form", [(7, 96, 96, STREAM), (128, 256, 5632, STREAM), (700, 736, 2080, MIDDLE), (1300, 96, 5024, SHARED), (2091, 736, 1952, LARGE),
+                                        (8192, 2048, 5632, LARGE), (2217, 1152, 3808, LARGE)])
+def test_every_call_gives_the_same_bits(M, K, F, form, kept):
+    # the forward call repeated, another one between, without a wait: what is kept (in 8 bits: codes that a last bit of a sum decides among them) and H
+    f = gws.gws_gated_form(gws.GATED_FWD, M, K, F, True, KEPT[kept])
+    assert f == form or f[0] == form
+    gen = torch.Generator(device=DEV).manual_seed(M)
+    def some(r, c, std):
+        return (torch.randn(r, c, device=DEV, generator=gen) * std).bfloat16()
+    x, other, wg, wu = some(M, K, 1.0), some(M, K, 1.0), some(F, K, 0.02), some(F, K, 0.02)
+    h = torch.zeros(M, F, dtype=torch.bfloat16, device=DEV)
+    saved, _ = kept_buffers(kept, M, F)
+    outs = [h] + ([saved.g, saved.u] if kept == "bf16" else [saved.g8.codes, saved.g8.xscale, saved.u8.codes, saved.u8.xscale])
+    gws.gws_gated_fwd(x, wg, wu, h, saved=saved, w_is_nk=True)
+    want = [t.clone() for t in outs]
+    for _ in range(4):
+        for v in (other, x, other, x):
+            gws.gws_gated_fwd(v, wg, wu, h, saved=saved, w_is_nk=True)
+        assert all(torch.equal(a, b) for a, b in zip(outs, want))
+
+
 @pytest.mark.parametrize("kept", ["none", "bf16", "e4m3"])
 @pytest.mark.parametrize("M,K,F,form", [(16384, 64, 5632, SHARED), (46007, 64, 2016, SHARED), (16384, 512, 5632, LARGE), (12211, 1024, 7520, LARGE)])
 def test_forward_past_the_caches(M, K, F, form, kept):
