@@ -1,6 +1,6 @@
 // The gated feed-forward block for any sizes (gfx950): the products of gws_gated_fwd, gws_gated_bwd and gws_gated_bwd_x by one
 // small tile that reads its operands straight into the MFMA's registers.  Right for every size the entry points take, and there for
-// those that the other kernels do not take (K = 32, leading dimensions of 2^23 elements and more).  Bound by those reads, 16 rows of 64 bytes
+// those that the other kernels do not take (K = 32, leading dimensions of 2^24 elements and more, of results 2^28).  Bound by those reads, 16 rows of 64 bytes
 // an instruction: 1021 x 768 -> 2048 forward 84 us (11.2 in 128 x 128 tiles).
 #include "gws_gated.h"
 #include "gws_gemm256_core.h"
