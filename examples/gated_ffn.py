@@ -31,6 +31,10 @@ class GatedFFN:
     """Weights stored [out x in] (w_is_nk), and the buffers that a step fills: allocated once, as they do not move between steps."""
 
     def __init__(self, tokens, width, block, seed=0):
+        # the weight gradients take tokens by 64 and weights by 256 x 256 (0: refused); gate and up have one shape, down its transpose
+        need = gws.gws_linear_bwd_w_act8_workspace_bytes(gws.TensorDesc(rows=block, cols=width, seed=0), tokens, w_is_nk=True)
+        if need == 0:
+            raise ValueError(f"the weight gradients take a multiple of 64 tokens and widths of multiples of 256, not {tokens} tokens, {width} -> {block}")
         gen = torch.Generator(device=DEV).manual_seed(seed)
         self.M, self.K, self.F = tokens, width, block
         self.master, self.desc = {}, {}
@@ -45,7 +49,6 @@ class GatedFFN:
         self.x8 = act8(M, K)
         self.saved = gws.GatedSaved(g8=act8(M, F), u8=act8(M, F))
         self.h, self.y, self.dx, self.dg, self.du = bf16(M, F), bf16(M, K), bf16(M, K), bf16(M, F), bf16(M, F)
-        need = max(gws.gws_linear_bwd_w_act8_workspace_bytes(self.desc["gate"], M, w_is_nk=True), 2 * M * K)
         self.workspace = torch.empty(need, dtype=torch.uint8, device=DEV)
 
     def sample(self, step):

@@ -302,7 +302,9 @@ int gws_gemm_bf16_sample_next_n(const void* x, int64_t M, int64_t K, int64_t ldx
  * a is SiLU, a(z) = z / (1 + exp(-z)), or GELU in its tanh form, a(z) = z (1 + tanh(sqrt(2/pi) (z + 0.044715 z^3))) / 2.
  * The sums of the products and the arithmetic of the gate are fp32; each output is rounded once.
  * K and F (and D) must be multiples of 32, leading dimensions multiples of 8, BF16 buffers 16-byte aligned.  M is any number of
- * tokens; M == 0 writes nothing.  Rows of X and of the gradients do not meet: a row of NaN leaves the others as they are.          */
+ * tokens; M == 0 writes nothing.  Rows of X and of the gradients do not meet: a row of NaN leaves the others as they are.
+ * The weight gradients that complete a training step, gws_linear_bwd_w, _ws and _act8, take a multiple of 64 tokens, and weights whose rows and
+ * columns are multiples of 256: other numbers of tokens train in buffers of the next multiple, with zeros in the last rows of X and dY.       */
 #define GWS_ACT_SILU 0
 #define GWS_ACT_GELU_TANH 1
 
@@ -356,7 +358,7 @@ int gws_gated_bwd_x(const void* dg, const void* du, int64_t M, int64_t F, int64_
  * `workspace` (256-byte aligned, owned by the caller, contents undefined afterwards, apart from every other buffer of the call), what is left
  * of it serves as gws_linear_bwd_w_ws's.  Everything else is as there.
  *   gws_linear_bwd_w_act8_workspace_bytes: the bytes it can use; the first 2 M K of them, rounded up to 256, it needs (else GWS_ERR_SHAPE).
- *   0 for sizes that the call refuses.  Host function, no GPU work.                                                               */
+ *   0 for sizes that the call refuses (M no multiple of 64, rows or columns no multiple of 256).  Host function, no GPU work.          */
 size_t gws_linear_bwd_w_act8_workspace_bytes(const gws_tensor* w, int w_is_nk, int64_t M);
 int gws_linear_bwd_w_act8(const gws_act8* x, const void* dy, int64_t M, int64_t ldy, const gws_tensor* w, int w_is_nk, uint64_t step,
                           void* workspace, size_t workspace_bytes, void* stream);

@@ -210,6 +210,20 @@ def test_python_types_and_strides():
     binding._check_plain(torch.zeros(4, 8, dtype=torch.bfloat16)[:, ::8])                           # one column has no next
 
 
+def test_the_example_refuses_what_its_weight_gradients_do():
+    # before any buffer is made, not in the first backward pass
+    import importlib.util
+    import os
+    path = os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "examples", "gated_ffn.py")
+    spec = importlib.util.spec_from_file_location("gated_ffn_sizes", path)
+    example = importlib.util.module_from_spec(spec)
+    spec.loader.exec_module(example)
+    ensure_built()
+    for tokens, width, block in ((1021, 256, 512), (0, 256, 512), (1024, 320, 512), (1024, 256, 544)):
+        with pytest.raises(ValueError, match="multiple of 64 tokens"):
+            example.GatedFFN(tokens, width, block)
+
+
 def test_definition_of_the_8_bit_form():
     # the reference that the GPU tests compare with, against torch's own casts where it has them
     gen = torch.Generator().manual_seed(1)
