@@ -134,6 +134,17 @@ def test_weight_gradient(lib):
     assert lib.gws_linear_bwd_w_act8(None, at(50), 128, 512, desc(), 0, 0, at(60), MB, None) == NULL
 
 
+def test_workspace_of_sizes_that_the_weight_gradient_refuses(lib):
+    def desc(rows, cols):
+        return ctypes.byref(_CTensor(dw=at(40), rows=rows, cols=cols, ld=cols, seed=1))
+
+    assert lib.gws_linear_bwd_w_act8_workspace_bytes(desc(256, 512), 0, 2 ** 31 - 64) >= (2 ** 31 - 64) * 256 * 2
+    for M, rows, cols in ((2 ** 31, 256, 512), (2 ** 40, 256, 512), (64, 2 ** 31, 256), (64, 256, 2 ** 31)):
+        a = act8(ldc=rows, lds=rows // 32)
+        assert lib.gws_linear_bwd_w_act8(ctypes.byref(a), at(50), M, cols, desc(rows, cols), 0, 0, at(60), MB, None) == SHAPE
+        assert lib.gws_linear_bwd_w_act8_workspace_bytes(desc(rows, cols), 0, M) == 0
+
+
 def test_python_shapes():
     z = lambda *s, d=torch.bfloat16: torch.zeros(*s, dtype=d)  # noqa: E731
     a = Act8(z(4, 64, d=torch.uint8), z(4, 2, d=torch.uint8))
