@@ -105,7 +105,7 @@ int gws_box_muller_check(uint64_t first, uint64_t n, void* out, void* stream);
  * kept form (0 none, 1 BF16, 2 in 8 bits; gws_gated_bwd_x: 0): GWS_GATED_*, of GWS_GATED_STREAM with the tile's rows / 16 in bits 16.. and
  * its columns / 16, of both weights together, in bits 8 .. 15.  Where the call takes two launches, the kernel of the first columns in the low
  * bits and the one of the others in bits 24 .. 27 (bit 28: the first and the other rows).  Bit 29: the call's tiles (not
- * those of GWS_GATED_ANY and GWS_GATED_STREAM) store H, or dG, dU and H, past the caches.  lda: of X, dY, dG.  0 for what the call refuses.  Host function.                                                                                                                                  */
+ * those of GWS_GATED_ANY and GWS_GATED_STREAM) store H, or dG, dU and H, past the caches.  lda: of X, dY, dG.  0 for what the call refuses.  Host function.                                       */
 #define GWS_GATED_FWD 0
 #define GWS_GATED_BWD 1
 #define GWS_GATED_BWD_X 2

@@ -3,10 +3,11 @@
 // The way out is in gws_gated_out.h.
 // What bounds them: the matrix cores at the card's power limit while the loop runs, and then, with one wavefront a SIMD, the way out by itself.
 //   input gradient: no way out to speak of, 8192 x 2 x 5632 -> 2048 in 263 - 278 us, 1.36 - 1.44 PFLOP/s (a large library product 1.35).
-//   forward, 8192 x 2048 -> 5632 (two products of 167 - 173 us each without a gate): 269 - 280 us; the vector ALU takes 3 us a tile more for keeping
-//   G and U (5.5 tiles a compute unit), and their bytes leave in bursts: 294 - 304 as BF16, 297 - 319 in 8 bits.
+//   forward, 8192 x 2048 -> 5632 (two products of 167 - 173 us each without a gate): 287 - 298 us; the vector ALU takes 3 us a tile more for keeping
+//   G and U (5.5 tiles a compute unit), and their bytes leave in bursts: 309 - 317 as BF16, 318 - 324 in 8 bits.  (With H past the caches 277 - 282,
+//   304 - 312 and 307, at the cost of the product that reads it.)
 //   backward of the same: 135 us of products, and 2.75 times all compute units at once ask for 134 MB: without the stores 171 us, without the
-//   kept values 175, without the gate's arithmetic 200, with everything 196 - 206 (bf16 205 - 215).
+//   kept values 175, without the gate's arithmetic 200, with everything 196 - 206 (bf16 205 - 216).
 // Less does not help where it was tried: three quarters of the kept values on their way instead of two (0.5 %, and registers to scratch), and
 // two smaller tiles a compute unit, whose ways out fall under each other's loops but whose loops wait for the L2 (265 us).
 #include "gws_gated_out.h"

@@ -77,12 +77,12 @@ void kept_buffers(const KeptArgs& k, Kept form, int64_t M, int64_t F, bool writt
 // The kernel by the sizes: the fastest by estimates in us, each a launch and, per round of workgroups, what a tile takes beside its K-steps,
 // the gate and the kept values among it, and the K-steps of 64, which take longer the more compute units are at work (busy).  Of 100 drawn
 // sizes of more than 256 tiles of 128 x 128 the choice takes at worst 1.09 of the fastest single launch's time, in the mean, two launches
-// included, 0.99.  Measured with the sums in 256 x 256 tiles, in 128 x 128, and in those two workgroups a compute unit:
-//   forward, nothing kept: 1021 x 768 -> 2048 20.8, 10.2, 11.9; 2048 x 2048 -> 5632 85, 94, 79; 8192 x 2048 -> 5632 271, 396, 345
-//   forward, 8 bits kept: 8192 x 2048 -> 5632 297, 443, 384; BF16 kept: 4096 x 768 -> 2048 28.7, 33.5, 28.9
-//   backward, BF16 kept: 1021 x 768 -> 2048 34.6, 14.9, 16.7 (8 x 4 of the streaming kernel: 12.5); 3000 x 1024 -> 4096 47, 52, 51
-//   backward, 8 bits kept: 8192 x 2048 -> 5632 196, 257, 223
-//   input gradient (no third form): 5000 x 2 x 1280 -> 640 51, 21.9; 2048 x 2 x 5632 -> 2048 213, 102; 8192 x 2 x 5632 -> 2048 262, 386
+// included, 0.99; of 40 backward passes with D under 1024 1.12 and 1.02, of 24 forward passes with H of 64 to 172 MB 1.04 and 0.99.  Measured with the sums in 256 x 256 tiles, in 128 x 128, and in those two workgroups a compute unit:
+//   forward, nothing kept: 1021 x 768 -> 2048 20.6, 10.0, 11.7; 2048 x 2048 -> 5632 87, 99, 84; 8192 x 2048 -> 5632 289, 424, 359
+//   forward, 8 bits kept: 8192 x 2048 -> 5632 320, 478, 402; BF16 kept: 4096 x 768 -> 2048 31.2, 36.4, 31.4
+//   backward, BF16 kept: 1021 x 768 -> 2048 35.5, 16.2, 17.7 (8 x 4 of the streaming kernel: 13.1); 3000 x 1024 -> 4096 51, 57, 55
+//   backward, 8 bits kept: 4096 x 768 -> 2048 38.8, 35.0, 27.8; 8192 x 2048 -> 5632 201, 261, 227
+//   input gradient (no third form): 5000 x 2 x 1280 -> 640 51, 22.7; 2048 x 2 x 5632 -> 2048 197, 102; 8192 x 2 x 5632 -> 2048 266, 387
 enum class GatedForm { kAny = GWS_GATED_ANY, kStream = GWS_GATED_STREAM, kMiddle = GWS_GATED_MIDDLE, kLarge = GWS_GATED_LARGE, kShared = GWS_GATED_SHARED };
 struct GatedPlan {
   GatedForm form;

@@ -59,7 +59,7 @@ __device__ __forceinline__ void rows_out(const uint8_t* cs, uint8_t* to, size_t 
 // (acc[i][j] with j < NG is G, acc[i][j + NG] U), and the four lanes of a block of 32 that is kept in 8 bits meet in two cross-lane
 // steps.  Everything leaves through LDS by rows, 64 rows at a time; codes, of which a wavefront's columns are half a line or less, by the two
 // wavefronts that share the rows (`odd`: this is the one with the later columns; first: the other's cs) together, G's by the one and U's by the
-// other (8192 tokens, 2048 -> 5632: 323 -> 319 us; in 128 x 128 tiles 1021 x 768 -> 2048 12.8 -> 12.2).
+// other (8192 tokens, 2048 -> 5632: 1 % of 320 us; in 128 x 128 tiles 1021 x 768 -> 2048 12.8 -> 12.2).
 template <Kept KEPT, bool EDGE, int NI, int NG, class G>
 __device__ __forceinline__ void fwd_out_by(G gate, const GatedArgs& g, const f32x4 (&acc)[NI][2 * NG], uint8_t* cs, uint8_t* first, bool odd, uint32_t p0,
                                         uint32_t q0, uint32_t lane) {
