@@ -444,19 +444,21 @@ def gws_linear_fwd_static(x, w: TensorDesc, y, fmt: int, step: int, w_is_nk: boo
                                    _p(y), int(y.stride(0)), _stream(stream)), "gws_linear_fwd_static")
 
 
-def _check_tokens(x, dy, w: TensorDesc, w_is_nk: bool, what: str) -> None:
-    """X and dY hold what the weight's sizes make the kernel read: the call sees leading dimensions alone, which columns of a wider buffer have too."""
+def _token_fields(x, dy, w: TensorDesc, w_is_nk: bool, what: str):
+    """Tokens and leading dimensions of X and dY, whose rows (of one dimension or more) hold what the weight's sizes make the kernel read: the call sees
+    leading dimensions alone, which columns of a wider buffer have too."""
+    M, m = x.shape[0], dy.shape[0]
     K, N = (w.cols, w.rows) if w_is_nk else (w.rows, w.cols)
-    if x.shape[-1] < K or dy.shape[-1] < N or dy.shape[0] < x.shape[0]:
+    if m < M or x.numel() < M * K or dy.numel() < m * N:
         raise GwsError(2, what)
+    return M, x.stride()[0], dy.stride()[0]
 
 
 def gws_linear_bwd_w(x, dy, w: TensorDesc, step: int, w_is_nk: bool = False, stream=None) -> None:
     """dW = X^T dY into ``w.dw`` and, when ``w.dbt`` is given, dL/db_t (paper Eq. 4) from the GEMM's epilogue."""
-    L = load_library()
-    _check_tokens(x, dy, w, w_is_nk, "gws_linear_bwd_w")
-    _check(L.gws_linear_bwd_w(_p(x), _p(dy), int(x.shape[0]), int(x.stride(0)), int(dy.stride(0)), _marshal([w]),
-                              int(bool(w_is_nk)), int(step), _stream(stream)), "gws_linear_bwd_w")
+    L = _lib or load_library()
+    _check(L.gws_linear_bwd_w(_p(x), _p(dy), *_token_fields(x, dy, w, w_is_nk, "gws_linear_bwd_w"), _marshal([w]),
+                              1 if w_is_nk else 0, int(step), _stream(stream)), "gws_linear_bwd_w")
 
 
 def gws_linear_bwd_w_workspace_bytes(w: TensorDesc, M: int) -> int:
@@ -467,11 +469,10 @@ def gws_linear_bwd_w_workspace_bytes(w: TensorDesc, M: int) -> int:
 
 def gws_linear_bwd_w_ws(x, dy, w: TensorDesc, step: int, workspace, w_is_nk: bool = False, stream=None) -> None:
     """``gws_linear_bwd_w`` with the tokens split into parts through ``workspace`` (a device tensor, or None)."""
-    L = load_library()
-    _check_tokens(x, dy, w, w_is_nk, "gws_linear_bwd_w_ws")
+    L = _lib or load_library()
     nbytes = 0 if workspace is None else int(workspace.numel() * workspace.element_size())
-    _check(L.gws_linear_bwd_w_ws(_p(x), _p(dy), int(x.shape[0]), int(x.stride(0)), int(dy.stride(0)), _marshal([w]),
-                                 int(bool(w_is_nk)), int(step), _p(workspace), nbytes, _stream(stream)), "gws_linear_bwd_w_ws")
+    _check(L.gws_linear_bwd_w_ws(_p(x), _p(dy), *_token_fields(x, dy, w, w_is_nk, "gws_linear_bwd_w_ws"), _marshal([w]),
+                                 1 if w_is_nk else 0, int(step), _p(workspace), nbytes, _stream(stream)), "gws_linear_bwd_w_ws")
 
 
 def gws_gemm_bf16(x, w, y, w_is_nk: bool = False, stream=None) -> None:

@@ -267,3 +267,5 @@ def test_weight_gradients_refuse_tokens_narrower_than_the_weight():
             with pytest.raises(binding.GwsError) as e:
                 binding.gws_linear_bwd_w_ws(x, dy, w, 0, None, w_is_nk=nk)
             assert e.value.status == 2
+        # rows of more than one dimension, more columns and more rows are what they were
+        assert binding._token_fields(z(128, 4, 64), z(192, 1024)[:, :768], w, nk, "") == (128, 256, 1024)
