@@ -54,7 +54,7 @@ typedef enum gws_status {
   GWS_ERR_SHAPE = 2,  /* negative size, ld < cols, ld % 8 != 0, size >= 2^31,
                          row0/col0 not a multiple of 32, n < 0                   */
   GWS_ERR_ALIGN = 3,  /* BF16 pointer not 16-byte aligned, fp32 pointer not 4-byte */
-  GWS_ERR_FORMAT = 4, /* unknown gws_format, activation or form of kept values   */
+  GWS_ERR_FORMAT = 4, /* unknown gws_format, activation, norm or form of kept values or states */
   GWS_ERR_LAUNCH = 5, /* the HIP runtime refused a kernel launch                 */
   GWS_ERR_ALIAS = 6,  /* an output overlaps an input it must not overlap         */
   GWS_ERR_TOO_LARGE = 7 /* the operand exceeds a fixed capacity of the library (gws_linear_fwd_static) */
@@ -362,6 +362,110 @@ int gws_gated_bwd_x(const void* dg, const void* du, int64_t M, int64_t F, int64_
 size_t gws_linear_bwd_w_act8_workspace_bytes(const gws_tensor* w, int w_is_nk, int64_t M);
 int gws_linear_bwd_w_act8(const gws_act8* x, const void* dy, int64_t M, int64_t ldy, const gws_tensor* w, int w_is_nk, uint64_t step,
                           void* workspace, size_t workspace_bytes, void* stream);
+
+/* ---- The norms beside the linears ----
+ * For a row x of X [M x C] (any C >= 1):
+ *   GWS_NORM_LAYER  mean = sum(x) / C, rstd = 1 / sqrt(sum((x - mean)^2) / C + eps), n = (x - mean) rstd, y = n .* gamma + beta
+ *   GWS_NORM_RMS    rstd = 1 / sqrt(sum(x^2) / C + eps),                             n = x rstd,          y = n .* gamma + beta
+ * X, Y and the gradients are BF16 (leading dimensions multiples of 8, 16-byte aligned), everything else fp32 (4-byte aligned): gamma and beta
+ * [C], NULL for ones and zeros; mean and rstd [M].  Sums and arithmetic are fp32 (the squares are those of x - mean, so a large common offset costs
+ * nothing), each output is rounded once.  Rows do not meet: a row of NaN leaves the others as they are.  Values past column C are neither read nor written.
+ * A row's result does not depend on the other rows, their number included, except in its last bits through the order of the sums.  M == 0 writes nothing (dgamma and dbeta become zeros). */
+#define GWS_NORM_LAYER 0
+#define GWS_NORM_RMS 1
+
+/* Forward.  eps > 0 and finite.  mean and rstd receive what the backward pass needs: GWS_NORM_LAYER both or neither (NULL: inference),
+ * GWS_NORM_RMS rstd or nothing (mean NULL).  y may lie on x (same address and leading dimension), else no output overlaps an input or another output. */
+int gws_norm_fwd(const void* x, int64_t M, int64_t C, int64_t ldx, int kind, const float* gamma, const float* beta, float eps,
+                 void* y, int64_t ldy, float* mean, float* rstd, void* stream);
+
+/* Backward: with t = dY .* gamma,
+ *   dX = rstd (t - sum(t) / C - n sum(t .* n) / C) + R   (GWS_NORM_RMS without sum(t); R: a gradient that comes past the norm, as of a residual stream;
+ *                                                         NULL: none),
+ *   dgamma = sum of dY .* n over the rows, dbeta = sum of dY (each NULL: not wanted; they are written, not added to).
+ * dX may lie on dY, X or R (same address and leading dimension), else no output overlaps an input or another output.
+ * With dgamma, dbeta or rows of more than 16384 columns the call needs `workspace` (16-byte aligned, apart from every other buffer, contents undefined
+ * afterwards) of gws_norm_bwd_workspace_bytes(M, C) bytes (GWS_ERR_NULL / GWS_ERR_SHAPE without): the sums of rows that meet there are added in one order,
+ * so every call gives the same bits. */
+size_t gws_norm_bwd_workspace_bytes(int64_t M, int64_t C);
+int gws_norm_bwd(const void* dy, int64_t lddy, const void* x, int64_t M, int64_t C, int64_t ldx, int kind, const float* gamma, const float* mean,
+                 const float* rstd, const void* residual, int64_t ldr, void* dx, int64_t lddx, float* dgamma, float* dbeta, void* workspace,
+                 size_t workspace_bytes, void* stream);
+
+/* ---- The dense layer: a product with bias, activation and residual on its way out ----
+ *   Z = X * W + b,  Y = a(Z) + R
+ * for M tokens, X [M x K], W [K x N] (N x K when w_is_nk) as in gws_gemm_bf16, b fp32 [N] (NULL: zeros), a one of GWS_ACT_SILU, GWS_ACT_GELU_TANH (as in
+ * gws_gated_fwd) and GWS_ACT_NONE, R BF16 [M x N] (NULL: none).  z [M x N] receives Z for the backward pass (NULL: it is not kept).  The sum, the bias,
+ * the activation and the residual are fp32; Y and Z are rounded once each.  K and N must be multiples of 32, leading dimensions multiples of 8, BF16
+ * buffers 16-byte aligned, b 4-byte.  M == 0 writes nothing.  y may lie on the residual (same address and leading dimension), else no output overlaps an
+ * input or another output.  With neither b, a, R nor z this is gws_gemm_bf16, bit for bit.                                                           */
+#define GWS_ACT_NONE 2
+typedef struct gws_epilogue {
+  const float* bias;
+  int act;
+  const void* residual;
+  int64_t ldr;
+  void* z;
+  int64_t ldz;
+} gws_epilogue;
+int gws_dense_fwd(const void* x, int64_t M, int64_t K, int64_t ldx, const void* w, int64_t N, int64_t ldw, int w_is_nk, void* y, int64_t ldy,
+                  const gws_epilogue* e, void* stream);
+
+/* Backward through the product that follows and the activation, in one pass over the sums: with dY [M x D] the gradient of Y = a(Z) * Wd (Wd stored
+ * [F x D] or, when w_is_nk, [D x F], as that product's forward call takes it), dH = dY * Wd^T kept in fp32,
+ *   dZ = dH .* a'(Z),   H = a(Z) again where h is not NULL (the input of Wd's weight gradient),   dbias = sum of dZ over the tokens where it is not NULL
+ * from the kept Z [M x F].  dbias (fp32 [F]) sums the fp32 dZ, in an order that is the same in every call of the same sizes; it needs `workspace` (16-byte
+ * aligned, apart from every other buffer, contents undefined afterwards) of gws_dense_bwd_workspace_bytes(M, F) bytes (GWS_ERR_NULL / GWS_ERR_SHAPE without).
+ * dZ or H may lie on Z (same address and leading dimension), else no output overlaps an input or another output.  With GWS_ACT_NONE and without h, z may be
+ * NULL.  D and F must be multiples of 32.  M == 0: dbias becomes zeros.
+ * (The other gradients: dX = dZ * W^T is gws_gemm_bf16, dW = X^T * dZ gws_linear_bwd_w, R's gradient is dY itself.)                                  */
+size_t gws_dense_bwd_workspace_bytes(int64_t M, int64_t F);
+int gws_dense_bwd(const void* dy, int64_t M, int64_t D, int64_t lddy, const void* wd, int64_t F, int64_t ldw, int w_is_nk, int act, const void* z,
+                  int64_t ldz, void* dz, int64_t lddz, void* h, int64_t ldh, float* dbias, void* workspace, size_t workspace_bytes, void* stream);
+
+/* The same from a given dH (BF16 [M x F], F a multiple of 8): a pass over memory.  An output may also lie on dH.  With GWS_ACT_NONE dz
+ * may be NULL too: the call is then dbias = sum of dH over the tokens, the bias gradient of a layer without activation.                                                           */
+int gws_dense_bwd_h(const void* dh, int64_t M, int64_t F, int64_t lddh, int act, const void* z, int64_t ldz, void* dz, int64_t lddz, void* h,
+                    int64_t ldh, float* dbias, void* workspace, size_t workspace_bytes, void* stream);
+
+/* ---- The update at the end of a step: AdamW over many tensors, and the norm of their gradients ----
+ * Step t (1, 2, ...) for every element, with s = *grad_scale (NULL: 1), c1 = 1 - beta1^t, c2 = 1 - beta2^t, in fp32, in the order written, without fused
+ * multiply-adds but in the division:
+ *   g' = g s;  m = beta1 m + (1 - beta1) g';  v = beta2 v + (1 - beta2) (g' g');  r = sqrt(v)
+ *   p = p (1 - lr wd) - ((lr / c1) m) / (r / sqrt(c2) + eps);   w = p rounded to BF16
+ * (lr = the call's times the tensor's lr_scale; what is in brackets and powers of the settings is formed in fp64 and rounded once).  A tensor [rows x cols] has one
+ * leading dimension ld (cols <= ld, a multiple of 8; a vector is one row) for p, g, w, and for m and v or their codes; 16-byte aligned (codes 8-byte).
+ * The states m and v are fp32 (m, v set, m8.codes and v8.codes NULL), or m and r are held in 8 bits (m and v NULL; m8 and v8 set, ldc = ld, one lds):
+ * the form of gws_act8, so gws_act8_decode reads it, but rounded at random and under X = the smallest power of two from 2^-117 to 2^119 for which the
+ * largest magnitude is at most 448 X.  A value v = u X with |u| between neighbouring E4M3 values goes to either with the probability of its place between them (in
+ * steps of 2^-16), so that the mean over many steps is right also where one step changes less than a spacing; a positive r never becomes 0.  The random
+ * bits are a function of (seed, step, row, column) alone: word c % 4 of Philox4x32-10(counter = (c / 4, row, step_lo, step_hi ^ 0x47414457), key = seed) for column c,
+ * low half for m, high half for r.  Buffers of zeros are states at the start.  A NaN or infinity among 32 values makes all of them NaN (fp32 states: itself alone).
+ * Where *grad_scale is not finite nothing is written: a step with an overflowed gradient norm leaves the model as it was.
+ * No buffer of a tensor may overlap another one of the call, its gradient included (checked within a tensor).  *grad_scale lies apart from all outputs.  Empty tensors are skipped. */
+typedef struct gws_adamw_tensor {
+  float* p;            /* device, the parameter                                     */
+  void* w;             /* device BF16, its copy; NULL: not wanted                   */
+  const void* g;       /* device, gradient                                          */
+  int g_is_fp32;       /* else BF16                                                 */
+  float *m, *v;        /* device, states in 32 bits                                 */
+  gws_act8 m8, v8;     /* or in 8                                                   */
+  int64_t rows, cols, ld;
+  float lr_scale, weight_decay;
+  uint64_t seed;       /* of the rounding of states in 8 bits                       */
+} gws_adamw_tensor;
+typedef struct gws_adamw_settings {
+  double lr, beta1, beta2, eps;   /* finite; 0 <= beta < 1, eps > 0                           */
+  uint64_t step;                  /* t >= 1                                                   */
+  const float* grad_scale;        /* device, 4-byte aligned; NULL: 1                          */
+} gws_adamw_settings;
+int gws_adamw(const gws_adamw_tensor* t, int n, const gws_adamw_settings* a, void* stream);
+
+/* out[0] = the 2-norm of the gradients of all n tensors (fields g, g_is_fp32, rows, cols, ld; summed in fp64 in one order), out[1] = max_norm / out[0] where that
+ * is less than 1, else 1 (max_norm <= 0: always 1); both NaN where a gradient is not finite.  out is device fp32 [2], out + 1 what gws_adamw takes as grad_scale.
+ * n = 0: 0 and 1.  workspace: device, 16-byte aligned, gws_grad_norm_workspace_bytes(t, n) bytes, apart from gradients and out, contents undefined afterwards. */
+size_t gws_grad_norm_workspace_bytes(const gws_adamw_tensor* t, int n);
+int gws_grad_norm(const gws_adamw_tensor* t, int n, double max_norm, float* out, void* workspace, size_t workspace_bytes, void* stream);
 
 /* The comparison systems of the paper's Sec. 4 behind the same interface: the same forward and
  * backward passes with R drawn from another noise basis.  The paper compares GaussWS with the same

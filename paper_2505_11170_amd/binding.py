@@ -18,7 +18,8 @@ _LIB_PATH = os.environ.get("GWS_LIBRARY") or os.path.join(_HERE, "libgws.so")
 FMT_BF16, FMT_FP8_E4M3, FMT_FP6_E3M2 = 0, 1, 2
 LINEAR_AUTO, LINEAR_IN_OPERAND, LINEAR_TWO_KERNELS = 0, 2, 3
 BASIS_BITS, BASIS_UNIFORM_BF16, BASIS_BOX_MULLER = 0, 1, 2
-ACT_SILU, ACT_GELU_TANH = 0, 1
+ACT_SILU, ACT_GELU_TANH, ACT_NONE = 0, 1, 2
+NORM_LAYER, NORM_RMS = 0, 1
 GATED_FWD, GATED_BWD, GATED_BWD_X = 0, 1, 2                                          # of gws_gated_form: the call,
 GATED_ANY, GATED_STREAM, GATED_MIDDLE, GATED_LARGE, GATED_SHARED = 1, 2, 3, 4, 5     # and its kernel
 
@@ -28,6 +29,8 @@ EXPORTS = ("gws_sample_fwd", "gws_sample_bwd", "gws_sample_fwd_bi", "gws_sample_
            "gws_sample_fwd_basis", "gws_sample_bwd_basis", "gws_noise_basis",
            "gws_act8_encode", "gws_act8_decode", "gws_gated_fwd", "gws_gated_bwd", "gws_gated_bwd_h", "gws_gated_bwd_x",
            "gws_linear_bwd_w_act8", "gws_linear_bwd_w_act8_workspace_bytes",
+           "gws_norm_fwd", "gws_norm_bwd", "gws_norm_bwd_workspace_bytes", "gws_dense_fwd", "gws_dense_bwd", "gws_dense_bwd_h", "gws_dense_bwd_workspace_bytes",
+           "gws_adamw", "gws_grad_norm", "gws_grad_norm_workspace_bytes",
            "gws_derive_seed", "gws_status_string", "gws_version")
 BENCH_EXPORTS = ("gws_copy_tiles", "gws_block_absmax", "gws_sample_bwd_tuned", "gws_sample_fwd_tuned", "gws_gemm_bf16_ride_probe", "gws_ride_plan",
                  "gws_ride_plan_layout", "gws_gemm_form", "gws_gemm_tile", "gws_gemm_stream_tile", "gws_linear_bwd_w_form", "gws_linear_bwd_w_form_rows", "gws_gated_form", "gws_box_muller_check")
@@ -69,6 +72,23 @@ class _CGatedSaved(ctypes.Structure):
                 ("g8", _CAct8), ("u8", _CAct8)]
 
 
+class _CEpilogue(ctypes.Structure):
+    _fields_ = [("bias", ctypes.c_void_p), ("act", ctypes.c_int), ("residual", ctypes.c_void_p), ("ldr", ctypes.c_int64),
+                ("z", ctypes.c_void_p), ("ldz", ctypes.c_int64)]
+
+
+class _CAdamWTensor(ctypes.Structure):
+    _fields_ = [("p", ctypes.c_void_p), ("w", ctypes.c_void_p), ("g", ctypes.c_void_p), ("g_is_fp32", ctypes.c_int),
+                ("m", ctypes.c_void_p), ("v", ctypes.c_void_p), ("m8", _CAct8), ("v8", _CAct8),
+                ("rows", ctypes.c_int64), ("cols", ctypes.c_int64), ("ld", ctypes.c_int64),
+                ("lr_scale", ctypes.c_float), ("weight_decay", ctypes.c_float), ("seed", ctypes.c_uint64)]
+
+
+class _CAdamWSettings(ctypes.Structure):
+    _fields_ = [("lr", ctypes.c_double), ("beta1", ctypes.c_double), ("beta2", ctypes.c_double), ("eps", ctypes.c_double),
+                ("step", ctypes.c_uint64), ("grad_scale", ctypes.c_void_p)]
+
+
 @dataclass(slots=True)
 class Act8:
     """Python-side mirror of ``gws_act8``: one-byte device tensors for the E4M3 codes [rows, columns] and the E8M0 block
@@ -86,6 +106,20 @@ class GatedSaved:
     u: Optional[object] = None
     g8: Optional[Act8] = None
     u8: Optional[Act8] = None
+
+
+@dataclass(slots=True)
+class AdamWTensor:
+    """Python-side mirror of ``gws_adamw_tensor``: a parameter ``p`` (fp32), its gradient (BF16 or fp32), its states ``m`` and ``v`` (both fp32, or
+    both :class:`Act8`, ``v`` then holding the root) and its BF16 copy ``w``: vectors, or matrices of one leading dimension."""
+    p: object
+    g: object
+    m: object
+    v: object
+    w: Optional[object] = None
+    weight_decay: float = 0.0
+    lr_scale: float = 1.0
+    seed: int = 0
 
 
 @dataclass
@@ -229,6 +263,27 @@ def load_library() -> ctypes.CDLL:
     L.gws_linear_bwd_w_act8_workspace_bytes.restype = sz
     L.gws_linear_bwd_w_act8.argtypes = [ap, vp, i64, i64, tp, ci, u64, vp, sz, vp]
     L.gws_linear_bwd_w_act8.restype = ci
+    L.gws_norm_fwd.argtypes = [vp, i64, i64, i64, ci, vp, vp, ctypes.c_float, vp, i64, vp, vp, vp]
+    L.gws_norm_fwd.restype = ci
+    L.gws_norm_bwd_workspace_bytes.argtypes = [i64, i64]
+    L.gws_norm_bwd_workspace_bytes.restype = sz
+    L.gws_norm_bwd.argtypes = [vp, i64, vp, i64, i64, i64, ci, vp, vp, vp, vp, i64, vp, i64, vp, vp, vp, sz, vp]
+    L.gws_norm_bwd.restype = ci
+    L.gws_dense_fwd.argtypes = [vp, i64, i64, i64, vp, i64, i64, ci, vp, i64, vp, vp]
+    L.gws_dense_fwd.restype = ci
+    L.gws_dense_bwd_workspace_bytes.argtypes = [i64, i64]
+    L.gws_dense_bwd_workspace_bytes.restype = sz
+    L.gws_dense_bwd.argtypes = [vp, i64, i64, i64, vp, i64, i64, ci, ci, vp, i64, vp, i64, vp, i64, vp, vp, sz, vp]
+    L.gws_dense_bwd.restype = ci
+    L.gws_dense_bwd_h.argtypes = [vp, i64, i64, i64, ci, vp, i64, vp, i64, vp, i64, vp, vp, sz, vp]
+    L.gws_dense_bwd_h.restype = ci
+    wp = ctypes.POINTER(_CAdamWTensor)
+    L.gws_adamw.argtypes = [wp, ci, vp, vp]
+    L.gws_adamw.restype = ci
+    L.gws_grad_norm_workspace_bytes.argtypes = [wp, ci]
+    L.gws_grad_norm_workspace_bytes.restype = sz
+    L.gws_grad_norm.argtypes = [wp, ci, ctypes.c_double, vp, vp, sz, vp]
+    L.gws_grad_norm.restype = ci
     L.gws_derive_seed.argtypes = [u64, u64]
     L.gws_derive_seed.restype = u64
     L.gws_status_string.argtypes = [ci]
@@ -760,6 +815,215 @@ def gws_linear_bwd_w_act8(x: Act8, dy, w: TensorDesc, step: int, workspace, w_is
     nbytes = 0 if workspace is None else int(workspace.numel() * workspace.element_size())
     _check(load_library().gws_linear_bwd_w_act8(_pack_act8(*_act8_fields(x, M, K)), _p(dy), M, ldy, _marshal([w]), 1 if w_is_nk else 0, int(step), _p(workspace),
                                                 nbytes, _stream(stream)), "gws_linear_bwd_w_act8")
+
+
+# fp32 vectors, told apart as the matrices above are.
+_fp32 = None
+
+
+def _check_vector(t, n: int) -> None:
+    global _fp32
+    if _fp32 is None:
+        import torch
+        _fp32 = torch.float32
+    if t.dtype is not _fp32 or t.shape != (n,) or (n > 1 and t.stride()[0] != 1):
+        raise ValueError(f"a vector here is fp32 of {n} elements next to each other, not {t.dtype} of shape {list(t.shape)} and strides {list(t.stride())}")
+
+
+def _vector(t, n: int, device: int):
+    if t is None:
+        return None
+    if t.dtype is not _fp32 or t.shape != (n,) or t.stride()[0] != 1:
+        _check_vector(t, n)
+    if t.get_device() != device:
+        _check_device(device, t)
+    return t.data_ptr()
+
+
+def _matrix(t, rows: int, cols: int, device: int):
+    """Address and leading dimension of a BF16 matrix; None: NULL."""
+    if t is None:
+        return None, 0
+    if t.shape != (rows, cols):
+        raise ValueError(f"a matrix has shape {list(t.shape)}, not [{rows}, {cols}]")
+    ld, one = t.stride()
+    if one != 1 or t.dtype is not _bf16:
+        _check_plain(t)
+    if t.get_device() != device:
+        _check_device(device, t)
+    return t.data_ptr(), ld if rows > 1 else max(ld, -(-cols // 8) * 8)   # one row's stride is arbitrary
+
+
+def _bytes_of(workspace, device: int):
+    if workspace is None:
+        return None, 0
+    if workspace.get_device() != device or not workspace.is_contiguous():
+        _check_device(device, workspace)
+        raise ValueError("a workspace is contiguous")
+    return workspace.data_ptr(), workspace.numel() * workspace.element_size()
+
+
+def _check_device(device: int, *tensors) -> None:
+    for t in tensors:
+        if t.get_device() != device:
+            raise ValueError(f"the tensors of a call are on one device, not on {device} and {t.get_device()} (-1: host memory)")
+
+
+def _stream_of(device: int, stream):
+    """The stream of a call on tensors of `device`, which has to be the current one: a launch goes to the current device's stream."""
+    raw = _stream(stream) if device >= 0 else None
+    import torch
+    if device < 0 or torch._C._cuda_getDevice() != device or (stream is not None and not isinstance(stream, int) and stream.device_index != device):
+        raise ValueError(f"the tensors are on device {device} (-1: host memory), which is not the current device or the stream's")
+    return raw
+
+
+def gws_norm_fwd(x, y, kind: int = NORM_LAYER, gamma=None, beta=None, eps: float = 1e-5, mean=None, rstd=None, stream=None) -> None:
+    """Layer norm or root-mean-square norm of the rows of ``x`` into ``y``; ``mean`` and ``rstd`` (fp32, one a row) receive what the backward pass needs."""
+    (M, C), on = x.shape, x.get_device()
+    (px, ldx), (py, ldy) = _matrix(x, M, C, on), _matrix(y, M, C, on)
+    _check((_lib or load_library()).gws_norm_fwd(px, M, C, ldx, kind, _vector(gamma, C, on), _vector(beta, C, on), eps, py, ldy, _vector(mean, M, on), _vector(rstd, M, on),
+                                                 _stream_of(on, stream)), "gws_norm_fwd")
+
+
+def gws_norm_bwd_workspace_bytes(M: int, C: int) -> int:
+    return int(load_library().gws_norm_bwd_workspace_bytes(M, C))
+
+
+def gws_norm_bwd(dy, x, dx, rstd, kind: int = NORM_LAYER, mean=None, gamma=None, residual=None, dgamma=None, dbeta=None, workspace=None, stream=None) -> None:
+    """dX of the norm, plus ``residual`` (a gradient that comes past it), with dgamma and dbeta; ``mean`` and ``rstd`` as ``gws_norm_fwd`` kept them."""
+    (M, C), on = x.shape, x.get_device()
+    (pdy, lddy), (px, ldx), (pr, ldr), (pdx, lddx) = _matrix(dy, M, C, on), _matrix(x, M, C, on), _matrix(residual, M, C, on), _matrix(dx, M, C, on)
+    _check((_lib or load_library()).gws_norm_bwd(pdy, lddy, px, M, C, ldx, kind, _vector(gamma, C, on), _vector(mean, M, on), _vector(rstd, M, on), pr, ldr, pdx, lddx,
+                                                 _vector(dgamma, C, on), _vector(dbeta, C, on), *_bytes_of(workspace, on), _stream_of(on, stream)), "gws_norm_bwd")
+
+
+_pack_epilogue = struct.Struct("=Qi4xQqQq").pack
+assert struct.calcsize("=Qi4xQqQq") == ctypes.sizeof(_CEpilogue)
+
+
+def gws_dense_fwd(x, w, y, bias=None, act: int = ACT_NONE, residual=None, z=None, w_is_nk: bool = False, stream=None) -> None:
+    """Y = a(X W + b) + R in one kernel; ``z`` receives X W + b for the backward pass."""
+    (M, K), size, on = x.shape, w.shape, x.get_device()
+    N, Kw = size if w_is_nk else (size[1], size[0])
+    if Kw != K:
+        raise ValueError(f"X {list(x.shape)} and W {list(size)} do not fit together")
+    (px, ldx), (pw, ldw), (py, ldy), (pr, ldr), (pz, ldz) = _matrix(x, M, K, on), _matrix(w, *size, on), _matrix(y, M, N, on), _matrix(residual, M, N, on), _matrix(z, M, N, on)
+    _check((_lib or load_library()).gws_dense_fwd(px, M, K, ldx, pw, N, ldw, 1 if w_is_nk else 0, py, ldy,
+                                                  _pack_epilogue(_vector(bias, N, on) or 0, act, pr or 0, ldr, pz or 0, ldz), _stream_of(on, stream)), "gws_dense_fwd")
+
+
+def gws_dense_bwd_workspace_bytes(M: int, F: int) -> int:
+    return int(load_library().gws_dense_bwd_workspace_bytes(M, F))
+
+
+def gws_dense_bwd(dy, wd, z, dz, act: int = ACT_NONE, h=None, dbias=None, workspace=None, w_is_nk: bool = False, stream=None) -> None:
+    """dZ (and H = a(Z) again, and the bias gradient) from the gradient of Y = H Wd and the kept Z; dH = dY Wd^T stays in the kernel."""
+    (M, D), size, on = dy.shape, wd.shape, dy.get_device()
+    F, Dw = (size[1], size[0]) if w_is_nk else size
+    if Dw != D:
+        raise ValueError(f"dY {list(dy.shape)} and Wd {list(size)} do not fit together")
+    (pdy, lddy), (pw, ldw) = _matrix(dy, M, D, on), _matrix(wd, *size, on)
+    _check((_lib or load_library()).gws_dense_bwd(pdy, M, D, lddy, pw, F, ldw, 1 if w_is_nk else 0, act, *_matrix(z, M, F, on), *_matrix(dz, M, F, on),
+                                                  *_matrix(h, M, F, on), _vector(dbias, F, on), *_bytes_of(workspace, on), _stream_of(on, stream)), "gws_dense_bwd")
+
+
+def gws_dense_bwd_h(dh, z, dz, act: int = ACT_NONE, h=None, dbias=None, workspace=None, stream=None) -> None:
+    """``gws_dense_bwd`` from a given dH; with ``ACT_NONE`` ``z`` and ``dz`` may be None, which leaves the bias gradient alone."""
+    (M, F), on = dh.shape, dh.get_device()
+    pdh, lddh = _matrix(dh, M, F, on)
+    _check((_lib or load_library()).gws_dense_bwd_h(pdh, M, F, lddh, act, *_matrix(z, M, F, on), *_matrix(dz, M, F, on), *_matrix(h, M, F, on), _vector(dbias, F, on),
+                                                    *_bytes_of(workspace, on), _stream_of(on, stream)), "gws_dense_bwd_h")
+
+
+class PackedAdamW:
+    """A list of parameters already marshalled into a C array of ``gws_adamw_tensor`` (see :func:`pack_adamw`)."""
+
+    def __init__(self, arr, n, keepalive, device):
+        self.arr, self.n, self._keepalive, self.device = arr, n, keepalive, device
+
+    def __len__(self):
+        return self.n
+
+
+def pack_adamw(tensors: Sequence[AdamWTensor]) -> PackedAdamW:
+    """The buffers of a training run do not move between steps, so the array can be built once and passed to every call."""
+    import torch
+
+    arr = (_CAdamWTensor * max(1, len(tensors)))()
+    on = tensors[0].p.get_device() if len(tensors) else None
+    for c, t in zip(arr, tensors):
+        shape = t.p.shape
+        if len(shape) not in (1, 2):
+            raise ValueError(f"a parameter is a vector or a matrix, not of shape {list(shape)}")
+        rows, cols = shape if len(shape) == 2 else (1, shape[0])
+
+        def place(name, x, dtypes, want=shape):
+            if x.shape != want or x.dtype not in dtypes or (want[-1] > 1 and x.stride()[-1] != 1):
+                raise ValueError(f"{name} is {' or '.join(str(d) for d in dtypes)} of shape {list(want)} with its columns next to each other, not {x.dtype} of "
+                                 f"shape {list(x.shape)} and strides {list(x.stride())}")
+            _check_device(on, x)
+            return x.data_ptr(), x.stride()[0] if len(want) == 2 and rows > 1 else None
+
+        found = []   # leading dimensions
+        c.p, ld = place("p", t.p, (torch.float32,))
+        found.append(ld)
+        c.g, ld = place("g", t.g, (torch.bfloat16, torch.float32))
+        found.append(ld)
+        c.g_is_fp32 = int(t.g.dtype is torch.float32)
+        if t.w is not None:
+            c.w, ld = place("w", t.w, (torch.bfloat16,))
+            found.append(ld)
+        if isinstance(t.m, Act8) != isinstance(t.v, Act8):
+            raise ValueError("m and v are held both in 32 bits or both in 8")
+        if isinstance(t.m, Act8):
+            one_byte = (torch.uint8, torch.int8, torch.float8_e4m3fn, torch.float8_e8m0fnu)
+            blocks = shape[:-1] + (-(-cols // 32),)
+            for name, s, to in (("m", t.m, c.m8), ("v", t.v, c.v8)):
+                to.codes, ld = place(f"{name}'s codes", s.codes, one_byte)
+                found.append(ld if s.ldc is None else s.ldc)
+                to.xscale, lds = place(f"{name}'s scales", s.xscale, one_byte, blocks)
+                to.lds = s.lds if s.lds is not None else lds if lds is not None else blocks[-1]
+        else:
+            c.m, ld = place("m", t.m, (torch.float32,))
+            found.append(ld)
+            c.v, ld = place("v", t.v, (torch.float32,))
+            found.append(ld)
+        lds = {x for x in found if x is not None} or {-(-cols // 8) * 8}   # one row: any
+        if len(lds) != 1:
+            raise ValueError(f"the arrays of a parameter have one leading dimension, not {sorted(lds)}")
+        c.rows, c.cols, c.ld = rows, cols, lds.pop()
+        c.m8.ldc = c.v8.ldc = c.ld
+        c.lr_scale, c.weight_decay, c.seed = t.lr_scale, t.weight_decay, t.seed & (2 ** 64 - 1)
+    return PackedAdamW(arr, len(tensors), list(tensors), on)
+
+
+def _as_adamw(t) -> PackedAdamW:
+    return t if isinstance(t, PackedAdamW) else pack_adamw(t)
+
+
+def gws_adamw(t, lr: float, step: int, beta1: float = 0.9, beta2: float = 0.95, eps: float = 1e-8, grad_scale=None, stream=None) -> None:
+    """One AdamW step (``step`` = 1, 2, ...) over a list of :class:`AdamWTensor`, or :func:`pack_adamw`'s array; ``grad_scale``: a device fp32 number that
+    the gradients are multiplied by, as ``gws_grad_norm`` leaves it (not finite: the step is left out)."""
+    t = _as_adamw(t)
+    if grad_scale is not None and (str(grad_scale.dtype) != "torch.float32" or grad_scale.numel() != 1):
+        raise ValueError(f"grad_scale is one fp32 number, not {grad_scale.dtype} of shape {list(grad_scale.shape)}")
+    if t.n and grad_scale is not None:
+        _check_device(t.device, grad_scale)
+    s = _CAdamWSettings(lr, beta1, beta2, eps, step, _p(grad_scale))
+    _check((_lib or load_library()).gws_adamw(t.arr, t.n, ctypes.byref(s), _stream_of(t.device, stream) if t.n else None), "gws_adamw")
+
+
+def gws_grad_norm_workspace_bytes(t) -> int:
+    t = _as_adamw(t)
+    return int(load_library().gws_grad_norm_workspace_bytes(t.arr, t.n))
+
+
+def gws_grad_norm(t, out, workspace, max_norm: float = 0.0, stream=None) -> None:
+    """``out`` (fp32 [2]): the norm of all gradients, and the factor that takes it down to ``max_norm`` where it is larger."""
+    t = _as_adamw(t)
+    on = t.device if t.n else out.get_device()
+    _check((_lib or load_library()).gws_grad_norm(t.arr, t.n, max_norm, _vector(out, 2, on), *_bytes_of(workspace, on), _stream_of(on, stream)), "gws_grad_norm")
 
 
 def gws_sample_fwd_basis(t: Sequence[TensorDesc], basis: int, fmt: int, step: int, stream=None) -> None:

@@ -960,6 +960,6 @@ const char* gws_status_string(int status) {
   }
 }
 
-int gws_version(void) { return 8; }
+int gws_version(void) { return 9; }
 
 }  // extern "C"

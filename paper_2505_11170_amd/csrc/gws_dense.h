@@ -1,0 +1,45 @@
+// The dense layer: launch arguments and the arithmetic on its sums, shared by its kernels (internal to csrc/).
+#pragma once
+
+#include "gws_gated.h"
+#include "gws_norm.h"
+
+namespace gws {
+
+// What happens to the sums of a product (GemmArgs: x, w, y) on their way out.
+//   forward : Z = sum + bias, kept in z; Y = a(Z) + r
+//   backward: dZ = sum a'(Z) to y, H = a(Z) to h, and the columns' sums over the tile's rows to part[tile row][N]
+struct DenseArgs {
+  const float* bias;      // may be NULL
+  const uint16_t* r;      // may be NULL
+  uint16_t* z;            // forward: written, may be NULL; backward: read (NULL only without activation)
+  uint16_t* h;            // may be NULL
+  float* part;            // may be NULL
+  uint32_t ldr, ldz, ldh;
+  int act;
+};
+enum class DenseOp { kFwd = 0, kBwd = 1 };
+
+// The activation that is none.
+struct NoGate {
+  __device__ static __forceinline__ float a(float z) { return z; }
+  __device__ static __forceinline__ void both(float z, float& a, float& slope) {
+    a = z;
+    slope = 1.0f;
+  }
+};
+template <class F>
+__device__ __forceinline__ void with_act(int act, F&& f) {   // a uniform branch
+  if (act == GWS_ACT_NONE) f(NoGate());
+  else with_gate(act, (F&&)f);
+}
+inline bool known_dense_act(int act) { return act == GWS_ACT_NONE || known_act(act); }
+
+// every size
+int launch_dense_any(const GemmArgs& g, const DenseArgs& e, DenseOp op, int w_is_nk, hipStream_t stream);
+constexpr uint32_t kDenseAnyRows = 64;   // of its tiles, for the partial sums
+// from a given dH (x, ldx): rows of tokens a workgroup takes
+uint32_t dense_h_rows(uint64_t M, uint64_t F);
+int launch_dense_bwd_h(const GemmArgs& g, const DenseArgs& e, hipStream_t stream);
+
+}  // namespace gws

@@ -11,38 +11,6 @@ namespace gws {
 
 namespace {
 
-constexpr int64_t kMaxDim = (int64_t)1 << 31;
-
-inline bool size_ok(int64_t n) { return n >= 0 && n < kMaxDim; }
-// A BF16 matrix's leading dimension.
-inline bool ld_ok(int64_t ld, int64_t cols) { return ld >= cols && ld < kMaxDim && (ld & 7) == 0; }
-inline Span2 span16(const void* p, int64_t rows, int64_t cols, int64_t ld) { return Span2{p, (size_t)rows, (size_t)cols * 2, (size_t)ld * 2}; }
-inline bool same_place(const Span2& a, const Span2& b) { return a.p == b.p && a.pitch == b.pitch; }
-
-int check_act8(const gws_act8& a, int64_t M, int64_t C) {
-  if (!a.codes || !a.xscale) return GWS_ERR_NULL;
-  if (a.ldc < C || a.ldc >= kMaxDim || (a.ldc & 7) != 0 || a.lds < (C + 31) / 32 || a.lds >= kMaxDim) return GWS_ERR_SHAPE;
-  return aligned(a.codes, 8) ? GWS_OK : GWS_ERR_ALIGN;
-}
-
-// A list of matrices of which some are written.
-struct Buffers {
-  Span2 in[8], out[8];
-  int ins = 0, outs = 0;
-  void reads(const Span2& s) { if (s.p) in[ins++] = s; }
-  void writes(const Span2& s) { if (s.p) out[outs++] = s; }
-  // No output on another one; none on an input, but for the ones at the very same place where `in_place` allows those.
-  bool apart_all(bool in_place) const {
-    for (int i = 0; i < outs; ++i) {
-      for (int j = 0; j < i; ++j)
-        if (!apart(out[i], out[j])) return false;
-      for (int j = 0; j < ins; ++j)
-        if (!apart(out[i], in[j]) && !(in_place && same_place(out[i], in[j]))) return false;
-    }
-    return true;
-  }
-};
-
 // G and U as they are kept; `optional`: NULL keeps nothing.
 int kept_args(const gws_gated_saved* s, int64_t M, int64_t F, bool optional, Kept& form, KeptArgs& k) {
   memset(&k, 0, sizeof k);

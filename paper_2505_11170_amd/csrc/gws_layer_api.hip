@@ -1,0 +1,406 @@
+// C ABI of the norms, the dense layer and the AdamW step: argument checks and the choice of kernel.  Declarations and the meaning of every
+// argument are in include/gws.h.
+#include <math.h>
+#include <string.h>
+
+#include "gws_adamw.h"
+#include "gws_bench.h"
+#include "gws_check.h"
+#include "gws_dense.h"
+#include "gws_norm.h"
+
+namespace gws {
+
+namespace {
+
+inline Span2 span_f32(const void* p, int64_t n) { return Span2{p, 1, (size_t)n * 4, (size_t)n * 4}; }
+inline Span2 span_bytes(const void* p, size_t n) { return Span2{p, 1, n, n}; }
+
+// ---- norms ----
+size_t norm_bytes(int64_t M, int64_t C) {
+  size_t n = (size_t)norm_bwd_parts((uint64_t)M, (uint64_t)C) * 2 * (size_t)C * sizeof(float);
+  n = (n + 15) & ~(size_t)15;
+  return n + (norm_is_wide((uint64_t)C) ? (size_t)M * 2 * sizeof(float) : 0);
+}
+
+// ---- the dense layer ----
+size_t dense_bytes(int64_t M, int64_t F) { return M <= 16 ? 0 : (size_t)((M + 15) / 16) * (size_t)F * sizeof(float); }
+
+// Outputs, kept Z and the bias gradient's workspace of the two backward calls.
+int dense_bwd_args(int64_t M, int64_t F, int act, const void* z, int64_t ldz, void* dz, int64_t lddz, void* h, int64_t ldh, float* dbias, void* workspace,
+                   size_t workspace_bytes, GemmArgs& g, DenseArgs& d, Buffers& b) {
+  if ((z == nullptr && (act != GWS_ACT_NONE || h != nullptr))) return GWS_ERR_NULL;
+  if ((z && !ld_ok(ldz, F)) || (dz && !ld_ok(lddz, F)) || (h && !ld_ok(ldh, F))) return GWS_ERR_SHAPE;
+  const size_t need = dbias ? dense_bytes(M, F) : 0;
+  if (need && !workspace) return GWS_ERR_NULL;
+  if (need && workspace_bytes < need) return GWS_ERR_SHAPE;
+  if (!aligned(z, 16) || !aligned(dz, 16) || !aligned(h, 16) || !aligned(dbias, 4) || (need && !aligned(workspace, 16))) return GWS_ERR_ALIGN;
+  if (act == GWS_ACT_NONE && h == nullptr) z = nullptr;   // what is not used is not read
+  b.reads(span16(z, M, F, ldz));
+  b.writes(span16(dz, M, F, lddz));
+  b.writes(span16(h, M, F, ldh));
+  b.writes(span_f32(dbias, F));
+  if (need) b.writes(span_bytes(workspace, need));
+  g.M = (uint32_t)M; g.N = (uint32_t)F;
+  g.y = (uint16_t*)dz; g.ldy = (uint32_t)lddz;
+  d.z = (uint16_t*)z; d.ldz = (uint32_t)ldz;
+  d.h = (uint16_t*)h; d.ldh = (uint32_t)ldh;
+  d.act = act;
+  return GWS_OK;
+}
+// Runs a backward pass whose tiles are `rows` rows high, and adds its partial sums up.
+template <class Launch>
+int with_bias_gradient(const GemmArgs& g, DenseArgs& d, uint64_t rows, float* dbias, void* workspace, hipStream_t stream, Launch&& launch) {
+  const uint64_t parts = ((uint64_t)g.M + rows - 1) / rows;
+  d.part = !dbias ? nullptr : parts == 1 ? dbias : (float*)workspace;
+  const int rc = launch();
+  if (rc != GWS_OK || !dbias || parts == 1) return rc;
+  return launch_sum_partials(d.part, (uint32_t)parts, g.N, g.N, dbias, nullptr, stream);
+}
+
+int launch_dense(const GemmArgs& g, const DenseArgs& d, DenseOp op, int w_is_nk, hipStream_t stream) { return launch_dense_any(g, d, op, w_is_nk, stream); }
+uint64_t dense_tile_rows(const GemmArgs&, int) { return kDenseAnyRows; }
+
+// ---- AdamW ----
+int check_gradient(const gws_adamw_tensor& t) {
+  if (!size_ok(t.rows) || !size_ok(t.cols)) return GWS_ERR_SHAPE;
+  if (t.rows == 0 || t.cols == 0) return GWS_OK;
+  if (!ld_ok(t.ld, t.cols) || (uint64_t)t.rows * (((uint64_t)t.cols + 31) / 32) >= (uint64_t)1 << 37) return GWS_ERR_SHAPE;
+  if (!t.g) return GWS_ERR_NULL;
+  return aligned(t.g, 16) ? GWS_OK : GWS_ERR_ALIGN;
+}
+inline Span2 gradient_span(const gws_adamw_tensor& t) {
+  const size_t e = t.g_is_fp32 ? 4 : 2;
+  return Span2{t.g, (size_t)t.rows, (size_t)t.cols * e, (size_t)t.ld * e};
+}
+int check_adamw(const gws_adamw_tensor& t, const float* grad_scale) {
+  int rc = check_gradient(t);
+  if (rc != GWS_OK || t.rows == 0 || t.cols == 0) return rc;
+  const bool codes = t.m8.codes || t.v8.codes;
+  if (codes && (t.m || t.v)) return GWS_ERR_FORMAT;
+  if (!t.p) return GWS_ERR_NULL;
+  if (!isfinite(t.lr_scale) || !isfinite(t.weight_decay)) return GWS_ERR_FORMAT;
+  Buffers b;
+  const size_t m = (size_t)t.rows, n = (size_t)t.cols, ld = (size_t)t.ld;
+  if (codes) {
+    if ((rc = check_act8(t.m8, t.rows, t.cols)) != GWS_OK || (rc = check_act8(t.v8, t.rows, t.cols)) != GWS_OK) return rc;
+    if (t.m8.ldc != t.ld || t.v8.ldc != t.ld || t.m8.lds != t.v8.lds) return GWS_ERR_SHAPE;
+    for (const gws_act8* s : {&t.m8, &t.v8}) {
+      b.writes(Span2{s->codes, m, n, ld});
+      b.writes(Span2{s->xscale, m, (n + 31) / 32, (size_t)s->lds});
+    }
+  } else {
+    if (!t.m || !t.v) return GWS_ERR_NULL;
+    if (!aligned(t.m, 16) || !aligned(t.v, 16)) return GWS_ERR_ALIGN;
+    b.writes(Span2{t.m, m, n * 4, ld * 4});
+    b.writes(Span2{t.v, m, n * 4, ld * 4});
+  }
+  if (!aligned(t.p, 16) || !aligned(t.w, 16)) return GWS_ERR_ALIGN;
+  b.writes(Span2{t.p, m, n * 4, ld * 4});
+  b.writes(Span2{t.w, m, n * 2, ld * 2});
+  b.reads(gradient_span(t));
+  b.reads(span_f32(grad_scale, 1));
+  return b.apart_all(false) ? GWS_OK : GWS_ERR_ALIAS;
+}
+
+// The tensors of a call in launches of as many as fit; make(d, tensor) fills a descriptor and gives the elements of a group, and of `per_wg` groups
+// is a workgroup.  flush(args, workgroups).
+template <class Make, class Flush>
+int in_launches(AdamwArgs& a, const gws_adamw_tensor* t, int n, uint32_t per_wg, Make&& make, Flush&& flush) {
+  int held = 0;
+  uint64_t wgs = 0;
+  auto launch = [&]() -> int {
+    if (held == 0) return GWS_OK;
+    for (int i = held; i < kAdamwTensors; ++i) a.begin[i] = 0x7FFFFFFFu;
+    const int rc = flush((uint32_t)wgs);
+    held = 0;
+    wgs = 0;
+    return rc;
+  };
+  for (int i = 0; i < n; ++i) {
+    if (t[i].rows == 0 || t[i].cols == 0) continue;
+    AdamwDesc d;
+    memset(&d, 0, sizeof d);
+    d.g = t[i].g;
+    d.rows = (uint32_t)t[i].rows; d.cols = (uint32_t)t[i].cols; d.ld = (uint32_t)t[i].ld;
+    if (t[i].g_is_fp32) d.form |= kGradFp32;
+    d.per_row = make(d, t[i]);
+    d.inv = reciprocal(d.per_row);
+    const uint64_t groups = (uint64_t)d.rows * d.per_row, wc = (groups + per_wg - 1) / per_wg;
+    if (wc >= 0x7FFFFFF0ull) return GWS_ERR_SHAPE;
+    if (groups + per_wg < ((uint64_t)1 << 32)) d.form |= kFewGroups;
+    if (held == kAdamwTensors || wgs + wc >= 0x7FFFFFF0ull) {
+      const int rc = launch();
+      if (rc != GWS_OK) return rc;
+    }
+    d.first_wg = (uint32_t)wgs;
+    a.begin[held] = (uint32_t)wgs;
+    a.t[held++] = d;
+    wgs += wc;
+  }
+  return launch();
+}
+inline uint64_t norm_wgs(const gws_adamw_tensor& t) {
+  return t.rows <= 0 || t.cols <= 0 ? 0 : ((uint64_t)t.rows * (((uint64_t)t.cols + 7) / 8) + kNormGroups - 1) / kNormGroups;
+}
+
+}  // namespace
+}  // namespace gws
+
+using namespace gws;
+
+extern "C" {
+
+int gws_norm_fwd(const void* x, int64_t M, int64_t C, int64_t ldx, int kind, const float* gamma, const float* beta, float eps, void* y, int64_t ldy,
+                 float* mean, float* rstd, void* stream) {
+  if (!size_ok(M) || !size_ok(C) || C == 0) return GWS_ERR_SHAPE;
+  if (kind != GWS_NORM_LAYER && kind != GWS_NORM_RMS) return GWS_ERR_FORMAT;
+  if (!(eps > 0.0f) || !isfinite(eps)) return GWS_ERR_FORMAT;
+  if (M == 0) return GWS_OK;
+  if (!ld_ok(ldx, C) || !ld_ok(ldy, C)) return GWS_ERR_SHAPE;
+  if (!x || !y) return GWS_ERR_NULL;
+  if (kind == GWS_NORM_LAYER ? (mean == nullptr) != (rstd == nullptr) : mean != nullptr) return GWS_ERR_NULL;
+  if (!aligned(x, 16) || !aligned(y, 16) || !aligned(gamma, 4) || !aligned(beta, 4) || !aligned(mean, 4) || !aligned(rstd, 4)) return GWS_ERR_ALIGN;
+  Buffers b;
+  b.reads(span_f32(gamma, C));
+  b.reads(span_f32(beta, C));
+  b.writes(span_f32(mean, M));
+  b.writes(span_f32(rstd, M));
+  const Span2 in = span16(x, M, C, ldx), out = span16(y, M, C, ldy);
+  if (!same_place(in, out)) b.reads(in);
+  b.writes(out);
+  if (!b.apart_all(false) || !apart(in, span_f32(mean, M)) || !apart(in, span_f32(rstd, M))) return GWS_ERR_ALIAS;
+  NormArgs a;
+  memset(&a, 0, sizeof a);
+  a.x = (const uint16_t*)x; a.y = (uint16_t*)y;
+  a.gamma = gamma; a.beta = beta; a.mean = mean; a.rstd = rstd;
+  a.M = (uint32_t)M; a.C = (uint32_t)C; a.ldx = (uint32_t)ldx; a.ldy = (uint32_t)ldy;
+  a.eps = eps;
+  return launch_norm_fwd(a, kind == GWS_NORM_RMS, (hipStream_t)stream);
+}
+
+size_t gws_norm_bwd_workspace_bytes(int64_t M, int64_t C) {
+  return !size_ok(M) || !size_ok(C) || M == 0 || C == 0 ? 0 : norm_bytes(M, C);
+}
+
+int gws_norm_bwd(const void* dy, int64_t lddy, const void* x, int64_t M, int64_t C, int64_t ldx, int kind, const float* gamma, const float* mean,
+                 const float* rstd, const void* residual, int64_t ldr, void* dx, int64_t lddx, float* dgamma, float* dbeta, void* workspace,
+                 size_t workspace_bytes, void* stream) {
+  if (!size_ok(M) || !size_ok(C) || C == 0) return GWS_ERR_SHAPE;
+  if (kind != GWS_NORM_LAYER && kind != GWS_NORM_RMS) return GWS_ERR_FORMAT;
+  if (!aligned(dgamma, 4) || !aligned(dbeta, 4)) return GWS_ERR_ALIGN;
+  if (!apart(span_f32(dgamma, C), span_f32(dbeta, C))) return GWS_ERR_ALIAS;
+  if (M == 0) {
+    int rc = dgamma ? launch_zero(dgamma, (uint64_t)C, (hipStream_t)stream) : GWS_OK;
+    if (rc == GWS_OK && dbeta) rc = launch_zero(dbeta, (uint64_t)C, (hipStream_t)stream);
+    return rc;
+  }
+  if (!ld_ok(ldx, C) || !ld_ok(lddy, C) || !ld_ok(lddx, C) || (residual && !ld_ok(ldr, C))) return GWS_ERR_SHAPE;
+  if (!dy || !x || !dx || !rstd || (kind == GWS_NORM_LAYER && !mean)) return GWS_ERR_NULL;
+  if (!aligned(x, 16) || !aligned(dy, 16) || !aligned(dx, 16) || !aligned(residual, 16) || !aligned(gamma, 4) || !aligned(mean, 4) || !aligned(rstd, 4))
+    return GWS_ERR_ALIGN;
+  const bool needed = dgamma || dbeta || norm_is_wide((uint64_t)C);
+  const size_t need = needed ? norm_bytes(M, C) : 0;
+  if (needed && !workspace) return GWS_ERR_NULL;
+  if (needed && !aligned(workspace, 16)) return GWS_ERR_ALIGN;
+  if (needed && workspace_bytes < need) return GWS_ERR_SHAPE;
+  Buffers b, v;   // dX, which may lie on a matrix; and everything else
+  const Span2 out = span16(dx, M, C, lddx);
+  b.writes(out);
+  for (const Span2& m : {span16(x, M, C, ldx), span16(dy, M, C, lddy), span16(residual, M, C, ldr)}) {
+    b.reads(m);
+    v.reads(m);
+  }
+  for (const Span2& m : {span_f32(gamma, C), span_f32(kind == GWS_NORM_LAYER ? mean : nullptr, M), span_f32(rstd, M)}) {
+    v.reads(m);
+    if (!apart(out, m)) return GWS_ERR_ALIAS;
+  }
+  for (const Span2& m : {span_f32(dgamma, C), span_f32(dbeta, C), span_bytes(needed ? workspace : nullptr, need)}) {
+    v.writes(m);
+    if (!apart(out, m)) return GWS_ERR_ALIAS;
+  }
+  if (!b.apart_all(true) || !v.apart_all(false)) return GWS_ERR_ALIAS;
+  NormArgs a;
+  memset(&a, 0, sizeof a);
+  a.x = (const uint16_t*)x; a.dy = (const uint16_t*)dy; a.r = (const uint16_t*)residual; a.y = (uint16_t*)dx;
+  a.gamma = gamma; a.mean = (float*)mean; a.rstd = (float*)rstd;
+  a.M = (uint32_t)M; a.C = (uint32_t)C;
+  a.ldx = (uint32_t)ldx; a.lddy = (uint32_t)lddy; a.ldr = (uint32_t)ldr; a.ldy = (uint32_t)lddx;
+  a.want_gamma = dgamma != nullptr;
+  a.want_beta = dbeta != nullptr;
+  a.part = (float*)workspace;
+  if (norm_is_wide((uint64_t)C)) a.rows = (float*)((char*)workspace + (need - (size_t)M * 2 * sizeof(float)));
+  return launch_norm_bwd(a, kind == GWS_NORM_RMS, dgamma, dbeta, (hipStream_t)stream);
+}
+
+int gws_dense_fwd(const void* x, int64_t M, int64_t K, int64_t ldx, const void* w, int64_t N, int64_t ldw, int w_is_nk, void* y, int64_t ldy,
+                  const gws_epilogue* e, void* stream) {
+  if (!size_ok(M) || !size_ok(K) || !size_ok(N)) return GWS_ERR_SHAPE;
+  if (!e) return GWS_ERR_NULL;
+  if (!known_dense_act(e->act)) return GWS_ERR_FORMAT;
+  if (M == 0 || N == 0) return GWS_OK;
+  if (K == 0 || ((K | N) & 31) != 0) return GWS_ERR_SHAPE;
+  if (!ld_ok(ldx, K) || !ld_ok(ldw, w_is_nk ? K : N) || !ld_ok(ldy, N)) return GWS_ERR_SHAPE;
+  if ((e->residual && !ld_ok(e->ldr, N)) || (e->z && !ld_ok(e->ldz, N))) return GWS_ERR_SHAPE;
+  if (!x || !w || !y) return GWS_ERR_NULL;
+  if (!aligned(x, 16) || !aligned(w, 16) || !aligned(y, 16) || !aligned(e->residual, 16) || !aligned(e->z, 16) || !aligned(e->bias, 4)) return GWS_ERR_ALIGN;
+  Buffers b;
+  b.reads(span16(x, M, K, ldx));
+  b.reads(w_is_nk ? span16(w, N, K, ldw) : span16(w, K, N, ldw));
+  b.reads(span_f32(e->bias, N));
+  const Span2 r = span16(e->residual, M, N, e->ldr), out = span16(y, M, N, ldy), z = span16(e->z, M, N, e->ldz);
+  if (!same_place(r, out)) b.reads(r);
+  b.writes(out);
+  b.writes(z);
+  if (!b.apart_all(false) || !apart(r, z)) return GWS_ERR_ALIAS;
+  GemmArgs g;
+  memset(&g, 0, sizeof g);
+  g.x = (const uint16_t*)x; g.w = (const uint16_t*)w; g.y = (uint16_t*)y;
+  g.M = (uint32_t)M; g.N = (uint32_t)N; g.K = (uint32_t)K;
+  g.ldx = (uint32_t)ldx; g.ldw = (uint32_t)ldw; g.ldy = (uint32_t)ldy;
+  if (!e->bias && !e->residual && !e->z && e->act == GWS_ACT_NONE) return launch_gemm(g, w_is_nk, 0, GWS_FMT_BF16, (hipStream_t)stream);
+  DenseArgs d;
+  memset(&d, 0, sizeof d);
+  d.bias = e->bias;
+  d.act = e->act;
+  d.r = (const uint16_t*)e->residual; d.ldr = (uint32_t)e->ldr;
+  d.z = (uint16_t*)e->z; d.ldz = (uint32_t)e->ldz;
+  return launch_dense(g, d, DenseOp::kFwd, w_is_nk, (hipStream_t)stream);
+}
+
+size_t gws_dense_bwd_workspace_bytes(int64_t M, int64_t F) { return !size_ok(M) || !size_ok(F) ? 0 : dense_bytes(M, F); }
+
+int gws_dense_bwd(const void* dy, int64_t M, int64_t D, int64_t lddy, const void* wd, int64_t F, int64_t ldw, int w_is_nk, int act, const void* z,
+                  int64_t ldz, void* dz, int64_t lddz, void* h, int64_t ldh, float* dbias, void* workspace, size_t workspace_bytes, void* stream) {
+  if (!size_ok(M) || !size_ok(D) || !size_ok(F)) return GWS_ERR_SHAPE;
+  if (!known_dense_act(act)) return GWS_ERR_FORMAT;
+  if (F == 0) return GWS_OK;
+  if (M == 0) return !dbias ? GWS_OK : !aligned(dbias, 4) ? GWS_ERR_ALIGN : launch_zero(dbias, (uint64_t)F, (hipStream_t)stream);
+  if (D == 0 || ((D | F) & 31) != 0) return GWS_ERR_SHAPE;
+  if (!ld_ok(lddy, D) || !ld_ok(ldw, w_is_nk ? F : D)) return GWS_ERR_SHAPE;
+  if (!dy || !wd || !dz) return GWS_ERR_NULL;
+  if (!aligned(dy, 16) || !aligned(wd, 16)) return GWS_ERR_ALIGN;
+  GemmArgs g;
+  DenseArgs d;
+  memset(&g, 0, sizeof g);
+  memset(&d, 0, sizeof d);
+  Buffers own, in;   // outputs on Z at the very same place, and on nothing else
+  int rc = dense_bwd_args(M, F, act, z, ldz, dz, lddz, h, ldh, dbias, workspace, workspace_bytes, g, d, own);
+  if (rc != GWS_OK) return rc;
+  in.reads(span16(dy, M, D, lddy));
+  in.reads(w_is_nk ? span16(wd, D, F, ldw) : span16(wd, F, D, ldw));
+  for (int i = 0; i < own.outs; ++i) in.writes(own.out[i]);
+  if (!own.apart_all(true) || !in.apart_all(false)) return GWS_ERR_ALIAS;
+  g.x = (const uint16_t*)dy; g.w = (const uint16_t*)wd;
+  g.K = (uint32_t)D; g.ldx = (uint32_t)lddy; g.ldw = (uint32_t)ldw;
+  const int nk = !w_is_nk;   // the product's columns are Wd's rows
+  return with_bias_gradient(g, d, dense_tile_rows(g, nk), dbias, workspace, (hipStream_t)stream,
+                            [&] { return launch_dense(g, d, DenseOp::kBwd, nk, (hipStream_t)stream); });
+}
+
+int gws_dense_bwd_h(const void* dh, int64_t M, int64_t F, int64_t lddh, int act, const void* z, int64_t ldz, void* dz, int64_t lddz, void* h,
+                    int64_t ldh, float* dbias, void* workspace, size_t workspace_bytes, void* stream) {
+  if (!size_ok(M) || !size_ok(F)) return GWS_ERR_SHAPE;
+  if (!known_dense_act(act)) return GWS_ERR_FORMAT;
+  if (F == 0) return GWS_OK;
+  if (M == 0) return !dbias ? GWS_OK : !aligned(dbias, 4) ? GWS_ERR_ALIGN : launch_zero(dbias, (uint64_t)F, (hipStream_t)stream);
+  if ((F & 7) != 0 || !ld_ok(lddh, F)) return GWS_ERR_SHAPE;
+  if (!dh || (!dz && act != GWS_ACT_NONE)) return GWS_ERR_NULL;
+  if (!aligned(dh, 16)) return GWS_ERR_ALIGN;
+  GemmArgs g;
+  DenseArgs d;
+  memset(&g, 0, sizeof g);
+  memset(&d, 0, sizeof d);
+  Buffers b;
+  int rc = dense_bwd_args(M, F, act, z, ldz, dz, lddz, h, ldh, dbias, workspace, workspace_bytes, g, d, b);
+  if (rc != GWS_OK) return rc;
+  b.reads(span16(dh, M, F, lddh));
+  if (!b.apart_all(true)) return GWS_ERR_ALIAS;
+  g.x = (const uint16_t*)dh; g.ldx = (uint32_t)lddh;
+  return with_bias_gradient(g, d, dense_h_rows(g.M, g.N), dbias, workspace, (hipStream_t)stream, [&] { return launch_dense_bwd_h(g, d, (hipStream_t)stream); });
+}
+
+int gws_adamw(const gws_adamw_tensor* t, int n, const gws_adamw_settings* s, void* stream) {
+  if (n < 0) return GWS_ERR_SHAPE;
+  if (!s) return GWS_ERR_NULL;
+  if (!isfinite(s->lr) || !isfinite(s->eps) || !((float)s->eps > 0.0f) || !(s->beta1 >= 0.0 && s->beta1 < 1.0) || !(s->beta2 >= 0.0 && s->beta2 < 1.0) || s->step == 0)
+    return GWS_ERR_FORMAT;
+  if (!aligned(s->grad_scale, 4)) return GWS_ERR_ALIGN;
+  if (n == 0) return GWS_OK;
+  if (!t) return GWS_ERR_NULL;
+  for (int i = 0; i < n; ++i) {
+    const int rc = check_adamw(t[i], s->grad_scale);
+    if (rc != GWS_OK) return rc;
+  }
+  AdamwArgs a;
+  a.beta1 = (float)s->beta1; a.one1 = (float)(1.0 - s->beta1);
+  a.beta2 = (float)s->beta2; a.one2 = (float)(1.0 - s->beta2);
+  const double c1 = 1.0 - pow(s->beta1, (double)s->step), c2 = 1.0 - pow(s->beta2, (double)s->step);
+  a.root2 = (float)(1.0 / sqrt(c2));
+  a.eps = (float)s->eps;
+  a.step_lo = (uint32_t)s->step;
+  a.step_hi = (uint32_t)(s->step >> 32);
+  a.grad_scale = s->grad_scale;
+  a.part = nullptr;
+  uint32_t with = 0, without = 0;
+  return in_launches(a, t, n, kAdamwGroups, [&](AdamwDesc& d, const gws_adamw_tensor& o) -> uint32_t {
+    d.p = o.p;
+    d.w = (uint16_t*)o.w;
+    const double lr = s->lr * o.lr_scale;
+    d.keep = (float)(1.0 - lr * o.weight_decay);
+    d.rate = (float)(lr / c1);
+    d.seed_lo = (uint32_t)o.seed;
+    d.seed_hi = (uint32_t)(o.seed >> 32);
+    if (o.m8.codes) {
+      d.m = o.m8.codes; d.v = o.v8.codes; d.ms = o.m8.xscale; d.vs = o.v8.xscale;
+      d.lds = (uint32_t)o.m8.lds;
+      d.form |= kCodes;
+      return (uint32_t)(((uint64_t)o.cols + 31) / 32 * 8);
+    }
+    d.m = o.m; d.v = o.v;
+    return (uint32_t)(((uint64_t)o.cols + 3) / 4);
+  }, [&](uint32_t wgs) {
+    with = without = 0;
+    for (int i = 0; i < kAdamwTensors && a.begin[i] != 0x7FFFFFFFu; ++i) (a.t[i].form & kCodes ? with : without) += 1;
+    return launch_adamw(a, wgs, with == 0 ? 0 : without == 0 ? 2 : 1, (hipStream_t)stream);
+  });
+}
+
+size_t gws_grad_norm_workspace_bytes(const gws_adamw_tensor* t, int n) {
+  uint64_t wgs = 0;
+  for (int i = 0; t && i < n; ++i) wgs += norm_wgs(t[i]);
+  return (size_t)(wgs * sizeof(double) + 15) & ~(size_t)15;
+}
+
+int gws_grad_norm(const gws_adamw_tensor* t, int n, double max_norm, float* out, void* workspace, size_t workspace_bytes, void* stream) {
+  if (n < 0) return GWS_ERR_SHAPE;
+  if (!out || (n > 0 && !t)) return GWS_ERR_NULL;
+  if (!aligned(out, 4)) return GWS_ERR_ALIGN;
+  if (!(max_norm <= 0.0) && !isfinite(max_norm)) return GWS_ERR_FORMAT;
+  for (int i = 0; i < n; ++i) {
+    const int rc = check_gradient(t[i]);
+    if (rc != GWS_OK) return rc;
+  }
+  const size_t need = gws_grad_norm_workspace_bytes(t, n);
+  if (need && !workspace) return GWS_ERR_NULL;
+  if (need && !aligned(workspace, 16)) return GWS_ERR_ALIGN;
+  if (need && workspace_bytes < need) return GWS_ERR_SHAPE;
+  const Span2 ws = span_bytes(need ? workspace : nullptr, need), to = span_f32(out, 2);
+  if (!apart(ws, to)) return GWS_ERR_ALIAS;
+  for (int i = 0; i < n; ++i)
+    if (t[i].rows > 0 && t[i].cols > 0 && (!apart(gradient_span(t[i]), ws) || !apart(gradient_span(t[i]), to))) return GWS_ERR_ALIAS;
+  AdamwArgs a;
+  memset(&a, 0, sizeof a);
+  a.part = (double*)workspace;
+  uint64_t total = 0;
+  const int rc = in_launches(a, t, n, kNormGroups, [&](AdamwDesc&, const gws_adamw_tensor& o) -> uint32_t { return (uint32_t)(((uint64_t)o.cols + 7) / 8); },
+                             [&](uint32_t wgs) {
+                               const int r = launch_grad_squares(a, wgs, (hipStream_t)stream);
+                               a.part += wgs;
+                               total += wgs;
+                               return r;
+                             });
+  return rc != GWS_OK ? rc : launch_grad_norm((const double*)workspace, total, max_norm, out, (hipStream_t)stream);
+}
+
+}  // extern "C"

@@ -1,0 +1,460 @@
+// Layer norm and root-mean-square norm, forward and backward (gfx950).
+//
+// One pass over memory: a row is in the registers of W wavefronts, 8 V columns a lane, from its load to its store; mean, squares of the deviations
+// and, backward, sum(t) and sum(t n) are sums over lanes (DPP) and, with W > 1, over the wavefronts through LDS.  The variance is the sum of (x - mean)^2,
+// not the difference of two sums: the row is there, and nothing cancels.
+// dgamma and dbeta are sums over the rows: every lane adds up its own columns over the rows that its wavefronts take, the workgroup's rows meet in
+// LDS, and what workgroups leave is added by a second kernel, always in one order.
+#include "gws_norm.h"
+
+namespace gws {
+
+namespace {
+
+// Sums of N values over the W wavefronts of a team, in every lane; `red` holds 2 x N x (wavefronts of the workgroup) floats.  With W > 1 all of the
+// workgroup comes here, and the two halves of `red` alternate, so that one barrier a sum is enough.
+template <int W, int N>
+__device__ __forceinline__ void team_sum(float (&v)[N], float* red, uint32_t& turn) {
+#pragma unroll
+  for (int n = 0; n < N; ++n) v[n] = wave_sum(v[n]);
+  if (W == 1) return;
+  const uint32_t waves = blockDim.x >> 6, wave = threadIdx.x >> 6, first = wave / W * W;
+  float* half = red + turn * N * waves;
+  turn ^= 1;
+  if ((threadIdx.x & 63) == 0)
+#pragma unroll
+    for (int n = 0; n < N; ++n) half[n * waves + wave] = v[n];
+  __syncthreads();
+#pragma unroll
+  for (int n = 0; n < N; ++n) {
+    float s = half[n * waves + first];
+#pragma unroll
+    for (int w = 1; w < W; ++w) s += half[n * waves + first + w];
+    v[n] = s;
+  }
+}
+
+}  // namespace
+
+// A row's mean and rstd, and its deviations in f; times `unit` the numbers stay what they are, for rows whose squares would pass fp32's range (beyond 10^19 or
+// so) 2^-80 of them.
+constexpr float kSmallUnit = 0x1p-80f;
+template <int W, int V, bool RMS>
+__device__ __forceinline__ void row_statistics(const NormArgs& a, const GWS_GLOBAL uint16_t* x, uint32_t lane, float unit, float (&f)[V][8], float& mean, float& rstd,
+                                               float* red, uint32_t& turn) {
+  const float count = (float)a.C;
+#pragma unroll
+  for (int k = 0; k < V; ++k) {
+    widen(load_eight(x, (lane + k * 64 * W) * 8, a.C), f[k]);
+    if (unit != 1.0f)
+#pragma unroll
+      for (int e = 0; e < 8; ++e) f[k][e] *= unit;
+  }
+  mean = 0.0f;
+  if (!RMS) {
+    float s[1] = {0.0f};
+#pragma unroll
+    for (int k = 0; k < V; ++k)
+#pragma unroll
+      for (int e = 0; e < 8; ++e) s[0] += f[k][e];
+    team_sum<W>(s, red, turn);
+    mean = s[0] / count;
+#pragma unroll
+    for (int k = 0; k < V; ++k) {
+      const uint32_t c = (lane + k * 64 * W) * 8;
+      if (c + 8 <= a.C) {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) f[k][e] -= mean;
+      } else {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) f[k][e] = c + e < a.C ? f[k][e] - mean : 0.0f;
+      }
+    }
+  }
+  float q[1] = {0.0f};
+#pragma unroll
+  for (int k = 0; k < V; ++k)
+#pragma unroll
+    for (int e = 0; e < 8; ++e) q[0] = __fmaf_rn(f[k][e], f[k][e], q[0]);
+  team_sum<W>(q, red, turn);
+  rstd = 1.0f / sqrtf(q[0] / count + a.eps * unit * unit);
+}
+// A sum of squares past fp32's range leaves 0 (or NaN where the mean was past it too): such a row is done again in the small unit.
+__device__ __forceinline__ bool out_of_range(float rstd) { return !(rstd > 0.0f); }
+
+// W wavefronts a row, V groups of eight columns a lane, R rows a workgroup at a time.
+template <int W, int V, int R, bool RMS>
+__global__ __launch_bounds__(64 * W * R) void norm_fwd_kernel(const NormArgs a) {
+  static_assert(W == 1 || R == 1, "all of a workgroup does a row again, or wavefronts that share nothing");
+  __shared__ float red[2 * W * R];
+  const uint32_t team = threadIdx.x / (64 * W), lane = threadIdx.x % (64 * W);
+  uint32_t turn = 0;
+  float gamma[V][8], beta[V][8];
+#pragma unroll
+  for (int k = 0; k < V; ++k) {
+    vector_eight(a.gamma, (lane + k * 64 * W) * 8, a.C, 1.0f, gamma[k]);
+    vector_eight(a.beta, (lane + k * 64 * W) * 8, a.C, 0.0f, beta[k]);
+  }
+  for (uint32_t row = blockIdx.x * R + team; row < a.M; row += gridDim.x * R) {
+    const GWS_GLOBAL uint16_t* x = global_ptr<uint16_t>(a.x) + (size_t)row * a.ldx;
+    float f[V][8], mean, rstd, kept_mean, kept_rstd;
+    row_statistics<W, V, RMS>(a, x, lane, 1.0f, f, mean, rstd, red, turn);
+    kept_mean = mean;
+    kept_rstd = rstd;
+    if (out_of_range(rstd)) {   // the same in all lanes of a row
+      row_statistics<W, V, RMS>(a, x, lane, kSmallUnit, f, mean, rstd, red, turn);
+      kept_mean = mean / kSmallUnit;
+      kept_rstd = rstd * kSmallUnit;
+    }
+    if (lane == 0) {
+      if (a.mean != nullptr) a.mean[row] = kept_mean;
+      if (a.rstd != nullptr) a.rstd[row] = kept_rstd;
+    }
+    GWS_GLOBAL uint16_t* y = global_ptr<uint16_t>(a.y) + (size_t)row * a.ldy;
+#pragma unroll
+    for (int k = 0; k < V; ++k) {
+      float o[8];
+#pragma unroll
+      for (int e = 0; e < 8; ++e) o[e] = __fmaf_rn(f[k][e] * rstd, gamma[k][e], beta[k][e]);
+      store_eight(y, (lane + k * 64 * W) * 8, a.C, narrow(o));
+    }
+  }
+}
+
+// Rows of any length: the row is read three times (out of the caches).
+template <bool RMS>
+__global__ __launch_bounds__(1024) void norm_fwd_wide_kernel(const NormArgs a) {
+  __shared__ float red[2 * 16];
+  uint32_t turn = 0;
+  const uint32_t row = blockIdx.x;
+  const GWS_GLOBAL uint16_t* x = global_ptr<uint16_t>(a.x) + (size_t)row * a.ldx;
+  const float count = (float)a.C;
+  float mean, rstd, unit = 1.0f;
+  for (;;) {
+    mean = 0.0f;
+    if (!RMS) {
+      float s[1] = {0.0f};
+      for (uint32_t c = threadIdx.x * 8; c < a.C; c += 8192) {
+        float f[8], t = 0.0f;
+        widen(load_eight(x, c, a.C), f);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) t += f[e] * unit;
+        s[0] += t;
+      }
+      team_sum<16>(s, red, turn);
+      mean = s[0] / count;
+    }
+    float q[1] = {0.0f};
+    for (uint32_t c = threadIdx.x * 8; c < a.C; c += 8192) {
+      float f[8], t = 0.0f;
+      widen(load_eight(x, c, a.C), f);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        const float d = f[e] * unit - mean;
+        t = c + e < a.C ? __fmaf_rn(d, d, t) : t;
+      }
+      q[0] += t;
+    }
+    team_sum<16>(q, red, turn);
+    rstd = 1.0f / sqrtf(q[0] / count + a.eps * unit * unit);
+    if (!out_of_range(rstd) || unit != 1.0f) break;   // the same in all threads
+    unit = kSmallUnit;
+  }
+  if (threadIdx.x == 0) {
+    if (a.mean != nullptr) a.mean[row] = mean / unit;
+    if (a.rstd != nullptr) a.rstd[row] = rstd * unit;
+  }
+  GWS_GLOBAL uint16_t* y = global_ptr<uint16_t>(a.y) + (size_t)row * a.ldy;
+  for (uint32_t c = threadIdx.x * 8; c < a.C; c += 8192) {
+    float f[8], gamma[8], beta[8];
+    widen(load_eight(x, c, a.C), f);
+    vector_eight(a.gamma, c, a.C, 1.0f, gamma);
+    vector_eight(a.beta, c, a.C, 0.0f, beta);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) f[e] = __fmaf_rn((f[e] * unit - mean) * rstd, gamma[e], beta[e]);
+    store_eight(y, c, a.C, narrow(f));
+  }
+}
+
+// n = (x - mean) rstd by halves: x - mean itself may pass fp32's range.
+struct Normalise {
+  float half_mean, twice_rstd;
+  __device__ __forceinline__ Normalise(float mean, float rstd) : half_mean(0.5f * mean), twice_rstd(2.0f * rstd) {}
+  __device__ __forceinline__ float operator()(float x) const { return __fmaf_rn(x, 0.5f, -half_mean) * twice_rstd; }
+};
+
+// Backward.  n = (x - mean) rstd and t = dY gamma of a row; dgamma and dbeta of the lane's columns over the workgroup's rows.
+template <int W, int V, int R, bool RMS>
+__global__ __launch_bounds__(64 * W * R) void norm_bwd_kernel(const NormArgs a) {
+  __shared__ float red[4 * W * R];
+  __shared__ float sums[R == 1 ? 1 : R * W * V * 512];
+  const uint32_t team = threadIdx.x / (64 * W), lane = threadIdx.x % (64 * W);
+  uint32_t turn = 0;
+  float gamma[V][8], dgamma[V][8], dbeta[V][8];
+#pragma unroll
+  for (int k = 0; k < V; ++k) {
+    vector_eight(a.gamma, (lane + k * 64 * W) * 8, a.C, 1.0f, gamma[k]);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) dgamma[k][e] = dbeta[k][e] = 0.0f;
+  }
+  const float count = (float)a.C;
+  for (uint32_t row0 = blockIdx.x * R; row0 < a.M; row0 += gridDim.x * R) {
+    const uint32_t row = row0 + team;
+    const bool live = row < a.M;
+    if (W == 1 && !live) break;
+    const size_t at = live ? row : row0;
+    const GWS_GLOBAL uint16_t *x = global_ptr<uint16_t>(a.x) + at * a.ldx, *dy = global_ptr<uint16_t>(a.dy) + at * a.lddy;
+    u32x4 xr[V], yr[V], rr[V];
+#pragma unroll
+    for (int k = 0; k < V; ++k) {
+      xr[k] = load_eight(x, (lane + k * 64 * W) * 8, a.C);
+      yr[k] = load_eight(dy, (lane + k * 64 * W) * 8, a.C);
+      if (a.r != nullptr) rr[k] = load_eight(global_ptr<uint16_t>(a.r) + at * a.ldr, (lane + k * 64 * W) * 8, a.C);
+    }
+    const float rstd = a.rstd[at];
+    const Normalise normal(RMS ? 0.0f : a.mean[at], rstd);
+    float s[2] = {0.0f, 0.0f};
+#pragma unroll
+    for (int k = 0; k < V; ++k) {   // columns past the row have dY = 0: they add nothing
+      float n[8], d[8];
+      widen(xr[k], n);
+      widen(yr[k], d);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        n[e] = normal(n[e]);
+        const float t = d[e] * gamma[k][e];
+        s[0] += t;
+        s[1] = __fmaf_rn(t, n[e], s[1]);
+        if (live) {
+          dbeta[k][e] += d[e];
+          dgamma[k][e] = __fmaf_rn(d[e], n[e], dgamma[k][e]);
+        }
+      }
+    }
+    team_sum<W>(s, red, turn);
+    if (!live) continue;
+    const float s0 = RMS ? 0.0f : s[0] / count, s1 = s[1] / count;
+    GWS_GLOBAL uint16_t* dx = global_ptr<uint16_t>(a.y) + at * a.ldy;
+#pragma unroll
+    for (int k = 0; k < V; ++k) {
+      float n[8], d[8], o[8], r[8];
+      widen(xr[k], n);
+      widen(yr[k], d);
+      if (a.r != nullptr) widen(rr[k], r);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        n[e] = normal(n[e]);
+        o[e] = (__fmaf_rn(d[e], gamma[k][e], -s0) - n[e] * s1) * rstd;
+        if (a.r != nullptr) o[e] += r[e];
+      }
+      store_eight(dx, (lane + k * 64 * W) * 8, a.C, narrow(o));
+    }
+  }
+  // the workgroup's sums: its R teams' in turn
+  float* part = a.part + (size_t)blockIdx.x * ((a.want_gamma ? 1 : 0) + (a.want_beta ? 1 : 0)) * a.C;
+#pragma unroll
+  for (int which = 0; which < 2; ++which) {
+    if (which == 0 ? !a.want_gamma : !a.want_beta) continue;
+    float(&mine)[V][8] = which == 0 ? dgamma : dbeta;
+    if (R > 1) {
+      __syncthreads();
+#pragma unroll
+      for (int k = 0; k < V; ++k)
+#pragma unroll
+        for (int e = 0; e < 8; e += 4) *(f4*)(sums + team * (W * V * 512) + (lane + k * 64 * W) * 8 + e) = f4{mine[k][e], mine[k][e + 1], mine[k][e + 2], mine[k][e + 3]};
+      __syncthreads();
+      for (uint32_t c = threadIdx.x; c < a.C; c += 64 * W * R) {
+        float s = sums[c];
+#pragma unroll
+        for (int t = 1; t < R; ++t) s += sums[t * (W * V * 512) + c];
+        part[c] = s;
+      }
+    } else {
+#pragma unroll
+      for (int k = 0; k < V; ++k)
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+          const uint32_t c = (lane + k * 64 * W) * 8 + e;
+          if (c < a.C) part[c] = mine[k][e];
+        }
+    }
+    part += a.C;
+  }
+}
+
+// Rows of any length, in two steps: sum(t) / C and sum(t n) / C of every row; then dX by pieces of 2048 columns, with dgamma and dbeta of them.
+template <bool RMS>
+__global__ __launch_bounds__(1024) void norm_bwd_rows_kernel(const NormArgs a) {
+  __shared__ float red[4 * 16];
+  uint32_t turn = 0;
+  const uint32_t row = blockIdx.x;
+  const GWS_GLOBAL uint16_t *x = global_ptr<uint16_t>(a.x) + (size_t)row * a.ldx, *dy = global_ptr<uint16_t>(a.dy) + (size_t)row * a.lddy;
+  const Normalise normal(RMS ? 0.0f : a.mean[row], a.rstd[row]);
+  float s[2] = {0.0f, 0.0f};
+  for (uint32_t c = threadIdx.x * 8; c < a.C; c += 8192) {
+    float n[8], d[8], gamma[8], s0 = 0.0f, s1 = 0.0f;
+    widen(load_eight(x, c, a.C), n);
+    widen(load_eight(dy, c, a.C), d);
+    vector_eight(a.gamma, c, a.C, 1.0f, gamma);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      const float t = d[e] * gamma[e];
+      s0 += t;
+      s1 = __fmaf_rn(t, normal(n[e]), s1);
+    }
+    s[0] += s0;
+    s[1] += s1;
+  }
+  team_sum<16>(s, red, turn);
+  if (threadIdx.x == 0) {
+    a.rows[2 * (size_t)row] = RMS ? 0.0f : s[0] / (float)a.C;
+    a.rows[2 * (size_t)row + 1] = s[1] / (float)a.C;
+  }
+}
+
+template <bool RMS>
+__global__ __launch_bounds__(256) void norm_bwd_columns_kernel(const NormArgs a) {
+  const uint32_t c = (blockIdx.x * 256 + threadIdx.x) * 8;
+  float gamma[8], dgamma[8], dbeta[8];
+  vector_eight(a.gamma, c, a.C, 1.0f, gamma);
+#pragma unroll
+  for (int e = 0; e < 8; ++e) dgamma[e] = dbeta[e] = 0.0f;
+  for (uint32_t row = blockIdx.y; row < a.M; row += gridDim.y) {
+    float n[8], d[8], o[8], r[8] = {0, 0, 0, 0, 0, 0, 0, 0};
+    widen(load_eight(global_ptr<uint16_t>(a.x) + (size_t)row * a.ldx, c, a.C), n);
+    widen(load_eight(global_ptr<uint16_t>(a.dy) + (size_t)row * a.lddy, c, a.C), d);
+    if (a.r != nullptr) widen(load_eight(global_ptr<uint16_t>(a.r) + (size_t)row * a.ldr, c, a.C), r);
+    const float rstd = a.rstd[row];
+    const Normalise normal(RMS ? 0.0f : a.mean[row], rstd);
+    const float s0 = a.rows[2 * (size_t)row], s1 = a.rows[2 * (size_t)row + 1];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      n[e] = normal(n[e]);
+      dbeta[e] += d[e];
+      dgamma[e] = __fmaf_rn(d[e], n[e], dgamma[e]);
+      o[e] = (__fmaf_rn(d[e], gamma[e], -s0) - n[e] * s1) * rstd;
+      if (a.r != nullptr) o[e] += r[e];
+    }
+    store_eight(global_ptr<uint16_t>(a.y) + (size_t)row * a.ldy, c, a.C, narrow(o));
+  }
+  float* part = a.part + (size_t)blockIdx.y * ((a.want_gamma ? 1 : 0) + (a.want_beta ? 1 : 0)) * a.C;
+#pragma unroll
+  for (int e = 0; e < 8; ++e) {
+    if (c + e >= a.C) break;
+    if (a.want_gamma) part[c + e] = dgamma[e];
+    if (a.want_beta) part[(a.want_gamma ? a.C : 0) + c + e] = dbeta[e];
+  }
+}
+
+// ---- sums of partial sums ----
+// A workgroup adds 64 columns, 16 lanes x 4 of them side by side and the P rows shared by 16 groups of lanes, whose sums meet in LDS.
+__global__ __launch_bounds__(256) void sum_partials_kernel(const float* part, const uint32_t P, const uint64_t n, const uint64_t n0, float* out0, float* out1) {
+  __shared__ f4 red[16][16];
+  const uint32_t group = threadIdx.x >> 4, at = threadIdx.x & 15;
+  const uint64_t c = (uint64_t)blockIdx.x * 64 + 4 * at;
+  f4 s = {0.0f, 0.0f, 0.0f, 0.0f};
+  for (uint32_t p = group; p < P; p += 16) {
+    const float* q = part + p * n + c;
+    if (c + 4 <= n) {
+      s += *(const GWS_GLOBAL f4_any*)global_ptr<float>(q);
+    } else {
+#pragma unroll
+      for (int e = 0; e < 3; ++e)
+        if (c + e < n) s[e] += q[e];
+    }
+  }
+  red[group][at] = s;
+  __syncthreads();
+  if (threadIdx.x >= 64) return;
+  const float* r = (const float*)red;
+  float t = r[threadIdx.x];
+#pragma unroll
+  for (int g = 1; g < 16; ++g) t += r[64 * g + threadIdx.x];
+  const uint64_t col = (uint64_t)blockIdx.x * 64 + threadIdx.x;
+  if (col < n0) out0[col] = t;
+  else if (col < n) out1[col - n0] = t;
+}
+
+int launch_sum_partials(const float* part, uint32_t P, uint64_t n, uint64_t n0, float* out0, float* out1, hipStream_t stream) {
+  hipLaunchKernelGGL(sum_partials_kernel, dim3((uint32_t)((n + 63) / 64)), dim3(256), 0, stream, part, P, n, n0, out0, out1);
+  return hipGetLastError() == hipSuccess ? GWS_OK : GWS_ERR_LAUNCH;
+}
+
+__global__ __launch_bounds__(256) void zero_kernel(float* p, const uint64_t n) {
+  const uint64_t i = (uint64_t)blockIdx.x * 256 + threadIdx.x;
+  if (i < n) p[i] = 0.0f;
+}
+int launch_zero(float* p, uint64_t n, hipStream_t stream) {
+  hipLaunchKernelGGL(zero_kernel, dim3((uint32_t)((n + 255) / 256)), dim3(256), 0, stream, p, n);
+  return hipGetLastError() == hipSuccess ? GWS_OK : GWS_ERR_LAUNCH;
+}
+
+// ---- launches ----
+constexpr uint64_t kWide = 16384;
+bool norm_is_wide(uint64_t C) { return C > kWide; }
+
+namespace {
+uint32_t cus() { return compute_units() > 0 ? (uint32_t)compute_units() : 256; }
+uint32_t fewer(uint64_t a, uint64_t b) { return (uint32_t)(a < b ? a : b); }
+
+template <int W, int V, int R>
+int fwd(const NormArgs& a, bool rms, hipStream_t s) {
+  const dim3 grid(fewer(((uint64_t)a.M + R - 1) / R, 8 * cus())), block(64 * W * R);
+  if (rms) hipLaunchKernelGGL((norm_fwd_kernel<W, V, R, true>), grid, block, 0, s, a);
+  else hipLaunchKernelGGL((norm_fwd_kernel<W, V, R, false>), grid, block, 0, s, a);
+  return hipGetLastError() == hipSuccess ? GWS_OK : GWS_ERR_LAUNCH;
+}
+template <int W, int V, int R>
+int bwd(const NormArgs& a, bool rms, hipStream_t s) {
+  const dim3 grid(norm_bwd_parts(a.M, a.C)), block(64 * W * R);
+  if (rms) hipLaunchKernelGGL((norm_bwd_kernel<W, V, R, true>), grid, block, 0, s, a);
+  else hipLaunchKernelGGL((norm_bwd_kernel<W, V, R, false>), grid, block, 0, s, a);
+  return hipGetLastError() == hipSuccess ? GWS_OK : GWS_ERR_LAUNCH;
+}
+// Rows a workgroup of the backward kernels takes at a time.
+uint32_t bwd_rows(uint64_t C) { return C <= 2048 ? 8 : C <= 8192 ? 2 : 1; }
+}  // namespace
+
+int launch_norm_fwd(const NormArgs& a, bool rms, hipStream_t s) {
+  if (norm_is_wide(a.C)) {
+    if (rms) hipLaunchKernelGGL(norm_fwd_wide_kernel<true>, dim3(a.M), dim3(1024), 0, s, a);
+    else hipLaunchKernelGGL(norm_fwd_wide_kernel<false>, dim3(a.M), dim3(1024), 0, s, a);
+    return hipGetLastError() == hipSuccess ? GWS_OK : GWS_ERR_LAUNCH;
+  }
+  if (a.C <= 512) return fwd<1, 1, 4>(a, rms, s);
+  if (a.C <= 1024) return fwd<1, 2, 4>(a, rms, s);
+  if (a.C <= 2048) return fwd<1, 4, 4>(a, rms, s);
+  if (a.C <= 4096) return fwd<4, 2, 1>(a, rms, s);
+  if (a.C <= 8192) return fwd<4, 4, 1>(a, rms, s);
+  return fwd<8, 4, 1>(a, rms, s);
+}
+
+uint32_t norm_bwd_parts(uint64_t M, uint64_t C) {
+  if (norm_is_wide(C)) return fewer(M, 64);
+  return fewer((M + bwd_rows(C) - 1) / bwd_rows(C), cus());
+}
+
+int launch_norm_bwd(const NormArgs& a, bool rms, float* dgamma, float* dbeta, hipStream_t s) {
+  int rc;
+  if (norm_is_wide(a.C)) {
+    const dim3 pieces((uint32_t)(((uint64_t)a.C + 2047) / 2048), norm_bwd_parts(a.M, a.C));
+    if (rms) {
+      hipLaunchKernelGGL(norm_bwd_rows_kernel<true>, dim3(a.M), dim3(1024), 0, s, a);
+      hipLaunchKernelGGL(norm_bwd_columns_kernel<true>, pieces, dim3(256), 0, s, a);
+    } else {
+      hipLaunchKernelGGL(norm_bwd_rows_kernel<false>, dim3(a.M), dim3(1024), 0, s, a);
+      hipLaunchKernelGGL(norm_bwd_columns_kernel<false>, pieces, dim3(256), 0, s, a);
+    }
+    rc = hipGetLastError() == hipSuccess ? GWS_OK : GWS_ERR_LAUNCH;
+  } else if (a.C <= 512) rc = bwd<1, 1, 8>(a, rms, s);
+  else if (a.C <= 1024) rc = bwd<1, 2, 8>(a, rms, s);
+  else if (a.C <= 2048) rc = bwd<1, 4, 8>(a, rms, s);
+  else if (a.C <= 4096) rc = bwd<4, 2, 2>(a, rms, s);
+  else if (a.C <= 8192) rc = bwd<4, 4, 2>(a, rms, s);
+  else rc = bwd<8, 4, 1>(a, rms, s);
+  if (rc != GWS_OK || (!a.want_gamma && !a.want_beta)) return rc;
+  const uint64_t n = a.want_gamma && a.want_beta ? 2 * (uint64_t)a.C : a.C;
+  return launch_sum_partials(a.part, norm_bwd_parts(a.M, a.C), n, a.C, a.want_gamma ? dgamma : dbeta, dbeta, s);
+}
+
+}  // namespace gws

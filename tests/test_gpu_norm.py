@@ -1,0 +1,205 @@
+"""Layer norm and root-mean-square norm, forward and backward, against 64 bits (bounds: layer_ref.py)."""
+import math
+
+import pytest
+import torch
+
+import layer_ref as ref
+import paper_2505_11170_amd as gws
+from gated_ref import assert_within
+from gpu_util import DEV, ensure_built
+from test_gpu_gated import rand, room
+
+pytestmark = pytest.mark.gpu
+LAYER, RMS = gws.NORM_LAYER, gws.NORM_RMS
+
+
+@pytest.fixture(scope="module", autouse=True)
+def _lib():
+    ensure_built()
+
+
+def vec(seed, n, mean=0.0, std=1.0):
+    gen = torch.Generator(device=DEV).manual_seed(seed)
+    return mean + std * torch.randn(n, generator=gen, device=DEV)
+
+
+def ld_of(C, wide=False):
+    return -(-C // 8) * 8 + (24 if wide else 0)
+
+
+def odd_start(v):
+    """The same vector from an address that is a multiple of four only."""
+    return torch.cat([torch.full((1,), math.nan, device=DEV), v])[1:]
+
+
+def untouched(whole, C):
+    return bool((whole[:, C:] == 7).all())
+
+
+# one lane's part of a row, a row of each width of kernel and one element to either side, rows that are read again
+SIZES = [(1, 1), (3, 7), (1, 2048), (5, 64), (2, 511), (300, 768), (7, 513), (3, 1025), (1021, 1000), (3, 2047), (9, 2049), (2, 4100), (5, 8192), (3, 8200),
+         (2, 16384), (2, 16385), (3, 40003)]
+
+
+@pytest.mark.parametrize("kind", [LAYER, RMS])
+@pytest.mark.parametrize("M,C", SIZES)
+def test_forward(M, C, kind):
+    wide = C % 2 == 1
+    x = rand(M + C, M, C, ld=ld_of(C, wide)) * 2 + 0.5
+    x = torch.nn.functional.pad(x, (0, ld_of(C, wide) - C), value=math.nan)[:, :C]
+    gamma, beta = odd_start(vec(1, C, 1.0, 0.2)), odd_start(vec(2, C, 0.0, 0.3))
+    (y, whole), mean, rstd = room(M, C, ld_of(C) + 8), torch.full((M,), math.nan, device=DEV), torch.full((M,), math.nan, device=DEV)
+    gws.gws_norm_fwd(x, y, kind, gamma=gamma, beta=beta, eps=1e-5, mean=mean if kind == LAYER else None, rstd=rstd)
+    want, tol = ref.norm_fwd(x, kind, gamma, beta, 1e-5)
+    assert_within(y, want[0], tol[0], "y")
+    assert_within(rstd, want[2], tol[2], "rstd")
+    if kind == LAYER:
+        assert_within(mean, want[1], tol[1], "mean")
+    assert untouched(whole, C)
+    # nothing kept, no gamma, no beta; the same numbers where they are the same
+    y2 = room(M, C, ld_of(C))[0]
+    gws.gws_norm_fwd(x, y2, kind, gamma=gamma, beta=beta, eps=1e-5)
+    assert torch.equal(y2, y)
+    gws.gws_norm_fwd(x, y2, kind)
+    want, tol = ref.norm_fwd(x, kind, None, None, 1e-5)
+    assert_within(y2, want[0], tol[0], "bare")
+
+
+@pytest.mark.parametrize("kind", [LAYER, RMS])
+@pytest.mark.parametrize("M,C", SIZES)
+def test_backward(M, C, kind):
+    wide = C % 2 == 0
+    ld = ld_of(C, wide)
+    x, dy, r = rand(1, M, C, 1.5, ld), rand(2, M, C, 1e-3, ld + 8), rand(3, M, C, 1e-3, ld_of(C))
+    gamma = odd_start(vec(4, C, 1.0, 0.2))
+    xd = x.double()
+    mean = xd.mean(1) if kind == LAYER else xd.new_zeros(M)
+    rstd = (1.0 / torch.sqrt(((xd - mean[:, None]) ** 2).mean(1) + 1e-5)).float()
+    mean = mean.float()
+    (dx, whole), dgamma, dbeta = room(M, C, ld_of(C) + 16), torch.full((C,), math.nan, device=DEV), torch.full((C,), math.nan, device=DEV)
+    ws = torch.full((gws.gws_norm_bwd_workspace_bytes(M, C) // 4,), math.nan, device=DEV)
+    kept = dict(kind=kind, mean=mean if kind == LAYER else None, gamma=gamma)
+    gws.gws_norm_bwd(dy, x, dx, rstd, residual=r, dgamma=dgamma, dbeta=dbeta, workspace=ws, **kept)
+    want, tol = ref.norm_bwd(dy, x, kind, gamma, mean, rstd, r)
+    for got, w, t, name in zip((dx, dgamma, dbeta), want, tol, ("dx", "dgamma", "dbeta")):
+        assert_within(got, w, t, name)
+    assert untouched(whole, C)
+    # one of the two sums alone, none, no residual; the same bits
+    one, dx2 = torch.full((C,), math.nan, device=DEV), room(M, C, ld_of(C))[0]
+    gws.gws_norm_bwd(dy, x, dx2, rstd, dbeta=one, workspace=ws, residual=r, **kept)
+    assert torch.equal(one, dbeta) and torch.equal(dx2, dx)
+    gws.gws_norm_bwd(dy, x, dx2, rstd, dgamma=one, workspace=ws, **kept)
+    assert torch.equal(one, dgamma)
+    want, tol = ref.norm_bwd(dy, x, kind, gamma, mean, rstd, None)
+    assert_within(dx2, want[0], tol[0], "without residual")
+    gws.gws_norm_bwd(dy, x, dx2, rstd, kind, mean=kept["mean"], workspace=ws if C > 16384 else None)
+    want, tol = ref.norm_bwd(dy, x, kind, None, mean, rstd, None)
+    assert_within(dx2, want[0], tol[0], "bare")
+
+
+def test_many_rows():
+    M, C = 20000, 96
+    x, dy = rand(1, M, C), rand(2, M, C, 1e-3)
+    y, mean, rstd = room(M, C)[0], torch.zeros(M, device=DEV), torch.zeros(M, device=DEV)
+    gws.gws_norm_fwd(x, y, mean=mean, rstd=rstd)
+    want, tol = ref.norm_fwd(x, LAYER, None, None, 1e-5)
+    assert_within(y, want[0], tol[0], "y")
+    dx, dgamma, dbeta = room(M, C)[0], torch.zeros(C, device=DEV), torch.zeros(C, device=DEV)
+    ws = torch.empty(gws.gws_norm_bwd_workspace_bytes(M, C), dtype=torch.uint8, device=DEV)
+    gws.gws_norm_bwd(dy, x, dx, rstd, mean=mean, dgamma=dgamma, dbeta=dbeta, workspace=ws)
+    want, tol = ref.norm_bwd(dy, x, LAYER, None, mean, rstd, None)
+    for got, w, t, name in zip((dx, dgamma, dbeta), want, tol, ("dx", "dgamma", "dbeta")):
+        assert_within(got, w, t, name)
+    first = [t.clone() for t in (dx, dgamma, dbeta)]
+    for _ in range(3):   # one order of all sums
+        gws.gws_norm_bwd(dy, x, dx, rstd, mean=mean, dgamma=dgamma, dbeta=dbeta, workspace=ws)
+        assert all(torch.equal(a, b) for a, b in zip(first, (dx, dgamma, dbeta)))
+
+
+@pytest.mark.parametrize("C", [768, 2048, 3000, 20000])
+def test_rows_at_the_edge_of_the_numbers(C):
+    """A far common offset, constant rows, zeros, the largest and smallest values; rows of NaN or infinity stay by themselves."""
+    x = rand(5, 12, C)
+    x[0] = (x[0].float() * 0.5 + 300.0).bfloat16()
+    x[1], x[2] = 3.0, 0.0
+    x[3] = (x[3].float() * 1e18).bfloat16()
+    x[4] = (x[4].float() * 1e-30).bfloat16()
+    x[6, C // 2], x[8, C - 1], x[10, 0] = math.nan, math.inf, -math.inf
+    for kind in (LAYER, RMS):
+        y, mean, rstd = room(12, C)[0], torch.zeros(12, device=DEV), torch.zeros(12, device=DEV)
+        gws.gws_norm_fwd(x, y, kind, mean=mean if kind == LAYER else None, rstd=rstd)
+        want, tol = ref.norm_fwd(x, kind, None, None, 1e-5)
+        good = [i for i in range(12) if i not in (6, 8, 10)]
+        assert_within(y[good], want[0][good], tol[0][good], kind)
+        assert torch.isnan(y[6]).all() and torch.isnan(y[8, C - 1]) and torch.isnan(y[10, 0])
+        assert (y[2] == 0).all() and rstd[2] == torch.tensor(1.0) / torch.sqrt(torch.tensor(1e-5))
+        if kind == LAYER:
+            assert (y[1] == 0).all()
+        dy, dx = rand(6, 12, C), room(12, C)[0]
+        dy[4, 1] = math.nan
+        bad = (4, 6, 8, 10)
+        ws = torch.empty(gws.gws_norm_bwd_workspace_bytes(12, C), dtype=torch.uint8, device=DEV)
+        gws.gws_norm_bwd(dy, x, dx, rstd, kind, mean=mean, workspace=ws)
+        want, tol = ref.norm_bwd(dy, x, kind, None, mean, rstd, None)
+        good = [i for i in range(12) if i not in bad]
+        assert_within(dx[good], want[0][good], tol[0][good], kind)
+        assert torch.isnan(dx[4]).all() and torch.isnan(dx[6]).all()
+
+
+@pytest.mark.parametrize("C", [100, 1000, 5000, 17000])
+def test_in_place(C):
+    M = 37
+    x, dy, r = rand(1, M, C, ld=ld_of(C)), rand(2, M, C, ld=ld_of(C)), rand(3, M, C, ld=ld_of(C))
+    y, mean, rstd = room(M, C, ld_of(C))[0], torch.zeros(M, device=DEV), torch.zeros(M, device=DEV)
+    gws.gws_norm_fwd(x, y, mean=mean, rstd=rstd)
+    same = torch.nn.functional.pad(x, (0, ld_of(C) - C))[:, :C]
+    gws.gws_norm_fwd(same, same)
+    assert torch.equal(same, y)
+    ws = torch.empty(gws.gws_norm_bwd_workspace_bytes(M, C), dtype=torch.uint8, device=DEV)
+    dx = room(M, C, ld_of(C))[0]
+    gws.gws_norm_bwd(dy, x, dx, rstd, mean=mean, residual=r, workspace=ws)
+    for k in range(3):
+        a = [torch.nn.functional.pad(t, (0, ld_of(C) - C))[:, :C] for t in (dy, x, r)]
+        gws.gws_norm_bwd(a[0], a[1], a[k], rstd, mean=mean, residual=a[2], workspace=ws)
+        assert torch.equal(a[k], dx)
+
+
+def test_gradients_against_differences():
+    """d(sum of dY y) along random directions of x, gamma and beta, from the 64-bit definition."""
+    M, C, h = 6, 200, 1e-4
+    for kind in (LAYER, RMS):
+        x, dy = rand(1, M, C).double(), rand(2, M, C).double()
+        gamma, beta = vec(3, C, 1.0, 0.2).double(), vec(4, C).double()
+        f = lambda x, gamma, beta: (ref.norm_fwd(x, kind, gamma, beta, 1e-5)[0][0] * dy).sum()  # noqa: E731
+        (_, mean, rstd), _ = ref.norm_fwd(x, kind, gamma, beta, 1e-5)
+        dx, dgamma, dbeta = room(M, C)[0], torch.zeros(C, device=DEV), torch.zeros(C, device=DEV)
+        ws = torch.empty(gws.gws_norm_bwd_workspace_bytes(M, C), dtype=torch.uint8, device=DEV)
+        gws.gws_norm_bwd(dy.bfloat16(), x.bfloat16(), dx, rstd.float(), kind, mean=mean.float(), gamma=gamma.float(), dgamma=dgamma, dbeta=dbeta, workspace=ws)
+        for grad, at in ((dx, 0), (dgamma, 1), (dbeta, 2)):
+            u = torch.randn(grad.shape, generator=torch.Generator(device=DEV).manual_seed(9), device=DEV).double()
+            args = [x, gamma, beta]
+            slope = (f(*[a + h * u if i == at else a for i, a in enumerate(args)]) - f(*[a - h * u if i == at else a for i, a in enumerate(args)])) / (2 * h)
+            # dX rounded to BF16; a third derivative of order 10 times h^2
+            assert abs((grad.double() * u).sum() - slope) <= (ref.BF16 if at == 0 else 1e-5) * (grad.double() * u).abs().sum() + 1e-4
+
+
+def test_no_rows():
+    x, e = torch.zeros(0, 64, dtype=torch.bfloat16, device=DEV), torch.zeros(0, device=DEV)
+    gws.gws_norm_fwd(x, x, mean=e, rstd=e)
+    dgamma, dbeta = torch.full((64,), 3.0, device=DEV), torch.full((64,), 3.0, device=DEV)
+    gws.gws_norm_bwd(x, x, x, e, mean=e, dgamma=dgamma, dbeta=dbeta)
+    assert (dgamma == 0).all() and (dbeta == 0).all()
+
+
+def test_offsets_past_32_bits():
+    """Rows that lie beyond 4 GiB of elements of a wide buffer."""
+    M, C, ld = 35, 100, 1 << 27                      # 35 x 2^27 elements x 2 bytes: 9.4 GB
+    if torch.cuda.mem_get_info()[0] < 30 << 30:
+        pytest.skip("no room")
+    buf = torch.empty(M, ld, dtype=torch.bfloat16, device=DEV)
+    x, y = buf[:, :C], buf[:, 128:128 + C]
+    x.copy_(rand(1, M, C))
+    gws.gws_norm_fwd(x, y)
+    want, tol = ref.norm_fwd(x, LAYER, None, None, 1e-5)
+    assert_within(y, want[0], tol[0], "y")
