@@ -18,9 +18,9 @@ _ROOT = os.path.dirname(_HERE)
 CSRC = os.path.join(_HERE, "csrc")
 SOURCES = ["gws_api.hip", "gws_sample.hip", "gws_linear.hip", "gws_gemm_stream.hip", "gws_gemm_stream_tn.hip", "gws_gemm128.hip", "gws_gemm256.hip", "gws_gemm256_tn.hip",
            "gws_gated_api.hip", "gws_gated.hip", "gws_gated256.hip", "gws_gated128.hip", "gws_gated_stream.hip", "gws_act8.hip",
-           "gws_layer_api.hip", "gws_norm.hip", "gws_dense.hip", "gws_adamw.hip"]
+           "gws_layer_api.hip", "gws_norm.hip", "gws_dense.hip", "gws_dense128.hip", "gws_dense256.hip", "gws_dense_stream.hip", "gws_adamw.hip"]
 HEADERS = ["gws_device.h", "gws_launch.h", "gws_sample_tile.h", "gws_gemm256_core.h", "gws_gemm_stream_core.h", "gws_check.h", "gws_gated.h", "gws_gated_out.h",
-           "gws_norm.h", "gws_dense.h", "gws_adamw.h"]
+           "gws_norm.h", "gws_dense.h", "gws_dense_out.h", "gws_adamw.h", "gws_gemm128_core.h", "gws_gemm_stream_kernel.h"]
 OUT = os.path.join(_HERE, "libgws.so")
 
 FLAGS = ["-O3", "--offload-arch=gfx950", "-fPIC", "-std=c++17", "-ffp-contract=off",

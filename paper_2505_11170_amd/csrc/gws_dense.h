@@ -17,8 +17,14 @@ struct DenseArgs {
   float* part;            // may be NULL
   uint32_t ldr, ldz, ldh;
   int act;
+  bool past_caches;       // forward: Y, backward: dZ and H, of the large tiles
 };
 enum class DenseOp { kFwd = 0, kBwd = 1 };
+// The way out of a product's kernels (gws_dense_out.h).
+template <DenseOp OP>
+struct DenseWay {
+  DenseArgs d;
+};
 
 // The activation that is none.
 struct NoGate {
@@ -35,6 +41,17 @@ __device__ __forceinline__ void with_act(int act, F&& f) {   // a uniform branch
 }
 inline bool known_dense_act(int act) { return act == GWS_ACT_NONE || known_act(act); }
 
+// Which kernel, and how many rows of the result one row of partial sums stands for.
+struct DensePlan {
+  GemmForm form;         // kAnyShape: dense_any_kernel
+  RoutePlan route;
+  uint32_t rows;
+};
+DensePlan plan_dense(const GemmArgs& g, const DenseArgs& d, int w_is_nk);
+// 256 x 256 tiles (whole, or with edges), 256 x 192
+int launch_dense256(const GemmArgs& g, const DenseArgs& d, DenseOp op, int w_is_nk, GemmForm form, hipStream_t stream);
+int launch_dense128(const GemmArgs& g, const DenseArgs& d, DenseOp op, int w_is_nk, int nj, hipStream_t stream);
+int launch_dense_stream(const GemmArgs& g, const DenseArgs& d, DenseOp op, int w_is_nk, const StreamPlan& p, hipStream_t stream);
 // every size
 int launch_dense_any(const GemmArgs& g, const DenseArgs& e, DenseOp op, int w_is_nk, hipStream_t stream);
 constexpr uint32_t kDenseAnyRows = 64;   // of its tiles, for the partial sums

@@ -6,7 +6,7 @@
 #include "gws_adamw.h"
 #include "gws_bench.h"
 #include "gws_check.h"
-#include "gws_dense.h"
+#include "gws_dense_out.h"
 #include "gws_norm.h"
 
 namespace gws {
@@ -58,8 +58,16 @@ int with_bias_gradient(const GemmArgs& g, DenseArgs& d, uint64_t rows, float* db
   return launch_sum_partials(d.part, (uint32_t)parts, g.N, g.N, dbias, nullptr, stream);
 }
 
-int launch_dense(const GemmArgs& g, const DenseArgs& d, DenseOp op, int w_is_nk, hipStream_t stream) { return launch_dense_any(g, d, op, w_is_nk, stream); }
-uint64_t dense_tile_rows(const GemmArgs&, int) { return kDenseAnyRows; }
+int launch_dense(const GemmArgs& g, const DenseArgs& d, const DensePlan& p, DenseOp op, int w_is_nk, hipStream_t stream) {
+  switch (p.form) {
+    case GemmForm::kStream: return launch_dense_stream(g, d, op, w_is_nk, p.route.stream, stream);
+    case GemmForm::kMiddle: return launch_dense128(g, d, op, w_is_nk, p.route.middle_nj, stream);
+    case GemmForm::kLarge:
+    case GemmForm::kLargeEdge:
+    case GemmForm::kNarrow: return launch_dense256(g, d, op, w_is_nk, p.form, stream);
+    default: return launch_dense_any(g, d, op, w_is_nk, stream);
+  }
+}
 
 // ---- AdamW ----
 int check_gradient(const gws_adamw_tensor& t) {
@@ -145,6 +153,24 @@ inline uint64_t norm_wgs(const gws_adamw_tensor& t) {
 }
 
 }  // namespace
+
+// The kernel that the plain product of these sizes takes, so the sums run in the same order; what comes on top, the way out, hardly differs between those that
+// are near each other.  Leading dimensions of outputs that the kernels' 32-bit lane offsets do not reach: the kernel for any sizes.
+DensePlan plan_dense(const GemmArgs& g, const DenseArgs& d, int w_is_nk) {
+  DensePlan p;
+  p.form = gemm_form(g, w_is_nk, 0, p.route);
+  if (g.ldy >= kMaxLdOut || d.ldr >= kMaxLdOut || d.ldz >= kMaxLdOut || d.ldh >= kMaxLdOut) p.form = GemmForm::kAnyShape;
+  switch (p.form) {
+    case GemmForm::kStream: p.rows = (uint32_t)p.route.stream.bm; break;
+    case GemmForm::kMiddle: p.rows = 64; break;
+    case GemmForm::kLarge:
+    case GemmForm::kLargeEdge:
+    case GemmForm::kNarrow: p.rows = 128; break;
+    default: p.rows = kDenseAnyRows;
+  }
+  return p;
+}
+
 }  // namespace gws
 
 using namespace gws;
@@ -265,7 +291,8 @@ int gws_dense_fwd(const void* x, int64_t M, int64_t K, int64_t ldx, const void* 
   d.act = e->act;
   d.r = (const uint16_t*)e->residual; d.ldr = (uint32_t)e->ldr;
   d.z = (uint16_t*)e->z; d.ldz = (uint32_t)e->ldz;
-  return launch_dense(g, d, DenseOp::kFwd, w_is_nk, (hipStream_t)stream);
+  d.past_caches = (uint64_t)M * (uint64_t)N * 2 >= (uint64_t)172 << 20;
+  return launch_dense(g, d, plan_dense(g, d, w_is_nk), DenseOp::kFwd, w_is_nk, (hipStream_t)stream);
 }
 
 size_t gws_dense_bwd_workspace_bytes(int64_t M, int64_t F) { return !size_ok(M) || !size_ok(F) ? 0 : dense_bytes(M, F); }
@@ -294,8 +321,10 @@ int gws_dense_bwd(const void* dy, int64_t M, int64_t D, int64_t lddy, const void
   g.x = (const uint16_t*)dy; g.w = (const uint16_t*)wd;
   g.K = (uint32_t)D; g.ldx = (uint32_t)lddy; g.ldw = (uint32_t)ldw;
   const int nk = !w_is_nk;   // the product's columns are Wd's rows
-  return with_bias_gradient(g, d, dense_tile_rows(g, nk), dbias, workspace, (hipStream_t)stream,
-                            [&] { return launch_dense(g, d, DenseOp::kBwd, nk, (hipStream_t)stream); });
+  d.past_caches = D >= 1024;
+  const DensePlan p = plan_dense(g, d, nk);
+  return with_bias_gradient(g, d, p.rows, dbias, workspace, (hipStream_t)stream,
+                            [&] { return launch_dense(g, d, p, DenseOp::kBwd, nk, (hipStream_t)stream); });
 }
 
 int gws_dense_bwd_h(const void* dh, int64_t M, int64_t F, int64_t lddh, int act, const void* z, int64_t ldz, void* dz, int64_t lddz, void* h,
