@@ -817,41 +817,47 @@ def gws_linear_bwd_w_act8(x: Act8, dy, w: TensorDesc, step: int, workspace, w_is
                                                 nbytes, _stream(stream)), "gws_linear_bwd_w_act8")
 
 
-# fp32 vectors, told apart as the matrices above are.
+# The calls below look at their tensors in line (each attribute of a tensor takes as long as a function's call) and come to these for what is out of the ordinary:
+# a message, or one row or column, whose stride says nothing.
 _fp32 = None
 
 
-def _check_vector(t, n: int) -> None:
+def _look_at_matrix(t, shape, device: int):
+    """Address and leading dimension of a BF16 matrix, or what is wrong with it."""
+    if tuple(t.shape) != tuple(shape):
+        raise ValueError(f"a matrix has shape {list(t.shape)}, not {list(shape)}")
+    if t.dtype is not _bf16 or (t.stride()[1] != 1 and shape[1] > 1):
+        _check_plain(t)
+    _check_device(device, t)
+    return t.data_ptr(), t.stride()[0] if shape[0] > 1 else -(-shape[1] // 8) * 8
+
+
+def _matrix(t, size, device: int):
+    if t is None:
+        return None, 0
+    ld, one = t.stride()
+    if t.shape != size or one != 1 or t.dtype is not _bf16 or t.get_device() != device:
+        return _look_at_matrix(t, size, device)
+    return t.data_ptr(), ld if size[0] != 1 else -(-size[1] // 8) * 8   # one row's stride says nothing
+
+
+def _look_at_vector(t, n: int, device: int):
     global _fp32
     if _fp32 is None:
         import torch
         _fp32 = torch.float32
-    if t.dtype is not _fp32 or t.shape != (n,) or (n > 1 and t.stride()[0] != 1):
+    if t.dtype is not _fp32 or t.numel() != n or not t.is_contiguous():
         raise ValueError(f"a vector here is fp32 of {n} elements next to each other, not {t.dtype} of shape {list(t.shape)} and strides {list(t.stride())}")
+    _check_device(device, t)
+    return t.data_ptr()
 
 
 def _vector(t, n: int, device: int):
     if t is None:
         return None
-    if t.dtype is not _fp32 or t.shape != (n,) or t.stride()[0] != 1:
-        _check_vector(t, n)
-    if t.get_device() != device:
-        _check_device(device, t)
+    if t.dtype is not _fp32 or t.numel() != n or not t.is_contiguous() or t.get_device() != device:
+        return _look_at_vector(t, n, device)
     return t.data_ptr()
-
-
-def _matrix(t, rows: int, cols: int, device: int):
-    """Address and leading dimension of a BF16 matrix; None: NULL."""
-    if t is None:
-        return None, 0
-    if t.shape != (rows, cols):
-        raise ValueError(f"a matrix has shape {list(t.shape)}, not [{rows}, {cols}]")
-    ld, one = t.stride()
-    if one != 1 or t.dtype is not _bf16:
-        _check_plain(t)
-    if t.get_device() != device:
-        _check_device(device, t)
-    return t.data_ptr(), ld if rows > 1 else max(ld, -(-cols // 8) * 8)   # one row's stride is arbitrary
 
 
 def _bytes_of(workspace, device: int):
@@ -860,7 +866,7 @@ def _bytes_of(workspace, device: int):
     if workspace.get_device() != device or not workspace.is_contiguous():
         _check_device(device, workspace)
         raise ValueError("a workspace is contiguous")
-    return workspace.data_ptr(), workspace.numel() * workspace.element_size()
+    return workspace.data_ptr(), workspace.nbytes
 
 
 def _check_device(device: int, *tensors) -> None:
@@ -869,31 +875,41 @@ def _check_device(device: int, *tensors) -> None:
             raise ValueError(f"the tensors of a call are on one device, not on {device} and {t.get_device()} (-1: host memory)")
 
 
+_get_device = _get_raw_stream = None   # torch's current device and its stream's handle, once torch is there
+
+
 def _stream_of(device: int, stream):
     """The stream of a call on tensors of `device`, which has to be the current one: a launch goes to the current device's stream."""
-    raw = _stream(stream) if device >= 0 else None
-    import torch
-    if device < 0 or torch._C._cuda_getDevice() != device or (stream is not None and not isinstance(stream, int) and stream.device_index != device):
+    global _get_device, _get_raw_stream
+    if _get_device is None:
+        import torch
+        if device >= 0:
+            torch.cuda.current_stream()   # initialises the device runtime
+        _get_device, _get_raw_stream = torch._C._cuda_getDevice, torch._C._cuda_getCurrentRawStream
+    if device < 0 or _get_device() != device or (stream is not None and not isinstance(stream, int) and stream.device_index != device):
         raise ValueError(f"the tensors are on device {device} (-1: host memory), which is not the current device or the stream's")
-    return raw
+    return (_get_raw_stream(device) or None) if stream is None else _stream(stream)
 
 
 def gws_norm_fwd(x, y, kind: int = NORM_LAYER, gamma=None, beta=None, eps: float = 1e-5, mean=None, rstd=None, stream=None) -> None:
     """Layer norm or root-mean-square norm of the rows of ``x`` into ``y``; ``mean`` and ``rstd`` (fp32, one a row) receive what the backward pass needs."""
-    (M, C), on = x.shape, x.get_device()
-    (px, ldx), (py, ldy) = _matrix(x, M, C, on), _matrix(y, M, C, on)
-    _check((_lib or load_library()).gws_norm_fwd(px, M, C, ldx, kind, _vector(gamma, C, on), _vector(beta, C, on), eps, py, ldy, _vector(mean, M, on), _vector(rstd, M, on),
-                                                 _stream_of(on, stream)), "gws_norm_fwd")
+    size, on = x.shape, x.get_device()
+    M, C = size
+    (px, ldx), (py, ldy) = _matrix(x, size, on), _matrix(y, size, on)
+    _check((_lib or load_library()).gws_norm_fwd(px, M, C, ldx, kind, _vector(gamma, C, on), _vector(beta, C, on), eps, py, ldy, _vector(mean, M, on),
+                                                 _vector(rstd, M, on), _stream_of(on, stream)), "gws_norm_fwd")
 
 
 def gws_norm_bwd_workspace_bytes(M: int, C: int) -> int:
+    """Bytes of workspace that ``gws_norm_bwd`` needs for dgamma, dbeta or rows of more than 16384 columns."""
     return int(load_library().gws_norm_bwd_workspace_bytes(M, C))
 
 
 def gws_norm_bwd(dy, x, dx, rstd, kind: int = NORM_LAYER, mean=None, gamma=None, residual=None, dgamma=None, dbeta=None, workspace=None, stream=None) -> None:
     """dX of the norm, plus ``residual`` (a gradient that comes past it), with dgamma and dbeta; ``mean`` and ``rstd`` as ``gws_norm_fwd`` kept them."""
-    (M, C), on = x.shape, x.get_device()
-    (pdy, lddy), (px, ldx), (pr, ldr), (pdx, lddx) = _matrix(dy, M, C, on), _matrix(x, M, C, on), _matrix(residual, M, C, on), _matrix(dx, M, C, on)
+    size, on = x.shape, x.get_device()
+    M, C = size
+    (pdy, lddy), (px, ldx), (pr, ldr), (pdx, lddx) = _matrix(dy, size, on), _matrix(x, size, on), _matrix(residual, size, on), _matrix(dx, size, on)
     _check((_lib or load_library()).gws_norm_bwd(pdy, lddy, px, M, C, ldx, kind, _vector(gamma, C, on), _vector(mean, M, on), _vector(rstd, M, on), pr, ldr, pdx, lddx,
                                                  _vector(dgamma, C, on), _vector(dbeta, C, on), *_bytes_of(workspace, on), _stream_of(on, stream)), "gws_norm_bwd")
 
@@ -904,36 +920,42 @@ assert struct.calcsize("=Qi4xQqQq") == ctypes.sizeof(_CEpilogue)
 
 def gws_dense_fwd(x, w, y, bias=None, act: int = ACT_NONE, residual=None, z=None, w_is_nk: bool = False, stream=None) -> None:
     """Y = a(X W + b) + R in one kernel; ``z`` receives X W + b for the backward pass."""
-    (M, K), size, on = x.shape, w.shape, x.get_device()
-    N, Kw = size if w_is_nk else (size[1], size[0])
+    xs, ws, on = x.shape, w.shape, x.get_device()
+    M, K = xs
+    N, Kw = ws if w_is_nk else (ws[1], ws[0])
     if Kw != K:
-        raise ValueError(f"X {list(x.shape)} and W {list(size)} do not fit together")
-    (px, ldx), (pw, ldw), (py, ldy), (pr, ldr), (pz, ldz) = _matrix(x, M, K, on), _matrix(w, *size, on), _matrix(y, M, N, on), _matrix(residual, M, N, on), _matrix(z, M, N, on)
+        raise ValueError(f"X {list(xs)} and W {list(ws)} do not fit together")
+    ys = (M, N)
+    (px, ldx), (pw, ldw), (py, ldy), (pr, ldr), (pz, ldz) = _matrix(x, xs, on), _matrix(w, ws, on), _matrix(y, ys, on), _matrix(residual, ys, on), _matrix(z, ys, on)
     _check((_lib or load_library()).gws_dense_fwd(px, M, K, ldx, pw, N, ldw, 1 if w_is_nk else 0, py, ldy,
                                                   _pack_epilogue(_vector(bias, N, on) or 0, act, pr or 0, ldr, pz or 0, ldz), _stream_of(on, stream)), "gws_dense_fwd")
 
 
 def gws_dense_bwd_workspace_bytes(M: int, F: int) -> int:
+    """Bytes of workspace that ``gws_dense_bwd`` and ``gws_dense_bwd_h`` need for ``dbias``."""
     return int(load_library().gws_dense_bwd_workspace_bytes(M, F))
 
 
 def gws_dense_bwd(dy, wd, z, dz, act: int = ACT_NONE, h=None, dbias=None, workspace=None, w_is_nk: bool = False, stream=None) -> None:
     """dZ (and H = a(Z) again, and the bias gradient) from the gradient of Y = H Wd and the kept Z; dH = dY Wd^T stays in the kernel."""
-    (M, D), size, on = dy.shape, wd.shape, dy.get_device()
-    F, Dw = (size[1], size[0]) if w_is_nk else size
+    ys, ws, on = dy.shape, wd.shape, dy.get_device()
+    M, D = ys
+    F, Dw = (ws[1], ws[0]) if w_is_nk else ws
     if Dw != D:
-        raise ValueError(f"dY {list(dy.shape)} and Wd {list(size)} do not fit together")
-    (pdy, lddy), (pw, ldw) = _matrix(dy, M, D, on), _matrix(wd, *size, on)
-    _check((_lib or load_library()).gws_dense_bwd(pdy, M, D, lddy, pw, F, ldw, 1 if w_is_nk else 0, act, *_matrix(z, M, F, on), *_matrix(dz, M, F, on),
-                                                  *_matrix(h, M, F, on), _vector(dbias, F, on), *_bytes_of(workspace, on), _stream_of(on, stream)), "gws_dense_bwd")
+        raise ValueError(f"dY {list(ys)} and Wd {list(ws)} do not fit together")
+    zs = (M, F)
+    (pdy, lddy), (pw, ldw), (pz, ldz), (pd, ldd), (ph, ldh) = _matrix(dy, ys, on), _matrix(wd, ws, on), _matrix(z, zs, on), _matrix(dz, zs, on), _matrix(h, zs, on)
+    _check((_lib or load_library()).gws_dense_bwd(pdy, M, D, lddy, pw, F, ldw, 1 if w_is_nk else 0, act, pz, ldz, pd, ldd, ph, ldh, _vector(dbias, F, on),
+                                                  *_bytes_of(workspace, on), _stream_of(on, stream)), "gws_dense_bwd")
 
 
 def gws_dense_bwd_h(dh, z, dz, act: int = ACT_NONE, h=None, dbias=None, workspace=None, stream=None) -> None:
     """``gws_dense_bwd`` from a given dH; with ``ACT_NONE`` ``z`` and ``dz`` may be None, which leaves the bias gradient alone."""
-    (M, F), on = dh.shape, dh.get_device()
-    pdh, lddh = _matrix(dh, M, F, on)
-    _check((_lib or load_library()).gws_dense_bwd_h(pdh, M, F, lddh, act, *_matrix(z, M, F, on), *_matrix(dz, M, F, on), *_matrix(h, M, F, on), _vector(dbias, F, on),
-                                                    *_bytes_of(workspace, on), _stream_of(on, stream)), "gws_dense_bwd_h")
+    size, on = dh.shape, dh.get_device()
+    M, F = size
+    (pdy, lddy), (pz, ldz), (pd, ldd), (ph, ldh) = _matrix(dh, size, on), _matrix(z, size, on), _matrix(dz, size, on), _matrix(h, size, on)
+    _check((_lib or load_library()).gws_dense_bwd_h(pdy, M, F, lddy, act, pz, ldz, pd, ldd, ph, ldh, _vector(dbias, F, on), *_bytes_of(workspace, on),
+                                                    _stream_of(on, stream)), "gws_dense_bwd_h")
 
 
 class PackedAdamW:
@@ -998,30 +1020,32 @@ def pack_adamw(tensors: Sequence[AdamWTensor]) -> PackedAdamW:
     return PackedAdamW(arr, len(tensors), list(tensors), on)
 
 
-def _as_adamw(t) -> PackedAdamW:
-    return t if isinstance(t, PackedAdamW) else pack_adamw(t)
+_pack_settings = struct.Struct("=4d2Q").pack
+assert struct.calcsize("=4d2Q") == ctypes.sizeof(_CAdamWSettings)
 
 
 def gws_adamw(t, lr: float, step: int, beta1: float = 0.9, beta2: float = 0.95, eps: float = 1e-8, grad_scale=None, stream=None) -> None:
     """One AdamW step (``step`` = 1, 2, ...) over a list of :class:`AdamWTensor`, or :func:`pack_adamw`'s array; ``grad_scale``: a device fp32 number that
     the gradients are multiplied by, as ``gws_grad_norm`` leaves it (not finite: the step is left out)."""
-    t = _as_adamw(t)
-    if grad_scale is not None and (str(grad_scale.dtype) != "torch.float32" or grad_scale.numel() != 1):
-        raise ValueError(f"grad_scale is one fp32 number, not {grad_scale.dtype} of shape {list(grad_scale.shape)}")
-    if t.n and grad_scale is not None:
-        _check_device(t.device, grad_scale)
-    s = _CAdamWSettings(lr, beta1, beta2, eps, step, _p(grad_scale))
-    _check((_lib or load_library()).gws_adamw(t.arr, t.n, ctypes.byref(s), _stream_of(t.device, stream) if t.n else None), "gws_adamw")
+    if not isinstance(t, PackedAdamW):
+        t = pack_adamw(t)
+    if not 0 < step < 2 ** 64:
+        raise ValueError(f"steps are 1, 2, ..., not {step}")
+    n, on = t.n, t.device
+    _check((_lib or load_library()).gws_adamw(t.arr, n, _pack_settings(lr, beta1, beta2, eps, step, _vector(grad_scale, 1, on) or 0 if n else 0),
+                                              _stream_of(on, stream) if n else None), "gws_adamw")
 
 
 def gws_grad_norm_workspace_bytes(t) -> int:
-    t = _as_adamw(t)
+    """Bytes of workspace that ``gws_grad_norm`` needs for these tensors."""
+    t = t if isinstance(t, PackedAdamW) else pack_adamw(t)
     return int(load_library().gws_grad_norm_workspace_bytes(t.arr, t.n))
 
 
 def gws_grad_norm(t, out, workspace, max_norm: float = 0.0, stream=None) -> None:
     """``out`` (fp32 [2]): the norm of all gradients, and the factor that takes it down to ``max_norm`` where it is larger."""
-    t = _as_adamw(t)
+    if not isinstance(t, PackedAdamW):
+        t = pack_adamw(t)
     on = t.device if t.n else out.get_device()
     _check((_lib or load_library()).gws_grad_norm(t.arr, t.n, max_norm, _vector(out, 2, on), *_bytes_of(workspace, on), _stream_of(on, stream)), "gws_grad_norm")
 

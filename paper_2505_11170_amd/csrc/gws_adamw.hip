@@ -19,23 +19,30 @@ namespace {
 typedef float f4 __attribute__((ext_vector_type(4)));
 typedef uint32_t u2 __attribute__((ext_vector_type(2)));
 
-// The tensor of workgroup `wg`: all first workgroups are compared at once.
-__device__ __forceinline__ uint32_t tensor_of(const uint32_t (&begin)[kAdamwTensors], uint32_t wg) {
-  uint32_t i = 0;
+// The tensor of workgroup `wg`: a lane compares with the first workgroup of one in 64, and the lanes whose tensors begin before it are counted.  One round
+// trip to the arguments, which lie in memory; a search by parts takes several, and a small call is hardly more than such trips.
+template <int N>
+__device__ __forceinline__ uint32_t tensor_of(const uint32_t (&begin)[N], uint32_t wg) {
+  const uint32_t lane = threadIdx.x & 63;
+  uint32_t before = 0;
 #pragma unroll
-  for (int k = 1; k < kAdamwTensors; ++k) i += wg >= begin[k] ? 1 : 0;
-  return __builtin_amdgcn_readfirstlane(i);
-}
-// Row and group within it of a tensor's group `id`; false past its end.
-__device__ __forceinline__ bool place(const AdamwDesc& t, uint64_t id, uint32_t& row, uint32_t& group) {
-  if (t.form & kFewGroups) {   // uniform
-    row = divide((uint32_t)id, t.per_row, t.inv);
-    group = (uint32_t)id - row * t.per_row;
-  } else {
-    row = (uint32_t)(id / t.per_row);
-    group = (uint32_t)(id - (uint64_t)row * t.per_row);
+  for (int k = 0; k < N; k += 64) {
+    const uint32_t i = k + lane;
+    const uint32_t first = begin[i < N ? i : N - 1];
+    before += (uint32_t)__builtin_popcountll(__builtin_amdgcn_ballot_w64(i < N && wg >= first));
   }
-  return id < (uint64_t)t.rows * t.per_row;
+  return __builtin_amdgcn_readfirstlane(before - 1);   // the first one begins at 0
+}
+// Row and group within it of a matrix's group `id`; false past its end.
+__device__ __forceinline__ bool place(uint64_t id, uint32_t rows, uint32_t per_row, uint32_t inv, bool few, uint32_t& row, uint32_t& group) {
+  if (few) {   // uniform
+    row = divide((uint32_t)id, per_row, inv);
+    group = (uint32_t)id - row * per_row;
+  } else {
+    row = (uint32_t)(id / per_row);
+    group = (uint32_t)(id - (uint64_t)row * per_row);
+  }
+  return id < (uint64_t)rows * per_row;
 }
 
 // Four elements of which `n` exist (the others read as zeros).
@@ -129,7 +136,7 @@ __device__ __forceinline__ uint32_t largest(const f4& v) {
   return max(m, dpp_u32<0x141>(m)); // row_half_mirror: the other four of eight
 }
 
-// Four elements on their way and their update.
+// Four elements on their way and their update: of a run of elements (fp32 states), or of a row of a matrix.
 template <bool CODES>
 struct Four {
   f4 p, g, m, v;
@@ -137,19 +144,16 @@ struct Four {
   uint32_t row, group;
   int n;
   size_t at, block;
-  __device__ __forceinline__ void load(const AdamwDesc& t, uint64_t id) {
-    const bool in = place(t, id, row, group);
-    const uint32_t c = 4 * group;
-    n = !in || c >= t.cols ? 0 : t.cols - c < 4 ? (int)(t.cols - c) : 4;
-    at = (size_t)row * t.ld + c;
+
+  template <class Desc>
+  __device__ __forceinline__ void load_at(const Desc& t, bool grad_fp32) {
     p = g = m = v = f4{0.0f, 0.0f, 0.0f, 0.0f};
     mc = vc = 0;
     mb = vb = kAct8Zero;
     if (n == 0) return;
     p = load_four(t.p, at, n);
-    g = t.form & kGradFp32 ? load_four((const float*)t.g, at, n) : load_four_bf16(t.g, at, n);
-    if (CODES) {
-      block = (size_t)row * t.lds + (c >> 5);
+    g = grad_fp32 ? load_four((const float*)t.g, at, n) : load_four_bf16(t.g, at, n);
+    if constexpr (CODES) {
       mc = load_codes(t.m, at, n);
       vc = load_codes(t.v, at, n);
       mb = global_ptr<uint8_t>(t.ms)[block];
@@ -159,8 +163,23 @@ struct Four {
       v = load_four((const float*)t.v, at, n);
     }
   }
+  __device__ __forceinline__ void load(const AdamwRun& t, uint64_t id) {
+    const uint64_t count = t.n & ~kRunGradFp32;
+    at = 4 * id;
+    n = at >= count ? 0 : count - at < 4 ? (int)(count - at) : 4;
+    load_at(t, (t.n & kRunGradFp32) != 0);
+  }
+  __device__ __forceinline__ void load(const AdamwMatrix& t, uint64_t id) {
+    const bool in = place(id, t.rows, t.per_row, t.inv, (t.form & kFewGroups) != 0, row, group);
+    const uint32_t c = 4 * group;
+    n = !in || c >= t.cols ? 0 : t.cols - c < 4 ? (int)(t.cols - c) : 4;
+    at = (size_t)row * t.ld + c;
+    block = (size_t)row * t.lds + (c >> 5);
+    load_at(t, (t.form & kGradFp32) != 0);
+  }
   // all lanes come here: the eight of a block meet
-  __device__ __forceinline__ void update(const AdamwDesc& t, const AdamwArgs& a, float scale) {
+  template <class Desc>
+  __device__ __forceinline__ void update(const Desc& t, const AdamwStep& a, float scale) {
     if (CODES) {
       m = values(mc, mb);
       v = values(vc, vb);
@@ -196,7 +215,7 @@ struct Four {
           if (e < n) q[e] = (uint16_t)(w[e >> 1] >> (16 * (e & 1)));
       }
     }
-    if (CODES) {
+    if constexpr (CODES) {
       const Philox4 x = philox4x32_10(group, row, a.step_lo, a.step_hi ^ 0x47414457u, t.seed_lo, t.seed_hi);
       const uint32_t bits[4] = {x.x0, x.x1, x.x2, x.x3};
       store_codes(t.m, at, n, state_codes<false>(m, mbyte, bits));
@@ -212,10 +231,10 @@ struct Four {
   }
 };
 
-template <bool CODES>
-__device__ __forceinline__ void update_groups(const AdamwArgs& a, const AdamwDesc& t, float scale) {
+template <bool CODES, class Desc>
+__device__ __forceinline__ void update_groups(const AdamwStep& a, const Desc& t, uint32_t wg, float scale) {
   constexpr int U = kAdamwGroups / 256;
-  const uint64_t first = (uint64_t)(blockIdx.x - t.first_wg) * kAdamwGroups + threadIdx.x;
+  const uint64_t first = (uint64_t)wg * kAdamwGroups + threadIdx.x;
   Four<CODES> f[U];
 #pragma unroll
   for (int u = 0; u < U; ++u) f[u].load(t, first + 256 * u);
@@ -223,24 +242,39 @@ __device__ __forceinline__ void update_groups(const AdamwArgs& a, const AdamwDes
   for (int u = 0; u < U; ++u) f[u].update(t, a, scale);
 }
 
-}  // namespace
-
-template <int CODES>
-__global__ __launch_bounds__(256) void adamw_kernel(const AdamwArgs a) {
-  float scale = 1.0f;
-  if (a.grad_scale != nullptr) {
-    scale = *a.grad_scale;
-    if ((__float_as_uint(scale) & 0x7F800000u) == 0x7F800000u) return;   // uniform: a step without a finite gradient norm is none
-  }
-  const AdamwDesc& t = a.t[tensor_of(a.begin, blockIdx.x)];
-  if (CODES == 2 || (CODES == 1 && (t.form & kCodes))) update_groups<true>(a, t, scale);
-  else update_groups<false>(a, t, scale);
+// *grad_scale, or 1; false where it is not finite: a step without a finite gradient norm is none.
+__device__ __forceinline__ bool scale_of(const AdamwStep& s, float& scale) {
+  scale = s.grad_scale != nullptr ? *s.grad_scale : 1.0f;
+  return (__float_as_uint(scale) & 0x7F800000u) != 0x7F800000u;
 }
 
-int launch_adamw(const AdamwArgs& a, uint32_t wgs, int codes, hipStream_t stream) {
-  if (codes == 0) hipLaunchKernelGGL(adamw_kernel<0>, dim3(wgs), dim3(256), 0, stream, a);
-  else if (codes == 1) hipLaunchKernelGGL(adamw_kernel<1>, dim3(wgs), dim3(256), 0, stream, a);
-  else hipLaunchKernelGGL(adamw_kernel<2>, dim3(wgs), dim3(256), 0, stream, a);
+}  // namespace
+
+__global__ __launch_bounds__(256) void adamw_runs_kernel(const AdamwRuns l, const AdamwStep s) {
+  float scale;
+  if (!scale_of(s, scale)) return;   // uniform
+  const uint32_t i = tensor_of(l.begin, blockIdx.x);
+  update_groups<false>(s, l.t[i], blockIdx.x - l.begin[i], scale);
+}
+
+template <int CODES>
+__global__ __launch_bounds__(256) void adamw_matrices_kernel(const AdamwMatrices l, const AdamwStep s) {
+  float scale;
+  if (!scale_of(s, scale)) return;   // uniform
+  const uint32_t i = tensor_of(l.begin, blockIdx.x), wg = blockIdx.x - l.begin[i];
+  const AdamwMatrix& t = l.t[i];
+  if (CODES == 2 || (CODES == 1 && (t.form & kCodes))) update_groups<true>(s, t, wg, scale);
+  else update_groups<false>(s, t, wg, scale);
+}
+
+int launch_adamw_runs(const AdamwRuns& t, const AdamwStep& s, uint32_t wgs, hipStream_t stream) {
+  hipLaunchKernelGGL(adamw_runs_kernel, dim3(wgs), dim3(256), 0, stream, t, s);
+  return hipGetLastError() == hipSuccess ? GWS_OK : GWS_ERR_LAUNCH;
+}
+int launch_adamw_matrices(const AdamwMatrices& t, const AdamwStep& s, uint32_t wgs, int codes, hipStream_t stream) {
+  if (codes == 0) hipLaunchKernelGGL(adamw_matrices_kernel<0>, dim3(wgs), dim3(256), 0, stream, t, s);
+  else if (codes == 1) hipLaunchKernelGGL(adamw_matrices_kernel<1>, dim3(wgs), dim3(256), 0, stream, t, s);
+  else hipLaunchKernelGGL(adamw_matrices_kernel<2>, dim3(wgs), dim3(256), 0, stream, t, s);
   return hipGetLastError() == hipSuccess ? GWS_OK : GWS_ERR_LAUNCH;
 }
 
@@ -258,28 +292,31 @@ __device__ __forceinline__ double block_sum(double v, double* red) {
 }
 }  // namespace
 
-__global__ __launch_bounds__(256) void grad_squares_kernel(const AdamwArgs a) {
+__global__ __launch_bounds__(256) void grad_squares_kernel(const GradList l, double* part) {
   __shared__ double red[4];
-  const AdamwDesc& t = a.t[tensor_of(a.begin, blockIdx.x)];
-  const uint64_t first = (uint64_t)(blockIdx.x - t.first_wg) * kNormGroups + threadIdx.x;
+  const uint32_t i = tensor_of(l.begin, blockIdx.x);
+  const GradSquares& t = l.t[i];
+  const uint64_t first = (uint64_t)(blockIdx.x - l.begin[i]) * kNormGroups + threadIdx.x;
+  const uint32_t rows = t.rows & ~kHighBit, cols = t.cols & ~kHighBit, per_row = (cols + 7) / 8;
+  const bool fp32 = (t.rows & kHighBit) != 0;
   double s = 0.0;
 #pragma unroll
   for (uint32_t u = 0; u < kNormGroups / 256; ++u) {
     uint32_t row, group;
-    if (!place(t, first + 256 * u, row, group)) continue;
+    if (!place(first + 256 * u, rows, per_row, t.inv, (t.cols & kHighBit) != 0, row, group)) continue;
     const uint32_t c = 8 * group;
     const size_t at = (size_t)row * t.ld + c;
 #pragma unroll
     for (uint32_t h = 0; h < 8; h += 4) {
-      if (c + h >= t.cols) continue;
-      const int n = t.cols - c - h < 4 ? (int)(t.cols - c - h) : 4;
-      const f4 g = t.form & kGradFp32 ? load_four((const float*)t.g, at + h, n) : load_four_bf16(t.g, at + h, n);
+      if (c + h >= cols) continue;
+      const int n = cols - c - h < 4 ? (int)(cols - c - h) : 4;
+      const f4 g = fp32 ? load_four((const float*)t.g, at + h, n) : load_four_bf16(t.g, at + h, n);
 #pragma unroll
       for (int e = 0; e < 4; ++e) s = __fma_rn((double)g[e], (double)g[e], s);
     }
   }
   s = block_sum(s, red);
-  if (threadIdx.x == 0) a.part[blockIdx.x] = s;
+  if (threadIdx.x == 0) part[blockIdx.x] = s;
 }
 
 __global__ __launch_bounds__(1024) void grad_norm_kernel(const double* part, const uint64_t n, const double max_norm, float* out) {
@@ -295,8 +332,8 @@ __global__ __launch_bounds__(1024) void grad_norm_kernel(const double* part, con
   out[1] = !finite ? nan : max_norm > 0.0 && norm > max_norm ? (float)(max_norm / norm) : 1.0f;
 }
 
-int launch_grad_squares(const AdamwArgs& a, uint32_t wgs, hipStream_t stream) {
-  hipLaunchKernelGGL(grad_squares_kernel, dim3(wgs), dim3(256), 0, stream, a);
+int launch_grad_squares(const GradList& t, double* part, uint32_t wgs, hipStream_t stream) {
+  hipLaunchKernelGGL(grad_squares_kernel, dim3(wgs), dim3(256), 0, stream, t, part);
   return hipGetLastError() == hipSuccess ? GWS_OK : GWS_ERR_LAUNCH;
 }
 int launch_grad_norm(const double* part, uint64_t n, double max_norm, float* out, hipStream_t stream) {

@@ -65,4 +65,11 @@ struct Buffers {
   }
 };
 
+// From a matrix's first byte to behind its last.
+struct Range {
+  uintptr_t from, to;
+};
+inline Range range_of(const Span2& s) { return Range{(uintptr_t)s.p, s.p ? (uintptr_t)s.p + s.bytes() : (uintptr_t)s.p}; }
+inline bool ranges_apart(const Range& a, const Range& b) { return a.to <= b.from || b.to <= a.from; }
+
 }  // namespace gws

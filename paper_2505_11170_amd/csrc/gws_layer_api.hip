@@ -73,7 +73,7 @@ int launch_dense(const GemmArgs& g, const DenseArgs& d, const DensePlan& p, Dens
 int check_gradient(const gws_adamw_tensor& t) {
   if (!size_ok(t.rows) || !size_ok(t.cols)) return GWS_ERR_SHAPE;
   if (t.rows == 0 || t.cols == 0) return GWS_OK;
-  if (!ld_ok(t.ld, t.cols) || (uint64_t)t.rows * (((uint64_t)t.cols + 31) / 32) >= (uint64_t)1 << 37) return GWS_ERR_SHAPE;
+  if (!ld_ok(t.ld, t.cols) || (uint64_t)t.rows * (((uint64_t)t.cols + 31) / 32) >= (uint64_t)1 << 36) return GWS_ERR_SHAPE;
   if (!t.g) return GWS_ERR_NULL;
   return aligned(t.g, 16) ? GWS_OK : GWS_ERR_ALIGN;
 }
@@ -88,66 +88,65 @@ int check_adamw(const gws_adamw_tensor& t, const float* grad_scale) {
   if (codes && (t.m || t.v)) return GWS_ERR_FORMAT;
   if (!t.p) return GWS_ERR_NULL;
   if (!isfinite(t.lr_scale) || !isfinite(t.weight_decay)) return GWS_ERR_FORMAT;
-  Buffers b;
   const size_t m = (size_t)t.rows, n = (size_t)t.cols, ld = (size_t)t.ld;
+  Span2 out[6], in[2] = {gradient_span(t), span_f32(grad_scale, 1)};
+  int outs = 0;
   if (codes) {
     if ((rc = check_act8(t.m8, t.rows, t.cols)) != GWS_OK || (rc = check_act8(t.v8, t.rows, t.cols)) != GWS_OK) return rc;
     if (t.m8.ldc != t.ld || t.v8.ldc != t.ld || t.m8.lds != t.v8.lds) return GWS_ERR_SHAPE;
     for (const gws_act8* s : {&t.m8, &t.v8}) {
-      b.writes(Span2{s->codes, m, n, ld});
-      b.writes(Span2{s->xscale, m, (n + 31) / 32, (size_t)s->lds});
+      out[outs++] = Span2{s->codes, m, n, ld};
+      out[outs++] = Span2{s->xscale, m, (n + 31) / 32, (size_t)s->lds};
     }
   } else {
     if (!t.m || !t.v) return GWS_ERR_NULL;
     if (!aligned(t.m, 16) || !aligned(t.v, 16)) return GWS_ERR_ALIGN;
-    b.writes(Span2{t.m, m, n * 4, ld * 4});
-    b.writes(Span2{t.v, m, n * 4, ld * 4});
+    out[outs++] = Span2{t.m, m, n * 4, ld * 4};
+    out[outs++] = Span2{t.v, m, n * 4, ld * 4};
   }
   if (!aligned(t.p, 16) || !aligned(t.w, 16)) return GWS_ERR_ALIGN;
-  b.writes(Span2{t.p, m, n * 4, ld * 4});
-  b.writes(Span2{t.w, m, n * 2, ld * 2});
-  b.reads(gradient_span(t));
-  b.reads(span_f32(grad_scale, 1));
-  return b.apart_all(false) ? GWS_OK : GWS_ERR_ALIAS;
+  out[outs++] = Span2{t.p, m, n * 4, ld * 4};
+  if (t.w) out[outs++] = Span2{t.w, m, n * 2, ld * 2};
+  // whole ranges first: a model has hundreds of tensors, and matrices that lie between each other's rows are rare
+  Range r[8];
+  for (int i = 0; i < outs; ++i) r[i] = range_of(out[i]);
+  r[outs] = range_of(in[0]);
+  r[outs + 1] = range_of(in[1]);
+  for (int i = 0; i < outs; ++i)
+    for (int j = i + 1; j < outs + 2; ++j)
+      if (!ranges_apart(r[i], r[j]) && !apart(out[i], j < outs ? out[j] : in[j - outs])) return GWS_ERR_ALIAS;
+  return GWS_OK;
 }
 
-// The tensors of a call in launches of as many as fit; make(d, tensor) fills a descriptor and gives the elements of a group, and of `per_wg` groups
-// is a workgroup.  flush(args, workgroups).
-template <class Make, class Flush>
-int in_launches(AdamwArgs& a, const gws_adamw_tensor* t, int n, uint32_t per_wg, Make&& make, Flush&& flush) {
+// Tensors in launches of as many as a list holds: add(descriptor, its workgroups), and finish() for the rest.
+template <class List, class Launch>
+struct Launches {
+  List list;
   int held = 0;
   uint64_t wgs = 0;
-  auto launch = [&]() -> int {
+  Launch launch;   // (list, workgroups)
+  explicit Launches(Launch l) : launch(l) {}
+  template <class Desc>
+  int add(const Desc& d, uint64_t wc) {
+    if (held == List::kMax || wgs + wc >= 0x7FFFFFF0ull) {
+      const int rc = finish();
+      if (rc != GWS_OK) return rc;
+    }
+    list.begin[held] = (uint32_t)wgs;
+    list.t[held++] = d;
+    wgs += wc;
+    return GWS_OK;
+  }
+  int finish() {
     if (held == 0) return GWS_OK;
-    for (int i = held; i < kAdamwTensors; ++i) a.begin[i] = 0x7FFFFFFFu;
-    const int rc = flush((uint32_t)wgs);
+    for (int i = held; i < List::kMax; ++i) list.begin[i] = 0x7FFFFFFFu;
+    const int rc = launch(list, (uint32_t)wgs);
     held = 0;
     wgs = 0;
     return rc;
-  };
-  for (int i = 0; i < n; ++i) {
-    if (t[i].rows == 0 || t[i].cols == 0) continue;
-    AdamwDesc d;
-    memset(&d, 0, sizeof d);
-    d.g = t[i].g;
-    d.rows = (uint32_t)t[i].rows; d.cols = (uint32_t)t[i].cols; d.ld = (uint32_t)t[i].ld;
-    if (t[i].g_is_fp32) d.form |= kGradFp32;
-    d.per_row = make(d, t[i]);
-    d.inv = reciprocal(d.per_row);
-    const uint64_t groups = (uint64_t)d.rows * d.per_row, wc = (groups + per_wg - 1) / per_wg;
-    if (wc >= 0x7FFFFFF0ull) return GWS_ERR_SHAPE;
-    if (groups + per_wg < ((uint64_t)1 << 32)) d.form |= kFewGroups;
-    if (held == kAdamwTensors || wgs + wc >= 0x7FFFFFF0ull) {
-      const int rc = launch();
-      if (rc != GWS_OK) return rc;
-    }
-    d.first_wg = (uint32_t)wgs;
-    a.begin[held] = (uint32_t)wgs;
-    a.t[held++] = d;
-    wgs += wc;
   }
-  return launch();
-}
+};
+inline bool few_groups(uint64_t groups) { return groups + 0x100000 < ((uint64_t)1 << 32); }   // those past the end of the last workgroup too
 inline uint64_t norm_wgs(const gws_adamw_tensor& t) {
   return t.rows <= 0 || t.cols <= 0 ? 0 : ((uint64_t)t.rows * (((uint64_t)t.cols + 7) / 8) + kNormGroups - 1) / kNormGroups;
 }
@@ -361,38 +360,39 @@ int gws_adamw(const gws_adamw_tensor* t, int n, const gws_adamw_settings* s, voi
     const int rc = check_adamw(t[i], s->grad_scale);
     if (rc != GWS_OK) return rc;
   }
-  AdamwArgs a;
-  a.beta1 = (float)s->beta1; a.one1 = (float)(1.0 - s->beta1);
-  a.beta2 = (float)s->beta2; a.one2 = (float)(1.0 - s->beta2);
   const double c1 = 1.0 - pow(s->beta1, (double)s->step), c2 = 1.0 - pow(s->beta2, (double)s->step);
-  a.root2 = (float)(1.0 / sqrt(c2));
-  a.eps = (float)s->eps;
-  a.step_lo = (uint32_t)s->step;
-  a.step_hi = (uint32_t)(s->step >> 32);
-  a.grad_scale = s->grad_scale;
-  a.part = nullptr;
-  uint32_t with = 0, without = 0;
-  return in_launches(a, t, n, kAdamwGroups, [&](AdamwDesc& d, const gws_adamw_tensor& o) -> uint32_t {
-    d.p = o.p;
-    d.w = (uint16_t*)o.w;
+  const AdamwStep a = {(float)s->beta1, (float)(1.0 - s->beta1), (float)s->beta2, (float)(1.0 - s->beta2), (float)(1.0 / sqrt(c2)), (float)s->eps,
+                       (uint32_t)s->step, (uint32_t)(s->step >> 32), s->grad_scale};
+  auto runs_launch = [&](const AdamwRuns& l, uint32_t wgs) { return launch_adamw_runs(l, a, wgs, (hipStream_t)stream); };
+  auto matrices_launch = [&](const AdamwMatrices& l, uint32_t wgs) {
+    bool with = false, without = false;
+    for (int i = 0; i < AdamwMatrices::kMax && l.begin[i] != 0x7FFFFFFFu; ++i) (l.t[i].form & kCodes ? with : without) = true;
+    return launch_adamw_matrices(l, a, wgs, !with ? 0 : without ? 1 : 2, (hipStream_t)stream);
+  };
+  Launches<AdamwRuns, decltype(runs_launch)> runs(runs_launch);
+  Launches<AdamwMatrices, decltype(matrices_launch)> matrices(matrices_launch);
+  for (int i = 0; i < n; ++i) {
+    const gws_adamw_tensor& o = t[i];
+    if (o.rows == 0 || o.cols == 0) continue;
     const double lr = s->lr * o.lr_scale;
-    d.keep = (float)(1.0 - lr * o.weight_decay);
-    d.rate = (float)(lr / c1);
-    d.seed_lo = (uint32_t)o.seed;
-    d.seed_hi = (uint32_t)(o.seed >> 32);
-    if (o.m8.codes) {
-      d.m = o.m8.codes; d.v = o.v8.codes; d.ms = o.m8.xscale; d.vs = o.v8.xscale;
-      d.lds = (uint32_t)o.m8.lds;
-      d.form |= kCodes;
-      return (uint32_t)(((uint64_t)o.cols + 31) / 32 * 8);
+    const float keep = (float)(1.0 - lr * o.weight_decay), rate = (float)(lr / c1);
+    int rc;
+    if (!o.m8.codes && (o.rows == 1 || o.cols == o.ld)) {
+      const uint64_t elements = (uint64_t)o.rows * (uint64_t)o.cols;
+      rc = runs.add(AdamwRun{o.p, (uint16_t*)o.w, o.g, o.m, o.v, elements | (o.g_is_fp32 ? kRunGradFp32 : 0), keep, rate}, (elements + 4 * kAdamwGroups - 1) / (4 * kAdamwGroups));
+    } else {
+      const bool codes = o.m8.codes != nullptr;
+      const uint32_t per_row = (uint32_t)(codes ? ((uint64_t)o.cols + 31) / 32 * 8 : ((uint64_t)o.cols + 3) / 4);
+      const uint64_t groups = (uint64_t)o.rows * per_row;
+      rc = matrices.add(AdamwMatrix{o.p, (uint16_t*)o.w, o.g, codes ? o.m8.codes : o.m, codes ? o.v8.codes : o.v, o.m8.xscale, o.v8.xscale, (uint32_t)o.rows, (uint32_t)o.cols,
+                                    (uint32_t)o.ld, (uint32_t)o.m8.lds, keep, rate, (uint32_t)o.seed, (uint32_t)(o.seed >> 32), per_row, reciprocal(per_row),
+                                    (o.g_is_fp32 ? kGradFp32 : 0) | (codes ? kCodes : 0) | (few_groups(groups) ? kFewGroups : 0), 0},
+                        (groups + kAdamwGroups - 1) / kAdamwGroups);
     }
-    d.m = o.m; d.v = o.v;
-    return (uint32_t)(((uint64_t)o.cols + 3) / 4);
-  }, [&](uint32_t wgs) {
-    with = without = 0;
-    for (int i = 0; i < kAdamwTensors && a.begin[i] != 0x7FFFFFFFu; ++i) (a.t[i].form & kCodes ? with : without) += 1;
-    return launch_adamw(a, wgs, with == 0 ? 0 : without == 0 ? 2 : 1, (hipStream_t)stream);
-  });
+    if (rc != GWS_OK) return rc;
+  }
+  const int rc = runs.finish();
+  return rc != GWS_OK ? rc : matrices.finish();
 }
 
 size_t gws_grad_norm_workspace_bytes(const gws_adamw_tensor* t, int n) {
@@ -416,20 +416,28 @@ int gws_grad_norm(const gws_adamw_tensor* t, int n, double max_norm, float* out,
   if (need && workspace_bytes < need) return GWS_ERR_SHAPE;
   const Span2 ws = span_bytes(need ? workspace : nullptr, need), to = span_f32(out, 2);
   if (!apart(ws, to)) return GWS_ERR_ALIAS;
-  for (int i = 0; i < n; ++i)
-    if (t[i].rows > 0 && t[i].cols > 0 && (!apart(gradient_span(t[i]), ws) || !apart(gradient_span(t[i]), to))) return GWS_ERR_ALIAS;
-  AdamwArgs a;
-  memset(&a, 0, sizeof a);
-  a.part = (double*)workspace;
-  uint64_t total = 0;
-  const int rc = in_launches(a, t, n, kNormGroups, [&](AdamwDesc&, const gws_adamw_tensor& o) -> uint32_t { return (uint32_t)(((uint64_t)o.cols + 7) / 8); },
-                             [&](uint32_t wgs) {
-                               const int r = launch_grad_squares(a, wgs, (hipStream_t)stream);
-                               a.part += wgs;
-                               total += wgs;
-                               return r;
-                             });
-  return rc != GWS_OK ? rc : launch_grad_norm((const double*)workspace, total, max_norm, out, (hipStream_t)stream);
+  const Range rw = range_of(ws), ro = range_of(to);
+  for (int i = 0; i < n; ++i) {
+    if (t[i].rows == 0 || t[i].cols == 0) continue;
+    const Range r = range_of(gradient_span(t[i]));
+    if ((!ranges_apart(r, rw) && !apart(gradient_span(t[i]), ws)) || (!ranges_apart(r, ro) && !apart(gradient_span(t[i]), to))) return GWS_ERR_ALIAS;
+  }
+  double* part = (double*)workspace;
+  auto launch = [&](const GradList& l, uint32_t wgs) {
+    const int r = launch_grad_squares(l, part, wgs, (hipStream_t)stream);
+    part += wgs;
+    return r;
+  };
+  Launches<GradList, decltype(launch)> list(launch);
+  for (int i = 0; i < n; ++i) {
+    if (t[i].rows == 0 || t[i].cols == 0) continue;
+    const uint32_t rows = (uint32_t)t[i].rows, cols = (uint32_t)t[i].cols, per_row = (uint32_t)(((uint64_t)cols + 7) / 8);
+    const int rc = list.add(GradSquares{t[i].g, rows | (t[i].g_is_fp32 ? kHighBit : 0), cols | (few_groups((uint64_t)rows * per_row) ? kHighBit : 0), (uint32_t)t[i].ld,
+                                        reciprocal(per_row)}, norm_wgs(t[i]));
+    if (rc != GWS_OK) return rc;
+  }
+  const int rc = list.finish();
+  return rc != GWS_OK ? rc : launch_grad_norm((const double*)workspace, (uint64_t)(part - (double*)workspace), max_norm, out, (hipStream_t)stream);
 }
 
 }  // extern "C"

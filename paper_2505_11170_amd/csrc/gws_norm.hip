@@ -183,36 +183,43 @@ struct Normalise {
   __device__ __forceinline__ float operator()(float x) const { return __fmaf_rn(x, 0.5f, -half_mean) * twice_rstd; }
 };
 
-// Backward.  n = (x - mean) rstd and t = dY gamma of a row; dgamma and dbeta of the lane's columns over the workgroup's rows.
-template <int W, int V, int R, bool RMS>
-__global__ __launch_bounds__(64 * W * R) void norm_bwd_kernel(const NormArgs a) {
-  __shared__ float red[4 * W * R];
-  __shared__ float sums[R == 1 ? 1 : R * W * V * 512];
+// Backward: dX of the rows from row0 on, R at a time, `step` apart; with SUMS dgamma and dbeta of the lane's columns over them.
+// n = (x - mean) rstd and t = dY gamma of a row.
+template <int W, int V, int R, bool RMS, bool SUMS>
+__device__ __forceinline__ void bwd_rows(const NormArgs& a, uint32_t row0, uint32_t step, float (&dgamma)[V][8], float (&dbeta)[V][8], float* red) {
   const uint32_t team = threadIdx.x / (64 * W), lane = threadIdx.x % (64 * W);
   uint32_t turn = 0;
-  float gamma[V][8], dgamma[V][8], dbeta[V][8];
+  float gamma[V][8];
 #pragma unroll
-  for (int k = 0; k < V; ++k) {
-    vector_eight(a.gamma, (lane + k * 64 * W) * 8, a.C, 1.0f, gamma[k]);
-#pragma unroll
-    for (int e = 0; e < 8; ++e) dgamma[k][e] = dbeta[k][e] = 0.0f;
-  }
+  for (int k = 0; k < V; ++k) vector_eight(a.gamma, (lane + k * 64 * W) * 8, a.C, 1.0f, gamma[k]);
   const float count = (float)a.C;
-  for (uint32_t row0 = blockIdx.x * R; row0 < a.M; row0 += gridDim.x * R) {
+  struct Raw {
+    u32x4 x[V], y[V], r[V];
+    float mean, rstd;
+  };
+  // past the last row the team's neighbour's is read, and nothing stored
+  auto load = [&](uint32_t first, Raw& raw) {
+    const size_t at = first + team < a.M ? first + team : first;
+    const GWS_GLOBAL uint16_t *x = global_ptr<uint16_t>(a.x) + at * a.ldx, *dy = global_ptr<uint16_t>(a.dy) + at * a.lddy;
+#pragma unroll
+    for (int k = 0; k < V; ++k) {
+      raw.x[k] = load_eight(x, (lane + k * 64 * W) * 8, a.C);
+      raw.y[k] = load_eight(dy, (lane + k * 64 * W) * 8, a.C);
+      if (a.r != nullptr) raw.r[k] = load_eight(global_ptr<uint16_t>(a.r) + at * a.ldr, (lane + k * 64 * W) * 8, a.C);
+    }
+    raw.rstd = a.rstd[at];
+    raw.mean = RMS ? 0.0f : a.mean[at];
+  };
+  Raw now;
+  for (; row0 < a.M; row0 += step) {
     const uint32_t row = row0 + team;
     const bool live = row < a.M;
     if (W == 1 && !live) break;
     const size_t at = live ? row : row0;
-    const GWS_GLOBAL uint16_t *x = global_ptr<uint16_t>(a.x) + at * a.ldx, *dy = global_ptr<uint16_t>(a.dy) + at * a.lddy;
-    u32x4 xr[V], yr[V], rr[V];
-#pragma unroll
-    for (int k = 0; k < V; ++k) {
-      xr[k] = load_eight(x, (lane + k * 64 * W) * 8, a.C);
-      yr[k] = load_eight(dy, (lane + k * 64 * W) * 8, a.C);
-      if (a.r != nullptr) rr[k] = load_eight(global_ptr<uint16_t>(a.r) + at * a.ldr, (lane + k * 64 * W) * 8, a.C);
-    }
-    const float rstd = a.rstd[at];
-    const Normalise normal(RMS ? 0.0f : a.mean[at], rstd);
+    load(row0, now);
+    u32x4(&xr)[V] = now.x, (&yr)[V] = now.y, (&rr)[V] = now.r;
+    const float rstd = now.rstd;
+    const Normalise normal(now.mean, rstd);
     float s[2] = {0.0f, 0.0f};
 #pragma unroll
     for (int k = 0; k < V; ++k) {   // columns past the row have dY = 0: they add nothing
@@ -225,7 +232,7 @@ __global__ __launch_bounds__(64 * W * R) void norm_bwd_kernel(const NormArgs a) 
         const float t = d[e] * gamma[k][e];
         s[0] += t;
         s[1] = __fmaf_rn(t, n[e], s[1]);
-        if (live) {
+        if (SUMS && live) {
           dbeta[k][e] += d[e];
           dgamma[k][e] = __fmaf_rn(d[e], n[e], dgamma[k][e]);
         }
@@ -244,12 +251,26 @@ __global__ __launch_bounds__(64 * W * R) void norm_bwd_kernel(const NormArgs a) 
 #pragma unroll
       for (int e = 0; e < 8; ++e) {
         n[e] = normal(n[e]);
-        o[e] = (__fmaf_rn(d[e], gamma[k][e], -s0) - n[e] * s1) * rstd;
+        o[e] = __fmaf_rn(-n[e], s1, __fmaf_rn(d[e], gamma[k][e], -s0)) * rstd;
         if (a.r != nullptr) o[e] += r[e];
       }
       store_eight(dx, (lane + k * 64 * W) * 8, a.C, narrow(o));
     }
   }
+}
+
+// Many rows: a workgroup's sums of its rows go to a.part, and a second kernel adds those up.
+template <int W, int V, int R, bool RMS>
+__global__ __launch_bounds__(64 * W * R) void norm_bwd_kernel(const NormArgs a) {
+  __shared__ float red[4 * W * R];
+  __shared__ float sums[R == 1 ? 1 : R * W * V * 512];
+  const uint32_t team = threadIdx.x / (64 * W), lane = threadIdx.x % (64 * W);
+  float dgamma[V][8], dbeta[V][8];
+#pragma unroll
+  for (int k = 0; k < V; ++k)
+#pragma unroll
+    for (int e = 0; e < 8; ++e) dgamma[k][e] = dbeta[k][e] = 0.0f;
+  bwd_rows<W, V, R, RMS, true>(a, blockIdx.x * R, gridDim.x * R, dgamma, dbeta, red);
   // the workgroup's sums: its R teams' in turn
   float* part = a.part + (size_t)blockIdx.x * ((a.want_gamma ? 1 : 0) + (a.want_beta ? 1 : 0)) * a.C;
 #pragma unroll
@@ -279,6 +300,68 @@ __global__ __launch_bounds__(64 * W * R) void norm_bwd_kernel(const NormArgs a) 
         }
     }
     part += a.C;
+  }
+}
+
+// Few elements: one launch.  Its first workgroups add up dgamma and dbeta of 32 columns each over all rows (mean and rstd are given, so nothing has to wait for
+// the rows' sums), the others make dX.  X and dY are read twice, out of a cache, where a second launch takes longer than that.
+constexpr uint32_t kPairCols = 32, kPairThreads = 512;
+template <int W, int V, bool RMS>
+__global__ __launch_bounds__(kPairThreads) void norm_bwd_pair_kernel(const NormArgs a, const uint32_t column_wgs, float* out_gamma, float* out_beta) {
+  constexpr int R = kPairThreads / (64 * W);
+  __shared__ float red[4 * W * R > 2 * 8 * 32 ? 4 * W * R : 2 * 8 * 32];
+  if (blockIdx.x >= column_wgs) {
+    float none[V][8];
+    bwd_rows<W, V, R, RMS, false>(a, (blockIdx.x - column_wgs) * R, (gridDim.x - column_wgs) * R, none, none, red);
+    return;
+  }
+  // four lanes with eight columns each, 128 rows at a time
+  const uint32_t c = blockIdx.x * kPairCols + (threadIdx.x & 3) * 8;
+  float dgamma[8], dbeta[8];
+#pragma unroll
+  for (int e = 0; e < 8; ++e) dgamma[e] = dbeta[e] = 0.0f;
+#pragma unroll 4
+  for (uint32_t row = threadIdx.x >> 2; row < a.M; row += kPairThreads / 4) {
+    float n[8], d[8];
+    widen(load_eight(global_ptr<uint16_t>(a.x) + (size_t)row * a.ldx, c, a.C), n);
+    widen(load_eight(global_ptr<uint16_t>(a.dy) + (size_t)row * a.lddy, c, a.C), d);
+    const Normalise normal(RMS ? 0.0f : a.mean[row], a.rstd[row]);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      dbeta[e] += d[e];
+      dgamma[e] = __fmaf_rn(d[e], normal(n[e]), dgamma[e]);
+    }
+  }
+  // the sixteen lanes of a wavefront with the same columns, then the wavefronts
+#pragma unroll
+  for (int e = 0; e < 8; ++e) {
+    float* const v[2] = {&dgamma[e], &dbeta[e]};
+#pragma unroll
+    for (int k = 0; k < 2; ++k) {
+      float s = *v[k];
+      s += __uint_as_float(dpp_u32<0x124>(__float_as_uint(s)));   // row_ror 4 and 8: lanes l, l + 4, l + 8, l + 12 of sixteen
+      s += __uint_as_float(dpp_u32<0x128>(__float_as_uint(s)));
+      const auto p = __builtin_amdgcn_permlane16_swap(__float_as_uint(s), __float_as_uint(s), false, false);
+      s = __uint_as_float(p[0]) + __uint_as_float(p[1]);
+      const auto q = __builtin_amdgcn_permlane32_swap(__float_as_uint(s), __float_as_uint(s), false, false);
+      *v[k] = __uint_as_float(q[0]) + __uint_as_float(q[1]);
+    }
+  }
+  const uint32_t wave = threadIdx.x >> 6;
+  if ((threadIdx.x & 63) < 4)
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      red[wave * 32 + (threadIdx.x & 3) * 8 + e] = dgamma[e];
+      red[256 + wave * 32 + (threadIdx.x & 3) * 8 + e] = dbeta[e];
+    }
+  __syncthreads();
+  const uint32_t col = blockIdx.x * kPairCols + (threadIdx.x & 31), which = threadIdx.x >> 5;
+  float* out = which == 0 ? out_gamma : out_beta;
+  if (which < 2 && out != nullptr && col < a.C) {
+    float s = red[256 * which + (threadIdx.x & 31)];
+#pragma unroll
+    for (int w = 1; w < 8; ++w) s += red[256 * which + 32 * w + (threadIdx.x & 31)];
+    out[col] = s;
   }
 }
 
@@ -332,7 +415,7 @@ __global__ __launch_bounds__(256) void norm_bwd_columns_kernel(const NormArgs a)
       n[e] = normal(n[e]);
       dbeta[e] += d[e];
       dgamma[e] = __fmaf_rn(d[e], n[e], dgamma[e]);
-      o[e] = (__fmaf_rn(d[e], gamma[e], -s0) - n[e] * s1) * rstd;
+      o[e] = __fmaf_rn(-n[e], s1, __fmaf_rn(d[e], gamma[e], -s0)) * rstd;
       if (a.r != nullptr) o[e] += r[e];
     }
     store_eight(global_ptr<uint16_t>(a.y) + (size_t)row * a.ldy, c, a.C, narrow(o));
@@ -347,36 +430,46 @@ __global__ __launch_bounds__(256) void norm_bwd_columns_kernel(const NormArgs a)
 }
 
 // ---- sums of partial sums ----
-// A workgroup adds 64 columns, 16 lanes x 4 of them side by side and the P rows shared by 16 groups of lanes, whose sums meet in LDS.
+// A workgroup adds 32 columns, 8 lanes x 4 of them side by side and the P rows shared by 32 groups of lanes, eight loads of each on their way at once; the groups'
+// sums meet in LDS.  Bound by that latency: 256 rows of 1536 columns 2.9 us (64 columns by 16 groups, one load after the other, 6.4).
 __global__ __launch_bounds__(256) void sum_partials_kernel(const float* part, const uint32_t P, const uint64_t n, const uint64_t n0, float* out0, float* out1) {
-  __shared__ f4 red[16][16];
-  const uint32_t group = threadIdx.x >> 4, at = threadIdx.x & 15;
-  const uint64_t c = (uint64_t)blockIdx.x * 64 + 4 * at;
+  __shared__ f4 red[32][8];
+  const uint32_t group = threadIdx.x >> 3, at = threadIdx.x & 7;
+  const uint64_t c = (uint64_t)blockIdx.x * 32 + 4 * at;
   f4 s = {0.0f, 0.0f, 0.0f, 0.0f};
-  for (uint32_t p = group; p < P; p += 16) {
-    const float* q = part + p * n + c;
-    if (c + 4 <= n) {
-      s += *(const GWS_GLOBAL f4_any*)global_ptr<float>(q);
-    } else {
+  for (uint32_t p0 = group; p0 < P; p0 += 256) {
+    f4 v[8];
 #pragma unroll
-      for (int e = 0; e < 3; ++e)
-        if (c + e < n) s[e] += q[e];
+    for (int k = 0; k < 8; ++k) {
+      const uint32_t p = p0 + 32 * k;
+      const GWS_GLOBAL float* q = global_ptr<float>(part) + (p < P ? p : p0) * n + c;
+      v[k] = f4{0.0f, 0.0f, 0.0f, 0.0f};
+      if (c + 4 <= n) {
+        v[k] = *(const GWS_GLOBAL f4_any*)q;
+      } else {
+#pragma unroll
+        for (int e = 0; e < 3; ++e)
+          if (c + e < n) v[k][e] = q[e];
+      }
     }
+#pragma unroll
+    for (int k = 0; k < 8; ++k)
+      if (p0 + 32 * k < P) s += v[k];
   }
   red[group][at] = s;
   __syncthreads();
-  if (threadIdx.x >= 64) return;
+  if (threadIdx.x >= 32) return;
   const float* r = (const float*)red;
   float t = r[threadIdx.x];
 #pragma unroll
-  for (int g = 1; g < 16; ++g) t += r[64 * g + threadIdx.x];
-  const uint64_t col = (uint64_t)blockIdx.x * 64 + threadIdx.x;
+  for (int g = 1; g < 32; ++g) t += r[32 * g + threadIdx.x];
+  const uint64_t col = (uint64_t)blockIdx.x * 32 + threadIdx.x;
   if (col < n0) out0[col] = t;
   else if (col < n) out1[col - n0] = t;
 }
 
 int launch_sum_partials(const float* part, uint32_t P, uint64_t n, uint64_t n0, float* out0, float* out1, hipStream_t stream) {
-  hipLaunchKernelGGL(sum_partials_kernel, dim3((uint32_t)((n + 63) / 64)), dim3(256), 0, stream, part, P, n, n0, out0, out1);
+  hipLaunchKernelGGL(sum_partials_kernel, dim3((uint32_t)((n + 31) / 32)), dim3(256), 0, stream, part, P, n, n0, out0, out1);
   return hipGetLastError() == hipSuccess ? GWS_OK : GWS_ERR_LAUNCH;
 }
 
@@ -412,7 +505,23 @@ int bwd(const NormArgs& a, bool rms, hipStream_t s) {
   return hipGetLastError() == hipSuccess ? GWS_OK : GWS_ERR_LAUNCH;
 }
 // Rows a workgroup of the backward kernels takes at a time.
-uint32_t bwd_rows(uint64_t C) { return C <= 2048 ? 8 : C <= 8192 ? 2 : 1; }
+uint32_t bwd_rows_of(uint64_t C) { return C <= 512 ? 16 : C <= 1024 ? 12 : C <= 2048 ? 8 : C <= 8192 ? 2 : 1; }
+
+template <int W, int V>
+int pair(const NormArgs& a, bool rms, float* dgamma, float* dbeta, hipStream_t s) {
+  constexpr uint32_t R = kPairThreads / (64 * W);
+  const uint32_t columns = (a.C + kPairCols - 1) / kPairCols;
+  const dim3 grid(columns + fewer(((uint64_t)a.M + R - 1) / R, 2 * cus())), block(kPairThreads);
+  if (rms) hipLaunchKernelGGL((norm_bwd_pair_kernel<W, V, true>), grid, block, 0, s, a, columns, dgamma, dbeta);
+  else hipLaunchKernelGGL((norm_bwd_pair_kernel<W, V, false>), grid, block, 0, s, a, columns, dgamma, dbeta);
+  return hipGetLastError() == hipSuccess ? GWS_OK : GWS_ERR_LAUNCH;
+}
+// Whether one launch that reads twice beats two.  us of one and two (in a graph; the host takes 3 more for a second launch): 64 x 768 3.6, 7.4; 1021 x 768 5.0,
+// 8.0; 2048 x 768 7.2, 8.6; 4096 x 768 18.6, 10.9; 1024 x 2048 5.2, 9.8; 2048 x 2048 14.8, 11.9; 1024 x 4096 12.5, 13.8; 512 x 8192 13.3, 16.8; 1024 x 8192
+// 24.0, 22.4; 100 x 16384 7.5, 26.3; 8000 x 128 15.5, 8.4.
+bool one_launch(uint64_t M, uint64_t C) {
+  return !norm_is_wide(C) && M <= 2048 && M * C <= (M <= 1024 ? 4200000u : 2200000u);
+}
 }  // namespace
 
 int launch_norm_fwd(const NormArgs& a, bool rms, hipStream_t s) {
@@ -431,11 +540,19 @@ int launch_norm_fwd(const NormArgs& a, bool rms, hipStream_t s) {
 
 uint32_t norm_bwd_parts(uint64_t M, uint64_t C) {
   if (norm_is_wide(C)) return fewer(M, 64);
-  return fewer((M + bwd_rows(C) - 1) / bwd_rows(C), cus());
+  return fewer((M + bwd_rows_of(C) - 1) / bwd_rows_of(C), cus());
 }
 
 int launch_norm_bwd(const NormArgs& a, bool rms, float* dgamma, float* dbeta, hipStream_t s) {
   int rc;
+  if ((a.want_gamma || a.want_beta) && one_launch(a.M, a.C) && a.y != a.x && a.y != a.dy) {   // in place the rows would change what the columns read
+    if (a.C <= 512) return pair<1, 1>(a, rms, dgamma, dbeta, s);
+    if (a.C <= 1024) return pair<1, 2>(a, rms, dgamma, dbeta, s);
+    if (a.C <= 2048) return pair<1, 4>(a, rms, dgamma, dbeta, s);
+    if (a.C <= 4096) return pair<4, 2>(a, rms, dgamma, dbeta, s);
+    if (a.C <= 8192) return pair<4, 4>(a, rms, dgamma, dbeta, s);
+    return pair<8, 4>(a, rms, dgamma, dbeta, s);
+  }
   if (norm_is_wide(a.C)) {
     const dim3 pieces((uint32_t)(((uint64_t)a.C + 2047) / 2048), norm_bwd_parts(a.M, a.C));
     if (rms) {
@@ -446,8 +563,8 @@ int launch_norm_bwd(const NormArgs& a, bool rms, float* dgamma, float* dbeta, hi
       hipLaunchKernelGGL(norm_bwd_columns_kernel<false>, pieces, dim3(256), 0, s, a);
     }
     rc = hipGetLastError() == hipSuccess ? GWS_OK : GWS_ERR_LAUNCH;
-  } else if (a.C <= 512) rc = bwd<1, 1, 8>(a, rms, s);
-  else if (a.C <= 1024) rc = bwd<1, 2, 8>(a, rms, s);
+  } else if (a.C <= 512) rc = bwd<1, 1, 16>(a, rms, s);
+  else if (a.C <= 1024) rc = bwd<1, 2, 12>(a, rms, s);
   else if (a.C <= 2048) rc = bwd<1, 4, 8>(a, rms, s);
   else if (a.C <= 4096) rc = bwd<4, 2, 2>(a, rms, s);
   else if (a.C <= 8192) rc = bwd<4, 4, 2>(a, rms, s);

@@ -113,6 +113,17 @@ def test_many_tensors_of_both_kinds_in_several_launches():
         p.check(3e-4, 7, 0.9, 0.95, 1e-8, scale=float(scale))
 
 
+def test_many_vectors():
+    """More than a launch holds, of fp32 states and next to each other; matrices without gaps among them."""
+    ps = [Parameter(i, 1 if i % 5 else 3, 8 * (1 + i % 13) if i % 5 == 0 else 1 + 97 * (i % 17), g_fp32=i % 2 == 0, copy=i % 4 != 0) for i in range(260)]
+    packed = gws.pack_adamw([p.desc for p in ps])
+    for p in ps:
+        p.before()
+    gws.gws_adamw(packed, lr=3e-4, step=2)
+    for p in ps:
+        p.check(3e-4, 2, 0.9, 0.95, 1e-8)
+
+
 def test_vectors_and_empty_tensors():
     f = lambda n, x=1.0: torch.full((n,), x, device=DEV)  # noqa: E731
     a = gws.AdamWTensor(p=f(33), g=f(33), m=f(33, 0.0), v=f(33, 0.0))
@@ -228,11 +239,11 @@ def test_gradient_norm_of_many_of_nothing_and_of_small_numbers():
     gws.gws_grad_norm([], out, None, max_norm=1.0)
     assert out.tolist() == [0.0, 1.0]
     g = torch.full((70, 64), 2.0 ** -100, device=DEV)                  # squares below fp32
-    ts = [gws.AdamWTensor(p=g, g=g, m=g, v=g) for _ in range(120)]
+    ts = [gws.AdamWTensor(p=g, g=g, m=g, v=g) for _ in range(500)]
     packed = gws.pack_adamw(ts)
     ws = torch.empty(gws.gws_grad_norm_workspace_bytes(packed), dtype=torch.uint8, device=DEV)
     gws.gws_grad_norm(packed, out, ws)
-    assert abs(float(out[0]) / (2.0 ** -100 * math.sqrt(120 * 70 * 64)) - 1) <= 2.0 ** -23
+    assert abs(float(out[0]) / (2.0 ** -100 * math.sqrt(500 * 70 * 64)) - 1) <= 2.0 ** -23
 
 
 def test_elements_past_32_bits():
