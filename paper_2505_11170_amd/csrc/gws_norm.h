@@ -62,16 +62,22 @@ __device__ __forceinline__ void vector_eight(const float* p, uint32_t c, uint32_
   }
 }
 
-// The sum over a wavefront, in every lane: DPP within rows of 16, then two swaps.
-__device__ __forceinline__ float wave_sum(float v) {
+// The sum over L = 16, 32 or 64 neighbouring lanes, in each of them: DPP within rows of 16, then swaps.
+template <int L>
+__device__ __forceinline__ float lanes_sum(float v) {
   v += __uint_as_float(dpp_u32<0xB1>(__float_as_uint(v)));    // lane ^ 1
   v += __uint_as_float(dpp_u32<0x4E>(__float_as_uint(v)));    // lane ^ 2
   v += __uint_as_float(dpp_u32<0x141>(__float_as_uint(v)));   // the other four of eight
   v += __uint_as_float(dpp_u32<0x140>(__float_as_uint(v)));   // the other eight of sixteen
-  const auto a = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
-  v = __uint_as_float(a[0]) + __uint_as_float(a[1]);
-  const auto b = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
-  return __uint_as_float(b[0]) + __uint_as_float(b[1]);
+  if (L > 16) {
+    const auto a = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    v = __uint_as_float(a[0]) + __uint_as_float(a[1]);
+  }
+  if (L > 32) {
+    const auto b = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    v = __uint_as_float(b[0]) + __uint_as_float(b[1]);
+  }
+  return v;
 }
 
 // Columns of partial sums added up: out[c] = sum over p < P of part[p * n + c] for c < n, columns from n0 on to out1.

@@ -1,7 +1,7 @@
 // Layer norm and root-mean-square norm, forward and backward (gfx950).
 //
-// One pass over memory: a row is in the registers of W wavefronts, 8 V columns a lane, from its load to its store; mean, squares of the deviations
-// and, backward, sum(t) and sum(t n) are sums over lanes (DPP) and, with W > 1, over the wavefronts through LDS.  The variance is the sum of (x - mean)^2,
+// One pass over memory: a row is in the registers of L lanes (16 to 512), 8 V columns a lane, from its load to its store; mean, squares of the deviations
+// and, backward, sum(t) and sum(t n) are sums over lanes (DPP) and, with more than a wavefront's 64, over the wavefronts through LDS.  The variance is the sum of (x - mean)^2,
 // not the difference of two sums: the row is there, and nothing cancels.
 // dgamma and dbeta are sums over the rows: every lane adds up its own columns over the rows that its wavefronts take, the workgroup's rows meet in
 // LDS, and what workgroups leave is added by a second kernel, always in one order.
@@ -11,14 +11,15 @@ namespace gws {
 
 namespace {
 
-// Sums of N values over the W wavefronts of a team, in every lane; `red` holds 2 x N x (wavefronts of the workgroup) floats.  With W > 1 all of the
+// Sums of N values over the L lanes of a row, in each of them; `red` holds 2 x N x (wavefronts of the workgroup) floats.  With more than a wavefront all of the
 // workgroup comes here, and the two halves of `red` alternate, so that one barrier a sum is enough.
-template <int W, int N>
+template <int L, int N>
 __device__ __forceinline__ void team_sum(float (&v)[N], float* red, uint32_t& turn) {
+  constexpr int W = L / 64;
 #pragma unroll
-  for (int n = 0; n < N; ++n) v[n] = wave_sum(v[n]);
-  if (W == 1) return;
-  const uint32_t waves = blockDim.x >> 6, wave = threadIdx.x >> 6, first = wave / W * W;
+  for (int n = 0; n < N; ++n) v[n] = lanes_sum<(L < 64 ? L : 64)>(v[n]);
+  if (W <= 1) return;
+  const uint32_t waves = blockDim.x >> 6, wave = threadIdx.x >> 6, first = wave / (W > 0 ? W : 1) * W;
   float* half = red + turn * N * waves;
   turn ^= 1;
   if ((threadIdx.x & 63) == 0)
@@ -39,13 +40,13 @@ __device__ __forceinline__ void team_sum(float (&v)[N], float* red, uint32_t& tu
 // A row's mean and rstd, and its deviations in f; times `unit` the numbers stay what they are, for rows whose squares would pass fp32's range (beyond 10^19 or
 // so) 2^-80 of them.
 constexpr float kSmallUnit = 0x1p-80f;
-template <int W, int V, bool RMS>
+template <int L, int V, bool RMS>
 __device__ __forceinline__ void row_statistics(const NormArgs& a, const GWS_GLOBAL uint16_t* x, uint32_t lane, float unit, float (&f)[V][8], float& mean, float& rstd,
                                                float* red, uint32_t& turn) {
   const float count = (float)a.C;
 #pragma unroll
   for (int k = 0; k < V; ++k) {
-    widen(load_eight(x, (lane + k * 64 * W) * 8, a.C), f[k]);
+    widen(load_eight(x, (lane + k * L) * 8, a.C), f[k]);
     if (unit != 1.0f)
 #pragma unroll
       for (int e = 0; e < 8; ++e) f[k][e] *= unit;
@@ -57,11 +58,11 @@ __device__ __forceinline__ void row_statistics(const NormArgs& a, const GWS_GLOB
     for (int k = 0; k < V; ++k)
 #pragma unroll
       for (int e = 0; e < 8; ++e) s[0] += f[k][e];
-    team_sum<W>(s, red, turn);
+    team_sum<L>(s, red, turn);
     mean = s[0] / count;
 #pragma unroll
     for (int k = 0; k < V; ++k) {
-      const uint32_t c = (lane + k * 64 * W) * 8;
+      const uint32_t c = (lane + k * L) * 8;
       if (c + 8 <= a.C) {
 #pragma unroll
         for (int e = 0; e < 8; ++e) f[k][e] -= mean;
@@ -76,33 +77,33 @@ __device__ __forceinline__ void row_statistics(const NormArgs& a, const GWS_GLOB
   for (int k = 0; k < V; ++k)
 #pragma unroll
     for (int e = 0; e < 8; ++e) q[0] = __fmaf_rn(f[k][e], f[k][e], q[0]);
-  team_sum<W>(q, red, turn);
+  team_sum<L>(q, red, turn);
   rstd = 1.0f / sqrtf(q[0] / count + a.eps * unit * unit);
 }
 // A sum of squares past fp32's range leaves 0 (or NaN where the mean was past it too): such a row is done again in the small unit.
 __device__ __forceinline__ bool out_of_range(float rstd) { return !(rstd > 0.0f); }
 
-// W wavefronts a row, V groups of eight columns a lane, R rows a workgroup at a time.
-template <int W, int V, int R, bool RMS>
-__global__ __launch_bounds__(64 * W * R) void norm_fwd_kernel(const NormArgs a) {
-  static_assert(W == 1 || R == 1, "all of a workgroup does a row again, or wavefronts that share nothing");
-  __shared__ float red[2 * W * R];
-  const uint32_t team = threadIdx.x / (64 * W), lane = threadIdx.x % (64 * W);
+// L lanes a row, V groups of eight columns a lane, R rows a workgroup at a time.
+template <int L, int V, int R, bool RMS>
+__global__ __launch_bounds__(L * R) void norm_fwd_kernel(const NormArgs a) {
+  static_assert(L <= 64 || R == 1, "all of a workgroup does a row again, or wavefronts that share nothing");
+  __shared__ float red[2 * L * R / 64];
+  const uint32_t team = threadIdx.x / L, lane = threadIdx.x % L;
   uint32_t turn = 0;
   float gamma[V][8], beta[V][8];
 #pragma unroll
   for (int k = 0; k < V; ++k) {
-    vector_eight(a.gamma, (lane + k * 64 * W) * 8, a.C, 1.0f, gamma[k]);
-    vector_eight(a.beta, (lane + k * 64 * W) * 8, a.C, 0.0f, beta[k]);
+    vector_eight(a.gamma, (lane + k * L) * 8, a.C, 1.0f, gamma[k]);
+    vector_eight(a.beta, (lane + k * L) * 8, a.C, 0.0f, beta[k]);
   }
   for (uint32_t row = blockIdx.x * R + team; row < a.M; row += gridDim.x * R) {
     const GWS_GLOBAL uint16_t* x = global_ptr<uint16_t>(a.x) + (size_t)row * a.ldx;
     float f[V][8], mean, rstd, kept_mean, kept_rstd;
-    row_statistics<W, V, RMS>(a, x, lane, 1.0f, f, mean, rstd, red, turn);
+    row_statistics<L, V, RMS>(a, x, lane, 1.0f, f, mean, rstd, red, turn);
     kept_mean = mean;
     kept_rstd = rstd;
     if (out_of_range(rstd)) {   // the same in all lanes of a row
-      row_statistics<W, V, RMS>(a, x, lane, kSmallUnit, f, mean, rstd, red, turn);
+      row_statistics<L, V, RMS>(a, x, lane, kSmallUnit, f, mean, rstd, red, turn);
       kept_mean = mean / kSmallUnit;
       kept_rstd = rstd * kSmallUnit;
     }
@@ -116,7 +117,7 @@ __global__ __launch_bounds__(64 * W * R) void norm_fwd_kernel(const NormArgs a) 
       float o[8];
 #pragma unroll
       for (int e = 0; e < 8; ++e) o[e] = __fmaf_rn(f[k][e] * rstd, gamma[k][e], beta[k][e]);
-      store_eight(y, (lane + k * 64 * W) * 8, a.C, narrow(o));
+      store_eight(y, (lane + k * L) * 8, a.C, narrow(o));
     }
   }
 }
@@ -141,7 +142,7 @@ __global__ __launch_bounds__(1024) void norm_fwd_wide_kernel(const NormArgs a) {
         for (int e = 0; e < 8; ++e) t += f[e] * unit;
         s[0] += t;
       }
-      team_sum<16>(s, red, turn);
+      team_sum<1024>(s, red, turn);
       mean = s[0] / count;
     }
     float q[1] = {0.0f};
@@ -155,7 +156,7 @@ __global__ __launch_bounds__(1024) void norm_fwd_wide_kernel(const NormArgs a) {
       }
       q[0] += t;
     }
-    team_sum<16>(q, red, turn);
+    team_sum<1024>(q, red, turn);
     rstd = 1.0f / sqrtf(q[0] / count + a.eps * unit * unit);
     if (!out_of_range(rstd) || unit != 1.0f) break;   // the same in all threads
     unit = kSmallUnit;
@@ -185,13 +186,13 @@ struct Normalise {
 
 // Backward: dX of the rows from row0 on, R at a time, `step` apart; with SUMS dgamma and dbeta of the lane's columns over them.
 // n = (x - mean) rstd and t = dY gamma of a row.
-template <int W, int V, int R, bool RMS, bool SUMS>
+template <int L, int V, int R, bool RMS, bool SUMS>
 __device__ __forceinline__ void bwd_rows(const NormArgs& a, uint32_t row0, uint32_t step, float (&dgamma)[V][8], float (&dbeta)[V][8], float* red) {
-  const uint32_t team = threadIdx.x / (64 * W), lane = threadIdx.x % (64 * W);
+  const uint32_t team = threadIdx.x / L, lane = threadIdx.x % L;
   uint32_t turn = 0;
   float gamma[V][8];
 #pragma unroll
-  for (int k = 0; k < V; ++k) vector_eight(a.gamma, (lane + k * 64 * W) * 8, a.C, 1.0f, gamma[k]);
+  for (int k = 0; k < V; ++k) vector_eight(a.gamma, (lane + k * L) * 8, a.C, 1.0f, gamma[k]);
   const float count = (float)a.C;
   struct Raw {
     u32x4 x[V], y[V], r[V];
@@ -203,9 +204,9 @@ __device__ __forceinline__ void bwd_rows(const NormArgs& a, uint32_t row0, uint3
     const GWS_GLOBAL uint16_t *x = global_ptr<uint16_t>(a.x) + at * a.ldx, *dy = global_ptr<uint16_t>(a.dy) + at * a.lddy;
 #pragma unroll
     for (int k = 0; k < V; ++k) {
-      raw.x[k] = load_eight(x, (lane + k * 64 * W) * 8, a.C);
-      raw.y[k] = load_eight(dy, (lane + k * 64 * W) * 8, a.C);
-      if (a.r != nullptr) raw.r[k] = load_eight(global_ptr<uint16_t>(a.r) + at * a.ldr, (lane + k * 64 * W) * 8, a.C);
+      raw.x[k] = load_eight(x, (lane + k * L) * 8, a.C);
+      raw.y[k] = load_eight(dy, (lane + k * L) * 8, a.C);
+      if (a.r != nullptr) raw.r[k] = load_eight(global_ptr<uint16_t>(a.r) + at * a.ldr, (lane + k * L) * 8, a.C);
     }
     raw.rstd = a.rstd[at];
     raw.mean = RMS ? 0.0f : a.mean[at];
@@ -214,7 +215,7 @@ __device__ __forceinline__ void bwd_rows(const NormArgs& a, uint32_t row0, uint3
   for (; row0 < a.M; row0 += step) {
     const uint32_t row = row0 + team;
     const bool live = row < a.M;
-    if (W == 1 && !live) break;
+    if (L == 64 && !live) break;   // with fewer lanes a row a wavefront has several
     const size_t at = live ? row : row0;
     load(row0, now);
     u32x4(&xr)[V] = now.x, (&yr)[V] = now.y, (&rr)[V] = now.r;
@@ -238,7 +239,7 @@ __device__ __forceinline__ void bwd_rows(const NormArgs& a, uint32_t row0, uint3
         }
       }
     }
-    team_sum<W>(s, red, turn);
+    team_sum<L>(s, red, turn);
     if (!live) continue;
     const float s0 = RMS ? 0.0f : s[0] / count, s1 = s[1] / count;
     GWS_GLOBAL uint16_t* dx = global_ptr<uint16_t>(a.y) + at * a.ldy;
@@ -254,40 +255,56 @@ __device__ __forceinline__ void bwd_rows(const NormArgs& a, uint32_t row0, uint3
         o[e] = __fmaf_rn(-n[e], s1, __fmaf_rn(d[e], gamma[k][e], -s0)) * rstd;
         if (a.r != nullptr) o[e] += r[e];
       }
-      store_eight(dx, (lane + k * 64 * W) * 8, a.C, narrow(o));
+      store_eight(dx, (lane + k * L) * 8, a.C, narrow(o));
     }
   }
 }
 
 // Many rows: a workgroup's sums of its rows go to a.part, and a second kernel adds those up.
-template <int W, int V, int R, bool RMS>
-__global__ __launch_bounds__(64 * W * R) void norm_bwd_kernel(const NormArgs a) {
-  __shared__ float red[4 * W * R];
-  __shared__ float sums[R == 1 ? 1 : R * W * V * 512];
-  const uint32_t team = threadIdx.x / (64 * W), lane = threadIdx.x % (64 * W);
+template <int L, int V, int R, bool RMS>
+__global__ __launch_bounds__(L * R) void norm_bwd_kernel(const NormArgs a) {
+  __shared__ float red[4 * L * R / 64];
+  constexpr int TEAMS = L < 64 ? L * R / 64 : R;
+  static_assert(L >= 64 || V == 1, "");
+  __shared__ float sums[TEAMS == 1 ? 1 : TEAMS * L * V * 8];
+  const uint32_t team = threadIdx.x / L, lane = threadIdx.x % L;
   float dgamma[V][8], dbeta[V][8];
 #pragma unroll
   for (int k = 0; k < V; ++k)
 #pragma unroll
     for (int e = 0; e < 8; ++e) dgamma[k][e] = dbeta[k][e] = 0.0f;
-  bwd_rows<W, V, R, RMS, true>(a, blockIdx.x * R, gridDim.x * R, dgamma, dbeta, red);
-  // the workgroup's sums: its R teams' in turn
+  bwd_rows<L, V, R, RMS, true>(a, blockIdx.x * R, gridDim.x * R, dgamma, dbeta, red);
+  // the workgroup's sums: rows that share a wavefront by lanes, then its TEAMS of a wavefront or more in turn
   float* part = a.part + (size_t)blockIdx.x * ((a.want_gamma ? 1 : 0) + (a.want_beta ? 1 : 0)) * a.C;
 #pragma unroll
   for (int which = 0; which < 2; ++which) {
     if (which == 0 ? !a.want_gamma : !a.want_beta) continue;
     float(&mine)[V][8] = which == 0 ? dgamma : dbeta;
-    if (R > 1) {
-      __syncthreads();
+    if (L < 64)
 #pragma unroll
-      for (int k = 0; k < V; ++k)
-#pragma unroll
-        for (int e = 0; e < 8; e += 4) *(f4*)(sums + team * (W * V * 512) + (lane + k * 64 * W) * 8 + e) = f4{mine[k][e], mine[k][e + 1], mine[k][e + 2], mine[k][e + 3]};
+      for (int e = 0; e < 8; ++e) {
+        uint32_t v = __float_as_uint(mine[0][e]);
+        if (L == 16) {
+          const auto p = __builtin_amdgcn_permlane16_swap(v, v, false, false);
+          v = __float_as_uint(__uint_as_float(p[0]) + __uint_as_float(p[1]));
+        }
+        const auto q = __builtin_amdgcn_permlane32_swap(v, v, false, false);
+        mine[0][e] = __uint_as_float(q[0]) + __uint_as_float(q[1]);
+      }
+    if (TEAMS > 1) {
       __syncthreads();
-      for (uint32_t c = threadIdx.x; c < a.C; c += 64 * W * R) {
+      if (L >= 64 || (threadIdx.x & 63) < L) {
+#pragma unroll
+        for (int k = 0; k < V; ++k)
+#pragma unroll
+          for (int e = 0; e < 8; e += 4)
+            *(f4*)(sums + (L < 64 ? threadIdx.x / 64 : team) * (L * V * 8) + (lane + k * L) * 8 + e) = f4{mine[k][e], mine[k][e + 1], mine[k][e + 2], mine[k][e + 3]};
+      }
+      __syncthreads();
+      for (uint32_t c = threadIdx.x; c < a.C; c += L * R) {
         float s = sums[c];
 #pragma unroll
-        for (int t = 1; t < R; ++t) s += sums[t * (W * V * 512) + c];
+        for (int t = 1; t < TEAMS; ++t) s += sums[t * (L * V * 8) + c];
         part[c] = s;
       }
     } else {
@@ -295,7 +312,7 @@ __global__ __launch_bounds__(64 * W * R) void norm_bwd_kernel(const NormArgs a) 
       for (int k = 0; k < V; ++k)
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
-          const uint32_t c = (lane + k * 64 * W) * 8 + e;
+          const uint32_t c = (lane + k * L) * 8 + e;
           if (c < a.C) part[c] = mine[k][e];
         }
     }
@@ -306,13 +323,13 @@ __global__ __launch_bounds__(64 * W * R) void norm_bwd_kernel(const NormArgs a) 
 // Few elements: one launch.  Its first workgroups add up dgamma and dbeta of 32 columns each over all rows (mean and rstd are given, so nothing has to wait for
 // the rows' sums), the others make dX.  X and dY are read twice, out of a cache, where a second launch takes longer than that.
 constexpr uint32_t kPairCols = 32, kPairThreads = 512;
-template <int W, int V, bool RMS>
+template <int L, int V, bool RMS>
 __global__ __launch_bounds__(kPairThreads) void norm_bwd_pair_kernel(const NormArgs a, const uint32_t column_wgs, float* out_gamma, float* out_beta) {
-  constexpr int R = kPairThreads / (64 * W);
-  __shared__ float red[4 * W * R > 2 * 8 * 32 ? 4 * W * R : 2 * 8 * 32];
+  constexpr int R = kPairThreads / L;
+  __shared__ float red[2 * 8 * 32];   // more than the 4 x 8 of the rows' sums
   if (blockIdx.x >= column_wgs) {
     float none[V][8];
-    bwd_rows<W, V, R, RMS, false>(a, (blockIdx.x - column_wgs) * R, (gridDim.x - column_wgs) * R, none, none, red);
+    bwd_rows<L, V, R, RMS, false>(a, (blockIdx.x - column_wgs) * R, (gridDim.x - column_wgs) * R, none, none, red);
     return;
   }
   // four lanes with eight columns each, 128 rows at a time
@@ -388,7 +405,7 @@ __global__ __launch_bounds__(1024) void norm_bwd_rows_kernel(const NormArgs a) {
     s[0] += s0;
     s[1] += s1;
   }
-  team_sum<16>(s, red, turn);
+  team_sum<1024>(s, red, turn);
   if (threadIdx.x == 0) {
     a.rows[2 * (size_t)row] = RMS ? 0.0f : s[0] / (float)a.C;
     a.rows[2 * (size_t)row + 1] = s[1] / (float)a.C;
@@ -490,30 +507,30 @@ namespace {
 uint32_t cus() { return compute_units() > 0 ? (uint32_t)compute_units() : 256; }
 uint32_t fewer(uint64_t a, uint64_t b) { return (uint32_t)(a < b ? a : b); }
 
-template <int W, int V, int R>
+template <int L, int V, int R>
 int fwd(const NormArgs& a, bool rms, hipStream_t s) {
-  const dim3 grid(fewer(((uint64_t)a.M + R - 1) / R, 8 * cus())), block(64 * W * R);
-  if (rms) hipLaunchKernelGGL((norm_fwd_kernel<W, V, R, true>), grid, block, 0, s, a);
-  else hipLaunchKernelGGL((norm_fwd_kernel<W, V, R, false>), grid, block, 0, s, a);
+  const dim3 grid(fewer(((uint64_t)a.M + R - 1) / R, 8 * cus())), block(L * R);
+  if (rms) hipLaunchKernelGGL((norm_fwd_kernel<L, V, R, true>), grid, block, 0, s, a);
+  else hipLaunchKernelGGL((norm_fwd_kernel<L, V, R, false>), grid, block, 0, s, a);
   return hipGetLastError() == hipSuccess ? GWS_OK : GWS_ERR_LAUNCH;
 }
-template <int W, int V, int R>
+template <int L, int V, int R>
 int bwd(const NormArgs& a, bool rms, hipStream_t s) {
-  const dim3 grid(norm_bwd_parts(a.M, a.C)), block(64 * W * R);
-  if (rms) hipLaunchKernelGGL((norm_bwd_kernel<W, V, R, true>), grid, block, 0, s, a);
-  else hipLaunchKernelGGL((norm_bwd_kernel<W, V, R, false>), grid, block, 0, s, a);
+  const dim3 grid(norm_bwd_parts(a.M, a.C)), block(L * R);
+  if (rms) hipLaunchKernelGGL((norm_bwd_kernel<L, V, R, true>), grid, block, 0, s, a);
+  else hipLaunchKernelGGL((norm_bwd_kernel<L, V, R, false>), grid, block, 0, s, a);
   return hipGetLastError() == hipSuccess ? GWS_OK : GWS_ERR_LAUNCH;
 }
 // Rows a workgroup of the backward kernels takes at a time.
-uint32_t bwd_rows_of(uint64_t C) { return C <= 512 ? 16 : C <= 1024 ? 12 : C <= 2048 ? 8 : C <= 8192 ? 2 : 1; }
+uint32_t bwd_rows_of(uint64_t C) { return C <= 128 ? 64 : C <= 256 ? 32 : C <= 512 ? 16 : C <= 1024 ? 12 : C <= 2048 ? 8 : C <= 8192 ? 2 : 1; }
 
-template <int W, int V>
+template <int L, int V>
 int pair(const NormArgs& a, bool rms, float* dgamma, float* dbeta, hipStream_t s) {
-  constexpr uint32_t R = kPairThreads / (64 * W);
+  constexpr uint32_t R = kPairThreads / L;
   const uint32_t columns = (a.C + kPairCols - 1) / kPairCols;
   const dim3 grid(columns + fewer(((uint64_t)a.M + R - 1) / R, 2 * cus())), block(kPairThreads);
-  if (rms) hipLaunchKernelGGL((norm_bwd_pair_kernel<W, V, true>), grid, block, 0, s, a, columns, dgamma, dbeta);
-  else hipLaunchKernelGGL((norm_bwd_pair_kernel<W, V, false>), grid, block, 0, s, a, columns, dgamma, dbeta);
+  if (rms) hipLaunchKernelGGL((norm_bwd_pair_kernel<L, V, true>), grid, block, 0, s, a, columns, dgamma, dbeta);
+  else hipLaunchKernelGGL((norm_bwd_pair_kernel<L, V, false>), grid, block, 0, s, a, columns, dgamma, dbeta);
   return hipGetLastError() == hipSuccess ? GWS_OK : GWS_ERR_LAUNCH;
 }
 // Whether one launch that reads twice beats two.  us of one and two (in a graph; the host takes 3 more for a second launch): 64 x 768 3.6, 7.4; 1021 x 768 5.0,
@@ -530,12 +547,16 @@ int launch_norm_fwd(const NormArgs& a, bool rms, hipStream_t s) {
     else hipLaunchKernelGGL(norm_fwd_wide_kernel<false>, dim3(a.M), dim3(1024), 0, s, a);
     return hipGetLastError() == hipSuccess ? GWS_OK : GWS_ERR_LAUNCH;
   }
-  if (a.C <= 512) return fwd<1, 1, 4>(a, rms, s);
-  if (a.C <= 1024) return fwd<1, 2, 4>(a, rms, s);
-  if (a.C <= 2048) return fwd<1, 4, 4>(a, rms, s);
-  if (a.C <= 4096) return fwd<4, 2, 1>(a, rms, s);
-  if (a.C <= 8192) return fwd<4, 4, 1>(a, rms, s);
-  return fwd<8, 4, 1>(a, rms, s);
+  if (a.C <= 128) return fwd<16, 1, 16>(a, rms, s);
+  if (a.C <= 256) return fwd<32, 1, 8>(a, rms, s);
+  if (a.C <= 512) return fwd<64, 1, 4>(a, rms, s);
+  if (a.C <= 1024) return fwd<64, 2, 4>(a, rms, s);
+  if (a.C <= 1536) return fwd<64, 3, 4>(a, rms, s);
+  if (a.C <= 2048) return fwd<64, 4, 4>(a, rms, s);
+  if (a.C <= 4096) return fwd<256, 2, 1>(a, rms, s);
+  if (a.C <= 6144) return fwd<256, 3, 1>(a, rms, s);
+  if (a.C <= 8192) return fwd<256, 4, 1>(a, rms, s);
+  return fwd<512, 4, 1>(a, rms, s);
 }
 
 uint32_t norm_bwd_parts(uint64_t M, uint64_t C) {
@@ -546,12 +567,14 @@ uint32_t norm_bwd_parts(uint64_t M, uint64_t C) {
 int launch_norm_bwd(const NormArgs& a, bool rms, float* dgamma, float* dbeta, hipStream_t s) {
   int rc;
   if ((a.want_gamma || a.want_beta) && one_launch(a.M, a.C) && a.y != a.x && a.y != a.dy) {   // in place the rows would change what the columns read
-    if (a.C <= 512) return pair<1, 1>(a, rms, dgamma, dbeta, s);
-    if (a.C <= 1024) return pair<1, 2>(a, rms, dgamma, dbeta, s);
-    if (a.C <= 2048) return pair<1, 4>(a, rms, dgamma, dbeta, s);
-    if (a.C <= 4096) return pair<4, 2>(a, rms, dgamma, dbeta, s);
-    if (a.C <= 8192) return pair<4, 4>(a, rms, dgamma, dbeta, s);
-    return pair<8, 4>(a, rms, dgamma, dbeta, s);
+    if (a.C <= 128) return pair<16, 1>(a, rms, dgamma, dbeta, s);
+    if (a.C <= 256) return pair<32, 1>(a, rms, dgamma, dbeta, s);
+    if (a.C <= 512) return pair<64, 1>(a, rms, dgamma, dbeta, s);
+    if (a.C <= 1024) return pair<64, 2>(a, rms, dgamma, dbeta, s);
+    if (a.C <= 2048) return pair<64, 4>(a, rms, dgamma, dbeta, s);
+    if (a.C <= 4096) return pair<256, 2>(a, rms, dgamma, dbeta, s);
+    if (a.C <= 8192) return pair<256, 4>(a, rms, dgamma, dbeta, s);
+    return pair<512, 4>(a, rms, dgamma, dbeta, s);
   }
   if (norm_is_wide(a.C)) {
     const dim3 pieces((uint32_t)(((uint64_t)a.C + 2047) / 2048), norm_bwd_parts(a.M, a.C));
@@ -563,12 +586,16 @@ int launch_norm_bwd(const NormArgs& a, bool rms, float* dgamma, float* dbeta, hi
       hipLaunchKernelGGL(norm_bwd_columns_kernel<false>, pieces, dim3(256), 0, s, a);
     }
     rc = hipGetLastError() == hipSuccess ? GWS_OK : GWS_ERR_LAUNCH;
-  } else if (a.C <= 512) rc = bwd<1, 1, 16>(a, rms, s);
-  else if (a.C <= 1024) rc = bwd<1, 2, 12>(a, rms, s);
-  else if (a.C <= 2048) rc = bwd<1, 4, 8>(a, rms, s);
-  else if (a.C <= 4096) rc = bwd<4, 2, 2>(a, rms, s);
-  else if (a.C <= 8192) rc = bwd<4, 4, 2>(a, rms, s);
-  else rc = bwd<8, 4, 1>(a, rms, s);
+  } else if (a.C <= 128) rc = bwd<16, 1, 64>(a, rms, s);
+  else if (a.C <= 256) rc = bwd<32, 1, 32>(a, rms, s);
+  else if (a.C <= 512) rc = bwd<64, 1, 16>(a, rms, s);
+  else if (a.C <= 1024) rc = bwd<64, 2, 12>(a, rms, s);
+  else if (a.C <= 1536) rc = bwd<64, 3, 8>(a, rms, s);
+  else if (a.C <= 2048) rc = bwd<64, 4, 8>(a, rms, s);
+  else if (a.C <= 4096) rc = bwd<256, 2, 2>(a, rms, s);
+  else if (a.C <= 6144) rc = bwd<256, 3, 2>(a, rms, s);
+  else if (a.C <= 8192) rc = bwd<256, 4, 2>(a, rms, s);
+  else rc = bwd<512, 4, 1>(a, rms, s);
   if (rc != GWS_OK || (!a.want_gamma && !a.want_beta)) return rc;
   const uint64_t n = a.want_gamma && a.want_beta ? 2 * (uint64_t)a.C : a.C;
   return launch_sum_partials(a.part, norm_bwd_parts(a.M, a.C), n, a.C, a.want_gamma ? dgamma : dbeta, dbeta, s);

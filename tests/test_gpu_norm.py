@@ -38,7 +38,7 @@ def untouched(whole, C):
 
 
 # one lane's part of a row, a row of each width of kernel and one element to either side, rows that are read again
-SIZES = [(1, 1), (3, 7), (1, 2048), (5, 64), (2, 511), (300, 768), (7, 513), (3, 1025), (1021, 1000), (3, 2047), (9, 2049), (2, 4100), (5, 8192), (3, 8200),
+SIZES = [(1, 1), (3, 7), (1, 2048), (5, 64), (131, 128), (77, 129), (2, 256), (2, 511), (300, 768), (6, 1536), (7, 513), (3, 1025), (1021, 1000), (3, 2047), (9, 2049), (2, 4100), (5, 8192), (3, 8200),
          (2, 16384), (2, 16385), (3, 40003)]
 
 
@@ -98,14 +98,14 @@ def test_backward(M, C, kind):
     assert_within(dx2, want[0], tol[0], "bare")
 
 
-def test_many_rows():
-    M, C = 20000, 96
-    x, dy = rand(1, M, C), rand(2, M, C, 1e-3)
-    y, mean, rstd = room(M, C)[0], torch.zeros(M, device=DEV), torch.zeros(M, device=DEV)
+@pytest.mark.parametrize("M,C", [(20000, 96), (5001, 250), (2100, 400), (2500, 1000), (2049, 1500), (2050, 2048), (1100, 4000), (1100, 6000), (1100, 8000), (600, 9000)])
+def test_many_rows(M, C):
+    x, dy = rand(1, M, C, ld=ld_of(C)), rand(2, M, C, 1e-3, ld_of(C))
+    y, mean, rstd = room(M, C, ld_of(C))[0], torch.zeros(M, device=DEV), torch.zeros(M, device=DEV)
     gws.gws_norm_fwd(x, y, mean=mean, rstd=rstd)
     want, tol = ref.norm_fwd(x, LAYER, None, None, 1e-5)
     assert_within(y, want[0], tol[0], "y")
-    dx, dgamma, dbeta = room(M, C)[0], torch.zeros(C, device=DEV), torch.zeros(C, device=DEV)
+    dx, dgamma, dbeta = room(M, C, ld_of(C))[0], torch.zeros(C, device=DEV), torch.zeros(C, device=DEV)
     ws = torch.empty(gws.gws_norm_bwd_workspace_bytes(M, C), dtype=torch.uint8, device=DEV)
     gws.gws_norm_bwd(dy, x, dx, rstd, mean=mean, dgamma=dgamma, dbeta=dbeta, workspace=ws)
     want, tol = ref.norm_bwd(dy, x, LAYER, None, mean, rstd, None)
