@@ -34,10 +34,15 @@ struct NoGate {
     slope = 1.0f;
   }
 };
+// GELU without the gate's bound on z^2: where z^2 is infinite, exp's argument is an infinity of the right sign, and q is 0 or 1 all the same.
+struct GeluGate : Gate<GWS_ACT_GELU_TANH> {
+  __device__ static __forceinline__ float a(float z) { return z * logistic(z * __fmaf_rn(-kLog2e * kGelu3, z * z, -kLog2e * kGelu1)); }
+};
 template <class F>
 __device__ __forceinline__ void with_act(int act, F&& f) {   // a uniform branch
   if (act == GWS_ACT_NONE) f(NoGate());
-  else with_gate(act, (F&&)f);
+  else if (act == GWS_ACT_SILU) f(Gate<GWS_ACT_SILU>());
+  else f(GeluGate());
 }
 inline bool known_dense_act(int act) { return act == GWS_ACT_NONE || known_act(act); }
 

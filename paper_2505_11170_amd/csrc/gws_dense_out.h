@@ -57,7 +57,7 @@ __device__ __forceinline__ void dense_out_by(G gate, const GemmArgs& g, const De
   uint16_t* const second = OP == DenseOp::kFwd ? d.z : d.h;   // the other output
   const uint32_t ld2 = OP == DenseOp::kFwd ? d.ldz : d.ldh, off2 = (r * ld2 + c) * 2;
   GWS_GLOBAL uint8_t* p2 = at_row(second, p0, (size_t)ld2 * 2, (size_t)q0 * 2);
-  const bool reads = (OP == DenseOp::kFwd ? d.r : d.z) != nullptr;
+  const bool reads = (OP == DenseOp::kFwd ? d.r : d.z) != nullptr, sums = OP == DenseOp::kBwd && d.part != nullptr;
   float total[8] = {0, 0, 0, 0, 0, 0, 0, 0};
 #pragma unroll
   for (int quarter = 0; quarter < NI / 2; ++quarter) {
@@ -74,23 +74,35 @@ __device__ __forceinline__ void dense_out_by(G gate, const GemmArgs& g, const De
       const uint32_t row = ROWS * it + r;
       if ((!EDGE || 32 * quarter + (int)row < rows) && col_in) {
         const f32x4 s0 = *(const f32x4*)(cs + row * PF + c), s1 = *(const f32x4*)(cs + row * PF + c + 4);
-        float s[8] = {s0[0], s0[1], s0[2], s0[3], s1[0], s1[1], s1[2], s1[3]}, o[8], other[8], e[8] = {0, 0, 0, 0, 0, 0, 0, 0};
-        if (reads) widen(in[it], e);
+        float s[8] = {s0[0], s0[1], s0[2], s0[3], s1[0], s1[1], s1[2], s1[3]}, o[8], other[8], e[8];
         const uint32_t row0 = 32 * quarter + ROWS * it;
+        // uniform branches around what a call leaves out: a vector instruction an element is 1 % of a large tile's time
         if (OP == DenseOp::kFwd) {
 #pragma unroll
           for (int k = 0; k < 8; ++k) {
             other[k] = s[k] + held.bias[k];
-            o[k] = gate.a(other[k]) + e[k];
+            o[k] = gate.a(other[k]);
+          }
+          if (reads) {
+            widen(in[it], e);
+#pragma unroll
+            for (int k = 0; k < 8; ++k) o[k] += e[k];
           }
         } else {
+          if (reads) widen(in[it], e);
+          else widen(u32x4{0, 0, 0, 0}, e);
 #pragma unroll
           for (int k = 0; k < 8; ++k) {
             float slope;
             gate.both(e[k], other[k], slope);
             o[k] = s[k] * slope;
-            total[k] += o[k];
-            asm volatile("" : "+v"(total[k]));   // here: put off to the end of it all, the additions keep every row's values (to scratch)
+          }
+          if (sums) {
+#pragma unroll
+            for (int k = 0; k < 8; ++k) {
+              total[k] += o[k];
+              asm volatile("" : "+v"(total[k]));   // here: put off to the end of it all, the additions keep every row's values (to scratch)
+            }
           }
         }
         store_out<STREAM>(narrow(o), yp + (size_t)row0 * g.ldy * 2 + y_off);
@@ -101,7 +113,7 @@ __device__ __forceinline__ void dense_out_by(G gate, const GemmArgs& g, const De
     }
     own_lds_wait();
   }
-  if (OP == DenseOp::kBwd && d.part != nullptr && rows > 0) {   // uniform: the sums of the wavefront's rows
+  if (sums && rows > 0) {   // uniform: the sums of the wavefront's rows
     if (LANES * ROWS == 64 || lane < LANES * ROWS) {
       *(f32x4*)(cs + r * (16 * NJ) + c) = f32x4{total[0], total[1], total[2], total[3]};
       *(f32x4*)(cs + r * (16 * NJ) + c + 4) = f32x4{total[4], total[5], total[6], total[7]};
