@@ -116,6 +116,14 @@ int gws_box_muller_check(uint64_t first, uint64_t n, void* out, void* stream);
 #define GWS_GATED_SHARED 5 /* the middle tile, two workgroups a compute unit */
 int gws_gated_form(int op, int64_t M, int64_t K, int64_t F, int64_t lda, int64_t ldw, int w_is_nk, int kept);
 
+/* The kernel that gws_dense_fwd (op GWS_DENSE_FWD; K columns of X, N of Y) or gws_dense_bwd (GWS_DENSE_BWD; K columns of dY, N of dZ) takes with an epilogue, w_is_nk
+ * as the call takes it: GWS_GEMM_STREAM, _MIDDLE, _LARGE, _LARGE_EDGE, _NARROW or _ANY_SHAPE with the tiles of gws_gemm_tile, or GWS_DENSE_SHARED.  0 for what the call
+ * refuses.  Host function.                                                                                                                     */
+#define GWS_DENSE_FWD 0
+#define GWS_DENSE_BWD 1
+#define GWS_DENSE_SHARED 10 /* 128 x 128 tiles, two workgroups a compute unit */
+int gws_dense_form(int op, int64_t M, int64_t K, int64_t N, int64_t ldx, int64_t ldw, int w_is_nk);
+
 #ifdef __cplusplus
 }
 #endif

@@ -33,11 +33,12 @@ EXPORTS = ("gws_sample_fwd", "gws_sample_bwd", "gws_sample_fwd_bi", "gws_sample_
            "gws_adamw", "gws_grad_norm", "gws_grad_norm_workspace_bytes",
            "gws_derive_seed", "gws_status_string", "gws_version")
 BENCH_EXPORTS = ("gws_copy_tiles", "gws_block_absmax", "gws_sample_bwd_tuned", "gws_sample_fwd_tuned", "gws_gemm_bf16_ride_probe", "gws_ride_plan",
-                 "gws_ride_plan_layout", "gws_gemm_form", "gws_gemm_tile", "gws_gemm_stream_tile", "gws_linear_bwd_w_form", "gws_linear_bwd_w_form_rows", "gws_gated_form", "gws_box_muller_check")
+                 "gws_ride_plan_layout", "gws_gemm_form", "gws_gemm_tile", "gws_gemm_stream_tile", "gws_linear_bwd_w_form", "gws_linear_bwd_w_form_rows", "gws_gated_form", "gws_dense_form", "gws_box_muller_check")
 # kernels as gws_gemm_form and gws_linear_bwd_w_form name them
 GEMM_STREAM, GEMM_MIDDLE, GEMM_LARGE, GEMM_LARGE_EDGE, GEMM_NARROW, GEMM_ANY_SHAPE, GEMM_STREAM_SAMPLE, GEMM_ROWS_SAMPLE, GEMM_ANY_SHAPE_SAMPLE = range(1, 10)
 BWD_W_WIDE, BWD_W_NARROW, BWD_W_PIECES_64, BWD_W_PIECES_128, BWD_W_SPLIT = 1, 2, 3, 4, 16
 BWD_W_PIECES_96, BWD_W_PIECES_128_128, BWD_W_PIECES_32 = 5, 6, 7
+DENSE_FWD, DENSE_BWD, DENSE_SHARED = 0, 1, 10        # of gws_dense_form: the calls, and the kernel that gws_gemm_bf16 has not
 
 
 class GwsError(RuntimeError):
@@ -277,6 +278,8 @@ def load_library() -> ctypes.CDLL:
     L.gws_dense_bwd.restype = ci
     L.gws_dense_bwd_h.argtypes = [vp, i64, i64, i64, ci, vp, i64, vp, i64, vp, i64, vp, vp, sz, vp]
     L.gws_dense_bwd_h.restype = ci
+    L.gws_dense_form.argtypes = [ci, i64, i64, i64, i64, i64, ci]
+    L.gws_dense_form.restype = ci
     wp = ctypes.POINTER(_CAdamWTensor)
     L.gws_adamw.argtypes = [wp, ci, vp, vp]
     L.gws_adamw.restype = ci
@@ -956,6 +959,12 @@ def gws_dense_bwd_h(dh, z, dz, act: int = ACT_NONE, h=None, dbias=None, workspac
     (pdy, lddy), (pz, ldz), (pd, ldd), (ph, ldh) = _matrix(dh, size, on), _matrix(z, size, on), _matrix(dz, size, on), _matrix(h, size, on)
     _check((_lib or load_library()).gws_dense_bwd_h(pdy, M, F, lddy, act, pz, ldz, pd, ldd, ph, ldh, _vector(dbias, F, on), *_bytes_of(workspace, on),
                                                     _stream_of(on, stream)), "gws_dense_bwd_h")
+
+
+def gws_dense_form(op: int, M: int, K: int, N: int, w_is_nk: bool = False, ldx: Optional[int] = None, ldw: Optional[int] = None) -> int:
+    """The kernel (``GEMM_*``, ``DENSE_SHARED``) of ``gws_dense_fwd`` (``DENSE_FWD``) or ``gws_dense_bwd`` (``DENSE_BWD``: K columns of dY, N of dZ)."""
+    along = bool(w_is_nk) == (op == DENSE_FWD)
+    return int(load_library().gws_dense_form(op, M, K, N, K if ldx is None else ldx, (K if along else N) if ldw is None else ldw, int(bool(w_is_nk))))
 
 
 class PackedAdamW:

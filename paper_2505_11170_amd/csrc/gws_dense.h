@@ -50,12 +50,14 @@ inline bool known_dense_act(int act) { return act == GWS_ACT_NONE || known_act(a
 struct DensePlan {
   GemmForm form;         // kAnyShape: dense_any_kernel
   RoutePlan route;
+  bool shared;           // kMiddle: two workgroups a compute unit
   uint32_t rows;
 };
-DensePlan plan_dense(const GemmArgs& g, const DenseArgs& d, int w_is_nk);
+DensePlan plan_dense(const GemmArgs& g, const DenseArgs& d, DenseOp op, int w_is_nk);
 // 256 x 256 tiles (whole, or with edges), 256 x 192
 int launch_dense256(const GemmArgs& g, const DenseArgs& d, DenseOp op, int w_is_nk, GemmForm form, hipStream_t stream);
-int launch_dense128(const GemmArgs& g, const DenseArgs& d, DenseOp op, int w_is_nk, int nj, hipStream_t stream);
+// tiles of 128 x 32 nj; shared: of 128 x 128, two workgroups a compute unit
+int launch_dense128(const GemmArgs& g, const DenseArgs& d, DenseOp op, int w_is_nk, int nj, bool shared, hipStream_t stream);
 int launch_dense_stream(const GemmArgs& g, const DenseArgs& d, DenseOp op, int w_is_nk, const StreamPlan& p, hipStream_t stream);
 // every size
 int launch_dense_any(const GemmArgs& g, const DenseArgs& e, DenseOp op, int w_is_nk, hipStream_t stream);

@@ -144,10 +144,11 @@ __device__ __forceinline__ DenseHeld<OP, true, 4, NJ> before128(const GemmArgs& 
   held.begin(g, way.d, m0 + 64 * (wave >> 1), n0 + 16 * NJ * (wave & 1), lane);
   return held;
 }
-template <int NJ, DenseOp OP>
+template <int NJ, int D, DenseOp OP>
 __device__ __forceinline__ void finish128(const GemmArgs& g, const f32x4 (&acc)[4][NJ], DenseHeld<OP, true, 4, NJ>& held, uint16_t* lds, uint32_t wave, uint32_t lane,
                                           uint32_t m0, uint32_t n0, const DenseWay<OP>& way) {
-  constexpr uint32_t SHARE = (128 + 32 * NJ) * 64;   // elements of the ring (four stages) that are a wavefront's
+  constexpr uint32_t SHARE = D * (128 + 32 * NJ) * 64 / 4;   // elements of the ring that are a wavefront's
+  static_assert(SHARE * 2 >= 32 * (16 * NJ + 4) * 4, "32 rows are staged in it");
   const uint32_t p0 = m0 + 64 * (wave >> 1);
   dense_out<OP, true, 4, NJ>(g, way.d, acc, held, (float*)(lds + wave * SHARE), p0, n0 + 16 * NJ * (wave & 1), lane, p0 / 64);
 }

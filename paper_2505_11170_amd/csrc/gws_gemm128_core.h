@@ -8,7 +8,7 @@ namespace gws {
 
 
 namespace g128 {
-constexpr int T = 128, TK = 64, D = 4;   // rows of a tile, depth of a K-step, stages
+constexpr int T = 128, TK = 64;          // rows of a tile, depth of a K-step
 constexpr uint32_t kMaxLd = 1u << 24;    // 32-bit lane offsets: 127 rows x 2 bytes
 __device__ __forceinline__ uint32_t umin(uint32_t a, uint32_t b) { return a < b ? a : b; }
 }  // namespace g128
@@ -18,12 +18,13 @@ struct NothingHeld {};
 template <int NJ>
 __device__ __forceinline__ NothingHeld before128(const GemmArgs&, uint32_t, uint32_t, uint32_t, uint32_t) { return {}; }
 
-template <int NJ>
+template <int NJ, int D>
 void finish128();   // the way outs' (gws_dense_out.h)
 
 // Without `way_out` the kernel stores Y; with one (its functions: before128, finish128) that takes the sums instead.
-template <bool W_NK, int NJ, class... WayOut>
-__global__ __launch_bounds__(256) void gemm128_kernel(GWS_GEMM_PARAMS, const WayOut... way_out) {
+// D: stages of the ring.  With two of them (only with a way out) a second workgroup shares the compute unit, and one's way out runs under the other's loop.
+template <bool W_NK, int NJ, int D, class... WayOut>
+__global__ __launch_bounds__(256, D == 2 ? 2 : 1) void gemm128_kernel(GWS_GEMM_PARAMS, const WayOut... way_out) {
   using namespace g128;
   const GemmArgs g = GWS_GEMM_GATHER({});
   constexpr int TN = 32 * NJ, OP = T * TK, STG = OP + TN * TK;   // columns of a tile; elements of the X tile, of a stage
@@ -191,7 +192,7 @@ __global__ __launch_bounds__(256) void gemm128_kernel(GWS_GEMM_PARAMS, const Way
   asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");   // the ring is read
 
   if constexpr (sizeof...(WayOut) > 0) {
-    finish128<NJ>(g, acc, held, lds, wave, lane, m0, n0, way_out...);
+    finish128<NJ, D>(g, acc, held, lds, wave, lane, m0, n0, way_out...);
   } else {
     // out through LDS, 16 bytes a lane
     uint16_t* cs = lds + wave * (64 * PC);
@@ -211,13 +212,13 @@ __global__ __launch_bounds__(256) void gemm128_kernel(GWS_GEMM_PARAMS, const Way
   }
 }
 
-template <int NJ, class... WayOut>
+template <int NJ, int D = 4, class... WayOut>
 inline int launch_middle_tiles(GemmArgs g, int w_is_nk, hipStream_t stream, const WayOut&... way_out) {
   const uint32_t mt = (uint32_t)(((uint64_t)g.M + g128::T - 1) / g128::T), nt = (uint32_t)(((uint64_t)g.N + 32 * NJ - 1) / (32 * NJ));
   if ((uint64_t)mt * nt >= 0x7FFFFFFFull) return GWS_ERR_SHAPE;
   set_tile_grid(g, mt, nt);
-  if (w_is_nk) hipLaunchKernelGGL((gemm128_kernel<true, NJ, WayOut...>), dim3(mt * nt), dim3(256), 0, stream, GWS_GEMM_PASS(g), way_out...);
-  else hipLaunchKernelGGL((gemm128_kernel<false, NJ, WayOut...>), dim3(mt * nt), dim3(256), 0, stream, GWS_GEMM_PASS(g), way_out...);
+  if (w_is_nk) hipLaunchKernelGGL((gemm128_kernel<true, NJ, D, WayOut...>), dim3(mt * nt), dim3(256), 0, stream, GWS_GEMM_PASS(g), way_out...);
+  else hipLaunchKernelGGL((gemm128_kernel<false, NJ, D, WayOut...>), dim3(mt * nt), dim3(256), 0, stream, GWS_GEMM_PASS(g), way_out...);
   return hipGetLastError() == hipSuccess ? GWS_OK : GWS_ERR_LAUNCH;
 }
 

@@ -61,7 +61,7 @@ int with_bias_gradient(const GemmArgs& g, DenseArgs& d, uint64_t rows, float* db
 int launch_dense(const GemmArgs& g, const DenseArgs& d, const DensePlan& p, DenseOp op, int w_is_nk, hipStream_t stream) {
   switch (p.form) {
     case GemmForm::kStream: return launch_dense_stream(g, d, op, w_is_nk, p.route.stream, stream);
-    case GemmForm::kMiddle: return launch_dense128(g, d, op, w_is_nk, p.route.middle_nj, stream);
+    case GemmForm::kMiddle: return launch_dense128(g, d, op, w_is_nk, p.route.middle_nj, p.shared, stream);
     case GemmForm::kLarge:
     case GemmForm::kLargeEdge:
     case GemmForm::kNarrow: return launch_dense256(g, d, op, w_is_nk, p.form, stream);
@@ -153,11 +153,48 @@ inline uint64_t norm_wgs(const gws_adamw_tensor& t) {
 
 }  // namespace
 
-// The kernel that the plain product of these sizes takes, so the sums run in the same order; what comes on top, the way out, hardly differs between those that
-// are near each other.  Leading dimensions of outputs that the kernels' 32-bit lane offsets do not reach: the kernel for any sizes.
-DensePlan plan_dense(const GemmArgs& g, const DenseArgs& d, int w_is_nk) {
+// Tiles of 128 x 128, two workgroups a compute unit, in us: one's way out runs under the other's loop, where in the forms with one workgroup (and one wavefront a
+// SIMD) it stands alone.  Rounds are of two tiles a compute unit; a last one of up to half is one tile each; many tiles go out of step.  Fitted to 151 sizes of 257
+// to 1734 tiles, GELU with Z kept and the backward pass with H and the bias gradient, 5 % off in the root mean square.
+static double shared_us(double M, double N, double K, DenseOp op) {
+  const bool back = op == DenseOp::kBwd;
+  const double cus = compute_units() > 0 ? compute_units() : 256, x = ceil(M / 128.0) * ceil(N / 128.0) / (2 * cus), nk = ceil(K / 64.0);
+  const double rounds = ceil(x), last = x - (rounds - 1), both = fmax(0.0, 2 * last - 1), alone = fmin(1.0, 2 * last);
+  const double start = back ? 8.2 : 5.6, full = back ? 9.3 + 0.85 * nk : 4.2 + 0.84 * nk;
+  const double one = back ? 6.1 + nk * (0.41 + 0.27 * alone) : 2.1 + nk * (0.61 + 0.045 * alone);
+  const double in_rounds = start + (rounds - 1 + both) * full + (1 - both) * one;
+  return rounds <= 2 ? in_rounds : fmin(in_rounds, start + (x + 0.25) * (back ? 23.8 + 0.81 * nk : 14.6 + 0.80 * nk));
+}
+// What the way out adds to the plain product's estimate: a part a round (of `tn` columns a tile).
+static double with_way_out(const GemmArgs& g, double us, double tm, double tn, double fixed, double a_round) {
+  const double cus = compute_units() > 0 ? compute_units() : 256;
+  return us + fixed + a_round * ceil(ceil(g.M / tm) * ceil(g.N / tn) / cus);
+}
+
+// The kernel that the plain product of these sizes takes, or two workgroups a compute unit where that is faster.  us of the plain product's kernel and of two, GELU,
+// Z kept: 798 x 672 -> 5632 19.8, 16.2; 1118 x 352 -> 4864 17.5, 13.1; 1545 x 1728 -> 2848 29.6, 26.0; 5469 x 5632 -> 800 104, 70; 4911 x 896 -> 5632 65.5, 62.4;
+// 7474 x 2304 -> 1504 54, 65; 8192 x 2048 -> 5632 160, 190; backward 5299 x 896 -> 1536 35.4, 28.1; 2381 x 288 -> 2528 25.7, 20.0; 3281 x 5632 -> 4320 135, 162.  Over 182
+// drawn sizes of more than 200 tiles the choice is 1.02 of the fastest form (without two workgroups 1.10).
+// Leading dimensions of outputs that the kernels' 32-bit lane offsets do not reach: the kernel for any sizes.
+DensePlan plan_dense(const GemmArgs& g, const DenseArgs& d, DenseOp op, int w_is_nk) {
   DensePlan p;
+  p.shared = false;
   p.form = gemm_form(g, w_is_nk, 0, p.route);
+  const bool back = op == DenseOp::kBwd;
+  double us = 0.0;
+  switch (p.form) {
+    case GemmForm::kStream: us = p.route.stream.us + (back ? 3.0 : 1.5); break;
+    case GemmForm::kMiddle: us = with_way_out(g, p.route.middle_us, 128, 32 * p.route.middle_nj, back ? 0.9 : -1.8, back ? 6.1 : 4.0); break;
+    case GemmForm::kLarge:
+    case GemmForm::kLargeEdge: us = with_way_out(g, p.route.large_us, 256, 256, back ? -0.7 : -2.4, back ? 16.0 : 8.5); break;
+    case GemmForm::kNarrow: us = with_way_out(g, p.route.narrow_us, 256, 192, back ? -2.6 : -4.7, back ? 16.0 : 10.3); break;
+    default: break;
+  }
+  const double tiles = ceil(g.M / 128.0) * ceil(g.N / 128.0), cus = compute_units() > 0 ? compute_units() : 256;
+  if (gemm128_applicable(g) && tiles > cus && shared_us(g.M, g.N, g.K, op) < 0.97 * us) {
+    p.form = GemmForm::kMiddle;
+    p.shared = true;
+  }
   if (g.ldy >= kMaxLdOut || d.ldr >= kMaxLdOut || d.ldz >= kMaxLdOut || d.ldh >= kMaxLdOut) p.form = GemmForm::kAnyShape;
   switch (p.form) {
     case GemmForm::kStream: p.rows = (uint32_t)p.route.stream.bm; break;
@@ -291,7 +328,7 @@ int gws_dense_fwd(const void* x, int64_t M, int64_t K, int64_t ldx, const void* 
   d.r = (const uint16_t*)e->residual; d.ldr = (uint32_t)e->ldr;
   d.z = (uint16_t*)e->z; d.ldz = (uint32_t)e->ldz;
   d.past_caches = (uint64_t)M * (uint64_t)N * 2 >= (uint64_t)172 << 20;
-  return launch_dense(g, d, plan_dense(g, d, w_is_nk), DenseOp::kFwd, w_is_nk, (hipStream_t)stream);
+  return launch_dense(g, d, plan_dense(g, d, DenseOp::kFwd, w_is_nk), DenseOp::kFwd, w_is_nk, (hipStream_t)stream);
 }
 
 size_t gws_dense_bwd_workspace_bytes(int64_t M, int64_t F) { return !size_ok(M) || !size_ok(F) ? 0 : dense_bytes(M, F); }
@@ -321,7 +358,7 @@ int gws_dense_bwd(const void* dy, int64_t M, int64_t D, int64_t lddy, const void
   g.K = (uint32_t)D; g.ldx = (uint32_t)lddy; g.ldw = (uint32_t)ldw;
   const int nk = !w_is_nk;   // the product's columns are Wd's rows
   d.past_caches = D >= 1024;
-  const DensePlan p = plan_dense(g, d, nk);
+  const DensePlan p = plan_dense(g, d, DenseOp::kBwd, nk);
   return with_bias_gradient(g, d, p.rows, dbias, workspace, (hipStream_t)stream,
                             [&] { return launch_dense(g, d, p, DenseOp::kBwd, nk, (hipStream_t)stream); });
 }
@@ -346,6 +383,21 @@ int gws_dense_bwd_h(const void* dh, int64_t M, int64_t F, int64_t lddh, int act,
   if (!b.apart_all(true)) return GWS_ERR_ALIAS;
   g.x = (const uint16_t*)dh; g.ldx = (uint32_t)lddh;
   return with_bias_gradient(g, d, dense_h_rows(g.M, g.N), dbias, workspace, (hipStream_t)stream, [&] { return launch_dense_bwd_h(g, d, (hipStream_t)stream); });
+}
+
+int gws_dense_form(int op, int64_t M, int64_t K, int64_t N, int64_t ldx, int64_t ldw, int w_is_nk) {
+  if (op != GWS_DENSE_FWD && op != GWS_DENSE_BWD) return 0;
+  if (!size_ok(M) || !size_ok(K) || !size_ok(N) || M == 0 || K == 0 || N == 0 || ((K | N) & 31) != 0) return 0;
+  const int nk = op == GWS_DENSE_FWD ? w_is_nk != 0 : w_is_nk == 0;
+  if (!ld_ok(ldx, K) || !ld_ok(ldw, nk ? K : N)) return 0;
+  GemmArgs g;
+  DenseArgs d;
+  memset(&g, 0, sizeof g);
+  memset(&d, 0, sizeof d);
+  g.M = (uint32_t)M; g.N = (uint32_t)N; g.K = (uint32_t)K;
+  g.ldx = (uint32_t)ldx; g.ldw = (uint32_t)ldw; g.ldy = (uint32_t)N;
+  const DensePlan p = plan_dense(g, d, op == GWS_DENSE_FWD ? DenseOp::kFwd : DenseOp::kBwd, nk);
+  return p.shared && p.form == GemmForm::kMiddle ? GWS_DENSE_SHARED : (int)p.form;
 }
 
 int gws_adamw(const gws_adamw_tensor* t, int n, const gws_adamw_settings* s, void* stream) {

@@ -1,4 +1,4 @@
-"""Every kernel that a call of the dense layer may take, by sizes for which it is the one (its choice is the plain product's, gws_gemm_form): tiles cut by the
+"""Every kernel that a call of the dense layer may take, by sizes for which it is the one (gws_dense_form): tiles cut by the
 edges of the result, K of whole and half steps, both layouts of the weight."""
 import math
 
@@ -34,11 +34,20 @@ STREAM = [
     (True, (16, 16, 0, 1), 14, 64, 512), (True, (16, 32, 0, 1), 10, 96, 4192), (True, (32, 32, 0, 0), 18, 96, 32), (True, (32, 32, 0, 1), 102, 64, 256),
     (True, (32, 32, 1, 0), 17, 1376, 768), (True, (32, 32, 1, 1), 18, 896, 1184), (True, (32, 64, 0, 0), 1819, 96, 160), (True, (32, 64, 0, 1), 194, 64, 1216),
     (True, (64, 64, 0, 0), 2814, 64, 160), (True, (64, 64, 0, 1), 260, 96, 1856), (True, (128, 64, 0, 1), 1238, 96, 800)]
-MIDDLE = [(False, 96, 645, 96, 2752), (False, 96, 1165, 64, 1696), (False, 128, 785, 64, 3520), (False, 128, 781, 96, 3584), (True, 96, 776, 96, 2336), (True, 96, 409, 64, 4352),
-          (True, 128, 674, 64, 4192), (True, 128, 1298, 96, 2304)]
-LARGE = [(False, gws.GEMM_LARGE_EDGE, 2728, 96, 4576), (True, gws.GEMM_LARGE_EDGE, 2578, 128, 4480), (True, gws.GEMM_LARGE_EDGE, 3220, 96, 3744),
-         (False, gws.GEMM_NARROW, 1954, 96, 4128), (False, gws.GEMM_NARROW, 4636, 64, 1696), (True, gws.GEMM_NARROW, 2475, 64, 3232), (True, gws.GEMM_NARROW, 3080, 96, 2624),
-         (False, gws.GEMM_LARGE, 4096, 192, 4096), (True, gws.GEMM_LARGE, 4096, 448, 4096)]
+MIDDLE = [(False, 96, 514, 64, 3392), (False, 96, 389, 96, 4160), (False, 128, 1036, 64, 2720), (False, 128, 771, 96, 3488), (True, 96, 396, 64, 4288),
+          (True, 96, 392, 96, 4224), (True, 128, 516, 64, 4928), (True, 128, 776, 96, 3616)]
+OTHERS = [(False, gws.GEMM_LARGE_EDGE, 3717, 448, 3360), (False, gws.GEMM_LARGE_EDGE, 3593, 480, 3424), (True, gws.GEMM_LARGE_EDGE, 3631, 384, 3616),
+          (True, gws.GEMM_LARGE_EDGE, 2404, 544, 4832), (False, gws.GEMM_NARROW, 2966, 320, 2784), (False, gws.GEMM_NARROW, 3276, 288, 2464), (True, gws.GEMM_NARROW, 3876, 320, 2112),
+          (True, gws.GEMM_NARROW, 2136, 288, 3872), (False, gws.GEMM_LARGE, 4096, 192, 4096), (True, gws.GEMM_LARGE, 4096, 448, 4096),
+          (False, gws.DENSE_SHARED, 782, 64, 4800), (False, gws.DENSE_SHARED, 781, 96, 4768), (True, gws.DENSE_SHARED, 906, 64, 4128), (True, gws.DENSE_SHARED, 769, 96, 4832),
+          (True, gws.DENSE_SHARED, 1118, 352, 4864), (False, gws.DENSE_SHARED, 2381, 288, 2528), (False, gws.GEMM_ANY_SHAPE, 129, 32, 64)]
+
+
+def form_of(M, K, N, nk):
+    """The one kernel of the forward and of the backward call, whose weight lies the other way round."""
+    f = gws.gws_dense_form(gws.DENSE_FWD, M, K, N, w_is_nk=nk)
+    assert f == gws.gws_dense_form(gws.DENSE_BWD, M, K, N, w_is_nk=not nk)
+    return f
 
 
 def both(M, K, N, nk, pad=0):
@@ -51,28 +60,28 @@ def both(M, K, N, nk, pad=0):
 
 @pytest.mark.parametrize("nk,tile,M,K,N", STREAM)
 def test_few_rows_or_tiles(nk, tile, M, K, N):
-    assert gws.gws_gemm_form(M, K, N, w_is_nk=nk) == gws.GEMM_STREAM and gws.gws_gemm_stream_tile(M, K, N, nk) == tile
+    assert form_of(M, K, N, nk) == gws.GEMM_STREAM and gws.gws_gemm_stream_tile(M, K, N, nk) == tile
     both(M, K, N, nk)
 
 
 @pytest.mark.parametrize("nk,cols,M,K,N", MIDDLE)
 def test_middle_tiles(nk, cols, M, K, N):
-    assert gws.gws_gemm_form(M, K, N, w_is_nk=nk) == gws.GEMM_MIDDLE and gws.gws_gemm_tile(M, K, N, nk) == (128, cols)
+    assert form_of(M, K, N, nk) == gws.GEMM_MIDDLE and gws.gws_gemm_tile(M, K, N, nk) == (128, cols)
     both(M, K, N, nk)
 
 
-@pytest.mark.parametrize("nk,form,M,K,N", LARGE)
-def test_large_tiles(nk, form, M, K, N):
-    assert gws.gws_gemm_form(M, K, N, w_is_nk=nk) == form
+@pytest.mark.parametrize("nk,form,M,K,N", OTHERS)
+def test_large_tiles_and_others(nk, form, M, K, N):
+    assert form_of(M, K, N, nk) == form
     both(M, K, N, nk)
 
 
-@pytest.mark.parametrize("M,K,N,nk", [(582, 96, 1664, False), (645, 96, 2752, False), (674, 64, 4192, True), (3220, 96, 3744, True), (1954, 96, 4128, False)])
+@pytest.mark.parametrize("M,K,N,nk", [(582, 96, 1664, False), (389, 96, 4160, False), (516, 64, 4928, True), (2404, 544, 4832, True), (3276, 288, 2464, False), (769, 96, 4832, True)])
 def test_matrices_in_wider_buffers(M, K, N, nk):
     both(M, K, N, nk, pad=8)
 
 
-@pytest.mark.parametrize("M,K,N", [(3, 2048, 256), (102, 64, 256), (785, 64, 3520), (4096, 192, 4096), (1954, 96, 4128)])
+@pytest.mark.parametrize("M,K,N", [(3, 2048, 256), (102, 64, 256), (771, 96, 3488), (4096, 192, 4096), (3276, 288, 2464), (781, 96, 4768)])
 def test_in_place(M, K, N):
     for nk in (False, True):
         check_fwd(M, K, N, nk, gws.ACT_SILU, in_place=True)
@@ -80,7 +89,7 @@ def test_in_place(M, K, N):
         check_bwd(M, K, N, not nk, gws.ACT_GELU_TANH, alias="h")
 
 
-@pytest.mark.parametrize("M,K,N", [(1, 2080, 64), (40, 1312, 832), (785, 64, 3520), (2728, 96, 4576), (4096, 192, 4096), (1954, 96, 4128)])
+@pytest.mark.parametrize("M,K,N", [(1, 2080, 64), (40, 1312, 832), (771, 96, 3488), (2404, 544, 4832), (4096, 192, 4096), (3276, 288, 2464), (781, 96, 4768)])
 def test_results_do_not_change_from_call_to_call_or_with_the_rows_beside(M, K, N):
     """Rows of NaN leave the others as they are; the bias gradient is the same bits every time."""
     x, w, b, r = rand(1, M, K), weight(2, K, N, True), vec(3, N), rand(4, M, N)

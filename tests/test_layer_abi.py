@@ -109,6 +109,21 @@ def test_dense_backward(lib):
     assert bwd(act=2, z=None, h=None, dz=None) == NULL
 
 
+def test_queries_of_the_dense_layers_kernel(lib):
+    # host function; without a device for 256 compute units
+    form = gws.gws_dense_form
+    assert form(gws.DENSE_FWD, 0, 64, 64) == 0 and form(gws.DENSE_FWD, 8, 48, 64) == 0 and form(2, 8, 64, 64) == 0 and form(gws.DENSE_FWD, 8, 64, 64, ldx=56) == 0
+    assert form(gws.DENSE_BWD, 8, 64, 96, ldw=56) == 0 and form(gws.DENSE_BWD, 8, 64, 96, True, ldw=88) == 0
+    assert form(gws.DENSE_FWD, 8, 32, 64) == gws.GEMM_ANY_SHAPE and form(gws.DENSE_FWD, 8, 64, 64, ldx=1 << 25) == gws.GEMM_ANY_SHAPE
+    # the plain product's, or two workgroups a compute unit where that measured faster
+    for op in (gws.DENSE_FWD, gws.DENSE_BWD):
+        nk = op == gws.DENSE_FWD
+        assert form(op, 1, 2048, 5632, nk) == gws.GEMM_STREAM and form(op, 8192, 2048, 5632, nk) == gws.GEMM_LARGE and form(op, 514, 64, 3392, not nk) == gws.GEMM_MIDDLE
+    assert [form(gws.DENSE_FWD, m, k, n, nk) for m, k, n, nk in ((798, 672, 5632, True), (1118, 352, 4864, False), (5469, 5632, 800, False), (7474, 2304, 1504, False))] == \
+        [gws.DENSE_SHARED] * 3 + [gws.GEMM_NARROW]
+    assert [form(gws.DENSE_BWD, m, k, n, True) for m, k, n in ((5299, 896, 1536), (2381, 288, 2528), (3281, 5632, 4320))] == [gws.DENSE_SHARED] * 2 + [gws.GEMM_LARGE_EDGE]
+
+
 def tensor(**over):
     c = _CAdamWTensor(p=at(0), w=at(1), g=at(2), g_is_fp32=0, m=at(3), v=at(4), rows=10, cols=70, ld=72, lr_scale=1.0, weight_decay=0.1, seed=1)
     for k, v in over.items():
