@@ -385,8 +385,8 @@ int gws_norm_fwd(const void* x, int64_t M, int64_t C, int64_t ldx, int kind, con
  *   dgamma = sum of dY .* n over the rows, dbeta = sum of dY (each NULL: not wanted; they are written, not added to).
  * dX may lie on dY, X or R (same address and leading dimension), else no output overlaps an input or another output.
  * With dgamma, dbeta or rows of more than 16384 columns the call needs `workspace` (16-byte aligned, apart from every other buffer, contents undefined
- * afterwards) of gws_norm_bwd_workspace_bytes(M, C) bytes (GWS_ERR_NULL / GWS_ERR_SHAPE without): the sums of rows that meet there are added in one order,
- * so every call gives the same bits. */
+ * afterwards) of gws_norm_bwd_workspace_bytes(M, C) bytes (GWS_ERR_NULL / GWS_ERR_SHAPE without): the sums of rows that meet there are added in an order that
+ * the sizes, the number of compute units and whether dX lies on X or dY decide, so the same call gives the same bits. */
 size_t gws_norm_bwd_workspace_bytes(int64_t M, int64_t C);
 int gws_norm_bwd(const void* dy, int64_t lddy, const void* x, int64_t M, int64_t C, int64_t ldx, int kind, const float* gamma, const float* mean,
                  const float* rstd, const void* residual, int64_t ldr, void* dx, int64_t lddx, float* dgamma, float* dbeta, void* workspace,
@@ -414,7 +414,7 @@ int gws_dense_fwd(const void* x, int64_t M, int64_t K, int64_t ldx, const void* 
 /* Backward through the product that follows and the activation, in one pass over the sums: with dY [M x D] the gradient of Y = a(Z) * Wd (Wd stored
  * [F x D] or, when w_is_nk, [D x F], as that product's forward call takes it), dH = dY * Wd^T kept in fp32,
  *   dZ = dH .* a'(Z),   H = a(Z) again where h is not NULL (the input of Wd's weight gradient),   dbias = sum of dZ over the tokens where it is not NULL
- * from the kept Z [M x F].  dbias (fp32 [F]) sums the fp32 dZ, in an order that is the same in every call of the same sizes; it needs `workspace` (16-byte
+ * from the kept Z [M x F].  dbias (fp32 [F]) sums the fp32 dZ, in an order that sizes and leading dimensions decide; it needs `workspace` (16-byte
  * aligned, apart from every other buffer, contents undefined afterwards) of gws_dense_bwd_workspace_bytes(M, F) bytes (GWS_ERR_NULL / GWS_ERR_SHAPE without).
  * dZ or H may lie on Z (same address and leading dimension), else no output overlaps an input or another output.  With GWS_ACT_NONE and without h, z may be
  * NULL.  D and F must be multiples of 32.  M == 0: dbias becomes zeros.
@@ -442,7 +442,9 @@ int gws_dense_bwd_h(const void* dh, int64_t M, int64_t F, int64_t lddh, int act,
  * bits are a function of (seed, step, row, column) alone: word c % 4 of Philox4x32-10(counter = (c / 4, row, step_lo, step_hi ^ 0x47414457), key = seed) for column c,
  * low half for m, high half for r.  Buffers of zeros are states at the start.  A NaN or infinity among 32 values makes all of them NaN (fp32 states: itself alone).
  * Where *grad_scale is not finite nothing is written: a step with an overflowed gradient norm leaves the model as it was.
- * No buffer of a tensor may overlap another one of the call, its gradient included (checked within a tensor).  *grad_scale lies apart from all outputs.  Empty tensors are skipped. */
+ * No buffer of a tensor may overlap another one of the call, its gradient included (checked within a tensor, and no buffer that is written may begin where
+ * one of an earlier tensor does: a tensor given twice is GWS_ERR_ALIAS).  *grad_scale lies apart from all outputs.  Empty tensors are skipped.
+ * A tensor has at most 2^35 - 2048 elements, its columns counted in fours, those of codes in blocks of 32 (GWS_ERR_SHAPE). */
 typedef struct gws_adamw_tensor {
   float* p;            /* device, the parameter                                     */
   void* w;             /* device BF16, its copy; NULL: not wanted                   */

@@ -112,7 +112,7 @@ __global__ __launch_bounds__(256) void dense_any_kernel(const GemmArgs g, const 
 
 int launch_dense_any(const GemmArgs& g, const DenseArgs& e, DenseOp op, int w_is_nk, hipStream_t stream) {
   const uint64_t tiles = (((uint64_t)g.M + kRows - 1) / kRows) * (((uint64_t)g.N + kCols - 1) / kCols);
-  if (tiles >= 0x7FFFFFFFull) return GWS_ERR_SHAPE;
+  if (tiles >= (uint64_t)1 << 24) return GWS_ERR_SHAPE;   // a launch has fewer than 2^32 threads
   const dim3 grid((uint32_t)tiles), block(256);
   if (op == DenseOp::kFwd) {
     if (w_is_nk) hipLaunchKernelGGL((dense_any_kernel<DenseOp::kFwd, true>), grid, block, 0, stream, g, e);

@@ -70,10 +70,16 @@ int launch_dense(const GemmArgs& g, const DenseArgs& d, const DensePlan& p, Dens
 }
 
 // ---- AdamW ----
+constexpr uint64_t kMaxWorkgroups = 0xFFFFFF;   // of 256 threads: a launch has fewer than 2^32
+inline uint64_t norm_wgs(const gws_adamw_tensor& t) {
+  return t.rows <= 0 || t.cols <= 0 ? 0 : ((uint64_t)t.rows * (((uint64_t)t.cols + 7) / 8) + kNormGroups - 1) / kNormGroups;
+}
+// Fours a row: of codes in whole blocks of 32.
+inline uint64_t fours(const gws_adamw_tensor& t, bool codes) { return codes ? ((uint64_t)t.cols + 31) / 32 * 8 : ((uint64_t)t.cols + 3) / 4; }
 int check_gradient(const gws_adamw_tensor& t) {
   if (!size_ok(t.rows) || !size_ok(t.cols)) return GWS_ERR_SHAPE;
   if (t.rows == 0 || t.cols == 0) return GWS_OK;
-  if (!ld_ok(t.ld, t.cols) || (uint64_t)t.rows * (((uint64_t)t.cols + 31) / 32) >= (uint64_t)1 << 36) return GWS_ERR_SHAPE;
+  if (!ld_ok(t.ld, t.cols) || norm_wgs(t) > kMaxWorkgroups) return GWS_ERR_SHAPE;
   if (!t.g) return GWS_ERR_NULL;
   return aligned(t.g, 16) ? GWS_OK : GWS_ERR_ALIGN;
 }
@@ -88,6 +94,7 @@ int check_adamw(const gws_adamw_tensor& t, const float* grad_scale) {
   if (codes && (t.m || t.v)) return GWS_ERR_FORMAT;
   if (!t.p) return GWS_ERR_NULL;
   if (!isfinite(t.lr_scale) || !isfinite(t.weight_decay)) return GWS_ERR_FORMAT;
+  if ((uint64_t)t.rows * fours(t, codes) > kMaxWorkgroups * kAdamwGroups) return GWS_ERR_SHAPE;
   const size_t m = (size_t)t.rows, n = (size_t)t.cols, ld = (size_t)t.ld;
   Span2 out[6], in[2] = {gradient_span(t), span_f32(grad_scale, 1)};
   int outs = 0;
@@ -128,7 +135,7 @@ struct Launches {
   explicit Launches(Launch l) : launch(l) {}
   template <class Desc>
   int add(const Desc& d, uint64_t wc) {
-    if (held == List::kMax || wgs + wc >= 0x7FFFFFF0ull) {
+    if (held == List::kMax || wgs + wc > kMaxWorkgroups) {
       const int rc = finish();
       if (rc != GWS_OK) return rc;
     }
@@ -147,9 +154,37 @@ struct Launches {
   }
 };
 inline bool few_groups(uint64_t groups) { return groups + 0x100000 < ((uint64_t)1 << 32); }   // those past the end of the last workgroup too
-inline uint64_t norm_wgs(const gws_adamw_tensor& t) {
-  return t.rows <= 0 || t.cols <= 0 ? 0 : ((uint64_t)t.rows * (((uint64_t)t.cols + 7) / 8) + kNormGroups - 1) / kNormGroups;
-}
+
+// Buffers that a call has been given before: the starts of what it writes, as bits of a table, and only where a bit is set a look at the tensors so far.
+class GivenBefore {
+  uint64_t bits_[2048];
+  bool set(const void* p) {
+    const uint64_t h = ((uint64_t)(uintptr_t)p * 0x9E3779B97F4A7C15ull) >> 47;   // 17 bits
+    const bool was = (bits_[h >> 6] >> (h & 63) & 1) != 0;
+    bits_[h >> 6] |= (uint64_t)1 << (h & 63);
+    return was;
+  }
+
+ public:
+  GivenBefore() { memset(bits_, 0, sizeof bits_); }
+  bool any(const gws_adamw_tensor* t, int i) {
+    const gws_adamw_tensor& n = t[i];
+    if (n.rows == 0 || n.cols == 0) return false;
+    const void* mine[4] = {n.p, n.m8.codes ? (const void*)n.m8.codes : n.m, n.v8.codes ? (const void*)n.v8.codes : n.v, n.w};
+    bool seen = false;
+    for (const void* p : mine) seen |= p != nullptr && set(p);
+    if (!seen) return false;
+    for (int j = 0; j < i; ++j) {
+      const gws_adamw_tensor& o = t[j];
+      if (o.rows == 0 || o.cols == 0) continue;
+      const void* theirs[4] = {o.p, o.m8.codes ? (const void*)o.m8.codes : o.m, o.v8.codes ? (const void*)o.v8.codes : o.v, o.w};
+      for (const void* p : mine)
+        for (const void* q : theirs)
+          if (p != nullptr && p == q) return true;
+    }
+    return false;
+  }
+};
 
 }  // namespace
 
@@ -408,9 +443,11 @@ int gws_adamw(const gws_adamw_tensor* t, int n, const gws_adamw_settings* s, voi
   if (!aligned(s->grad_scale, 4)) return GWS_ERR_ALIGN;
   if (n == 0) return GWS_OK;
   if (!t) return GWS_ERR_NULL;
+  GivenBefore before;
   for (int i = 0; i < n; ++i) {
     const int rc = check_adamw(t[i], s->grad_scale);
     if (rc != GWS_OK) return rc;
+    if (before.any(t, i)) return GWS_ERR_ALIAS;
   }
   const double c1 = 1.0 - pow(s->beta1, (double)s->step), c2 = 1.0 - pow(s->beta2, (double)s->step);
   const AdamwStep a = {(float)s->beta1, (float)(1.0 - s->beta1), (float)s->beta2, (float)(1.0 - s->beta2), (float)(1.0 / sqrt(c2)), (float)s->eps,
@@ -434,7 +471,7 @@ int gws_adamw(const gws_adamw_tensor* t, int n, const gws_adamw_settings* s, voi
       rc = runs.add(AdamwRun{o.p, (uint16_t*)o.w, o.g, o.m, o.v, elements | (o.g_is_fp32 ? kRunGradFp32 : 0), keep, rate}, (elements + 4 * kAdamwGroups - 1) / (4 * kAdamwGroups));
     } else {
       const bool codes = o.m8.codes != nullptr;
-      const uint32_t per_row = (uint32_t)(codes ? ((uint64_t)o.cols + 31) / 32 * 8 : ((uint64_t)o.cols + 3) / 4);
+      const uint32_t per_row = (uint32_t)fours(o, codes);
       const uint64_t groups = (uint64_t)o.rows * per_row;
       rc = matrices.add(AdamwMatrix{o.p, (uint16_t*)o.w, o.g, codes ? o.m8.codes : o.m, codes ? o.v8.codes : o.v, o.m8.xscale, o.v8.xscale, (uint32_t)o.rows, (uint32_t)o.cols,
                                     (uint32_t)o.ld, (uint32_t)o.m8.lds, keep, rate, (uint32_t)o.seed, (uint32_t)(o.seed >> 32), per_row, reciprocal(per_row),

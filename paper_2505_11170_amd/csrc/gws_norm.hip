@@ -37,6 +37,13 @@ __device__ __forceinline__ void team_sum(float (&v)[N], float* red, uint32_t& tu
 
 }  // namespace
 
+// Workgroups in a grid of two dimensions: one has fewer than 2^32 threads.
+constexpr uint32_t kGridWidth = 1u << 20;
+__device__ __forceinline__ uint32_t workgroup() { return blockIdx.y * kGridWidth + blockIdx.x; }
+inline dim3 grid_of(uint64_t workgroups) {
+  return workgroups <= kGridWidth ? dim3((uint32_t)workgroups) : dim3(kGridWidth, (uint32_t)((workgroups + kGridWidth - 1) / kGridWidth));
+}
+
 // A row's mean and rstd, and its deviations in f; times `unit` the numbers stay what they are, for rows whose squares would pass fp32's range (beyond 10^19 or
 // so) 2^-80 of them.
 constexpr float kSmallUnit = 0x1p-80f;
@@ -127,7 +134,8 @@ template <bool RMS>
 __global__ __launch_bounds__(1024) void norm_fwd_wide_kernel(const NormArgs a) {
   __shared__ float red[2 * 16];
   uint32_t turn = 0;
-  const uint32_t row = blockIdx.x;
+  const uint32_t row = workgroup();
+  if (row >= a.M) return;
   const GWS_GLOBAL uint16_t* x = global_ptr<uint16_t>(a.x) + (size_t)row * a.ldx;
   const float count = (float)a.C;
   float mean, rstd, unit = 1.0f;
@@ -387,7 +395,8 @@ template <bool RMS>
 __global__ __launch_bounds__(1024) void norm_bwd_rows_kernel(const NormArgs a) {
   __shared__ float red[4 * 16];
   uint32_t turn = 0;
-  const uint32_t row = blockIdx.x;
+  const uint32_t row = workgroup();
+  if (row >= a.M) return;
   const GWS_GLOBAL uint16_t *x = global_ptr<uint16_t>(a.x) + (size_t)row * a.ldx, *dy = global_ptr<uint16_t>(a.dy) + (size_t)row * a.lddy;
   const Normalise normal(RMS ? 0.0f : a.mean[row], a.rstd[row]);
   float s[2] = {0.0f, 0.0f};
@@ -452,7 +461,7 @@ __global__ __launch_bounds__(256) void norm_bwd_columns_kernel(const NormArgs a)
 __global__ __launch_bounds__(256) void sum_partials_kernel(const float* part, const uint32_t P, const uint64_t n, const uint64_t n0, float* out0, float* out1) {
   __shared__ f4 red[32][8];
   const uint32_t group = threadIdx.x >> 3, at = threadIdx.x & 7;
-  const uint64_t c = (uint64_t)blockIdx.x * 32 + 4 * at;
+  const uint64_t c = (uint64_t)workgroup() * 32 + 4 * at;
   f4 s = {0.0f, 0.0f, 0.0f, 0.0f};
   for (uint32_t p0 = group; p0 < P; p0 += 256) {
     f4 v[8];
@@ -480,22 +489,22 @@ __global__ __launch_bounds__(256) void sum_partials_kernel(const float* part, co
   float t = r[threadIdx.x];
 #pragma unroll
   for (int g = 1; g < 32; ++g) t += r[32 * g + threadIdx.x];
-  const uint64_t col = (uint64_t)blockIdx.x * 32 + threadIdx.x;
+  const uint64_t col = (uint64_t)workgroup() * 32 + threadIdx.x;
   if (col < n0) out0[col] = t;
   else if (col < n) out1[col - n0] = t;
 }
 
 int launch_sum_partials(const float* part, uint32_t P, uint64_t n, uint64_t n0, float* out0, float* out1, hipStream_t stream) {
-  hipLaunchKernelGGL(sum_partials_kernel, dim3((uint32_t)((n + 31) / 32)), dim3(256), 0, stream, part, P, n, n0, out0, out1);
+  hipLaunchKernelGGL(sum_partials_kernel, grid_of((n + 31) / 32), dim3(256), 0, stream, part, P, n, n0, out0, out1);
   return hipGetLastError() == hipSuccess ? GWS_OK : GWS_ERR_LAUNCH;
 }
 
 __global__ __launch_bounds__(256) void zero_kernel(float* p, const uint64_t n) {
-  const uint64_t i = (uint64_t)blockIdx.x * 256 + threadIdx.x;
+  const uint64_t i = (uint64_t)workgroup() * 256 + threadIdx.x;
   if (i < n) p[i] = 0.0f;
 }
 int launch_zero(float* p, uint64_t n, hipStream_t stream) {
-  hipLaunchKernelGGL(zero_kernel, dim3((uint32_t)((n + 255) / 256)), dim3(256), 0, stream, p, n);
+  hipLaunchKernelGGL(zero_kernel, grid_of((n + 255) / 256), dim3(256), 0, stream, p, n);
   return hipGetLastError() == hipSuccess ? GWS_OK : GWS_ERR_LAUNCH;
 }
 
@@ -543,8 +552,8 @@ bool one_launch(uint64_t M, uint64_t C) {
 
 int launch_norm_fwd(const NormArgs& a, bool rms, hipStream_t s) {
   if (norm_is_wide(a.C)) {
-    if (rms) hipLaunchKernelGGL(norm_fwd_wide_kernel<true>, dim3(a.M), dim3(1024), 0, s, a);
-    else hipLaunchKernelGGL(norm_fwd_wide_kernel<false>, dim3(a.M), dim3(1024), 0, s, a);
+    if (rms) hipLaunchKernelGGL(norm_fwd_wide_kernel<true>, grid_of(a.M), dim3(1024), 0, s, a);
+    else hipLaunchKernelGGL(norm_fwd_wide_kernel<false>, grid_of(a.M), dim3(1024), 0, s, a);
     return hipGetLastError() == hipSuccess ? GWS_OK : GWS_ERR_LAUNCH;
   }
   if (a.C <= 128) return fwd<16, 1, 16>(a, rms, s);
@@ -579,10 +588,10 @@ int launch_norm_bwd(const NormArgs& a, bool rms, float* dgamma, float* dbeta, hi
   if (norm_is_wide(a.C)) {
     const dim3 pieces((uint32_t)(((uint64_t)a.C + 2047) / 2048), norm_bwd_parts(a.M, a.C));
     if (rms) {
-      hipLaunchKernelGGL(norm_bwd_rows_kernel<true>, dim3(a.M), dim3(1024), 0, s, a);
+      hipLaunchKernelGGL(norm_bwd_rows_kernel<true>, grid_of(a.M), dim3(1024), 0, s, a);
       hipLaunchKernelGGL(norm_bwd_columns_kernel<true>, pieces, dim3(256), 0, s, a);
     } else {
-      hipLaunchKernelGGL(norm_bwd_rows_kernel<false>, dim3(a.M), dim3(1024), 0, s, a);
+      hipLaunchKernelGGL(norm_bwd_rows_kernel<false>, grid_of(a.M), dim3(1024), 0, s, a);
       hipLaunchKernelGGL(norm_bwd_columns_kernel<false>, pieces, dim3(256), 0, s, a);
     }
     rc = hipGetLastError() == hipSuccess ? GWS_OK : GWS_ERR_LAUNCH;

@@ -261,3 +261,32 @@ def test_elements_past_32_bits():
     gws.gws_adamw([gws.AdamWTensor(p=p, g=g, m=m, v=v, w=w)], lr=1e-2, step=3)
     gws.gws_adamw([gws.AdamWTensor(p=small[0], g=small[1], m=small[2], v=small[3], w=small[4])], lr=1e-2, step=3)
     assert all(torch.equal(a, b) for a, b in zip((p, m, v, w), (small[0], small[2], small[3], small[4])))
+
+
+def test_more_groups_than_32_bits_count():
+    """Half a billion rows of one column, whose blocks of 32 are more groups of four than 2^32; and a gradient of as many groups of eight."""
+    if torch.cuda.mem_get_info()[0] < 120 << 30:
+        pytest.skip("no room")
+    rows = (1 << 29) + 1000
+    z = lambda *s, dtype: torch.zeros(*s, dtype=dtype, device=DEV)  # noqa: E731
+    p, g = z(rows, 8, dtype=torch.float32)[:, :1], z(rows, 8, dtype=torch.bfloat16)[:, :1]
+    held = [gws.Act8(z(rows, 8, dtype=torch.uint8)[:, :1], z(rows, 1, dtype=torch.uint8)) for _ in range(2)]
+    marks = [0, 1, 12345, (1 << 29) - 1, 1 << 29, rows - 1]
+    for r in marks:
+        g[r] = 1.0 + r % 7
+    gws.gws_adamw([gws.AdamWTensor(p=p, g=g, m=held[0], v=held[1], seed=3)], lr=0.25, step=1)
+    assert int((p != 0).sum()) == len(marks)
+    assert all(abs(float(p[r]) + 0.25) < 1e-6 and int(held[0].codes[r]) != 0 and int(held[0].xscale[r]) != 127 for r in marks)
+    assert int((held[1].codes != 0).sum()) == len(marks)
+    del p, g, held
+    torch.cuda.empty_cache()
+    rows, cols = 1 << 15, (1 << 20) + 8
+    g = z(rows, cols, dtype=torch.bfloat16)
+    for r, c in ((0, 0), (7, cols - 1), (rows - 1, cols - 1), (rows // 2, 5)):
+        g[r, c] = 2.0
+    small = z(rows, 8, dtype=torch.float32)
+    t = gws.pack_adamw([gws.AdamWTensor(p=small, g=small, m=small, v=small)])
+    t.arr[0].g, t.arr[0].g_is_fp32, t.arr[0].cols, t.arr[0].ld = g.data_ptr(), 0, cols, cols       # of the fields the norm reads
+    out, ws = z(2, dtype=torch.float32), torch.empty(gws.gws_grad_norm_workspace_bytes(t), dtype=torch.uint8, device=DEV)
+    gws.gws_grad_norm(t, out, ws, max_norm=1.0)
+    assert out.tolist() == [4.0, 0.25]

@@ -203,3 +203,29 @@ def test_offsets_past_32_bits():
     gws.gws_norm_fwd(x, y)
     want, tol = ref.norm_fwd(x, LAYER, None, None, 1e-5)
     assert_within(y, want[0], tol[0], "y")
+
+
+def test_grids_of_more_than_32_bits_of_threads():
+    """Four million long rows, in place; a row of half a billion columns with both gradients."""
+    if torch.cuda.mem_get_info()[0] < 150 << 30:
+        pytest.skip("no room")
+    M, C = (1 << 22) + 3, 16392
+    x, rstd = torch.zeros(M, C, dtype=torch.bfloat16, device=DEV), torch.full((M,), -1.0, device=DEV)
+    marks = [0, 1, (1 << 20) - 1, 1 << 20, (1 << 22) - 1, 1 << 22, M - 1]
+    for r in marks:
+        x[r] = 3.0
+    gws.gws_norm_fwd(x, x, RMS, eps=2.0 ** -20, rstd=rstd)
+    ones = torch.zeros(M, dtype=torch.bool, device=DEV)
+    ones[marks] = True
+    assert torch.equal(x[:, 5] != 0, ones) and torch.equal(x[:, C - 1], ones.bfloat16())      # 3 / sqrt(9 + 2^-20) rounds to 1
+    assert bool((rstd[~ones] == 1024.0).all()) and bool(((rstd[ones] * 3.0 - 1.0).abs() < 1e-6).all())
+    del x, rstd, ones
+    torch.cuda.empty_cache()
+    C = (1 << 29) + 40
+    x = torch.randint(0, 4, (1, C), dtype=torch.int8, device=DEV).bfloat16()
+    dy = torch.randint(-1, 2, (1, C), dtype=torch.int8, device=DEV).bfloat16()
+    dx, dgamma, dbeta = torch.empty_like(x), torch.full((C,), 9.0, device=DEV), torch.full((C,), 9.0, device=DEV)
+    mean, rstd = torch.tensor([0.25], device=DEV), torch.tensor([2.0], device=DEV)
+    ws = torch.empty(gws.gws_norm_bwd_workspace_bytes(1, C), dtype=torch.uint8, device=DEV)
+    gws.gws_norm_bwd(dy, x, dx, rstd, kind=LAYER, mean=mean, dgamma=dgamma, dbeta=dbeta, workspace=ws)
+    assert torch.equal(dbeta, dy[0].float()) and torch.equal(dgamma, dy[0].float() * (x[0].float() * 2 - 0.5))   # exact in every step

@@ -159,6 +159,29 @@ def test_adamw(lib):
     assert step(in8(v8=_CAct8(None, at(8), 72, 3))) == NULL and step(in8(v8=_CAct8(at(7), None, 72, 3))) == NULL
     assert step(in8(m8=_CAct8(at(5), at(6), 80, 3))) == SHAPE and step(in8(m8=_CAct8(at(5), at(6), 72, 2))) == SHAPE and step(in8(m8=_CAct8(at(5), at(6), 72, 4))) == SHAPE
     assert step(in8(m8=_CAct8(at(5) + 4, at(6), 72, 3))) == ALIGN and step(in8(m8=_CAct8(at(7), at(6), 72, 3))) == ALIAS and step(in8(v8=_CAct8(at(7), at(6), 72, 3))) == ALIAS
+    # sizes of more workgroups than a launch has
+    assert step(tensor(rows=2 ** 30, cols=40, ld=40)) == SHAPE and step(in8(rows=2 ** 30, cols=8, ld=8, m8=_CAct8(at(5), at(6), 8, 1), v8=_CAct8(at(7), at(8), 8, 1))) == SHAPE
+
+
+def test_adamw_refuses_a_tensor_that_it_was_given_before(lib):
+    s = ctypes.byref(_CAdamWSettings(1e-3, 0.9, 0.99, 1e-8, 1, None))
+
+    def step(*t):
+        return lib.gws_adamw((_CAdamWTensor * len(t))(*t), len(t), s, None)
+
+    far = lambda buffer, i: buffer * 2 ** 32 + 2 ** 16 * i  # noqa: E731 - 900 tensors of one buffer stay below the next one's
+    good = lambda i: tensor(p=far(1, i), w=far(2, i), m=far(3, i), v=far(4, i))  # noqa: E731
+    for n in (1, 7, 900):
+        before = [good(i) for i in range(n)]
+        assert step(*before, good(n - 1)) == ALIAS and step(*before, good(0)) == ALIAS
+        for field in ("p", "w", "m", "v"):
+            t = good(n)
+            setattr(t, field, getattr(good(0), field))
+            assert step(*before, t) == ALIAS, field
+            if field != "w":
+                c = in8(p=at(20), w=at(21), m8=_CAct8(far(3, 0), at(6), 72, 3))          # codes where the first one's m lies
+                assert step(*before, c) == ALIAS
+        assert step(*before, tensor(rows=0, p=far(1, 0)), tensor(ld=64)) == SHAPE       # an empty one may be anything
 
 
 def test_gradient_norm(lib):
