@@ -292,29 +292,63 @@ __device__ __forceinline__ double block_sum(double v, double* red) {
 }
 }  // namespace
 
+// Eight elements of a gradient, group `id` of it, as they lie in memory (BF16: the first half); zeros past its end.
+__device__ __forceinline__ void load_group(const GradSquares& t, bool fp32, uint64_t id, u32x4 (&raw)[2]) {
+  const uint32_t cols = t.cols & ~kHighBit;
+  uint32_t row, group;
+  raw[0] = raw[1] = u32x4{0, 0, 0, 0};
+  if (!place(id, t.rows & ~kHighBit, (cols + 7) / 8, t.inv, (t.cols & kHighBit) != 0, row, group)) return;
+  const uint32_t c = 8 * group;
+  const size_t at = (size_t)row * t.ld + c;
+  if (fp32) {   // uniform
+    const GWS_GLOBAL uint32_t* q = global_ptr<uint32_t>(t.g) + at;
+    if (c + 8 <= cols) {
+      raw[0] = *(const GWS_GLOBAL u32x4*)q;
+      raw[1] = *(const GWS_GLOBAL u32x4*)(q + 4);
+    } else {
+#pragma unroll
+      for (int e = 0; e < 7; ++e)
+        if (c + e < cols) raw[e >> 2][e & 3] = q[e];
+    }
+  } else {
+    const GWS_GLOBAL uint16_t* q = global_ptr<uint16_t>(t.g) + at;
+    if (c + 8 <= cols) {
+      raw[0] = *(const GWS_GLOBAL u32x4*)q;
+    } else {
+#pragma unroll
+      for (int e = 0; e < 7; ++e)
+        if (c + e < cols) raw[0][e >> 1] |= (uint32_t)q[e] << (16 * (e & 1));
+    }
+  }
+}
+__device__ __forceinline__ double add_squares(double s, bool fp32, const u32x4 (&raw)[2]) {
+#pragma unroll
+  for (int e = 0; e < 4; ++e) {
+    const double a = (double)(fp32 ? __uint_as_float(raw[0][e]) : bf16_lo(raw[0][e])), b = (double)(fp32 ? __uint_as_float(raw[1][e]) : bf16_hi(raw[0][e]));
+    s = __fma_rn(b, b, __fma_rn(a, a, s));
+  }
+  return s;
+}
+// Groups first, first + 256, ...: U loads are on their way before the first sum (48 gradients of 768 x 1760 BF16 30.0 us, one load after the other 37.1).
+template <int U, bool FP32>
+__device__ __forceinline__ double squares_of(const GradSquares& t, uint64_t first) {
+  double s = 0.0;
+  for (uint32_t k = 0; k < kNormGroups / 256; k += U) {
+    u32x4 raw[U][2];
+#pragma unroll
+    for (int u = 0; u < U; ++u) load_group(t, FP32, first + 256 * (k + u), raw[u]);
+#pragma unroll
+    for (int u = 0; u < U; ++u) s = add_squares(s, FP32, raw[u]);
+  }
+  return s;
+}
+
 __global__ __launch_bounds__(256) void grad_squares_kernel(const GradList l, double* part) {
   __shared__ double red[4];
   const uint32_t i = tensor_of(l.begin, blockIdx.x);
   const GradSquares& t = l.t[i];
   const uint64_t first = (uint64_t)(blockIdx.x - l.begin[i]) * kNormGroups + threadIdx.x;
-  const uint32_t rows = t.rows & ~kHighBit, cols = t.cols & ~kHighBit, per_row = (cols + 7) / 8;
-  const bool fp32 = (t.rows & kHighBit) != 0;
-  double s = 0.0;
-#pragma unroll
-  for (uint32_t u = 0; u < kNormGroups / 256; ++u) {
-    uint32_t row, group;
-    if (!place(first + 256 * u, rows, per_row, t.inv, (t.cols & kHighBit) != 0, row, group)) continue;
-    const uint32_t c = 8 * group;
-    const size_t at = (size_t)row * t.ld + c;
-#pragma unroll
-    for (uint32_t h = 0; h < 8; h += 4) {
-      if (c + h >= cols) continue;
-      const int n = cols - c - h < 4 ? (int)(cols - c - h) : 4;
-      const f4 g = fp32 ? load_four((const float*)t.g, at + h, n) : load_four_bf16(t.g, at + h, n);
-#pragma unroll
-      for (int e = 0; e < 4; ++e) s = __fma_rn((double)g[e], (double)g[e], s);
-    }
-  }
+  double s = t.rows & kHighBit ? squares_of<4, true>(t, first) : squares_of<8, false>(t, first);   // uniform
   s = block_sum(s, red);
   if (threadIdx.x == 0) part[blockIdx.x] = s;
 }
