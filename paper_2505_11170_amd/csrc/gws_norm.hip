@@ -3,8 +3,13 @@
 // One pass over memory: a row is in the registers of L lanes (16 to 512), 8 V columns a lane, from its load to its store; mean, squares of the deviations
 // and, backward, sum(t) and sum(t n) are sums over lanes (DPP) and, with more than a wavefront's 64, over the wavefronts through LDS.  The variance is the sum of (x - mean)^2,
 // not the difference of two sums: the row is there, and nothing cancels.
+// Bound by memory: 8192 x 2048 forward 12.4 us (5.4 TB/s), backward with both vectors 27.7 in a graph (23.6 for the rows, 4.0 for the workgroups' sums); few rows by
+// latency, 1 x 2048 2.2 us.  Up to 2048 columns a row is one wavefront's, whose sums need no barrier; up to 512 a
+// wavefront has several (20000 x 128 forward 6.9 -> 3.5 us, backward 13.0 -> 8.7).
 // dgamma and dbeta are sums over the rows: every lane adds up its own columns over the rows that its wavefronts take, the workgroup's rows meet in
 // LDS, and what workgroups leave is added by a second kernel, always in one order.
+#include <algorithm>
+
 #include "gws_norm.h"
 
 namespace gws {
@@ -457,7 +462,7 @@ __global__ __launch_bounds__(256) void norm_bwd_columns_kernel(const NormArgs a)
 
 // ---- sums of partial sums ----
 // A workgroup adds 32 columns, 8 lanes x 4 of them side by side and the P rows shared by 32 groups of lanes, eight loads of each on their way at once; the groups'
-// sums meet in LDS.  Bound by that latency: 256 rows of 1536 columns 2.9 us (64 columns by 16 groups, one load after the other, 6.4).
+// sums meet in LDS.  Bound by that latency: 256 rows of 1536 columns 2.0 us (64 columns by 16 groups, one load after the other, 6.3), of 4096 4.0.
 __global__ __launch_bounds__(256) void sum_partials_kernel(const float* part, const uint32_t P, const uint64_t n, const uint64_t n0, float* out0, float* out1) {
   __shared__ f4 red[32][8];
   const uint32_t group = threadIdx.x >> 3, at = threadIdx.x & 7;
@@ -542,11 +547,11 @@ int pair(const NormArgs& a, bool rms, float* dgamma, float* dbeta, hipStream_t s
   else hipLaunchKernelGGL((norm_bwd_pair_kernel<L, V, false>), grid, block, 0, s, a, columns, dgamma, dbeta);
   return hipGetLastError() == hipSuccess ? GWS_OK : GWS_ERR_LAUNCH;
 }
-// Whether one launch that reads twice beats two.  us of one and two (in a graph; the host takes 3 more for a second launch): 64 x 768 3.6, 7.4; 1021 x 768 5.0,
-// 8.0; 2048 x 768 7.2, 8.6; 4096 x 768 18.6, 10.9; 1024 x 2048 5.2, 9.8; 2048 x 2048 14.8, 11.9; 1024 x 4096 12.5, 13.8; 512 x 8192 13.3, 16.8; 1024 x 8192
-// 24.0, 22.4; 100 x 16384 7.5, 26.3; 8000 x 128 15.5, 8.4.
+// Whether one launch that reads twice beats two.  us of one and two in a graph (the host takes 3 more for a second launch): 512 x 768 3.9, 7.9; 1024 x 768 6.4, 8.2;
+// 1280 x 768 7.8, 8.7; 2048 x 768 11.2, 9.4; 1024 x 2048 8.8, 10.9; 2048 x 2048 15.0, 13.5; 1280 x 4096 14.7, 16.0; 1024 x 6144 18.7, 19.1; 768 x 8192 20.0, 20.3; 1536 x 8192 34.8, 31.1; 256 x 16384
+// 14.8, 35.4; 1536 x 16384 66.1, 69.4; 3000 x 16384 125, 105: with rows that long two launches write and read as much of partial sums as of X.
 bool one_launch(uint64_t M, uint64_t C) {
-  return !norm_is_wide(C) && M <= 2048 && M * C <= (M <= 1024 ? 4200000u : 2200000u);
+  return !norm_is_wide(C) && M <= (C > 8192 ? 1536u : C > 6144 ? 768u : C > 4096 ? 1024u : 1280u);
 }
 }  // namespace
 
@@ -569,7 +574,13 @@ int launch_norm_fwd(const NormArgs& a, bool rms, hipStream_t s) {
 }
 
 uint32_t norm_bwd_parts(uint64_t M, uint64_t C) {
-  if (norm_is_wide(C)) return fewer(M, 64);
+  // Of long rows: a workgroup a compute unit, but at least eight rows each, whose partial sums are then a quarter of what it reads.  us with 8, 16, 32, 64 parts: 64 x 32768
+  // 19.3, 18.1, 20.2, 26.1; 64 x 131072 38, 43, 81, 139; 300 x 20000 60, 39, 31, 29; 1000 x 32768 154,
+  // 112, 92, 88, with 125 117.
+  if (norm_is_wide(C)) {
+    const uint64_t pieces = (C + 2047) / 2048, filled = (cus() + pieces - 1) / pieces;
+    return fewer(M, fewer(std::max(filled, M / 8), 64));
+  }
   return fewer((M + bwd_rows_of(C) - 1) / bwd_rows_of(C), cus());
 }
 
@@ -580,8 +591,10 @@ int launch_norm_bwd(const NormArgs& a, bool rms, float* dgamma, float* dbeta, hi
     if (a.C <= 256) return pair<32, 1>(a, rms, dgamma, dbeta, s);
     if (a.C <= 512) return pair<64, 1>(a, rms, dgamma, dbeta, s);
     if (a.C <= 1024) return pair<64, 2>(a, rms, dgamma, dbeta, s);
+    if (a.C <= 1536) return pair<64, 3>(a, rms, dgamma, dbeta, s);
     if (a.C <= 2048) return pair<64, 4>(a, rms, dgamma, dbeta, s);
     if (a.C <= 4096) return pair<256, 2>(a, rms, dgamma, dbeta, s);
+    if (a.C <= 6144) return pair<256, 3>(a, rms, dgamma, dbeta, s);
     if (a.C <= 8192) return pair<256, 4>(a, rms, dgamma, dbeta, s);
     return pair<512, 4>(a, rms, dgamma, dbeta, s);
   }

@@ -98,7 +98,7 @@ def test_backward(M, C, kind):
     assert_within(dx2, want[0], tol[0], "bare")
 
 
-@pytest.mark.parametrize("M,C", [(20000, 96), (5001, 250), (2100, 400), (2500, 1000), (2049, 1500), (2050, 2048), (1100, 4000), (1100, 6000), (1100, 8000), (600, 9000)])
+@pytest.mark.parametrize("M,C", [(20000, 96), (5001, 250), (2100, 400), (2500, 1000), (2049, 1500), (2050, 2048), (1100, 4000), (1100, 6000), (1100, 8000), (600, 9000), (1300, 4000), (1600, 9000), (1000, 1500), (1000, 6000), (200, 30000)])
 def test_many_rows(M, C):
     x, dy = rand(1, M, C, ld=ld_of(C)), rand(2, M, C, 1e-3, ld_of(C))
     y, mean, rstd = room(M, C, ld_of(C))[0], torch.zeros(M, device=DEV), torch.zeros(M, device=DEV)
