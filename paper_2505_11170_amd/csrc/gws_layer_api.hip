@@ -58,6 +58,9 @@ int with_bias_gradient(const GemmArgs& g, DenseArgs& d, uint64_t rows, float* db
   return launch_sum_partials(d.part, (uint32_t)parts, g.N, g.N, dbias, nullptr, stream);
 }
 
+// Whether what the large tiles leave goes past the caches.  us with the products that read it, ordinary and past: forward (two products) 4096 tokens, 2048 -> 5632 -> 2048
+// 189, 198, 8192 310, 318; backward (dZ and H, two weight gradients and dX) 2048 tokens 216, 221, 4096 385, 394, 8192 664, 657; 4096 x 768 <- 2048 94.7, 101.8.
+bool stored_past(int64_t M, int64_t N, int matrices) { return (uint64_t)M * (uint64_t)N * 2 * matrices >= (uint64_t)172 << 20; }
 int launch_dense(const GemmArgs& g, const DenseArgs& d, const DensePlan& p, DenseOp op, int w_is_nk, hipStream_t stream) {
   switch (p.form) {
     case GemmForm::kStream: return launch_dense_stream(g, d, op, w_is_nk, p.route.stream, stream);
@@ -362,7 +365,7 @@ int gws_dense_fwd(const void* x, int64_t M, int64_t K, int64_t ldx, const void* 
   d.act = e->act;
   d.r = (const uint16_t*)e->residual; d.ldr = (uint32_t)e->ldr;
   d.z = (uint16_t*)e->z; d.ldz = (uint32_t)e->ldz;
-  d.past_caches = (uint64_t)M * (uint64_t)N * 2 >= (uint64_t)172 << 20;
+  d.past_caches = stored_past(M, N, 1);
   return launch_dense(g, d, plan_dense(g, d, DenseOp::kFwd, w_is_nk), DenseOp::kFwd, w_is_nk, (hipStream_t)stream);
 }
 
@@ -392,7 +395,7 @@ int gws_dense_bwd(const void* dy, int64_t M, int64_t D, int64_t lddy, const void
   g.x = (const uint16_t*)dy; g.w = (const uint16_t*)wd;
   g.K = (uint32_t)D; g.ldx = (uint32_t)lddy; g.ldw = (uint32_t)ldw;
   const int nk = !w_is_nk;   // the product's columns are Wd's rows
-  d.past_caches = D >= 1024;
+  d.past_caches = stored_past(M, F, h ? 2 : 1);
   const DensePlan p = plan_dense(g, d, DenseOp::kBwd, nk);
   return with_bias_gradient(g, d, p.rows, dbias, workspace, (hipStream_t)stream,
                             [&] { return launch_dense(g, d, p, DenseOp::kBwd, nk, (hipStream_t)stream); });
