@@ -140,3 +140,12 @@ def test_large_leading_dimensions():
     r.copy_(rand(4, M, N))
     gws.gws_dense_fwd(x, w, y, bias=b, act=gws.ACT_SILU, residual=r, z=z, w_is_nk=True)
     assert_within(y, wy, ty, "y")
+
+
+@pytest.mark.parametrize("form,M,K,N", [(gws.GEMM_LARGE, 14336, 1024, 6400), (gws.GEMM_LARGE_EDGE, 14300, 512, 6432), (gws.GEMM_NARROW, 15663, 1696, 6208)])
+def test_results_that_go_past_the_caches(form, M, K, N):
+    """Y, dZ and H of more than 172 MB."""
+    for nk in (True, False):
+        assert M * N * 2 >= 172 << 20 and form_of(M, K, N, nk) == form
+        check_fwd(M, K, N, nk, gws.ACT_GELU_TANH)
+        check_bwd(M, K, N, not nk, gws.ACT_SILU)
