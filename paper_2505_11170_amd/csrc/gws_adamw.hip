@@ -1,7 +1,9 @@
 // The AdamW step over many tensors and the norm of their gradients (gfx950).
 //
 // One pass over memory, four elements a lane; the tensors of a launch are found in its arguments (up to 54 descriptors), so a model's update is a few launches.
-// Bound by memory: 28 bytes a parameter with fp32 states and BF16 gradients, 16.1 with states in 8 bits.
+// Bound by memory: 28 bytes a parameter with fp32 states and BF16 gradients (twelve layers of width 768, 66 million, with the gradients' norm 384 us: 4.8 TB/s), 16.1 with
+// states in 8 bits (four layers of width 2048, 160 million, 491 us: 5.2 TB/s).  Few parameters are bound by the host's call, 97 vectors 17 us of which the kernels take 11.
+// 512 groups of four a workgroup: two loads of each buffer on their way a lane, and a workgroup a vector of up to 2048.
 //
 // States in 8 bits.  What is held is m and r = sqrt(v): v's range in a block squared would not fit E4M3's 2^18, r's does, and the step divides by
 // r anyway.  In one step m and r move by a tenth to a thousandth of themselves, an E4M3 spacing is a sixteenth to an eighth: rounded to nearest they would

@@ -1,6 +1,7 @@
 // The dense layer for any sizes (gfx950): the products of gws_dense_fwd and gws_dense_bwd by one small tile that reads its operands straight into the
 // MFMA's registers, and gws_dense_bwd_h, a pass over memory.  The small tile is right for every size that the entry points take and there for
-// those that the other kernels do not take (K = 32, very large leading dimensions).
+// those that the other kernels do not take (K = 32, very large leading dimensions).  Bound by its operands' latency (8192 x 2048 -> 5632 1550 us, ten times the large
+// tiles).
 #include "gws_dense.h"
 #include "gws_gemm256_core.h"
 

@@ -1,4 +1,6 @@
-// The dense layer's products in 128 x 128 and 128 x 96 tiles (gfx950): the loop of gemm128_kernel, its sums through gws_dense_out.h.
+// The dense layer's products in 128 x 128 and 128 x 96 tiles (gfx950): the loop of gemm128_kernel, its sums through gws_dense_out.h.  For some thousand rows and for
+// up to one round of tiles: 4096 x 768 -> 2048 with Z kept 20.2 us, bound by the tiles' operands out of the L2 and the way out.  `shared`: two LDS stages
+// instead of four, so two workgroups a compute unit, and one's way out runs under the other's loop (5469 x 5632 -> 800 104 -> 70 us).
 #include "gws_dense_out.h"
 #include "gws_gemm128_core.h"
 
