@@ -7,7 +7,7 @@ import torch
 
 import paper_2505_11170_amd as gws
 from paper_2505_11170_amd import binding
-from paper_2505_11170_amd.binding import _CAct8, _CAdamWSettings, _CAdamWTensor, _CEpilogue
+from paper_2505_11170_amd.binding import _CAct8, _CGatedSaved, _CAdamWSettings, _CAdamWTensor, _CEpilogue
 
 OK, NULL, SHAPE, ALIGN, FORMAT, LAUNCH, ALIAS = range(7)
 INF, NAN = float("inf"), float("nan")
@@ -232,3 +232,12 @@ def test_binding_refuses_what_the_kernels_would_misread(lib):
         gws.gws_adamw(packed, 1e-3, 1, grad_scale=torch.zeros(2))
     with pytest.raises(ValueError, match="device"):
         gws.gws_adamw(packed, 1e-3, 1)
+
+
+def test_a_gate_s_gradients_do_not_lie_on_codes(lib):
+    """Not even where the codes' rows lie as far apart as theirs: at the same place only a matrix of the same rows and bytes is."""
+    saved = _CGatedSaved(g8=_CAct8(at(5), at(6), 128, 2), u8=_CAct8(at(7), at(8), 128, 2))
+    for n in (5, 7):
+        out = [at(n), at(10)] if n == 5 else [at(10), at(n)]
+        assert lib.gws_gated_bwd_h(at(0), 8, 64, 64, gws.ACT_SILU, ctypes.byref(saved), *out, 64, None, 0, None) == ALIAS
+        assert lib.gws_gated_bwd(at(0), 8, 64, 64, at(1), 64, 64, 0, gws.ACT_SILU, ctypes.byref(saved), *out, 64, None, 0, None) == ALIAS
