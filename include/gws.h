@@ -444,6 +444,7 @@ int gws_dense_bwd_h(const void* dh, int64_t M, int64_t F, int64_t lddh, int act,
  * Where *grad_scale is not finite nothing is written: a step with an overflowed gradient norm leaves the model as it was.
  * No buffer of a tensor may overlap another one of the call, its gradient included (checked within a tensor, and no buffer that is written may begin where
  * one of an earlier tensor does: a tensor given twice is GWS_ERR_ALIAS).  *grad_scale lies apart from all outputs.  Empty tensors are skipped.
+ * A captured call keeps its settings, the step among them (*grad_scale is read when it runs).
  * A tensor has at most 2^35 - 2048 elements, its columns counted in fours, those of codes in blocks of 32 (GWS_ERR_SHAPE). */
 typedef struct gws_adamw_tensor {
   float* p;            /* device, the parameter                                     */
