@@ -4,8 +4,8 @@
 // and, backward, sum(t) and sum(t n) are sums over lanes (DPP) and, with more than a wavefront's 64, over the wavefronts through LDS.  The variance is the sum of (x - mean)^2,
 // not the difference of two sums: the row is there, and nothing cancels.
 // Bound by memory: 8192 x 2048 forward 12.4 us (5.4 TB/s), backward with both vectors 27.7 in a graph (23.6 for the rows, 4.0 for the workgroups' sums); few rows by
-// latency, 1 x 2048 2.2 us.  Up to 2048 columns a row is one wavefront's, whose sums need no barrier; up to 512 a
-// wavefront has several (20000 x 128 forward 6.9 -> 3.5 us, backward 13.0 -> 8.7).
+// latency, 1 x 2048 2.2 us.  Up to 2048 columns a row is one wavefront's, whose sums need no barrier; up to 256, and
+// between 512 and 768, a wavefront has several (20000 x 128 forward 6.9 -> 3.5 us, backward 13.0 -> 8.7; 8192 x 768 8.1 -> 6.8, 16.4 -> 14.8; 512 and 1024 columns lose by it).
 // dgamma and dbeta are sums over the rows: every lane adds up its own columns over the rows that its wavefronts take, the workgroup's rows meet in
 // LDS, and what workgroups leave is added by a second kernel, always in one order.
 #include <algorithm>
@@ -278,7 +278,6 @@ template <int L, int V, int R, bool RMS>
 __global__ __launch_bounds__(L * R) void norm_bwd_kernel(const NormArgs a) {
   __shared__ float red[4 * L * R / 64];
   constexpr int TEAMS = L < 64 ? L * R / 64 : R;
-  static_assert(L >= 64 || V == 1, "");
   __shared__ float sums[TEAMS == 1 ? 1 : TEAMS * L * V * 8];
   const uint32_t team = threadIdx.x / L, lane = threadIdx.x % L;
   float dgamma[V][8], dbeta[V][8];
@@ -295,14 +294,15 @@ __global__ __launch_bounds__(L * R) void norm_bwd_kernel(const NormArgs a) {
     float(&mine)[V][8] = which == 0 ? dgamma : dbeta;
     if (L < 64)
 #pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        uint32_t v = __float_as_uint(mine[0][e]);
+      for (int n = 0; n < 8 * V; ++n) {
+        float& m = mine[n / 8][n % 8];
+        uint32_t v = __float_as_uint(m);
         if (L == 16) {
           const auto p = __builtin_amdgcn_permlane16_swap(v, v, false, false);
           v = __float_as_uint(__uint_as_float(p[0]) + __uint_as_float(p[1]));
         }
         const auto q = __builtin_amdgcn_permlane32_swap(v, v, false, false);
-        mine[0][e] = __uint_as_float(q[0]) + __uint_as_float(q[1]);
+        m = __uint_as_float(q[0]) + __uint_as_float(q[1]);
       }
     if (TEAMS > 1) {
       __syncthreads();
@@ -536,7 +536,7 @@ int bwd(const NormArgs& a, bool rms, hipStream_t s) {
   return hipGetLastError() == hipSuccess ? GWS_OK : GWS_ERR_LAUNCH;
 }
 // Rows a workgroup of the backward kernels takes at a time.
-uint32_t bwd_rows_of(uint64_t C) { return C <= 128 ? 64 : C <= 256 ? 32 : C <= 512 ? 16 : C <= 1024 ? 12 : C <= 2048 ? 8 : C <= 8192 ? 2 : 1; }
+uint32_t bwd_rows_of(uint64_t C) { return C <= 128 ? 64 : C <= 256 ? 32 : C <= 768 ? 16 : C <= 1024 ? 12 : C <= 2048 ? 8 : C <= 8192 ? 2 : 1; }
 
 template <int L, int V>
 int pair(const NormArgs& a, bool rms, float* dgamma, float* dbeta, hipStream_t s) {
@@ -564,6 +564,7 @@ int launch_norm_fwd(const NormArgs& a, bool rms, hipStream_t s) {
   if (a.C <= 128) return fwd<16, 1, 16>(a, rms, s);
   if (a.C <= 256) return fwd<32, 1, 8>(a, rms, s);
   if (a.C <= 512) return fwd<64, 1, 4>(a, rms, s);
+  if (a.C <= 768) return fwd<32, 3, 8>(a, rms, s);
   if (a.C <= 1024) return fwd<64, 2, 4>(a, rms, s);
   if (a.C <= 1536) return fwd<64, 3, 4>(a, rms, s);
   if (a.C <= 2048) return fwd<64, 4, 4>(a, rms, s);
@@ -590,6 +591,7 @@ int launch_norm_bwd(const NormArgs& a, bool rms, float* dgamma, float* dbeta, hi
     if (a.C <= 128) return pair<16, 1>(a, rms, dgamma, dbeta, s);
     if (a.C <= 256) return pair<32, 1>(a, rms, dgamma, dbeta, s);
     if (a.C <= 512) return pair<64, 1>(a, rms, dgamma, dbeta, s);
+    if (a.C <= 768) return pair<32, 3>(a, rms, dgamma, dbeta, s);
     if (a.C <= 1024) return pair<64, 2>(a, rms, dgamma, dbeta, s);
     if (a.C <= 1536) return pair<64, 3>(a, rms, dgamma, dbeta, s);
     if (a.C <= 2048) return pair<64, 4>(a, rms, dgamma, dbeta, s);
@@ -611,6 +613,7 @@ int launch_norm_bwd(const NormArgs& a, bool rms, float* dgamma, float* dbeta, hi
   } else if (a.C <= 128) rc = bwd<16, 1, 64>(a, rms, s);
   else if (a.C <= 256) rc = bwd<32, 1, 32>(a, rms, s);
   else if (a.C <= 512) rc = bwd<64, 1, 16>(a, rms, s);
+  else if (a.C <= 768) rc = bwd<32, 3, 16>(a, rms, s);
   else if (a.C <= 1024) rc = bwd<64, 2, 12>(a, rms, s);
   else if (a.C <= 1536) rc = bwd<64, 3, 8>(a, rms, s);
   else if (a.C <= 2048) rc = bwd<64, 4, 8>(a, rms, s);
