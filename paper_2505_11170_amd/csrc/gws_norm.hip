@@ -49,11 +49,11 @@ inline dim3 grid_of(uint64_t workgroups) {
   return workgroups <= kGridWidth ? dim3((uint32_t)workgroups) : dim3(kGridWidth, (uint32_t)((workgroups + kGridWidth - 1) / kGridWidth));
 }
 
-// A row's mean and rstd, and its deviations in f; times `unit` the numbers stay what they are, for rows whose squares would pass fp32's range (beyond 10^19 or
-// so) 2^-80 of them.
+// A row's mean and rstd, and its deviations in f; times `unit` the numbers stay what they are, for rows whose sums or squares would pass fp32's range (beyond 10^19 or
+// so) 2^-80 of them.  Returns the sum of the deviations' squares.
 constexpr float kSmallUnit = 0x1p-80f;
 template <int L, int V, bool RMS>
-__device__ __forceinline__ void row_statistics(const NormArgs& a, const GWS_GLOBAL uint16_t* x, uint32_t lane, float unit, float (&f)[V][8], float& mean, float& rstd,
+__device__ __forceinline__ float row_statistics(const NormArgs& a, const GWS_GLOBAL uint16_t* x, uint32_t lane, float unit, float (&f)[V][8], float& mean, float& rstd,
                                                float* red, uint32_t& turn) {
   const float count = (float)a.C;
 #pragma unroll
@@ -91,9 +91,14 @@ __device__ __forceinline__ void row_statistics(const NormArgs& a, const GWS_GLOB
     for (int e = 0; e < 8; ++e) q[0] = __fmaf_rn(f[k][e], f[k][e], q[0]);
   team_sum<L>(q, red, turn);
   rstd = 1.0f / sqrtf(q[0] / count + a.eps * unit * unit);
+  return q[0];
 }
 // A sum of squares past fp32's range leaves 0 (or NaN where the mean was past it too): such a row is done again in the small unit.
 __device__ __forceinline__ bool out_of_range(float rstd) { return !(rstd > 0.0f); }
+// There eps times 2^-160 may be 0, which is right beside squares, but a constant row whose sum was past the range has none: its rstd is that of eps alone, in the
+// numbers' own unit.  (Its mean is exact, a value of eight bits times a count of up to fourteen.  Rows that are not constant keep squares: a sum past the range
+// of up to 16384 values has one of 2^114 and more, and so two that are 2^106 apart.)
+__device__ __forceinline__ float rstd_alone(float eps) { return 1.0f / sqrtf(eps); }
 
 // L lanes a row, V groups of eight columns a lane, R rows a workgroup at a time.
 template <int L, int V, int R, bool RMS>
@@ -115,9 +120,10 @@ __global__ __launch_bounds__(L * R) void norm_fwd_kernel(const NormArgs a) {
     kept_mean = mean;
     kept_rstd = rstd;
     if (out_of_range(rstd)) {   // the same in all lanes of a row
-      row_statistics<L, V, RMS>(a, x, lane, kSmallUnit, f, mean, rstd, red, turn);
+      const float squares = row_statistics<L, V, RMS>(a, x, lane, kSmallUnit, f, mean, rstd, red, turn);
       kept_mean = mean / kSmallUnit;
       kept_rstd = rstd * kSmallUnit;
+      if (squares == 0.0f) rstd = kept_rstd = rstd_alone(a.eps);
     }
     if (lane == 0) {
       if (a.mean != nullptr) a.mean[row] = kept_mean;
@@ -143,7 +149,7 @@ __global__ __launch_bounds__(1024) void norm_fwd_wide_kernel(const NormArgs a) {
   if (row >= a.M) return;
   const GWS_GLOBAL uint16_t* x = global_ptr<uint16_t>(a.x) + (size_t)row * a.ldx;
   const float count = (float)a.C;
-  float mean, rstd, unit = 1.0f;
+  float mean, rstd, variance, unit = 1.0f;
   for (;;) {
     mean = 0.0f;
     if (!RMS) {
@@ -170,13 +176,28 @@ __global__ __launch_bounds__(1024) void norm_fwd_wide_kernel(const NormArgs a) {
       q[0] += t;
     }
     team_sum<1024>(q, red, turn);
-    rstd = 1.0f / sqrtf(q[0] / count + a.eps * unit * unit);
+    variance = q[0] / count;
+    rstd = 1.0f / sqrtf(variance + a.eps * unit * unit);
     if (!out_of_range(rstd) || unit != 1.0f) break;   // the same in all threads
     unit = kSmallUnit;
   }
+  float kept_mean = mean / unit, kept_rstd = rstd * unit;
+  // Deviations of less than a BF16 spacing in the mean: a constant row maybe, whose sum has more bits than fp32 holds from 65537 columns on (a value has eight, the count
+  // seventeen), and whose mean is then not its value.
+  if (!RMS && variance <= 0x1p-16f * mean * mean) {   // the same in all threads
+    const uint32_t first = x[0];
+    float others[1] = {0.0f};
+    for (uint32_t c = threadIdx.x; c < a.C; c += 1024) others[0] = x[c] != first ? 1.0f : others[0];
+    team_sum<1024>(others, red, turn);
+    if (others[0] == 0.0f) {
+      mean = lo_of(first) * unit;
+      kept_mean = lo_of(first);
+      rstd = kept_rstd = rstd_alone(a.eps);
+    }
+  }
   if (threadIdx.x == 0) {
-    if (a.mean != nullptr) a.mean[row] = mean / unit;
-    if (a.rstd != nullptr) a.rstd[row] = rstd * unit;
+    if (a.mean != nullptr) a.mean[row] = kept_mean;
+    if (a.rstd != nullptr) a.rstd[row] = kept_rstd;
   }
   GWS_GLOBAL uint16_t* y = global_ptr<uint16_t>(a.y) + (size_t)row * a.ldy;
   for (uint32_t c = threadIdx.x * 8; c < a.C; c += 8192) {

@@ -229,3 +229,28 @@ def test_grids_of_more_than_32_bits_of_threads():
     ws = torch.empty(gws.gws_norm_bwd_workspace_bytes(1, C), dtype=torch.uint8, device=DEV)
     gws.gws_norm_bwd(dy, x, dx, rstd, kind=LAYER, mean=mean, dgamma=dgamma, dbeta=dbeta, workspace=ws)
     assert torch.equal(dbeta, dy[0].float()) and torch.equal(dgamma, dy[0].float() * (x[0].float() * 2 - 0.5))   # exact in every step
+
+
+CONSTANTS = [2.0 ** 120, -3e38, 2.0 ** 126, 1e36, 3e38, 255.0, -255 * 2.0 ** 20, 3.0, 2.0 ** -130, 0.0]
+
+
+@pytest.mark.parametrize("C", [8, 768, 2048, 3000, 20000, 70001])
+@pytest.mark.parametrize("eps", [1e-5, 3000.0])
+def test_constant_rows(C, eps):
+    """Y is beta and rstd 1 / sqrt(eps), also where the row's sum leaves fp32's range or has more bits than fp32 holds."""
+    values, n = CONSTANTS, len(CONSTANTS)
+    x = rand(7, n + 3, C, 1.0, ld_of(C))
+    for i, v in enumerate(values):
+        x[i] = v
+    x[n, 0] = 2.0 ** 120                                # not constant: a row of N(0, 1) beside 2^120
+    gamma, beta = vec(9, C, 1.0, 0.2), vec(10, C)
+    y, mean, rstd = room(n + 3, C, ld_of(C))[0], torch.full((n + 3,), math.nan, device=DEV), torch.full((n + 3,), math.nan, device=DEV)
+    gws.gws_norm_fwd(x, y, gamma=gamma, beta=beta, eps=eps, mean=mean, rstd=rstd)
+    assert torch.equal(mean[:n], x[:n, 0].float())
+    alone = 1.0 / math.sqrt(torch.tensor(eps).item())   # of eps as fp32; a root and a quotient, each rounded
+    assert bool(((rstd[:n].double() - alone).abs() <= 2 * ref.U * alone).all())
+    for i in range(n):
+        assert torch.equal(y[i], beta.bfloat16()), values[i]
+    want, tol = ref.norm_fwd(x, LAYER, gamma, beta, eps)
+    assert_within(y[n:], want[0][n:], tol[0][n:], "y")
+    assert_within(rstd[n:], want[2][n:], tol[2][n:], "rstd")
