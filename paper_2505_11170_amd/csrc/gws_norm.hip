@@ -211,10 +211,14 @@ __global__ __launch_bounds__(1024) void norm_fwd_wide_kernel(const NormArgs a) {
   }
 }
 
-// n = (x - mean) rstd by halves: x - mean itself may pass fp32's range.
+// n = (x - mean) rstd by halves: x - mean itself may pass fp32's range.  Columns past the row are zeros with dY = 0, and their n = -mean rstd, which the sums multiply by that 0,
+// has to be finite.  It is but in constant rows (in others two values are a BF16 spacing apart, and rstd is at most 2^8 sqrt(2 C) / mean), where n is 0 in the row's columns:
+// there it is made 0 in all of them.
 struct Normalise {
   float half_mean, twice_rstd;
-  __device__ __forceinline__ Normalise(float mean, float rstd) : half_mean(0.5f * mean), twice_rstd(2.0f * rstd) {}
+  __device__ __forceinline__ Normalise(float mean, float rstd) : half_mean(0.5f * mean), twice_rstd(2.0f * rstd) {
+    if (__builtin_fabsf(half_mean * twice_rstd) == __builtin_inff()) twice_rstd = 0.0f;
+  }
   __device__ __forceinline__ float operator()(float x) const { return __fmaf_rn(x, 0.5f, -half_mean) * twice_rstd; }
 };
 

@@ -254,3 +254,25 @@ def test_constant_rows(C, eps):
     want, tol = ref.norm_fwd(x, LAYER, gamma, beta, eps)
     assert_within(y[n:], want[0][n:], tol[0][n:], "y")
     assert_within(rstd[n:], want[2][n:], tol[2][n:], "rstd")
+
+
+@pytest.mark.parametrize("M,C", [(13, 8), (13, 100), (13, 700), (13, 2000), (13, 3000), (13, 20001), (1300, 8), (1300, 100), (1300, 700), (1300, 2000), (1300, 3000)])
+def test_gradients_of_constant_rows(M, C):
+    """n is 0 in them, however large mean times rstd: their dX has the row's t alone, and they add nothing to dgamma."""
+    n = len(CONSTANTS)
+    x, dy = rand(7, M, C, 1.0, ld_of(C)), rand(8, M, C, 1.0, ld_of(C))
+    for i, v in enumerate(CONSTANTS):
+        x[i] = v
+    gamma = vec(9, C, 1.0, 0.2)
+    mean = x.double().mean(1)
+    rstd = (1.0 / torch.sqrt(((x.double() - mean[:, None]) ** 2).mean(1) + 1e-5)).float()
+    mean = mean.float()
+    dx, dgamma, dbeta = room(M, C, ld_of(C))[0], torch.zeros(C, device=DEV), torch.zeros(C, device=DEV)
+    ws = torch.empty(gws.gws_norm_bwd_workspace_bytes(M, C), dtype=torch.uint8, device=DEV)
+    want, tol = ref.norm_bwd(dy, x, LAYER, gamma, mean, rstd, None)
+    for _ in range(2):
+        gws.gws_norm_bwd(dy, x, dx, rstd, mean=mean, gamma=gamma, dgamma=dgamma, dbeta=dbeta, workspace=ws)
+        for got, w, t, name in zip((dx, dgamma, dbeta), want, tol, ("dx", "dgamma", "dbeta")):
+            assert_within(got, w, t, name)
+        dx = torch.nn.functional.pad(dy, (0, ld_of(C) - C))[:, :C]     # then in place, by the other kernel
+        dy = dx
