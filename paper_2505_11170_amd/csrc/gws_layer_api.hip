@@ -167,22 +167,27 @@ class GivenBefore {
     bits_[h >> 6] |= (uint64_t)1 << (h & 63);
     return was;
   }
+  struct Written {
+    const void* at[6];
+    explicit Written(const gws_adamw_tensor& t)
+        : at{t.p, t.w, t.m8.codes ? t.m8.codes : t.m, t.v8.codes ? t.v8.codes : t.v, t.m8.codes ? t.m8.xscale : nullptr, t.v8.codes ? t.v8.xscale : nullptr} {}
+  };
 
  public:
   GivenBefore() { memset(bits_, 0, sizeof bits_); }
   bool any(const gws_adamw_tensor* t, int i) {
     const gws_adamw_tensor& n = t[i];
     if (n.rows == 0 || n.cols == 0) return false;
-    const void* mine[4] = {n.p, n.m8.codes ? (const void*)n.m8.codes : n.m, n.v8.codes ? (const void*)n.v8.codes : n.v, n.w};
+    const Written mine(n);
     bool seen = false;
-    for (const void* p : mine) seen |= p != nullptr && set(p);
+    for (const void* p : mine.at) seen |= p != nullptr && set(p);
     if (!seen) return false;
     for (int j = 0; j < i; ++j) {
       const gws_adamw_tensor& o = t[j];
       if (o.rows == 0 || o.cols == 0) continue;
-      const void* theirs[4] = {o.p, o.m8.codes ? (const void*)o.m8.codes : o.m, o.v8.codes ? (const void*)o.v8.codes : o.v, o.w};
-      for (const void* p : mine)
-        for (const void* q : theirs)
+      const Written theirs(o);
+      for (const void* p : mine.at)
+        for (const void* q : theirs.at)
           if (p != nullptr && p == q) return true;
     }
     return false;

@@ -241,3 +241,24 @@ def test_a_gate_s_gradients_do_not_lie_on_codes(lib):
         out = [at(n), at(10)] if n == 5 else [at(10), at(n)]
         assert lib.gws_gated_bwd_h(at(0), 8, 64, 64, gws.ACT_SILU, ctypes.byref(saved), *out, 64, None, 0, None) == ALIAS
         assert lib.gws_gated_bwd(at(0), 8, 64, 64, at(1), 64, 64, 0, gws.ACT_SILU, ctypes.byref(saved), *out, 64, None, 0, None) == ALIAS
+
+
+def test_adamw_refuses_scales_that_it_was_given_before(lib):
+    """Block scales are written too: of m or v, of a tensor before or of what another one has at the same address."""
+    s = ctypes.byref(_CAdamWSettings(1e-3, 0.9, 0.99, 1e-8, 1, None))
+
+    def step(*t):
+        return lib.gws_adamw((_CAdamWTensor * len(t))(*t), len(t), s, None)
+
+    far = lambda buffer, i: buffer * 2 ** 32 + 2 ** 16 * i  # noqa: E731
+    good = lambda i, m=None, v=None: in8(p=far(1, i), w=far(2, i), m8=_CAct8(far(3, i), m or far(4, i), 72, 3), v8=_CAct8(far(5, i), v or far(6, i), 72, 3))  # noqa: E731
+    for n in (1, 7, 400):
+        before = [good(i) for i in range(n)]
+        for i in (0, n - 1):
+            for taken in (far(4, i), far(6, i), far(3, i), far(5, i), far(1, i)):
+                assert step(*before, good(n, m=taken)) == ALIAS and step(*before, good(n, v=taken)) == ALIAS
+            for field in ("p", "m", "v"):
+                t = tensor(p=far(7, 0), w=far(8, 0), m=far(9, 0), v=far(10, 0))
+                setattr(t, field, far(4, i))
+                assert step(*before, t) == ALIAS, field
+        assert step(*before, good(n), tensor(ld=64)) == SHAPE       # apart: only the one behind is refused
