@@ -24,6 +24,8 @@ size_t norm_bytes(int64_t M, int64_t C) {
 }
 
 // ---- the dense layer ----
+// A leading dimension by which the kernel is chosen: of a matrix that is not there any number may stand in the call.
+inline uint32_t ld_of(const void* p, int64_t ld) { return p ? (uint32_t)ld : 0; }
 size_t dense_bytes(int64_t M, int64_t F) { return M <= 16 ? 0 : (size_t)((M + 15) / 16) * (size_t)F * sizeof(float); }
 
 // Outputs, kept Z and the bias gradient's workspace of the two backward calls.
@@ -42,9 +44,9 @@ int dense_bwd_args(int64_t M, int64_t F, int act, const void* z, int64_t ldz, vo
   b.writes(span_f32(dbias, F));
   if (need) b.writes(span_bytes(workspace, need));
   g.M = (uint32_t)M; g.N = (uint32_t)F;
-  g.y = (uint16_t*)dz; g.ldy = (uint32_t)lddz;
-  d.z = (uint16_t*)z; d.ldz = (uint32_t)ldz;
-  d.h = (uint16_t*)h; d.ldh = (uint32_t)ldh;
+  g.y = (uint16_t*)dz; g.ldy = ld_of(dz, lddz);
+  d.z = (uint16_t*)z; d.ldz = ld_of(z, ldz);
+  d.h = (uint16_t*)h; d.ldh = ld_of(h, ldh);
   d.act = act;
   return GWS_OK;
 }
@@ -368,8 +370,8 @@ int gws_dense_fwd(const void* x, int64_t M, int64_t K, int64_t ldx, const void* 
   memset(&d, 0, sizeof d);
   d.bias = e->bias;
   d.act = e->act;
-  d.r = (const uint16_t*)e->residual; d.ldr = (uint32_t)e->ldr;
-  d.z = (uint16_t*)e->z; d.ldz = (uint32_t)e->ldz;
+  d.r = (const uint16_t*)e->residual; d.ldr = ld_of(e->residual, e->ldr);
+  d.z = (uint16_t*)e->z; d.ldz = ld_of(e->z, e->ldz);
   d.past_caches = stored_past(M, N, 1);
   return launch_dense(g, d, plan_dense(g, d, DenseOp::kFwd, w_is_nk), DenseOp::kFwd, w_is_nk, (hipStream_t)stream);
 }

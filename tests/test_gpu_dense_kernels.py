@@ -1,5 +1,6 @@
 """Every kernel that a call of the dense layer may take, by sizes for which it is the one (gws_dense_form): tiles cut by the
 edges of the result, K of whole and half steps, both layouts of the weight."""
+import ctypes
 import math
 
 import pytest
@@ -10,6 +11,7 @@ import layer_ref as ref
 import paper_2505_11170_amd as gws
 from gated_ref import assert_within
 from gpu_util import DEV, ensure_built
+from paper_2505_11170_amd import binding
 from test_gpu_dense import check_bwd, check_fwd, weight
 from test_gpu_gated import rand, room
 from test_gpu_norm import vec
@@ -149,3 +151,27 @@ def test_results_that_go_past_the_caches(form, M, K, N):
         assert M * N * 2 >= 172 << 20 and form_of(M, K, N, nk) == form
         check_fwd(M, K, N, nk, gws.ACT_GELU_TANH)
         check_bwd(M, K, N, not nk, gws.ACT_SILU)
+
+
+@pytest.mark.parametrize("M,K,N", [(1021, 2048, 768), (4096, 192, 4096)])
+def test_leading_dimensions_of_what_is_left_out_say_nothing(M, K, N):
+    """NULL residual, Z and H: whatever stands beside them, the kernel and the bits are the same."""
+    lib, stream = binding.load_library(), torch.cuda.current_stream().cuda_stream
+    x, w, b, z = rand(1, M, K), weight(2, K, N, True), vec(3, N), rand(4, M, N)
+    ws = torch.empty(gws.gws_dense_bwd_workspace_bytes(M, N), dtype=torch.uint8, device=DEV)
+    nothing, first = None, None
+    for ld in (0, -1, 1 << 30, (1 << 28) + 8):
+        y, dz, db = room(M, N)[0], room(M, N)[0], torch.zeros(N, device=DEV)
+        e = binding._CEpilogue(b.data_ptr(), gws.ACT_NONE, nothing, ld, nothing, ld)
+        assert lib.gws_dense_fwd(x.data_ptr(), M, K, K, w.data_ptr(), N, K, 1, y.data_ptr(), N, ctypes.byref(e), stream) == 0
+        # with Z; without; from dH, where only the sum is wanted
+        bwd = lambda z, ldz, act: lib.gws_dense_bwd(x.data_ptr(), M, K, K, w.data_ptr(), N, K, 0, act, z, ldz, dz.data_ptr(), N, nothing, ld, db.data_ptr(), ws.data_ptr(),  # noqa: E731
+                                                    ws.nbytes, stream)
+        out = [y]
+        for args in ((z.data_ptr(), N, gws.ACT_SILU), (nothing, ld, gws.ACT_NONE)):
+            assert bwd(*args) == 0
+            out += [dz.clone(), db.clone()]
+        assert lib.gws_dense_bwd_h(z.data_ptr(), M, N, N, gws.ACT_NONE, nothing, ld, nothing, ld, nothing, ld, db.data_ptr(), ws.data_ptr(), ws.nbytes, stream) == 0
+        out.append(db)
+        first = first or out
+        assert all(torch.equal(p, q) for p, q in zip(first, out)), ld
