@@ -38,6 +38,8 @@ constexpr int64_t kMaxDim = (int64_t)1 << 31;
 inline bool size_ok(int64_t n) { return n >= 0 && n < kMaxDim; }
 // A BF16 matrix's leading dimension.
 inline bool ld_ok(int64_t ld, int64_t cols) { return ld >= cols && ld < kMaxDim && (ld & 7) == 0; }
+// By leading dimensions the kernel is chosen: of a matrix that is not there any number may stand in the call.
+inline uint32_t ld_of(const void* p, int64_t ld) { return p ? (uint32_t)ld : 0; }
 inline Span2 span16(const void* p, int64_t rows, int64_t cols, int64_t ld) { return Span2{p, (size_t)rows, (size_t)cols * 2, (size_t)ld * 2}; }
 inline bool same_place(const Span2& a, const Span2& b) { return a.p == b.p && a.pitch == b.pitch && a.width == b.width && a.rows == b.rows; }
 

@@ -267,7 +267,7 @@ static int bwd_args(int64_t M, int64_t F, const gws_gated_saved* saved, void* dg
   if (rc != GWS_OK) return rc;
   g.M = (uint32_t)M; g.N = (uint32_t)F;
   g.dg = (uint16_t*)dg; g.du = (uint16_t*)du; g.h = (uint16_t*)h;
-  g.ldd = (uint32_t)ldd; g.ldh = (uint32_t)ldh;
+  g.ldd = (uint32_t)ldd; g.ldh = ld_of(h, ldh);
   b.writes(span16(dg, M, F, ldd));
   b.writes(span16(du, M, F, ldd));
   b.writes(span16(h, M, F, ldh));

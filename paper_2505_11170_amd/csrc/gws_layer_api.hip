@@ -24,8 +24,6 @@ size_t norm_bytes(int64_t M, int64_t C) {
 }
 
 // ---- the dense layer ----
-// A leading dimension by which the kernel is chosen: of a matrix that is not there any number may stand in the call.
-inline uint32_t ld_of(const void* p, int64_t ld) { return p ? (uint32_t)ld : 0; }
 size_t dense_bytes(int64_t M, int64_t F) { return M <= 16 ? 0 : (size_t)((M + 15) / 16) * (size_t)F * sizeof(float); }
 
 // Outputs, kept Z and the bias gradient's workspace of the two backward calls.

@@ -1,12 +1,15 @@
 """Every kernel and tile behind the gated block's entry points, at sizes that take it: whole tiles, edges of rows and columns, half a K-step
 of 64 at the end of the contraction (of either product of the input gradient), one K-step, and activations whose scale saturates."""
+import ctypes
+
 import pytest
 import torch
 
 import gated_ref as ref
 import paper_2505_11170_amd as gws
 from gpu_util import DEV, ensure_built
-from test_gpu_gated import check_bwd, check_dx, check_fwd, kept_buffers
+from paper_2505_11170_amd import binding
+from test_gpu_gated import check_bwd, check_dx, check_fwd, kept_buffers, rand
 
 pytestmark = pytest.mark.gpu
 ANY, STREAM, MIDDLE, LARGE, SHARED = (1, 0, 0), 2, (3, 0, 0), (4, 0, 0), (5, 0, 0)
@@ -189,3 +192,16 @@ def test_values_beyond_the_largest_scale(M, F, form):
     assert int(scales.max()) == 246
     assert torch.equal(saved.g8.codes, codes) and torch.equal(saved.g8.xscale, scales)
     assert (saved.u8.codes & 127 == 0).all() and (saved.u8.xscale == 127).all()
+
+
+@pytest.mark.parametrize("M,D,F", [(1021, 2048, 768), (2048, 256, 2048)])
+def test_the_leading_dimension_of_an_h_that_is_left_out_says_nothing(M, D, F):
+    lib, stream = binding.load_library(), torch.cuda.current_stream().cuda_stream
+    dy, wd, g, u = rand(1, M, D), rand(2, F, D, 0.05), rand(3, M, F), rand(4, M, F)
+    saved = binding._CGatedSaved(g.data_ptr(), u.data_ptr(), F, F)
+    first = None
+    for ldh in (0, -1, 1 << 30):
+        dg, du = torch.zeros_like(g), torch.zeros_like(u)
+        assert lib.gws_gated_bwd(dy.data_ptr(), M, D, D, wd.data_ptr(), F, D, 0, gws.ACT_SILU, ctypes.byref(saved), dg.data_ptr(), du.data_ptr(), F, None, ldh, stream) == 0
+        first = first or (dg, du)
+        assert torch.equal(first[0], dg) and torch.equal(first[1], du), ldh
