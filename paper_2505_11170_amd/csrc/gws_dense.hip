@@ -36,7 +36,8 @@ template <DenseOp OP, bool W_NK>
 __global__ __launch_bounds__(256) void dense_any_kernel(const GemmArgs g, const DenseArgs d) {
   __shared__ float sums[4][kCols];
   const uint32_t lane = threadIdx.x & 63, li = lane & 15, grp = lane >> 4, wave = threadIdx.x >> 6;
-  const uint32_t nt = (g.N + kCols - 1) / kCols, tile_m = blockIdx.x / nt, m0 = tile_m * kRows + 16 * wave, n0 = blockIdx.x % nt * kCols;
+  const uint32_t nt = (g.N + kCols - 1) / kCols, tile = workgroup(), tile_m = tile / nt, m0 = tile_m * kRows + 16 * wave, n0 = tile % nt * kCols;
+  if (tile_m >= (g.M + kRows - 1) / kRows) return;   // uniform: past the last tile of a grid of two dimensions
   const bool live = m0 + li < g.M;
   const uint32_t row = live ? m0 + li : g.M - 1;   // past the edge the last ones are read, and nothing is stored
   uint32_t col[4];
@@ -113,8 +114,8 @@ __global__ __launch_bounds__(256) void dense_any_kernel(const GemmArgs g, const 
 
 int launch_dense_any(const GemmArgs& g, const DenseArgs& e, DenseOp op, int w_is_nk, hipStream_t stream) {
   const uint64_t tiles = (((uint64_t)g.M + kRows - 1) / kRows) * (((uint64_t)g.N + kCols - 1) / kCols);
-  if (tiles >= (uint64_t)1 << 24) return GWS_ERR_SHAPE;   // a launch has fewer than 2^32 threads
-  const dim3 grid((uint32_t)tiles), block(256);
+  if (tiles >= (uint64_t)1 << 31) return GWS_ERR_SHAPE;   // results of 8 TB and more
+  const dim3 grid = grid_of(tiles), block(256);
   if (op == DenseOp::kFwd) {
     if (w_is_nk) hipLaunchKernelGGL((dense_any_kernel<DenseOp::kFwd, true>), grid, block, 0, stream, g, e);
     else hipLaunchKernelGGL((dense_any_kernel<DenseOp::kFwd, false>), grid, block, 0, stream, g, e);

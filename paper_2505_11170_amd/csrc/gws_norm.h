@@ -108,6 +108,13 @@ __device__ __forceinline__ float lanes_sum(float v) {
   return v;
 }
 
+// Workgroups in a grid of two dimensions: one has fewer than 2^32 threads.
+constexpr uint32_t kGridWidth = 1u << 20;
+__device__ __forceinline__ uint32_t workgroup() { return blockIdx.y * kGridWidth + blockIdx.x; }
+inline dim3 grid_of(uint64_t workgroups) {
+  return workgroups <= kGridWidth ? dim3((uint32_t)workgroups) : dim3(kGridWidth, (uint32_t)((workgroups + kGridWidth - 1) / kGridWidth));
+}
+
 // Columns of partial sums added up: out[c] = sum over p < P of part[p * n + c] for c < n, columns from n0 on to out1.
 int launch_sum_partials(const float* part, uint32_t P, uint64_t n, uint64_t n0, float* out0, float* out1, hipStream_t stream);
 int launch_zero(float* p, uint64_t n, hipStream_t stream);

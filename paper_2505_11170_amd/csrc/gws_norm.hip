@@ -42,13 +42,6 @@ __device__ __forceinline__ void team_sum(float (&v)[N], float* red, uint32_t& tu
 
 }  // namespace
 
-// Workgroups in a grid of two dimensions: one has fewer than 2^32 threads.
-constexpr uint32_t kGridWidth = 1u << 20;
-__device__ __forceinline__ uint32_t workgroup() { return blockIdx.y * kGridWidth + blockIdx.x; }
-inline dim3 grid_of(uint64_t workgroups) {
-  return workgroups <= kGridWidth ? dim3((uint32_t)workgroups) : dim3(kGridWidth, (uint32_t)((workgroups + kGridWidth - 1) / kGridWidth));
-}
-
 // A row's mean and rstd, and its deviations in f; times `unit` the numbers stay what they are, for rows whose sums or squares would pass fp32's range (beyond 10^19 or
 // so) 2^-80 of them.  Returns the sum of the deviations' squares.
 constexpr float kSmallUnit = 0x1p-80f;

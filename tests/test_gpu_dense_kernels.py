@@ -175,3 +175,34 @@ def test_leading_dimensions_of_what_is_left_out_say_nothing(M, K, N):
         out.append(db)
         first = first or out
         assert all(torch.equal(p, q) for p, q in zip(first, out)), ld
+
+
+def test_grids_of_more_than_32_bits_of_threads():
+    """More than 2^24 of the smallest tiles: every row is written, and the bias gradient has them all."""
+    if torch.cuda.mem_get_info()[0] < 190 << 30:
+        pytest.skip("no room")
+    more_than_32_bits_of_threads()
+    torch.cuda.empty_cache()       # 170 GB, which other tests have a use for
+
+
+def more_than_32_bits_of_threads():
+    M, K, N = (1 << 25) + 70, 32, 2048
+    assert form_of(M, K, N, True) == gws.GEMM_ANY_SHAPE
+    marks = [0, 63, 64, (1 << 21) - 1, 1 << 21, (1 << 24) + 5, (1 << 25) - 1, 1 << 25, M - 1]
+    x, w = torch.zeros(M, K, dtype=torch.bfloat16, device=DEV), torch.randint(1, 100, (N, K), generator=torch.Generator(device=DEV).manual_seed(1), device=DEV).bfloat16()
+    for i, r in enumerate(marks):
+        x[r, i] = 1.0
+    y, b = torch.full((M, N), 7, dtype=torch.bfloat16, device=DEV), torch.zeros(N, device=DEV)
+
+    def rows_of_w():
+        assert all(torch.equal(y[r], w[:, i]) for i, r in enumerate(marks))
+        y[marks] = 0
+        assert not any(bool((y[r:r + (1 << 21)] != 0).any()) for r in range(0, M, 1 << 21))
+
+    gws.gws_dense_fwd(x, w, y, bias=b, w_is_nk=True)
+    rows_of_w()
+    y.fill_(7)
+    ws = torch.empty(gws.gws_dense_bwd_workspace_bytes(M, N), dtype=torch.uint8, device=DEV)
+    gws.gws_dense_bwd(x, w, None, y, dbias=b, workspace=ws)
+    rows_of_w()
+    assert torch.equal(b, w[:, :len(marks)].float().sum(1))      # whole numbers: exact
