@@ -58,9 +58,16 @@ int with_bias_gradient(const GemmArgs& g, DenseArgs& d, uint64_t rows, float* db
   return launch_sum_partials(d.part, (uint32_t)parts, g.N, g.N, dbias, nullptr, stream);
 }
 
-// Whether what the large tiles leave goes past the caches.  us with the products that read it, ordinary and past: forward (two products) 4096 tokens, 2048 -> 5632 -> 2048
-// 189, 198, 8192 310, 318; backward (dZ and H, two weight gradients and dX) 2048 tokens 216, 221, 4096 385, 394, 8192 664, 657; 4096 x 768 <- 2048 94.7, 101.8.
-bool stored_past(int64_t M, int64_t N, int matrices) { return (uint64_t)M * (uint64_t)N * 2 * matrices >= (uint64_t)172 << 20; }
+// Whether Y, or dZ and H, of 128 x 128 tiles and larger ones go past the caches: by the call's time together with what reads them next (a graph over two sets of buffers,
+// ratios of past to ordinary stores; Y, or dZ and H together, of 64 to 88, 110 to 165, 172 to 352 MB).
+// Forward, with the product that follows: 2048 -> 5632 1.00 to 1.07, 1.00 to 1.03, 0.99 (16384 tokens 617, 609 us, 32768 1173, 1163); 1024 -> 4096 1.02 to 1.05, 0.99 to 1.05, 0.97 to
+// 1.01; 768 -> 2048 1.00 to 1.05, 0.99 to 1.03, 0.96 to 0.98 (45056 tokens 345, 333).  Nothing kept: 0.99 to 1.04, 0.98 to 1.06, 0.96 to 1.04.
+// Backward, with dX and the two weight gradients: D = 2048, F = 5632 1.00 to 1.02, 0.96 to 1.01, 0.99 to 1.03 (8192 tokens 633, 654; on another box 664, 657; 12288 993, 987);
+// 1024, 4096 1.00 to 1.02, 1.01 to 1.03, 0.97 to 1.00; 768, 2048 1.06 to 1.10, 1.05 to 1.10, 1.00 to 1.05 (22528 tokens 434, 455): its products wait for what they read.  Without H 2048, 5632
+// 1.02 to 1.04, 1.02 to 1.03, 0.98 to 1.02.  The call alone is 2 to 13 % faster past the caches.
+bool stored_past(DenseOp op, int64_t M, int64_t N, int64_t K, int matrices) {
+  return (uint64_t)M * (uint64_t)N * 2 * matrices >= (uint64_t)172 << 20 && (op == DenseOp::kFwd || K >= 1024);
+}
 int launch_dense(const GemmArgs& g, const DenseArgs& d, const DensePlan& p, DenseOp op, int w_is_nk, hipStream_t stream) {
   switch (p.form) {
     case GemmForm::kStream: return launch_dense_stream(g, d, op, w_is_nk, p.route.stream, stream);
@@ -370,7 +377,7 @@ int gws_dense_fwd(const void* x, int64_t M, int64_t K, int64_t ldx, const void* 
   d.act = e->act;
   d.r = (const uint16_t*)e->residual; d.ldr = ld_of(e->residual, e->ldr);
   d.z = (uint16_t*)e->z; d.ldz = ld_of(e->z, e->ldz);
-  d.past_caches = stored_past(M, N, 1);
+  d.past_caches = stored_past(DenseOp::kFwd, M, N, K, 1);
   return launch_dense(g, d, plan_dense(g, d, DenseOp::kFwd, w_is_nk), DenseOp::kFwd, w_is_nk, (hipStream_t)stream);
 }
 
@@ -400,7 +407,7 @@ int gws_dense_bwd(const void* dy, int64_t M, int64_t D, int64_t lddy, const void
   g.x = (const uint16_t*)dy; g.w = (const uint16_t*)wd;
   g.K = (uint32_t)D; g.ldx = (uint32_t)lddy; g.ldw = (uint32_t)ldw;
   const int nk = !w_is_nk;   // the product's columns are Wd's rows
-  d.past_caches = stored_past(M, F, h ? 2 : 1);
+  d.past_caches = stored_past(DenseOp::kBwd, M, F, D, h ? 2 : 1);
   const DensePlan p = plan_dense(g, d, DenseOp::kBwd, nk);
   return with_bias_gradient(g, d, p.rows, dbias, workspace, (hipStream_t)stream,
                             [&] { return launch_dense(g, d, p, DenseOp::kBwd, nk, (hipStream_t)stream); });

@@ -206,3 +206,12 @@ def more_than_32_bits_of_threads():
     gws.gws_dense_bwd(x, w, None, y, dbias=b, workspace=ws)
     rows_of_w()
     assert torch.equal(b, w[:, :len(marks)].float().sum(1))      # whole numbers: exact
+
+
+@pytest.mark.parametrize("form,M,K,N", [(gws.GEMM_LARGE_EDGE, 14300, 1056, 6432), (gws.DENSE_SHARED, 117567, 1056, 800), (gws.GEMM_NARROW, 73332, 992, 1344)])
+def test_results_that_go_past_the_caches_where_their_readers_wait_for_the_products(form, M, K, N):
+    """Of the other forms those that the backward pass too takes past the caches (D of 1024 and more), and one of shorter products, whose backward pass does not."""
+    for nk in (True, False):
+        assert M * N * 2 >= 172 << 20 and form_of(M, K, N, nk) == form
+        check_fwd(M, K, N, nk, gws.ACT_SILU)
+        check_bwd(M, K, N, not nk, gws.ACT_GELU_TANH)
