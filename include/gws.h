@@ -369,7 +369,7 @@ int gws_linear_bwd_w_act8(const gws_act8* x, const void* dy, int64_t M, int64_t 
  *   GWS_NORM_RMS    rstd = 1 / sqrt(sum(x^2) / C + eps),                             n = x rstd,          y = n .* gamma + beta
  * X, Y and the gradients are BF16 (leading dimensions multiples of 8, 16-byte aligned), everything else fp32 (4-byte aligned): gamma and beta
  * [C], NULL for ones and zeros; mean and rstd [M].  Sums and arithmetic are fp32 (the squares are those of x - mean, so a large common offset costs
- * nothing), each output is rounded once.  Rows do not meet: a row of NaN leaves the others as they are.  Values past column C are neither read nor written.
+ * nothing, and a constant row gives beta with rstd = 1 / sqrt(eps)), each output is rounded once.  Rows do not meet: a row of NaN leaves the others as they are.  Values past column C are neither read nor written.
  * A row's result does not depend on the other rows, their number included, except in its last bits through the order of the sums.  M == 0 writes nothing (dgamma and dbeta become zeros). */
 #define GWS_NORM_LAYER 0
 #define GWS_NORM_RMS 1
@@ -432,7 +432,7 @@ int gws_dense_bwd_h(const void* dh, int64_t M, int64_t F, int64_t lddh, int act,
  * Step t (1, 2, ...) for every element, with s = *grad_scale (NULL: 1), c1 = 1 - beta1^t, c2 = 1 - beta2^t, in fp32, in the order written, without fused
  * multiply-adds but in the division:
  *   g' = g s;  m = beta1 m + (1 - beta1) g';  v = beta2 v + (1 - beta2) (g' g');  r = sqrt(v)
- *   p = p (1 - lr wd) - ((lr / c1) m) / (r / sqrt(c2) + eps);   w = p rounded to BF16
+ *   p = p (1 - lr wd) - ((lr / c1) m) / (r (1 / sqrt(c2)) + eps);   w = p rounded to BF16
  * (lr = the call's times the tensor's lr_scale; what is in brackets and powers of the settings is formed in fp64 and rounded once).  A tensor [rows x cols] has one
  * leading dimension ld (cols <= ld, a multiple of 8; a vector is one row) for p, g, w, and for m and v or their codes; 16-byte aligned (codes 8-byte).
  * The states m and v are fp32 (m, v set, m8.codes and v8.codes NULL), or m and r are held in 8 bits (m and v NULL; m8 and v8 set, ldc = ld, one lds):

@@ -1,6 +1,6 @@
 // The AdamW step over many tensors and the norm of their gradients (gfx950).
 //
-// One pass over memory, four elements a lane; the tensors of a launch are found in its arguments (up to 54 descriptors), so a model's update is a few launches.
+// One pass over memory, four elements a lane; the tensors of a launch are found in its arguments (up to 100 runs of elements, 54 other matrices or 216 gradients), so a model's update is a few launches.
 // Bound by memory: 28 bytes a parameter with fp32 states and BF16 gradients (twelve layers of width 768, 66 million, with the gradients' norm 384 us: 4.8 TB/s), 16.1 with
 // states in 8 bits (four layers of width 2048, 160 million, 491 us: 5.2 TB/s).  Few parameters are bound by the host's call, 97 vectors 17 us of which the kernels take 11.
 // 512 groups of four a workgroup: two loads of each buffer on their way a lane, and a workgroup a vector of up to 2048.

@@ -225,33 +225,21 @@ __device__ __forceinline__ void bwd_rows(const NormArgs& a, uint32_t row0, uint3
 #pragma unroll
   for (int k = 0; k < V; ++k) vector_eight(a.gamma, (lane + k * L) * 8, a.C, 1.0f, gamma[k]);
   const float count = (float)a.C;
-  struct Raw {
-    u32x4 x[V], y[V], r[V];
-    float mean, rstd;
-  };
-  // past the last row the team's neighbour's is read, and nothing stored
-  auto load = [&](uint32_t first, Raw& raw) {
-    const size_t at = first + team < a.M ? first + team : first;
-    const GWS_GLOBAL uint16_t *x = global_ptr<uint16_t>(a.x) + at * a.ldx, *dy = global_ptr<uint16_t>(a.dy) + at * a.lddy;
-#pragma unroll
-    for (int k = 0; k < V; ++k) {
-      raw.x[k] = load_eight(x, (lane + k * L) * 8, a.C);
-      raw.y[k] = load_eight(dy, (lane + k * L) * 8, a.C);
-      if (a.r != nullptr) raw.r[k] = load_eight(global_ptr<uint16_t>(a.r) + at * a.ldr, (lane + k * L) * 8, a.C);
-    }
-    raw.rstd = a.rstd[at];
-    raw.mean = RMS ? 0.0f : a.mean[at];
-  };
-  Raw now;
   for (; row0 < a.M; row0 += step) {
     const uint32_t row = row0 + team;
     const bool live = row < a.M;
     if (L == 64 && !live) break;   // with fewer lanes a row a wavefront has several
-    const size_t at = live ? row : row0;
-    load(row0, now);
-    u32x4(&xr)[V] = now.x, (&yr)[V] = now.y, (&rr)[V] = now.r;
-    const float rstd = now.rstd;
-    const Normalise normal(now.mean, rstd);
+    const size_t at = live ? row : row0;   // past the last row a neighbour's is read, and nothing stored
+    const GWS_GLOBAL uint16_t *x = global_ptr<uint16_t>(a.x) + at * a.ldx, *dy = global_ptr<uint16_t>(a.dy) + at * a.lddy;
+    u32x4 xr[V], yr[V], rr[V];
+#pragma unroll
+    for (int k = 0; k < V; ++k) {
+      xr[k] = load_eight(x, (lane + k * L) * 8, a.C);
+      yr[k] = load_eight(dy, (lane + k * L) * 8, a.C);
+      if (a.r != nullptr) rr[k] = load_eight(global_ptr<uint16_t>(a.r) + at * a.ldr, (lane + k * L) * 8, a.C);
+    }
+    const float rstd = a.rstd[at];
+    const Normalise normal(RMS ? 0.0f : a.mean[at], rstd);
     float s[2] = {0.0f, 0.0f};
 #pragma unroll
     for (int k = 0; k < V; ++k) {   // columns past the row have dY = 0: they add nothing
@@ -593,7 +581,8 @@ int launch_norm_fwd(const NormArgs& a, bool rms, hipStream_t s) {
 }
 
 uint32_t norm_bwd_parts(uint64_t M, uint64_t C) {
-  // Of long rows: a workgroup a compute unit, but at least eight rows each, whose partial sums are then a quarter of what it reads.  us with 8, 16, 32, 64 parts: 64 x 32768
+  // Of long rows: parts enough for a workgroup a compute unit (64 x 32768 16 parts of four rows, few rows one each), more only where each keeps eight rows and more,
+  // whose partial sums are then at most a quarter of what it reads, and no more than 64.  us with 8, 16, 32, 64 parts: 64 x 32768
   // 19.3, 18.1, 20.2, 26.1; 64 x 131072 38, 43, 81, 139; 300 x 20000 60, 39, 31, 29; 1000 x 32768 154,
   // 112, 92, 88, with 125 117.
   if (norm_is_wide(C)) {
